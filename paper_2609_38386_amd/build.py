@@ -18,7 +18,8 @@ INCLUDE = os.path.join(ROOT, "include")
 LIB_PATH = os.path.join(HERE, "libdlfp.so")
 ARCH = "gfx950"
 
-SOURCES = ["dlfp_host.cpp", "dlfp_timer.cpp", "kv_append.hip", "attention_mixed.hip", "stream_hold.hip",
+SOURCES = ["attention_window.hip", "attention_kv8.hip", "attention_mixed.hip", "dlfp_host.cpp",
+           "dlfp_cache.cpp", "dlfp_timer.cpp", "kv_append.hip", "kv8_append.hip", "stream_hold.hip",
            "linear.hip"]
 
 # Packed FP32 instructions are kept out of device code.
@@ -43,7 +44,7 @@ def build_probes(verbose: bool = False) -> str:
     return _build(PROBE_SOURCES, PROBE_LIB_PATH, verbose, 1)
 
 
-def build_library(verbose: bool = False, jobs: int = 3) -> str:
+def build_library(verbose: bool = False, jobs: int = 4) -> str:
     return _build(SOURCES, LIB_PATH, verbose, jobs)
 
 

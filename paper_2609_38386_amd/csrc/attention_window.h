@@ -1,0 +1,1078 @@
+// Paged attention with a sliding window and sinks, over bf16 or 8-bit pages: the
+// kernels of dlfp_attention_window and dlfp_attention_kv8, which differ in how a
+// page reaches the matrix products (template parameter KV8).
+//
+// A row at position p sees key j <= p with p - j < window or j < sinks.  A unit
+// (the rows of one tile of a prompt, or one decoding token, for one KV head)
+// reads only pages that hold a key some row of it sees: its sink pages, then,
+// past a gap of whole pages, those from its first row's window on.  Work records
+// count keys without the gap ("virtual" keys, whole pages), so a unit is a range
+// [KVBEGIN, KVEND) of them whatever the mask, and a unit's table of block ids in
+// LDS lists its pages in that order; only masks go back to positions.
+//
+// 8-bit pages: with a power of two as a page's scale, v_cvt_scalef32_pk_bf16_fp8
+// turns two codes into the two bf16 numbers that they stand for, so that from the
+// operands on both kinds are the same kernel.  The pages travel to LDS as they
+// are stored, by direct copies, half the bytes; operands are converted as they
+// are read, 16 codes (one 16-byte LDS read) into two operands of eight.  Which
+// dims and keys a lane's eight are is free as long as both factors of a product
+// agree, so a lane takes 16 codes that are next to each other: of a key row, dims
+// 32 j + 16 hi .. + 15 (of 32 x 32 products; of 16 x 16 ones 64 j + 16 q ..); of a
+// value row, all 16 slots of one page.
+//
+// Everything else is as in attention_mixed.hip: S^T = K Q^T and O^T += V^T P^T
+// with row statistics in a lane, a lazily raised reference maximum in the exp2
+// domain, split ranges merged by the last to finish.
+#ifndef DLFP_ATTENTION_WINDOW_H
+#define DLFP_ATTENTION_WINDOW_H
+
+#include <hip/hip_runtime.h>
+
+#include <algorithm>
+#include <cstdint>
+#include <type_traits>
+
+#include "attention_device.h"
+#include "dlfp_cache.h"
+#include "dlfp_internal.h"
+
+namespace {
+
+constexpr int KV_TILE = 64;  // keys per prefill tile (4 pages)
+constexpr int THREADS = 256;
+constexpr int PRE_PTAB = DLFP_MAX_PREFILL_UNIT_KEYS / PAGE;
+constexpr int DEC_PTAB = DLFP_MAX_DECODE_UNIT_KEYS / PAGE;
+
+struct Args {
+  const int32_t* work;
+  const int32_t* block_table;
+  const uint16_t* q;
+  const char* kc;
+  const char* vc;
+  const uint8_t* k_exp;  // 8-bit pages only
+  const uint8_t* v_exp;
+  void* out;
+  float* ws;
+  int32_t max_blocks;
+  int32_t num_blocks;
+  int32_t hq;
+  int32_t hkv;
+  int32_t num_units;
+  int32_t num_prefill;
+  int32_t out_f32;
+  int32_t lead;         // prefill workgroups before the first decode workgroup
+  int32_t decode_lead;  // decode workgroups before the remaining prefill ones
+  float scale_log2;
+};
+
+// Bytes of a (block, head) page of keys or values.
+template <bool KV8>
+constexpr int page_bytes() {
+  return KV8 ? PAGE_ELEMS : 2 * PAGE_ELEMS;
+}
+
+// Two bf16 operands from 16 codes of a page whose scale is `scale`.
+typedef uint32_t codes_t __attribute__((ext_vector_type(4)));
+__device__ __forceinline__ void widen(codes_t c, float scale, bf16x8_t* lo, bf16x8_t* hi) {
+  u32x4_t a, b;
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    a[2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[w], scale, false));
+    a[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[w], scale, true));
+    b[2 * w] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[w + 2], scale, false));
+    b[2 * w + 1] = __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(c[w + 2], scale, true));
+  }
+  *lo = __builtin_bit_cast(bf16x8_t, a);
+  *hi = __builtin_bit_cast(bf16x8_t, b);
+}
+// The scale of an exponent byte (0: 2^-127, a subnormal; 255: infinity, NaN out).
+__device__ __forceinline__ float scale_of(int byte) {
+  return __builtin_bit_cast(float, byte ? (uint32_t)byte << 23 : 0x00400000u);
+}
+
+// Which keys a unit's rows see.
+struct Span {
+  int window, sinks;
+  int sink_pages, gap;  // virtual pages from sink_pages on are `gap` pages further
+  __device__ __forceinline__ int page(int vp) const { return vp >= sink_pages ? vp + gap : vp; }
+  __device__ __forceinline__ bool sees(int pos, int key) const {
+    return key <= pos && (pos - key < window || key < sinks);
+  }
+  // Whether virtual keys [v0, v1) hold one that a row among positions first ..
+  // last does not see (may say so of some that do not).
+  __device__ __forceinline__ bool edge(int v0, int v1, int first, int last) const {
+    const int k0 = page(v0 / PAGE) * PAGE, k1 = page((v1 - 1) / PAGE) * PAGE + PAGE - 1;
+    return k1 > first || (last - k0 >= window && k1 >= sinks);
+  }
+};
+template <class R>
+__device__ __forceinline__ Span span_of(const R& f) {
+  Span s;
+  s.window = f[DLFP_W_WINDOW];
+  s.sinks = f[DLFP_W_SINKS];
+  s.gap = f[DLFP_W_GAP];
+  s.sink_pages = s.gap ? (s.sinks + PAGE - 1) / PAGE : 0;
+  return s;
+}
+
+// Probabilities of two keys as bf16 pairs, for the matrix products.  bf16 output:
+// one term, rounded to nearest: 1.1e-3 to 1.6e-3 of a row in the 2-norm, below
+// what rounding the output leaves (1.7e-3).  fp32 output: three terms, the first
+// two cut off so that all are positive (an infinite value then stays one), 24
+// bits together.
+__device__ __forceinline__ uint32_t cut(float& a, float& b) {
+  const uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
+  a -= __builtin_bit_cast(float, x & 0xFFFF0000u);
+  b -= __builtin_bit_cast(float, y & 0xFFFF0000u);
+  return __builtin_amdgcn_perm(y, x, 0x07060302u);
+}
+
+// ---------------------------------------------------------------- prefill
+
+// Prefill LDS map: K tiles in two slots, V^T tiles in two slots, the unit's block
+// ids, and for 8-bit pages their exponent bytes (keys' | values' << 8).
+template <bool KV8>
+struct PreLds {
+  static constexpr int TILE = 4 * page_bytes<KV8>();
+  static constexpr int V_BASE = 2 * TILE;
+  static constexpr int PTAB = 4 * TILE;
+  static constexpr int ETAB = PTAB + 4 * PRE_PTAB;
+  static constexpr int BYTES = ETAB + (KV8 ? 2 * PRE_PTAB : 0);
+};
+
+template <int G, bool KV8, bool OUT32>
+__device__ void prefill_unit(const Args& a, const record_t f, char* smem, int* flag) {
+  using L = PreLds<KV8>;
+  constexpr int PB = page_bytes<KV8>();
+  const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+  const int col = lane & 31, hi = lane >> 5;
+  const int s = f[DLFP_W_SEQ], kh = f[DLFP_W_KVHEAD];
+  const int nt = f[DLFP_W_QNTOK];
+  const int vb = f[DLFP_W_KVBEGIN], ve = f[DLFP_W_KVEND];
+  const int nsplits = f[DLFP_W_NSPLITS];
+  const int row0 = f[DLFP_W_QROW0], pos0 = f[DLFP_W_QPOS0];
+  const Span sp = span_of(f);
+  const int32_t* bt = a.block_table + (int64_t)s * a.max_blocks;
+
+  const int r = wave * 32 + col;  // this lane's row within the tile
+  const int tr = r / G, hh = r % G;
+  const bool row_ok = tr < nt;
+  const int pos = row_ok ? pos0 + tr : -1;  // rows past the tile see nothing
+  const int wave_tok0 = uniform((wave * 32) / G);
+  const bool wave_active = wave_tok0 < nt;
+  // Positions of the wavefront's first and last row.
+  const int wave_first = pos0 + wave_tok0;
+  const int wave_last = pos0 + min(nt - 1, uniform((wave * 32 + 31) / G));
+
+  // Q^T as the B operand.  Rows past the tile load its first one.
+  bf16x8_t qf[8];
+  {
+    const int64_t qrow = ((int64_t)(row0 + (row_ok ? tr : 0)) * a.hq + kh * G + hh) * D;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) {
+      const int d = KV8 ? 32 * (kk >> 1) + 16 * hi + 8 * (kk & 1) : 16 * kk + 8 * hi;
+      qf[kk] = *reinterpret_cast<const bf16x8_t*>(a.q + qrow + d);
+    }
+  }
+
+  const int ntiles = (ve - vb + KV_TILE - 1) / KV_TILE;
+  const int first_page = vb / PAGE, npages = (ve - 1) / PAGE - first_page + 1;
+  int32_t* ptab = reinterpret_cast<int32_t*>(smem + L::PTAB);
+  uint16_t* etab = reinterpret_cast<uint16_t*>(smem + L::ETAB);
+  for (int i = tid; i < npages; i += THREADS) {
+    int id = bt[sp.page(first_page + i)];
+    if ((unsigned)id >= (unsigned)a.num_blocks) {
+      raise_error(a.ws);
+      id = 0;
+    }
+    ptab[i] = id;
+    if constexpr (KV8) {
+      const int64_t e = (int64_t)id * a.hkv + kh;
+      etab[i] = (uint16_t)(a.k_exp[e] | a.v_exp[e] << 8);
+    }
+  }
+  wait_memory_complete();
+  __syncthreads();
+
+  // Copies: wave w moves page w of each tile; past the unit's last page, that
+  // page again (its keys there are masked).  LDS chunk (16 bytes) x of K row R
+  // holds the row's chunk x ^ R (bf16), or x ^ f(R) (8 bits: 8 chunks a row, the
+  // rows that LDS serves together are the slots {0-3, 8-11} of two pages).
+  constexpr int NC = PB / 1024;  // copies of a page
+  uint32_t koff[NC], voff[NC];
+#pragma unroll
+  for (int i = 0; i < NC; ++i) {
+    const int ck = 64 * i + lane;
+    if constexpr (KV8) {
+      const int rr = ck >> 3;
+      koff[i] = rr * 128 + (((ck & 7) ^ ((rr >> 1) & 7) ^ ((wave & 1) << 1)) << 4);
+      voff[i] = ck << 4;
+    } else {
+      const int rr = ck >> 4, d = ck >> 1;
+      koff[i] = rr * 256 + (((ck & 15) ^ rr) << 4);
+      voff[i] = d * 32 + (((ck & 1) ^ vt_swz(d)) << 4);
+    }
+  }
+  auto page_off = [&](int t) -> int64_t {
+    const int id = uniform(ptab[min(4 * t + wave, npages - 1)]);
+    return ((int64_t)id * a.hkv + kh) * PB;
+  };
+  const uint32_t lds_wave = lds_addr(smem) + uniform(wave) * PB;
+  auto issue_k = [&](int64_t off, int slot) {
+    const char* src = uniform_ptr(a.kc + off);
+#pragma unroll
+    for (int i = 0; i < NC; ++i) lds_copy16(src, koff[i], lds_wave + slot * L::TILE + i * 1024);
+  };
+  auto issue_v = [&](int64_t off, int slot) {
+    const char* src = uniform_ptr(a.vc + off);
+#pragma unroll
+    for (int i = 0; i < NC; ++i)
+      lds_copy16(src, voff[i], lds_wave + L::V_BASE + slot * L::TILE + i * 1024);
+  };
+  // Values that no row of the unit sees are zeroed in LDS (a probability of 0
+  // times a NaN would still be NaN).
+  auto unseen = [&](int vkey) {
+    const int key = sp.page(vkey / PAGE) * PAGE + vkey % PAGE;
+    return vkey >= ve || (pos0 - key >= sp.window && key >= sp.sinks);
+  };
+  auto zero_unseen = [&](int slot, int v0) {
+    const int pg = tid >> 6;
+    constexpr int CH = PB / 1024;  // 16-byte chunks of the page for this thread
+#pragma unroll
+    for (int c = 0; c < CH; ++c) {
+      if constexpr (KV8) {
+        u32x4_t* p = reinterpret_cast<u32x4_t*>(smem + L::V_BASE + slot * L::TILE + pg * PB) +
+                     64 * c + lane;
+        u32x4_t v = *p;
+#pragma unroll
+        for (int e = 0; e < 16; ++e)
+          if (unseen(v0 + pg * PAGE + vt_pos(e))) v[e >> 2] &= ~(0xFFu << (8 * (e & 3)));
+        *p = v;
+      } else {
+        const int d = 2 * lane + (c >> 1), h = c & 1, half = h ^ vt_swz(d);
+        u32x4_t* p = reinterpret_cast<u32x4_t*>(smem + L::V_BASE + slot * L::TILE + pg * PB +
+                                                d * 32 + (h << 4));
+        u32x4_t v = *p;
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (unseen(v0 + pg * PAGE + vt_pos(8 * half + e)))
+            v[e >> 1] &= e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+        *p = v;
+      }
+    }
+  };
+  // Tiles with such values: where some key is past the end, or before the first
+  // row's window and no sink.
+  auto has_unseen = [&](int t) {
+    const int v0 = vb + t * KV_TILE;
+    return v0 + KV_TILE > ve || sp.edge(v0, v0 + KV_TILE, 0x7FFFFFFF, pos0);
+  };
+
+  // Per-lane LDS offsets of the operands.
+  int kbase, vbase, krow[2];
+  if constexpr (KV8) {
+    // Row `col` of 32-key block j is position 4 (col / 8) + col % 4 of page
+    // 2 j + (col / 4) % 2, so that accumulator register rr of lane half hi is
+    // position rr of page 2 j + hi.
+    const int pg = (col >> 2) & 1, slot = vt_pos(4 * (col >> 3) + (col & 3));
+    kbase = pg * PB + slot * 128;
+    krow[0] = ((slot >> 1) & 7) ^ (pg << 1);
+    vbase = L::V_BASE + hi * PB + col * 16;
+  } else {
+    kbase = col * 256 + ((hi ^ (col & 15)) << 4);
+    vbase = L::V_BASE + col * 32 + ((hi ^ vt_swz(col)) << 4);
+  }
+
+  float m_run = NEG_BIG, l_run = 0.f;
+  f32x16_t o[4];
+#pragma unroll
+  for (int mb = 0; mb < 4; ++mb) o[mb] = f32x16_t{};
+  const float c = a.scale_log2;
+
+  // Scales of a tile's pages: keys' of this lane's row page, values' of page
+  // 2 j + hi.
+  auto tile_scale = [&](int t, int j, int pg, int shift) {
+    const int e = etab[min(4 * t + 2 * j + pg, npages - 1)];
+    return scale_of((e >> shift) & 0xFF);
+  };
+  // S^T = K Q^T for the tile in K slot `slot`, two 32-key accumulators.
+  auto qk = [&](f32x16_t* sacc, int slot, int t) {
+    sacc[0] = f32x16_t{};
+    sacc[1] = f32x16_t{};
+    if constexpr (KV8) {
+      const float s0 = tile_scale(t, 0, (col >> 2) & 1, 0), s1 = tile_scale(t, 1, (col >> 2) & 1, 0);
+#pragma unroll
+      for (int kk = 0; kk < 8; kk += 2) {
+        const char* kp = smem + slot * L::TILE + kbase + (((kk + hi) ^ krow[0]) << 4);
+        bf16x8_t x[2], y[2];
+        widen(*reinterpret_cast<const codes_t*>(kp), s0, &x[0], &x[1]);
+        widen(*reinterpret_cast<const codes_t*>(kp + 2 * PB), s1, &y[0], &y[1]);
+#pragma unroll
+        for (int i = 0; i < 2; ++i) {
+          sacc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[i], qf[kk + i], sacc[0], 0, 0, 0);
+          sacc[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(y[i], qf[kk + i], sacc[1], 0, 0, 0);
+        }
+      }
+    } else {
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk) {
+        const char* kp = smem + slot * L::TILE + (kbase ^ (kk << 5));
+        const bf16x8_t k0f = *reinterpret_cast<const bf16x8_t*>(kp);
+        const bf16x8_t k1f = *reinterpret_cast<const bf16x8_t*>(kp + 32 * 256);
+        sacc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k0f, qf[kk], sacc[0], 0, 0, 0);
+        sacc[1] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(k1f, qf[kk], sacc[1], 0, 0, 0);
+      }
+    }
+  };
+  // Masks the scores of a tile starting at virtual key v0.
+  auto mask = [&](f32x16_t* sacc, int v0) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+#pragma unroll
+      for (int rr = 0; rr < 16; ++rr) {
+        const int pg = KV8 ? 2 * j + hi : 2 * j + (rr >> 3);
+        const int slot = KV8 ? vt_pos(rr) : 8 * ((rr >> 2) & 1) + 4 * hi + (rr & 3);
+        const int vkey = v0 + pg * PAGE + slot, key = sp.page(v0 / PAGE + pg) * PAGE + slot;
+        sacc[j][rr] = vkey < ve && sp.sees(pos, key) ? sacc[j][rr] : -__builtin_inff();
+      }
+  };
+  auto rowmax = [&](const f32x16_t* sacc) {
+    float m4[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      m4[i] = fmaxf(sacc[i >> 1][8 * (i & 1)], sacc[i >> 1][8 * (i & 1) + 1]);
+#pragma unroll
+    for (int rr = 2; rr < 8; ++rr)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) m4[i] = fmaxf(m4[i], sacc[i >> 1][8 * (i & 1) + rr]);
+    return fmaxf(fmaxf(m4[0], m4[1]), fmaxf(m4[2], m4[3]));
+  };
+  auto rebase = [&](float mx) {
+    const float m_tile = max_xor32(mx) * c;
+    if (__builtin_amdgcn_ballot_w64(m_tile > m_run + RESCALE_LOG2)) {
+      const float m_new = m_tile > m_run + RESCALE_LOG2 ? m_tile : m_run;
+      const float alpha = fexp2(m_run - m_new);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int mb = 0; mb < 4; ++mb) o[mb] *= alpha;
+    }
+  };
+  // P^T = exp2(S^T c - m) as the B operands of the 16-key steps k0 .. k1 - 1.
+  auto probs = [&](f32x16_t* sacc, bf16x8_t* pf, int k0, int k1) {
+#pragma unroll
+    for (int kk = k0; kk < k1; ++kk) {
+      u32x4_t pk;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int x = 8 * (kk & 1) + 2 * w;
+        float p0 = fexp2(__builtin_fmaf(sacc[kk >> 1][x], c, -m_run));
+        float p1 = fexp2(__builtin_fmaf(sacc[kk >> 1][x + 1], c, -m_run));
+        if constexpr (OUT32) {
+          l_run += p0 + p1;
+          pk[w] = cut(p0, p1);
+          sacc[kk >> 1][x] = p0;
+          sacc[kk >> 1][x + 1] = p1;
+        } else {
+          pk[w] = pack_bf16(p0, p1);
+        }
+      }
+      pf[kk] = __builtin_bit_cast(bf16x8_t, pk);
+    }
+  };
+  // The next term of the probabilities (fp32 output): what the terms before left.
+  auto next_term = [&](f32x16_t* sacc, bf16x8_t* pf, bool last) {
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      u32x4_t pk;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int x = 8 * (kk & 1) + 2 * w;
+        float p0 = sacc[kk >> 1][x], p1 = sacc[kk >> 1][x + 1];
+        pk[w] = last ? pack_bf16(p0, p1) : cut(p0, p1);
+        sacc[kk >> 1][x] = p0;
+        sacc[kk >> 1][x + 1] = p1;
+      }
+      pf[kk] = __builtin_bit_cast(bf16x8_t, pk);
+    }
+  };
+  // Row sum of the rounded probabilities (this half of the row).
+  auto rowsum = [&](const bf16x8_t* pf) {
+    if constexpr (OUT32) return;
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      const u32x4_t pk = __builtin_bit_cast(u32x4_t, pf[kk]);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) l_run = dot2(pk[w], 0x3F803F80u, l_run);  // two bf16 1.0
+    }
+  };
+  // O^T += V^T P^T over the 32-key halves j0 .. j1 - 1 of the tile in V slot `slot`.
+  auto pv = [&](const bf16x8_t* pf, int slot, int t, int j0, int j1) {
+#pragma unroll
+    for (int j = j0; j < j1; ++j) {
+      if constexpr (KV8) {
+        const float vs = tile_scale(t, j, hi, 8);
+#pragma unroll
+        for (int mb = 0; mb < 4; ++mb) {
+          bf16x8_t vf[2];
+          widen(*reinterpret_cast<const codes_t*>(smem + vbase + slot * L::TILE + 2 * j * PB + mb * 512),
+                vs, &vf[0], &vf[1]);
+#pragma unroll
+          for (int i = 0; i < 2; ++i)
+            o[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf[i], pf[2 * j + i], o[mb], 0, 0, 0);
+        }
+      } else {
+#pragma unroll
+        for (int kk = 2 * j; kk < 2 * j + 2; ++kk)
+#pragma unroll
+          for (int mb = 0; mb < 4; ++mb) {
+            const bf16x8_t vf = *reinterpret_cast<const bf16x8_t*>(smem + vbase + slot * L::TILE +
+                                                                   kk * PB + mb * 1024);
+            o[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[kk], o[mb], 0, 0, 0);
+          }
+      }
+    }
+  };
+
+  // Tiles 0 (K and V) and 1 (K) in flight, then S_0.
+  int64_t off_next = page_off(0);
+  issue_k(off_next, 0);
+  issue_v(off_next, 0);
+  if (ntiles > 1) {
+    off_next = page_off(1);
+    issue_k(off_next, 1);
+  }
+  wait_memory_complete();
+  __syncthreads();
+  if (has_unseen(0)) {
+    zero_unseen(0, vb);
+    __syncthreads();
+  }
+  f32x16_t sa[2], sb[2];
+  if (wave_active) {
+    qk(sa, 0, 0);
+    if (vb + KV_TILE > ve || sp.edge(vb, vb + KV_TILE, wave_first, wave_last)) mask(sa, vb);
+    rebase(rowmax(sa));
+  }
+  __syncthreads();  // K slot 0 is refilled below
+
+  // Step j: loads of K_{j+2} and V_{j+1} go out; S_{j+1} = K_{j+1} Q^T beside the
+  // first half of tile j's exponentials; the second half beside the first half of
+  // O += V_j P_j; the row maxima of tile j + 1 beside the rest.
+  auto step = [&](int j, f32x16_t* cur, f32x16_t* nxt, auto parity) {
+    constexpr int PAR = decltype(parity)::value;  // j & 1
+    const bool more = j + 1 < ntiles;
+    if (more) issue_v(off_next, PAR ^ 1);
+    if (j + 2 < ntiles) {
+      off_next = page_off(j + 2);
+      issue_k(off_next, PAR);
+    }
+    if (wave_active) {
+      bf16x8_t pf[4];
+      // On the last tile this reads a stale slot; the result is not used.
+      qk(nxt, PAR ^ 1, j + 1);
+      probs(cur, pf, 0, 2);
+      __builtin_amdgcn_s_setprio(1);
+      probs(cur, pf, 2, 4);
+      pv(pf, PAR, j, 0, 1);
+      __builtin_amdgcn_sched_barrier(0);
+      pv(pf, PAR, j, 1, 2);
+      rowsum(pf);
+      if constexpr (OUT32) {
+        next_term(cur, pf, false);
+        pv(pf, PAR, j, 0, 2);
+        next_term(cur, pf, true);
+        pv(pf, PAR, j, 0, 2);
+      }
+      float mx = rowmax(nxt);
+      __builtin_amdgcn_s_setprio(0);
+      if (more) {
+        const int v1 = vb + (j + 1) * KV_TILE;
+        if (v1 + KV_TILE > ve || sp.edge(v1, v1 + KV_TILE, wave_first, wave_last)) {
+          mask(nxt, v1);
+          mx = rowmax(nxt);
+        }
+        rebase(mx);
+      }
+    }
+    wait_memory_complete();
+    __syncthreads();
+    if (more && has_unseen(j + 1)) {
+      zero_unseen(PAR ^ 1, vb + (j + 1) * KV_TILE);
+      __syncthreads();
+    }
+  };
+  const std::integral_constant<int, 0> even;
+  const std::integral_constant<int, 1> odd;
+  for (int j = 0; j < ntiles; j += 2) {
+    step(j, sa, sb, even);
+    if (j + 1 < ntiles) step(j + 1, sb, sa, odd);
+  }
+
+  l_run = sum_xor32(l_run);
+  const int rows = nt * G;
+  // o[mb][rr] = O[row][32 mb + 8 (rr / 4) + 4 hi + rr % 4]
+  if (nsplits == 1) {
+    if (row_ok) {
+      const float inv = 1.f / l_run;
+      const int64_t orow = ((int64_t)(row0 + tr) * a.hq + kh * G + hh) * D;
+#pragma unroll
+      for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+        for (int g4 = 0; g4 < 4; ++g4)
+          store4(a, orow + mb * 32 + 8 * g4 + 4 * hi, o[mb][4 * g4] * inv,
+                 o[mb][4 * g4 + 1] * inv, o[mb][4 * g4 + 2] * inv, o[mb][4 * g4 + 3] * inv);
+    }
+    return;
+  }
+
+  // Partial result, in the layout that prefill_merge reads.
+  const int slot_floats = slot_floats_for(rows);
+  const Slots sl = group_slots(a.ws, f[DLFP_W_WSGROUP], nsplits, slot_floats);
+  const int my = f[DLFP_W_SPLIT] * slot_floats;
+  if (row_ok) {
+#pragma unroll
+    for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+      for (int g4 = 0; g4 < 4; ++g4) {
+        const f32x4_t v = {o[mb][4 * g4], o[mb][4 * g4 + 1], o[mb][4 * g4 + 2],
+                           o[mb][4 * g4 + 3]};
+        pstore4(sl, my + ((4 * mb + g4) * rows + r) * 8 + 4 * hi, v);
+      }
+    if (hi == 0) {
+      pstore1(sl, my + rows * D + r, m_run);
+      pstore1(sl, my + rows * D + rows + r, l_run);
+    }
+  }
+  wait_memory_complete();
+  __syncthreads();  // every wave of the unit has completed its stores
+  const int grp = f[DLFP_W_GROUP];
+  if (tid == 0) *flag = arrive(a.ws, grp) == nsplits - 1;
+  __syncthreads();
+  if (!*flag) return;
+  if (rows > 64)
+    prefill_merge<G, 2>(a, sl, slot_floats, nsplits, rows, row0, kh);
+  else if (rows > 32)
+    prefill_merge<G, 4>(a, sl, slot_floats, nsplits, rows, row0, kh);
+  else
+    prefill_merge<G, 8>(a, sl, slot_floats, nsplits, rows, row0, kh);
+  if (tid == 0)
+    __hip_atomic_store(group_counter(a.ws, grp), 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// ---------------------------------------------------------------- decode
+
+// Per wavefront of a decode unit: a key slot and a value slot of one block each
+// (32 keys of bf16 pages, 64 of 8-bit ones), ids and exponents of its pages.
+constexpr int SLOT = 8192;
+template <bool KV8, int NW>
+constexpr int decode_wave_lds() {
+  return 2 * SLOT + ((DEC_PTAB / NW + 4) * (KV8 ? 6 : 4) + 63) / 64 * 64;
+}
+
+// Decode unit of a workgroup of NW wavefronts: wavefront w takes blocks w, w + NW,
+// ... of the unit; their results meet in LDS, those of split ranges in memory.
+// The unit's g heads are columns 0-7 of 16x16 products and, with the second term
+// of the probabilities, columns 8-15.  Lane l owns column l % 16; its group
+// q = l / 16 owns, of 8-bit pages, the 16 keys of page q of the block, of bf16
+// pages the eight at positions 8 (q / 2) .. of page q % 2.
+template <int G, bool KV8, bool OUT32, int NW>
+__device__ void decode_unit(const Args& a, const int32_t* rec, char* smem, int* flag) {
+  static_assert(G >= 1 && G <= 8, "heads");
+  constexpr int PB = page_bytes<KV8>();
+  constexpr int BP = SLOT / PB;       // pages of a block
+  constexpr int NCH = KV8 ? 4 : 2;    // 16-key products of a block
+  constexpr int NC = PB / 1024;       // copies of a page
+  const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
+  char* wl = smem + wave * decode_wave_lds<KV8, NW>();
+  const int col = lane & 15, gq = lane >> 4, head = col & 7;
+  const record_t f = load_record(rec);
+  const int s = f[DLFP_W_SEQ], kh = f[DLFP_W_KVHEAD];
+  const int vb = f[DLFP_W_KVBEGIN], ve = f[DLFP_W_KVEND];
+  const int nsplits = f[DLFP_W_NSPLITS];
+  const int tok = f[DLFP_W_QROW0], pos = f[DLFP_W_QPOS0];
+  const Span sp = span_of(f);
+  const int32_t* bt = a.block_table + (int64_t)s * a.max_blocks;
+  int32_t* ptab = reinterpret_cast<int32_t*>(wl + 2 * SLOT);
+  uint16_t* etab = reinterpret_cast<uint16_t*>(ptab + DEC_PTAB / NW + 4);
+
+  const int first_page = vb / PAGE;
+  const int npages = (ve + PAGE - 1) / PAGE - first_page, nblocks = (npages + BP - 1) / BP;
+  const int mine = nblocks > wave ? (nblocks - wave + NW - 1) / NW : 0;
+  // Page h of this wavefront's block i (past the unit's last page, that page);
+  // pages that the block has.
+  auto page_of = [&](int i, int h) { return min(BP * (wave + NW * i) + h, npages - 1); };
+  auto pages_in = [&](int i) { return min(BP, npages - BP * (wave + NW * i)); };
+
+  // Ids (and exponents) of the wavefront's pages; the queries as the B operand.
+  for (int x = lane; x < BP * mine; x += 64) {
+    int id = bt[sp.page(first_page + page_of(x / BP, x % BP))];
+    if ((unsigned)id >= (unsigned)a.num_blocks) {
+      raise_error(a.ws);
+      id = 0;
+    }
+    ptab[x] = id;
+    if constexpr (KV8) {
+      const int64_t e = (int64_t)id * a.hkv + kh;
+      etab[x] = (uint16_t)(a.k_exp[e] | a.v_exp[e] << 8);
+    }
+  }
+  bf16x8_t qb[4];
+  {
+    const uint16_t* qp = a.q + ((int64_t)tok * a.hq + kh * G + min(head, G - 1)) * D;
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      const int d = KV8 ? 64 * (kk >> 1) + 16 * gq + 8 * (kk & 1) : 32 * kk + 8 * gq;
+      const u32x4_t v = *reinterpret_cast<const u32x4_t*>(qp + d);
+      qb[kk] = __builtin_bit_cast(bf16x8_t, head < G ? v : u32x4_t{0u, 0u, 0u, 0u});
+    }
+  }
+  wait_memory_complete();
+  wave_sync();
+
+  // Copies.  LDS chunk x of K row R of page h holds the row's chunk x ^ R ^ 8 h
+  // (bf16), x ^ (R / 2 % 2) ^ 2 h (8 bits); V^T rows of bf16 pages (32 bytes) keep
+  // their halves swapped when vt_swz(d), those of 8-bit pages are as stored.
+  uint32_t kofs[NC], vofs[NC];
+#pragma unroll
+  for (int j = 0; j < NC; ++j) {
+    const int ck = 64 * j + lane;
+    if constexpr (KV8) {
+      const int R = ck >> 3;
+      kofs[j] = R * 128 + (((ck & 7) ^ ((R >> 1) & 1)) << 4);
+      vofs[j] = ck << 4;
+    } else {
+      const int R = ck >> 4, d = ck >> 1;
+      kofs[j] = R * 256 + (((ck & 15) ^ R) << 4);
+      vofs[j] = d * 32 + (((ck & 1) ^ vt_swz(d)) << 4);
+    }
+  }
+  const uint32_t lds_wave = (uint32_t)uniform((int)lds_addr(wl));
+  auto issue_k = [&](int i) {
+    const int n = pages_in(i);
+#pragma unroll
+    for (int h = 0; h < BP; ++h) {
+      if (h >= n) break;
+      const char* src = a.kc + ((int64_t)uniform(ptab[BP * i + h]) * a.hkv + kh) * PB;
+      const uint32_t x = KV8 ? h << 5 : h << 7;
+#pragma unroll
+      for (int j = 0; j < NC; ++j) lds_copy16_nt(src + (kofs[j] ^ x), lds_wave + h * PB + j * 1024);
+    }
+  };
+  auto issue_v = [&](int i) {
+    const int n = pages_in(i);
+#pragma unroll
+    for (int h = 0; h < BP; ++h) {
+      if (h >= n) break;
+      const char* src = a.vc + ((int64_t)uniform(ptab[BP * i + h]) * a.hkv + kh) * PB;
+#pragma unroll
+      for (int j = 0; j < NC; ++j)
+        lds_copy16_nt(src + vofs[j], lds_wave + SLOT + h * PB + j * 1024);
+    }
+  };
+  if (mine > 0) {
+    issue_k(0);
+    issue_v(0);
+  }
+
+  float m_run = NEG_BIG, l_run = 0.f;
+  f32x4_t o[8];
+#pragma unroll
+  for (int mb = 0; mb < 8; ++mb) o[mb] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+  const float c = a.scale_log2;
+  // Rows of the K operand: 8 bits, product b: row r is position 4 b + r % 4 of
+  // page r / 4; bf16: position 8 (r / 8) + 4 b + r % 4 of page r / 4 % 2.  Rows
+  // 4 q .. of the accumulators are then the keys of lane group q.
+  const int kpage = KV8 ? col >> 2 : (col >> 2) & 1;
+  int krow[NCH], kxor[NCH];
+#pragma unroll
+  for (int b = 0; b < NCH; ++b) {
+    const int R = vt_pos(KV8 ? 4 * b + (col & 3) : 8 * (col >> 3) + 4 * b + (col & 3));
+    krow[b] = kpage * PB + R * (KV8 ? 128 : 256);
+    kxor[b] = KV8 ? ((R >> 1) & 1) ^ (kpage << 1) : R ^ (kpage << 3);
+  }
+  const int vpage = KV8 ? gq : gq & 1;  // page of this lane group's keys
+  // Slot of its first key of product b.
+  auto slot_of = [&](int b) { return vt_pos(KV8 ? 4 * b : 8 * (gq >> 1) + 4 * b); };
+  const int vbyte = SLOT + vpage * PB + (KV8 ? col * 16 : col * 32 + (((gq >> 1) ^ vt_swz(col)) << 4));
+
+  for (int i = 0; i < mine; ++i) {
+    const int v0 = vb + BP * PAGE * (wave + NW * i);  // first virtual key of the block
+    const int n = pages_in(i);
+    const bool more = i + 1 < mine, full = n == BP;
+    const bool edge = v0 + BP * PAGE > ve || sp.edge(v0, v0 + BP * PAGE, pos, pos);
+    // In flight, oldest first: this block's keys, its values (eight copies each
+    // of a full block; others are the unit's last).
+    if (full)
+      wait_copies<8>();
+    else
+      wait_copies<0>();
+    float sc[4 * NCH];
+    {
+      f32x4_t sacc[NCH];
+#pragma unroll
+      for (int b = 0; b < NCH; ++b) sacc[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+      if constexpr (KV8) {
+        const float ks = scale_of(etab[BP * i + kpage] & 0xFF);
+        codes_t kc[NCH][2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int b = 0; b < NCH; ++b)
+            kc[b][j] = *reinterpret_cast<const codes_t*>(wl + krow[b] + (((4 * j + gq) ^ kxor[b]) << 4));
+#pragma unroll
+        for (int j = 0; j < 2; ++j)
+#pragma unroll
+          for (int b = 0; b < NCH; ++b) {
+            bf16x8_t x[2];
+            widen(kc[b][j], ks, &x[0], &x[1]);
+            sacc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[0], qb[2 * j], sacc[b], 0, 0, 0);
+            sacc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[1], qb[2 * j + 1], sacc[b], 0, 0, 0);
+          }
+      } else {
+        bf16x8_t kf[NCH][4];
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+          for (int b = 0; b < NCH; ++b)
+            kf[b][kk] =
+                *reinterpret_cast<const bf16x8_t*>(wl + krow[b] + (((4 * kk + gq) ^ kxor[b]) << 4));
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+          for (int b = 0; b < NCH; ++b)
+            sacc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[b][kk], qb[kk], sacc[b], 0, 0, 0);
+      }
+#pragma unroll
+      for (int x = 0; x < 4 * NCH; ++x) sc[x] = sacc[x >> 2][x & 3];
+    }
+    wait_lds();  // the key slot is free
+    if (more) issue_k(i + 1);
+    const bool next_full = more && pages_in(i + 1) == BP;
+    // Position and virtual key of slot 0 of this lane group's page.
+    const int base = sp.page(v0 / PAGE + vpage) * PAGE, vbase = v0 + vpage * PAGE;
+    if (edge) {
+#pragma unroll
+      for (int x = 0; x < 4 * NCH; ++x) {
+        const int slot = slot_of(x >> 2) + (x & 3);
+        sc[x] = vbase + slot < ve && sp.sees(pos, base + slot) ? sc[x] : -__builtin_inff();
+      }
+    }
+    float mx = -__builtin_inff();
+#pragma unroll
+    for (int x = 0; x < 4 * NCH; ++x) mx = fmaxf(mx, sc[x]);
+    const float m_tile = max_xor32(max_xor16(mx)) * c;
+    if (__builtin_amdgcn_ballot_w64(m_tile > m_run + RESCALE_LOG2)) {
+      const float m_new = m_tile > m_run + RESCALE_LOG2 ? m_tile : m_run;
+      const float alpha = fexp2(m_run - m_new);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int mb = 0; mb < 8; ++mb) o[mb] *= alpha;
+    }
+    // P^T: this lane's keys of its column, its term of each, the B operands.
+    u32x4_t pk[NCH / 2], third[NCH / 2];
+#pragma unroll
+    for (int w = 0; w < 2 * NCH; ++w) {
+      float e0 = fexp2(__builtin_fmaf(sc[2 * w], c, -m_run));
+      float e1 = fexp2(__builtin_fmaf(sc[2 * w + 1], c, -m_run));
+      l_run += e0 + e1;
+      if constexpr (OUT32) {
+        const uint32_t t0 = cut(e0, e1), t1 = cut(e0, e1);
+        pk[w >> 2][w & 3] = col >= 8 ? t1 : t0;
+        third[w >> 2][w & 3] = col >= 8 ? 0u : pack_bf16(e0, e1);
+      } else {
+        pk[w >> 2][w & 3] = pack_term(e0, e1, col >= 8);
+      }
+    }
+    // The values; behind them the next block's keys may be in flight.
+    if (next_full)
+      wait_copies<8>();
+    else
+      wait_copies<0>();
+    if (edge) {
+      // Values that the token does not see are zeroed (a probability of 0 times
+      // a NaN would still be NaN).
+#pragma unroll
+      for (int j = 0; j < 8; ++j) {
+        const int pg = j / NC, ck = 64 * (j % NC) + lane;
+        const int vkey = v0 + pg * PAGE, key = sp.page(v0 / PAGE + pg) * PAGE;
+        u32x4_t* p = reinterpret_cast<u32x4_t*>(wl + SLOT + pg * PB + ck * 16);
+        u32x4_t v = *p;
+        if constexpr (KV8) {
+#pragma unroll
+          for (int e = 0; e < 16; ++e) {
+            const int slot = vt_pos(e);
+            if (vkey + slot >= ve || !sp.sees(pos, key + slot))
+              v[e >> 2] &= ~(0xFFu << (8 * (e & 3)));
+          }
+        } else {
+          const int half = (ck & 1) ^ vt_swz(ck >> 1);
+#pragma unroll
+          for (int e = 0; e < 8; ++e) {
+            const int slot = vt_pos(8 * half + e);
+            if (vkey + slot >= ve || !sp.sees(pos, key + slot))
+              v[e >> 1] &= e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+          }
+        }
+        *p = v;
+      }
+      wave_sync();
+    }
+    // O^T += V^T P^T, eight blocks of 16 dims.
+    if constexpr (KV8) {
+      const float vs = scale_of(etab[BP * i + vpage] >> 8);
+      codes_t vc[8];
+#pragma unroll
+      for (int mb = 0; mb < 8; ++mb)
+        vc[mb] = *reinterpret_cast<const codes_t*>(wl + vbyte + mb * 256);
+#pragma unroll
+      for (int mb = 0; mb < 8; ++mb) {
+        bf16x8_t x[2];
+        widen(vc[mb], vs, &x[0], &x[1]);
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          o[mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(x[h], __builtin_bit_cast(bf16x8_t, pk[h]),
+                                                          o[mb], 0, 0, 0);
+          if constexpr (OUT32)
+            o[mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+                x[h], __builtin_bit_cast(bf16x8_t, third[h]), o[mb], 0, 0, 0);
+        }
+      }
+    } else {
+      bf16x8_t vf[8];
+#pragma unroll
+      for (int mb = 0; mb < 8; ++mb)
+        vf[mb] = *reinterpret_cast<const bf16x8_t*>(wl + vbyte + mb * 512);
+#pragma unroll
+      for (int mb = 0; mb < 8; ++mb) {
+        o[mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vf[mb], __builtin_bit_cast(bf16x8_t, pk[0]),
+                                                        o[mb], 0, 0, 0);
+        if constexpr (OUT32)
+          o[mb] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(
+              vf[mb], __builtin_bit_cast(bf16x8_t, third[0]), o[mb], 0, 0, 0);
+      }
+    }
+    wait_lds();  // the value slot is free
+    if (more) issue_v(i + 1);
+  }
+
+  // Each lane group holds a quarter of its head's keys, a head's two columns a
+  // term each (both the same row sum).  Then the wavefronts' results are added
+  // through LDS: quad (head, 4 mb + gq) holds dims 16 mb + 4 gq .. + 3.
+  const float l_tot = sum_xor32(sum_xor16(l_run));
+#pragma unroll
+  for (int mb = 0; mb < 8; ++mb)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) o[mb][i] = sum_xor8(o[mb][i]);
+  wait_memory_complete();
+  __syncthreads();  // every wavefront is done with its slots
+  f32x4_t* red = reinterpret_cast<f32x4_t*>(smem);
+  float* stat = reinterpret_cast<float*>(smem + NW * G * 512);  // m[NW][G], l[NW][G]
+  auto at = [](int w, int h, int q) { return (w * G + h) * 32 + (q ^ ((h & 7) << 2)); };
+  if (col < G) {
+#pragma unroll
+    for (int mb = 0; mb < 8; ++mb) red[at(wave, col, 4 * mb + gq)] = o[mb];
+    if (gq == 0) {
+      stat[wave * G + col] = m_run;
+      stat[NW * G + wave * G + col] = l_tot;
+    }
+  }
+  __syncthreads();
+  const int slot_floats = slot_floats_for(G);
+  const Slots sl = group_slots(a.ws, f[DLFP_W_WSGROUP], nsplits, slot_floats);
+  const int my = f[DLFP_W_SPLIT] * slot_floats;
+  // Thread: quad q4 of head h, and of heads 2 NW further with few wavefronts.
+  const int q4 = tid & 31;
+#pragma unroll
+  for (int h0 = 0; h0 < G; h0 += 2 * NW) {
+    const int h = h0 + (tid >> 5);
+    if (h >= G) continue;
+    float M = NEG_BIG, L = 0.f;
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < NW; ++w) M = fmaxf(M, stat[w * G + h]);
+#pragma unroll
+    for (int w = 0; w < NW; ++w) {
+      const float e = fexp2(stat[w * G + h] - M);
+      L += e * stat[NW * G + w * G + h];
+      acc += e * red[at(w, h, q4)];
+    }
+    if (nsplits == 1) {
+      const float inv = 1.f / L;
+      store4(a, ((int64_t)tok * a.hq + kh * G + h) * D + 4 * q4, acc[0] * inv, acc[1] * inv,
+             acc[2] * inv, acc[3] * inv);
+    } else {
+      pstore4(sl, my + h * D + 4 * q4, acc);
+      if (q4 == 0) {
+        pstore1(sl, my + G * D + h, M);
+        pstore1(sl, my + G * D + G + h, L);
+      }
+    }
+  }
+  if (nsplits == 1) return;
+
+  // The last arriver merges the splits in order.
+  const int grp = f[DLFP_W_GROUP];
+  wait_memory_complete();
+  __syncthreads();  // every wave of the unit has completed its stores
+  if (tid == 0) *flag = arrive(a.ws, grp) == nsplits - 1;
+  __syncthreads();
+  if (!*flag) return;
+#pragma unroll
+  for (int h0 = 0; h0 < G; h0 += 2 * NW) {
+    const int h = h0 + (tid >> 5);
+    if (h >= G) continue;
+    // Batches of NB splits: all loads of a batch go out before any is used.
+    constexpr int NB = 16;
+    float M = NEG_BIG, L = 0.f;
+    f32x4_t acc = {0.f, 0.f, 0.f, 0.f};
+    for (int j = 0; j < nsplits; j += NB) {
+      float mj[NB], lj[NB];
+      f32x4_t x[NB];
+#pragma unroll
+      for (int u = 0; u < NB; ++u) {
+        const int b = (j + u) * slot_floats;
+        mj[u] = pload1(sl, b + G * D + h);
+        lj[u] = pload1(sl, b + G * D + G + h);
+        x[u] = pload4(sl, b + h * D + 4 * q4);
+      }
+      float mn = M;
+#pragma unroll
+      for (int u = 0; u < NB; ++u)
+        if (j + u < nsplits) mn = fmaxf(mn, mj[u]);
+      const float rs = fexp2(M - mn);
+      M = mn;
+      L *= rs;
+      acc *= rs;
+#pragma unroll
+      for (int u = 0; u < NB; ++u) {
+        const float e = j + u < nsplits ? fexp2(mj[u] - mn) : 0.f;
+        L += e * lj[u];
+        acc += e * x[u];
+      }
+    }
+    const float inv = 1.f / L;
+    store4(a, ((int64_t)tok * a.hq + kh * G + h) * D + 4 * q4, acc[0] * inv, acc[1] * inv,
+           acc[2] * inv, acc[3] * inv);
+  }
+  if (tid == 0)
+    __hip_atomic_store(group_counter(a.ws, grp), 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
+// ---------------------------------------------------------------- kernels
+
+template <bool KV8>
+constexpr int window_lds() {
+  constexpr int pre = PreLds<KV8>::BYTES, dec = 4 * decode_wave_lds<KV8, 4>();
+  return pre > dec ? pre : dec;
+}
+
+// Prefill units, then (with `lead`, from the middle on) decode units of a
+// workgroup each.
+template <int G, bool KV8, bool OUT32>
+__global__ __launch_bounds__(THREADS, 2) void window_kernel(Args a) {
+  __shared__ __attribute__((aligned(16))) char smem[window_lds<KV8>()];
+  __shared__ int flag;
+  const int b = blockIdx.x, np = a.num_prefill, L = a.lead, DL = a.decode_lead;
+  const int u = b < L ? xcd_remap(b, np)
+                      : b < L + DL ? L - 1 - b : b < np + DL ? xcd_remap(b - DL, np) : np - 1 - b;
+  if (u >= 0)
+    prefill_unit<G, KV8, OUT32>(a, load_record(a.work + (int64_t)u * DLFP_WORK_INTS), smem, &flag);
+  else
+    decode_unit<G, KV8, OUT32, 4>(a, a.work + (int64_t)(np - 1 - u) * DLFP_WORK_INTS, smem, &flag);
+}
+
+template <int G, bool KV8, bool OUT32, int NW>
+__global__ __launch_bounds__(NW * 64, 2) void window_decode_kernel(Args a) {
+  __shared__ __attribute__((aligned(16))) char smem[NW * decode_wave_lds<KV8, NW>()];
+  __shared__ int flag;
+  decode_unit<G, KV8, OUT32, NW>(a, a.work + (int64_t)blockIdx.x * DLFP_WORK_INTS, smem, &flag);
+}
+
+template <int G, bool KV8, bool OUT32>
+hipError_t launch_window(const Args& a, int nw, hipStream_t stream) {
+  if (a.num_prefill > 0)
+    window_kernel<G, KV8, OUT32><<<a.num_units, THREADS, 0, stream>>>(a);
+  else if (nw == 8)
+    window_decode_kernel<G, KV8, OUT32, 8><<<a.num_units, 8 * 64, 0, stream>>>(a);
+  else
+    window_decode_kernel<G, KV8, OUT32, 4><<<a.num_units, 4 * 64, 0, stream>>>(a);
+  return hipGetLastError();
+}
+
+template <int G, bool KV8>
+hipError_t launch_window(const Args& a, int nw, hipStream_t stream) {
+  return a.out_f32 ? launch_window<G, KV8, true>(a, nw, stream)
+                   : launch_window<G, KV8, false>(a, nw, stream);
+}
+
+// Validation and launch shared by the two entry points.
+template <bool KV8>
+int attention_window(const dlfp_dims* dims, const dlfp_meta* meta, const int32_t* d_work,
+                     const int32_t* d_block_table, int32_t max_blocks, int32_t num_blocks,
+                     const void* q, const void* k_cache, const void* v_cache,
+                     const uint8_t* k_exp, const uint8_t* v_exp, float scale, void* out,
+                     int32_t out_dtype, void* workspace, size_t workspace_bytes,
+                     hipStream_t stream) {
+  int g = 0;
+  const int st = dlfp::check_dims(dims, &g);
+  if (st != DLFP_OK) return st;
+  if (!meta) return DLFP_EINVAL;
+  if (out_dtype != 0 && out_dtype != 1) return DLFP_EINVAL;
+  if (!(scale > 0.f) || !(scale < 3.0e38f)) return DLFP_EINVAL;
+  if (meta->num_units < 0 || meta->num_prefill_units < 0 ||
+      meta->num_prefill_units > meta->num_units || meta->num_groups < 0 ||
+      meta->num_groups > DLFP_MAX_GROUPS)
+    return DLFP_EINVAL;
+  if (meta->num_units == 0) return DLFP_OK;
+  // The records of dlfp_build_varlen_meta have other fields.
+  if (meta->decode_pages_in_flight != DLFP_WINDOW_META) return DLFP_EINVAL;
+  if (meta->prefill_lead_units < 0 || meta->prefill_lead_units > meta->num_prefill_units)
+    return DLFP_EINVAL;
+  if (!d_work || !d_block_table || !q || !k_cache || !v_cache || !out || !workspace)
+    return DLFP_EINVAL;
+  if (KV8 && (!k_exp || !v_exp)) return DLFP_EINVAL;
+  if (max_blocks <= 0 || num_blocks <= 0) return DLFP_EINVAL;
+  if ((int64_t)workspace_bytes < meta->workspace_bytes ||
+      workspace_bytes < (size_t)DLFP_WORKSPACE_PARTIALS)
+    return DLFP_ENOSPC;
+  Args a;
+  a.work = d_work;
+  a.block_table = d_block_table;
+  a.q = static_cast<const uint16_t*>(q);
+  a.kc = static_cast<const char*>(k_cache);
+  a.vc = static_cast<const char*>(v_cache);
+  a.k_exp = k_exp;
+  a.v_exp = v_exp;
+  a.out = out;
+  a.ws = static_cast<float*>(workspace);
+  a.max_blocks = max_blocks;
+  a.num_blocks = num_blocks;
+  a.hq = dims->num_q_heads;
+  a.hkv = dims->num_kv_heads;
+  a.num_units = meta->num_units;
+  a.num_prefill = meta->num_prefill_units;
+  a.out_f32 = out_dtype;
+  a.scale_log2 = scale * LOG2E;
+  // Beside more prefill units than compute units the decode units start after
+  // one prefill unit for each of those.
+  const int decode_units = a.num_units - a.num_prefill;
+  a.lead = meta->prefill_lead_units;
+  a.decode_lead = a.lead < a.num_prefill ? std::min(decode_units, 256) / 8 * 8 : 0;
+  if (a.decode_lead == 0) a.lead = a.num_prefill;
+  const int nw = a.num_units > 4 * 256 ? 4 : 8;
+  (void)hipGetLastError();
+  hipError_t e;
+  switch (g) {
+    case 1: e = launch_window<1, KV8>(a, nw, stream); break;
+    case 2: e = launch_window<2, KV8>(a, nw, stream); break;
+    case 4: e = launch_window<4, KV8>(a, nw, stream); break;
+    default: e = launch_window<8, KV8>(a, nw, stream); break;
+  }
+  return e == hipSuccess ? DLFP_OK : DLFP_EHIP;
+}
+
+}  // namespace
+
+#endif  // DLFP_ATTENTION_WINDOW_H

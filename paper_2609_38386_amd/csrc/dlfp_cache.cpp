@@ -1,0 +1,268 @@
+// Host half of dlfp_cache.h: the checks of the rotating appends, and the metadata
+// and work list of attention with a window.  Plain C++ (no HIP calls), so it also
+// builds with a host compiler and its sanitizers.
+#include <algorithm>
+#include <cstdint>
+#include <cstring>
+#include <limits>
+#include <new>
+#include <vector>
+
+#include "dlfp_cache.h"
+#include "dlfp_internal.h"
+
+namespace {
+
+constexpr int64_t PAGE = DLFP_PAGE_SIZE;
+constexpr int64_t I32_MAX = std::numeric_limits<int32_t>::max();
+
+int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+int64_t round_up(int64_t a, int64_t b) { return ceil_div(a, b) * b; }
+// Floats of one partial result: O (rows x 128), m[rows], l[rows], padded to 256 bytes.
+int64_t slot_floats(int64_t rows) { return round_up(rows * (DLFP_HEAD_DIM + 2), 64); }
+
+struct Unit {
+  int32_t f[DLFP_WORK_INTS];
+};
+static_assert(sizeof(Unit) == DLFP_WORK_INTS * sizeof(int32_t), "work records are packed");
+
+// The rows of a unit before its keys are split, and the keys that it reads.
+struct Rows {
+  int32_t seq, t0, nt;
+  int64_t gap;   // pages left out
+  int64_t keys;  // keys read, the gap left out
+};
+
+bool aligned16(const void* p) { return reinterpret_cast<uintptr_t>(p) % 16 == 0; }
+bool good_stride(int64_t ld, int64_t heads) {
+  return ld % 8 == 0 && ld >= heads * DLFP_HEAD_DIM;
+}
+
+}  // namespace
+
+namespace dlfp {
+
+int check_rope_append(const dlfp_dims* dims, const dlfp_rope* rope, int32_t num_tokens,
+                      const int32_t* positions, const int32_t* slot_mapping, const void* q,
+                      int64_t ldq, const void* k_new, int64_t ldk, const void* v_new, int64_t ldv,
+                      const void* q_out, int64_t ldo, const void* k_cache, const void* v_cache,
+                      int32_t num_blocks) {
+  const int st = check_dims(dims, nullptr);
+  if (st != DLFP_OK) return st;
+  if (!rope || num_tokens < 0 || num_blocks < 0) return DLFP_EINVAL;
+  if (rope->rotary_dim != 32 && rope->rotary_dim != 64 && rope->rotary_dim != 128)
+    return DLFP_EUNSUPPORTED;
+  if (rope->interleaved != 0 && rope->interleaved != 1) return DLFP_EINVAL;
+  const int64_t hq = dims->num_q_heads, hkv = dims->num_kv_heads;
+  if (hkv + ceil_div(hq, 4) > 65535) return DLFP_EUNSUPPORTED;  // a grid's second dimension
+  if (!good_stride(ldq, hq) || !good_stride(ldo, hq) || !good_stride(ldk, hkv) ||
+      !good_stride(ldv, hkv))
+    return DLFP_EINVAL;
+  if (num_tokens == 0) return DLFP_OK;
+  if (!rope->table || rope->positions <= 0) return DLFP_EINVAL;
+  if (!positions || !slot_mapping || !q || !k_new || !v_new || !q_out || !k_cache || !v_cache)
+    return DLFP_EINVAL;
+  if (!aligned16(rope->table) || !aligned16(q) || !aligned16(k_new) || !aligned16(v_new) ||
+      !aligned16(q_out) || !aligned16(k_cache) || !aligned16(v_cache))
+    return DLFP_EINVAL;
+  return DLFP_OK;
+}
+
+}  // namespace dlfp
+
+namespace {
+
+int build(const dlfp_dims* dims, const dlfp_tuning* tuning, const dlfp_window* win,
+          int32_t num_seqs, const int32_t* q_len, const int32_t* kv_len,
+          const int32_t* block_table, int32_t max_blocks, int32_t num_blocks, dlfp_meta* meta) {
+  int g = 0;
+  const int st = dlfp::check_dims(dims, &g);
+  if (st != DLFP_OK) return st;
+  if (!meta || num_seqs < 0 || num_blocks < 0) return DLFP_EINVAL;
+  if (num_seqs > 0 && (!q_len || !kv_len || !block_table || max_blocks <= 0)) return DLFP_EINVAL;
+  if (win && (win->window < 1 || win->sinks < 0)) return DLFP_EINVAL;
+  dlfp_tuning tn = {0, 0, 0, 0, 0, 0};
+  if (tuning) tn = *tuning;
+  if (tn.prefill_lead_units < -1) return DLFP_EINVAL;
+  if (tn.decode_pages_in_flight < 0 || tn.decode_pages_in_flight > 2) return DLFP_EINVAL;
+  if (tn.decode_split_tokens < 0 || tn.decode_split_tokens % PAGE ||
+      tn.decode_split_tokens > DLFP_MAX_DECODE_UNIT_KEYS)
+    return DLFP_EINVAL;
+  if (tn.prefill_split_tokens < 0 || tn.prefill_split_tokens % 64 ||
+      tn.prefill_split_tokens > DLFP_MAX_PREFILL_UNIT_KEYS)
+    return DLFP_EINVAL;
+  if (tn.target_units < 0) return DLFP_EINVAL;
+  if (tn.prefill_tile_tokens < 0 || tn.prefill_tile_tokens > DLFP_TILE_ROWS / g)
+    return DLFP_EINVAL;
+  if ((int64_t)num_blocks * PAGE > I32_MAX && num_seqs > 0) return DLFP_ERANGE;
+  const int64_t resident = tn.target_units ? tn.target_units : DLFP_DEFAULT_RESIDENT_WAVES;
+  const int64_t slots = std::max<int64_t>(1, resident / 4);  // workgroups resident together
+  const int64_t cus = std::max<int64_t>(1, resident / 8);
+  const int64_t hkv = dims->num_kv_heads;
+  const int64_t window = win ? win->window : I32_MAX;
+  const int64_t sinks = win ? win->sinks : 0;
+
+  // Pages of a range of rows at positions first .. last: all from page 0, or the
+  // sink pages and, past a gap, those from the first row's window on.
+  auto rows_of = [&](int32_t s, int64_t t0, int64_t nt) {
+    const int64_t first = (int64_t)kv_len[s] - q_len[s] + t0, last = first + nt - 1;
+    const int64_t low = std::max<int64_t>(0, first - window + 1) / PAGE;
+    const int64_t sunk = ceil_div(std::min(sinks, last + 1), PAGE);
+    const int64_t gap = std::max<int64_t>(0, low - sunk);
+    return Rows{s, (int32_t)t0, (int32_t)nt, gap, last + 1 - PAGE * gap};
+  };
+
+  // Validate the sequences and the pages they use.
+  int64_t tokens = 0;
+  std::vector<int32_t> prompts, decoders;
+  for (int s = 0; s < num_seqs; ++s) {
+    const int32_t ql = q_len[s], kl = kv_len[s];
+    if (ql < 1 || kl < ql) return DLFP_EINVAL;
+    const int64_t pages = ceil_div(kl, PAGE);
+    if (pages > max_blocks) return DLFP_ERANGE;
+    const int32_t* row = block_table + (int64_t)s * max_blocks;
+    const Rows r = rows_of(s, 0, ql);
+    // Pages before and past the gap of the sequence's first row.
+    const int64_t sunk = r.gap ? ceil_div(sinks, PAGE) : 0;
+    int32_t lo = std::numeric_limits<int32_t>::max(), hi = std::numeric_limits<int32_t>::min();
+    for (int64_t p = 0; p < sunk; ++p) lo = std::min(lo, row[p]), hi = std::max(hi, row[p]);
+    for (int64_t p = sunk + r.gap; p < pages; ++p)
+      lo = std::min(lo, row[p]), hi = std::max(hi, row[p]);
+    if (lo < 0 || hi >= num_blocks) return DLFP_ERANGE;
+    tokens += ql;
+    (ql == 1 ? decoders : prompts).push_back(s);
+  }
+  if (tokens > I32_MAX) return DLFP_ERANGE;
+
+  // Tiles of a prompt's rows, as tall as one unit takes.
+  const int64_t tile_tokens = tn.prefill_tile_tokens ? tn.prefill_tile_tokens : DLFP_TILE_ROWS / g;
+  std::vector<Rows> tiles, ones;
+  int64_t tile_keys = 0, tile_longest = 0, one_keys = 0, one_longest = 0;
+  for (int32_t s : prompts)
+    for (int64_t t0 = 0; t0 < q_len[s]; t0 += tile_tokens) {
+      tiles.push_back(rows_of(s, t0, std::min<int64_t>(tile_tokens, q_len[s] - t0)));
+      tile_keys += tiles.back().keys;
+      tile_longest = std::max(tile_longest, tiles.back().keys);
+    }
+  for (int32_t s : decoders) {
+    ones.push_back(rows_of(s, 0, 1));
+    one_keys += ones.back().keys;
+    one_longest = std::max(one_longest, ones.back().keys);
+  }
+  auto longest_first = [](const Rows& x, const Rows& y) { return x.keys > y.keys; };
+  std::stable_sort(tiles.begin(), tiles.end(), longest_first);
+  std::stable_sort(ones.begin(), ones.end(), longest_first);
+
+  // Splits: enough units to fill the device, parts not shorter than pays.
+  int64_t split_p = tn.prefill_split_tokens;
+  if (!split_p) {
+    const int64_t part = ceil_div(tile_keys * hkv, slots);
+    split_p = std::clamp<int64_t>(round_up(part, 64), 512, DLFP_MAX_PREFILL_UNIT_KEYS);
+  }
+  int64_t split_d = tn.decode_split_tokens;
+  if (!split_d) {
+    const int64_t part = ceil_div(one_keys * hkv, slots);
+    split_d = std::clamp<int64_t>(round_up(part, 64), 256, DLFP_MAX_DECODE_UNIT_KEYS);
+  }
+
+  std::vector<Unit> units;
+  int64_t groups = 0, off = DLFP_WORKSPACE_PARTIALS / 4;
+  auto emit = [&](const Rows& r, int64_t kh, int64_t split, int64_t granule, int32_t kind) {
+    const int64_t n = ceil_div(r.keys, split), part = round_up(ceil_div(r.keys, n), granule);
+    const int64_t parts = ceil_div(r.keys, part);
+    const int64_t floats = slot_floats((int64_t)r.nt * g);
+    for (int64_t j = 0; j < parts; ++j) {
+      Unit u;
+      std::memset(&u, 0, sizeof(u));
+      u.f[DLFP_W_SEQ] = r.seq;
+      u.f[DLFP_W_KVHEAD] = (int32_t)kh;
+      u.f[DLFP_W_QTOK0] = r.t0;
+      u.f[DLFP_W_QNTOK] = r.nt;
+      u.f[DLFP_W_KVBEGIN] = (int32_t)(j * part);
+      u.f[DLFP_W_KVEND] = (int32_t)std::min(r.keys, (j + 1) * part);
+      u.f[DLFP_W_GROUP] = parts > 1 ? (int32_t)groups : -1;
+      u.f[DLFP_W_SPLIT] = (int32_t)j;
+      u.f[DLFP_W_NSPLITS] = (int32_t)parts;
+      u.f[DLFP_W_WINDOW] = (int32_t)window;
+      u.f[DLFP_W_WSGROUP] = parts > 1 ? (int32_t)std::min(off, I32_MAX) : 0;
+      u.f[DLFP_W_KIND] = kind;
+      u.f[DLFP_W_QROW0] = r.t0;  // the sequence's first row is added below
+      u.f[DLFP_W_QPOS0] = kv_len[r.seq] - q_len[r.seq] + r.t0;
+      u.f[DLFP_W_SINKS] = (int32_t)std::min<int64_t>(sinks, I32_MAX - PAGE);
+      u.f[DLFP_W_GAP] = (int32_t)r.gap;
+      units.push_back(u);
+    }
+    if (parts > 1) {
+      ++groups;
+      off += parts * floats;
+    }
+  };
+  // Prefill units of one KV head together: the launch gives each XCD a contiguous
+  // range of them, so that units reading the same keys share an L2.
+  for (int64_t kh = 0; kh < hkv; ++kh)
+    for (const Rows& r : tiles) emit(r, kh, split_p, 64, DLFP_KIND_PREFILL);
+  const int64_t num_prefill = (int64_t)units.size();
+  for (const Rows& r : ones)
+    for (int64_t kh = 0; kh < hkv; ++kh) emit(r, kh, split_d, 64, DLFP_KIND_DECODE);
+  std::stable_sort(units.begin() + num_prefill, units.end(), [](const Unit& x, const Unit& y) {
+    return x.f[DLFP_W_KVEND] - x.f[DLFP_W_KVBEGIN] > y.f[DLFP_W_KVEND] - y.f[DLFP_W_KVBEGIN];
+  });
+  const int64_t n_units = (int64_t)units.size();
+  if (n_units > I32_MAX / DLFP_WORK_INTS || groups > DLFP_MAX_GROUPS || off > I32_MAX)
+    return DLFP_ERANGE;
+
+  meta->num_seqs = num_seqs;
+  meta->num_tokens = (int32_t)tokens;
+  meta->num_units = (int32_t)n_units;
+  meta->num_prefill_units = (int32_t)num_prefill;
+  meta->num_groups = (int32_t)groups;
+  meta->decode_split_tokens = (int32_t)split_d;
+  meta->prefill_split_tokens = (int32_t)split_p;
+  meta->workspace_bytes = 4 * off;
+  meta->num_append = 0;
+  meta->num_waiting_units = 0;
+  // With more prefill units than compute units, one for each of those leads and
+  // the decode units follow, so that the two shares run side by side.
+  int64_t lead = num_prefill;
+  if (tn.prefill_lead_units > 0)
+    lead = std::min<int64_t>(tn.prefill_lead_units, num_prefill);
+  else if (tn.prefill_lead_units == 0 && n_units > num_prefill && num_prefill > cus)
+    lead = cus;
+  meta->prefill_lead_units = (int32_t)lead;
+  meta->decode_pages_in_flight = DLFP_WINDOW_META;
+  if (meta->cap_seqs < num_seqs || meta->cap_tokens < tokens || meta->cap_work < n_units)
+    return DLFP_ENOSPC;
+  if ((num_seqs > 0 && (!meta->cu_q || !meta->q_pos0)) || (tokens > 0 && !meta->slot_mapping) ||
+      (n_units > 0 && !meta->work))
+    return DLFP_EINVAL;
+  if (meta->cu_q) meta->cu_q[0] = 0;
+  int64_t t = 0;
+  for (int s = 0; s < num_seqs; ++s) {
+    const int32_t pos0 = kv_len[s] - q_len[s];
+    meta->q_pos0[s] = pos0;
+    const int32_t* row = block_table + (int64_t)s * max_blocks;
+    for (int32_t i = 0; i < q_len[s]; ++i) {
+      const int32_t p = pos0 + i;
+      meta->slot_mapping[t++] = row[p / PAGE] * (int32_t)PAGE + p % (int32_t)PAGE;
+    }
+    meta->cu_q[s + 1] = (int32_t)t;
+  }
+  for (Unit& u : units) u.f[DLFP_W_QROW0] += meta->cu_q[u.f[DLFP_W_SEQ]];
+  if (!units.empty()) std::memcpy(meta->work, units.data(), units.size() * sizeof(Unit));
+  return DLFP_OK;
+}
+
+}  // namespace
+
+extern "C" int dlfp_build_window_meta(const dlfp_dims* dims, const dlfp_tuning* tuning,
+                                      const dlfp_window* window, int32_t num_seqs,
+                                      const int32_t* q_len, const int32_t* kv_len,
+                                      const int32_t* block_table, int32_t max_blocks,
+                                      int32_t num_blocks, dlfp_meta* meta) {
+  try {
+    return build(dims, tuning, window, num_seqs, q_len, kv_len, block_table, max_blocks, num_blocks,
+                 meta);
+  } catch (const std::bad_alloc&) {
+    return DLFP_ENOSPC;
+  }
+}

@@ -3,11 +3,19 @@
 #define DLFP_INTERNAL_H
 
 #include "dlfp.h"
+#include "dlfp_cache.h"
 
 namespace dlfp {
 
 // DLFP_OK if dims are supported; *group receives Hq / Hkv.
 int check_dims(const dlfp_dims* dims, int* group);
+
+// The checks that the two rotating appends share (dlfp_cache.h).
+int check_rope_append(const dlfp_dims* dims, const dlfp_rope* rope, int32_t num_tokens,
+                      const int32_t* positions, const int32_t* slot_mapping, const void* q,
+                      int64_t ldq, const void* k_new, int64_t ldk, const void* v_new, int64_t ldv,
+                      const void* q_out, int64_t ldo, const void* k_cache, const void* v_cache,
+                      int32_t num_blocks);
 
 // Workgroups of an attention launch that write `records` append records: about
 // two records per wavefront, a multiple of 8; none past 16, where the records

@@ -20,12 +20,20 @@
 // 6.7 us, 8192 from 1001 28.3 -> 15.7; from 4096, where a page's values are
 // loaded beside the slots, 2048 tokens 4.84 -> 4.23 and 8192 11.8 -> 11.3 (one
 // slot load per wavefront, contiguous stores of the value rows).
+//
+// With ROPE the same kernel turns the keys to their positions on the way (the
+// angles cost a round trip more, after the positions) and its workgroups past
+// the KV heads turn the queries: one wavefront for up to 16 heads of a token, so
+// that the angles are loaded once for them.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
+#include <type_traits>
 
 #include "dlfp.h"
+#include "dlfp_cache.h"
 #include "dlfp_internal.h"
+#include "rope_device.h"
 
 namespace {
 
@@ -39,14 +47,45 @@ constexpr int THREADS = 128;
 // Position of token slot t in a value page row (bits 2 and 3 swap).
 __device__ __forceinline__ int vt_pos(int t) { return (t & 3) | ((t & 4) << 1) | ((t & 8) >> 1); }
 
+// Arguments of a launch that rotates: the strides of the new tokens' rows, the
+// queries, the wavefronts that share a token's query heads.
+struct Rotation {
+  RopeArgs rope;
+  QueryArgs query;
+  const int32_t* positions;
+  int64_t ldk, ldv;
+};
+struct NoRotation {};
+constexpr int QUERY_HEADS = 16;  // query heads of a token that a wavefront turns
+
+template <class R>
 __global__ __launch_bounds__(THREADS) void kv_append_kernel(
     const uint16_t* __restrict__ k_new, const uint16_t* __restrict__ v_new,
     const int32_t* __restrict__ slots, uint16_t* __restrict__ k_cache,
-    uint16_t* __restrict__ v_cache, int num_tokens, int hkv, int64_t num_slots) {
+    uint16_t* __restrict__ v_cache, int num_tokens, int hkv, int64_t num_slots, const R rot) {
+  constexpr bool ROPE = std::is_same<R, Rotation>::value;
   const int t0 = blockIdx.x * TOK;
+  if constexpr (ROPE) {
+    if ((int)blockIdx.y >= hkv) {  // queries: a wavefront takes every other token of the block
+      const int h0 = ((int)blockIdx.y - hkv) * QUERY_HEADS;
+      for (int t = t0 + (int)(threadIdx.x >> 6); t < min(t0 + TOK, num_tokens); t += THREADS / 64)
+        rotate_queries(rot.query, rot.rope, rot.positions, t, h0,
+                       min(h0 + QUERY_HEADS, rot.query.hq));
+      return;
+    }
+  }
   const int h = blockIdx.y;
   const int tid = threadIdx.x;
   const int nt = min(TOK, num_tokens - t0);
+  // Rows of this head.
+  auto k_row = [&](int t) -> const uint16_t* {
+    if constexpr (ROPE) return k_new + t * rot.ldk + h * D;
+    return k_new + ((int64_t)t * hkv + h) * D;
+  };
+  auto v_row = [&](int t) -> const uint16_t* {
+    if constexpr (ROPE) return v_new + t * rot.ldv + h * D;
+    return v_new + ((int64_t)t * hkv + h) * D;
+  };
 
   // The loads of the block are issued before any store (one memory round
   // trip): slots, two 16-byte key chunks per thread (tokens tid / 16 and
@@ -56,20 +95,38 @@ __global__ __launch_bounds__(THREADS) void kv_append_kernel(
   const int lane = tid & 63;
   const int tl = t0 - TOK + lane;
   const bool real = tl >= 0 && tl < num_tokens && lane < 3 * TOK;
-  const int slot_l = real ? slots[tl] : -1;
+  int slot_l = real ? slots[tl] : -1;
+  int pos_l = 0;
+  if constexpr (ROPE) {
+    pos_l = real ? rot.positions[tl] : -1;
+    const bool known = (unsigned)pos_l < (unsigned)rot.rope.positions;
+    slot_l = known ? slot_l : -1;
+    pos_l = known ? pos_l : 0;
+  }
   const int c = tid & 15;
   u32x4_t kv[2];
 #pragma unroll
   for (int j = 0; j < 2; ++j) {
     const int tt = (tid >> 4) + 8 * j;
-    kv[j] = tt < nt ? *reinterpret_cast<const u32x4_t*>(k_new + ((int64_t)(t0 + tt) * hkv + h) * D + c * 8)
+    kv[j] = tt < nt ? *reinterpret_cast<const u32x4_t*>(k_row(t0 + tt) + c * 8)
                     : u32x4_t{0u, 0u, 0u, 0u};
   }
   const int d = tid;
   uint16_t vals[TOK];
 #pragma unroll
   for (int tt = 0; tt < TOK; ++tt)
-    vals[tt] = tt < nt ? v_new[((int64_t)(t0 + tt) * hkv + h) * D + d] : 0;
+    vals[tt] = tt < nt ? v_row(t0 + tt)[d] : 0;
+  if constexpr (ROPE) {
+#pragma unroll
+    for (int j = 0; j < 2; ++j) {
+      const Turn turn = load_turn(rot.rope, __shfl(pos_l, TOK + (tid >> 4) + 8 * j), c);
+      const uint32_t x[4] = {kv[j][0], kv[j][1], kv[j][2], kv[j][3]};
+      float y[8];
+      rotate(rot.rope, turn, c, x, y);
+#pragma unroll
+      for (int w = 0; w < 4; ++w) kv[j][w] = rope_pack(y[2 * w], y[2 * w + 1]);
+    }
+  }
 
   // Keys: token rows, 16-byte chunks.
 #pragma unroll
@@ -119,7 +176,7 @@ __global__ __launch_bounds__(THREADS) void kv_append_kernel(
     if (here > 0) {
 #pragma unroll
       for (int tt = 0; tt < TOK; ++tt)
-        vals[tt] = v_new[((int64_t)(t0 + here + tt) * hkv + h) * D + d];
+        vals[tt] = v_row(t0 + here + tt)[d];
     }
     const int64_t blk = __builtin_amdgcn_readlane(slot_l, TOK + here) / PAGE;
     u32x4_t lo, hi;
@@ -159,6 +216,30 @@ extern "C" int dlfp_kv_append(const dlfp_dims* dims, int32_t num_tokens, const v
   kv_append_kernel<<<grid, THREADS, 0, stream>>>(
       static_cast<const uint16_t*>(k_new), static_cast<const uint16_t*>(v_new), slot_mapping,
       static_cast<uint16_t*>(k_cache), static_cast<uint16_t*>(v_cache), num_tokens,
-      dims->num_kv_heads, (int64_t)num_blocks * PAGE);
+      dims->num_kv_heads, (int64_t)num_blocks * PAGE, NoRotation{});
+  return hipGetLastError() == hipSuccess ? DLFP_OK : DLFP_EHIP;
+}
+
+extern "C" int dlfp_rope_append(const dlfp_dims* dims, const dlfp_rope* rope, int32_t num_tokens,
+                                const int32_t* positions, const int32_t* slot_mapping,
+                                const void* q, int64_t ldq, const void* k_new, int64_t ldk,
+                                const void* v_new, int64_t ldv, void* q_out, int64_t ldo,
+                                void* k_cache, void* v_cache, int32_t num_blocks,
+                                hipStream_t stream) {
+  const int st = dlfp::check_rope_append(dims, rope, num_tokens, positions, slot_mapping, q, ldq,
+                                         k_new, ldk, v_new, ldv, q_out, ldo, k_cache, v_cache,
+                                         num_blocks);
+  if (st != DLFP_OK || num_tokens == 0) return st;
+  const Rotation rot = {
+      {rope->table, rope->positions, rope->rotary_dim, rope->interleaved},
+      {static_cast<const uint16_t*>(q), static_cast<uint16_t*>(q_out), ldq, ldo, dims->num_q_heads},
+      positions, ldk, ldv};
+  (void)hipGetLastError();
+  const dim3 grid((num_tokens + TOK - 1) / TOK,
+                  dims->num_kv_heads + (dims->num_q_heads + QUERY_HEADS - 1) / QUERY_HEADS);
+  kv_append_kernel<<<grid, THREADS, 0, stream>>>(
+      static_cast<const uint16_t*>(k_new), static_cast<const uint16_t*>(v_new), slot_mapping,
+      static_cast<uint16_t*>(k_cache), static_cast<uint16_t*>(v_cache), num_tokens,
+      dims->num_kv_heads, (int64_t)num_blocks * PAGE, rot);
   return hipGetLastError() == hipSuccess ? DLFP_OK : DLFP_EHIP;
 }

@@ -78,6 +78,19 @@ EXPORTS = ["dlfp_build_varlen_meta", "dlfp_kv_append", "dlfp_attention_mixed",
            "dlfp_timer_stop", "dlfp_timer_elapsed_ms", "dlfp_stream_hold", "dlfp_status_string",
            "dlfp_version"]
 
+# Declared in dlfp_cache.h.
+CACHE_EXPORTS = ["dlfp_rope_append", "dlfp_rope_append_kv8", "dlfp_build_window_meta",
+                 "dlfp_attention_window", "dlfp_attention_kv8"]
+
+
+class dlfp_rope(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("positions", ctypes.c_int32),
+                ("rotary_dim", ctypes.c_int32), ("interleaved", ctypes.c_int32)]
+
+
+class dlfp_window(ctypes.Structure):
+    _fields_ = [("window", ctypes.c_int32), ("sinks", ctypes.c_int32)]
+
 
 def lib_path() -> str:
     return _LIB_PATH
@@ -124,7 +137,18 @@ def lib():
     L.dlfp_status_string.argtypes = [ctypes.c_int]
     L.dlfp_status_string.restype = ctypes.c_char_p
     L.dlfp_version.argtypes = []
-    for name in EXPORTS:
+    append = [ctypes.POINTER(dlfp_dims), ctypes.POINTER(dlfp_rope), i32, vp, vp, vp, i64, vp, i64,
+              vp, i64, vp, i64, vp, vp]
+    L.dlfp_rope_append.argtypes = append + [i32, vp]
+    L.dlfp_rope_append_kv8.argtypes = append + [vp, vp, i32, vp]
+    L.dlfp_build_window_meta.argtypes = [ctypes.POINTER(dlfp_dims), ctypes.POINTER(dlfp_tuning),
+                                         ctypes.POINTER(dlfp_window), i32, _P32, _P32, _P32, i32,
+                                         i32, ctypes.POINTER(dlfp_meta)]
+    attention = [ctypes.POINTER(dlfp_dims), ctypes.POINTER(dlfp_meta), vp, vp, i32, i32, vp, vp, vp]
+    rest = [ctypes.c_float, vp, i32, vp, sz, vp]
+    L.dlfp_attention_window.argtypes = attention + rest
+    L.dlfp_attention_kv8.argtypes = attention + [vp, vp] + rest
+    for name in EXPORTS + CACHE_EXPORTS:
         if name != "dlfp_status_string":
             getattr(L, name).restype = ctypes.c_int
     _lib = L
@@ -227,26 +251,44 @@ class Meta:
 def dlfp_build_varlen_meta(dims: dlfp_dims, q_len, kv_len, block_table: np.ndarray,
                            num_blocks: int, tuning: Optional[dlfp_tuning] = None) -> Meta:
     """Build metadata; sizes the host arrays with a first capacity-probing call."""
-    L = lib()
+    return _build_meta("dlfp_build_varlen_meta", (), dims, q_len, kv_len, block_table, num_blocks,
+                       tuning)
+
+
+def _build_meta(name, window, dims, q_len, kv_len, block_table, num_blocks, tuning) -> Meta:
+    build = getattr(lib(), name)
     q_len = np.ascontiguousarray(q_len, dtype=np.int32)
     kv_len = np.ascontiguousarray(kv_len, dtype=np.int32)
     bt = np.ascontiguousarray(block_table, dtype=np.int32)
     n = len(q_len)
+    if len(kv_len) != n:
+        raise ValueError("q_len and kv_len must be as long")
     if bt.ndim != 2 or bt.shape[0] != n:
         raise ValueError("block_table must be [num_seqs][max_blocks]")
     tn = tuning if tuning is not None else dlfp_tuning(0, 0, 0)
+
+    def call(meta):
+        return build(ctypes.byref(dims), ctypes.byref(tn), *window, n, _ptr32(q_len),
+                     _ptr32(kv_len), _ptr32(bt), bt.shape[1], int(num_blocks),
+                     ctypes.byref(meta.c))
+
     probe = Meta(0, 0, 0)
-    st = L.dlfp_build_varlen_meta(ctypes.byref(dims), ctypes.byref(tn), n, _ptr32(q_len),
-                                  _ptr32(kv_len), _ptr32(bt), bt.shape[1], int(num_blocks),
-                                  ctypes.byref(probe.c))
+    st = call(probe)
     if st not in (0, -3):
-        _check(st, "dlfp_build_varlen_meta")
+        _check(st, name)
     meta = Meta(probe.c.num_seqs, probe.c.num_tokens, probe.c.num_units + probe.c.num_append)
-    st = L.dlfp_build_varlen_meta(ctypes.byref(dims), ctypes.byref(tn), n, _ptr32(q_len),
-                                  _ptr32(kv_len), _ptr32(bt), bt.shape[1], int(num_blocks),
-                                  ctypes.byref(meta.c))
-    _check(st, "dlfp_build_varlen_meta")
+    _check(call(meta), name)
     return meta
+
+
+def dlfp_build_window_meta(dims: dlfp_dims, q_len, kv_len, block_table: np.ndarray,
+                           num_blocks: int, window: Optional[dlfp_window] = None,
+                           tuning: Optional[dlfp_tuning] = None) -> Meta:
+    """Metadata of dlfp_attention_window and dlfp_attention_kv8; window None: every key up to
+    a row's own."""
+    w = ctypes.byref(window) if window is not None else None
+    return _build_meta("dlfp_build_window_meta", (w,), dims, q_len, kv_len, block_table, num_blocks,
+                       tuning)
 
 
 def dlfp_kv_append(dims: dlfp_dims, k_new, v_new, slot_mapping, k_cache, v_cache,
@@ -297,6 +339,81 @@ def dlfp_append_attention_mixed_static(dims: dlfp_dims, meta: Meta, d_work, d_bl
         v_cache.data_ptr(), float(scale), out.data_ptr(), _out_code(out.dtype), _stream(stream))
     if st:
         _check(st, "dlfp_append_attention_mixed_static")
+
+
+def _rows(t, heads: int, tokens: int) -> int:
+    """Elements between the tokens' rows of a [tokens][heads][128] bf16 tensor whose heads
+    are contiguous."""
+    if t.dim() != 3 or t.size(0) != tokens or t.size(1) != heads or t.size(2) != HEAD_DIM:
+        raise ValueError("shapes disagree")
+    if t.element_size() != 2 or t.stride(2) != 1 or (heads > 1 and t.stride(1) != HEAD_DIM):
+        raise ValueError("a token's heads must be contiguous bf16")
+    return t.stride(0) if tokens > 1 else heads * HEAD_DIM
+
+
+def make_rope(table, interleaved: bool = False) -> dlfp_rope:
+    """table: float32 [positions][rotary_dim], cosines then sines; it has to outlive the rope."""
+    if table.dim() != 2 or table.element_size() != 4 or not table.is_contiguous():
+        raise ValueError("the table must be contiguous float32 [positions][rotary_dim]")
+    return dlfp_rope(table.data_ptr(), table.size(0), table.size(1), 1 if interleaved else 0)
+
+
+def _append_args(dims, rope, positions, slot_mapping, q, k_new, v_new, q_out, k_cache, v_cache):
+    n, hq, hkv = slot_mapping.size(0), dims.num_q_heads, dims.num_kv_heads
+    if positions.size(0) != n:
+        raise ValueError("shapes disagree")
+    if positions.element_size() != 4 or slot_mapping.element_size() != 4:
+        raise ValueError("positions and slots must be int32")
+    return (dims, rope, n, positions.data_ptr(), slot_mapping.data_ptr(), q.data_ptr(),
+            _rows(q, hq, n), k_new.data_ptr(), _rows(k_new, hkv, n), v_new.data_ptr(),
+            _rows(v_new, hkv, n), q_out.data_ptr(), _rows(q_out, hq, n), k_cache.data_ptr(),
+            v_cache.data_ptr())
+
+
+def dlfp_rope_append(dims: dlfp_dims, rope: dlfp_rope, positions, slot_mapping, q, k_new, v_new,
+                     q_out, k_cache, v_cache, stream=None) -> None:
+    """q, q_out: bf16 [T][Hq][128], k_new, v_new: bf16 [T][Hkv][128] (tokens may be strided);
+    positions, slot_mapping: int32 [T]; bf16 caches per the pool layout."""
+    st = lib().dlfp_rope_append(*_append_args(dims, rope, positions, slot_mapping, q, k_new, v_new,
+                                              q_out, k_cache, v_cache),
+                                k_cache.size(0), _stream(stream))
+    if st:
+        _check(st, "dlfp_rope_append")
+
+
+def dlfp_rope_append_kv8(dims: dlfp_dims, rope: dlfp_rope, positions, slot_mapping, q, k_new,
+                         v_new, q_out, k_cache, v_cache, k_exp, v_exp, stream=None) -> None:
+    """The same into 8-bit caches with their exponents (uint8 [num_blocks][Hkv])."""
+    st = lib().dlfp_rope_append_kv8(*_append_args(dims, rope, positions, slot_mapping, q, k_new,
+                                                  v_new, q_out, k_cache, v_cache),
+                                    k_exp.data_ptr(), v_exp.data_ptr(), k_cache.size(0),
+                                    _stream(stream))
+    if st:
+        _check(st, "dlfp_rope_append_kv8")
+
+
+def dlfp_attention_window(dims: dlfp_dims, meta: Meta, d_work, d_block_table, q, k_cache, v_cache,
+                          scale: float, out, workspace, stream=None) -> None:
+    """meta: of dlfp_build_window_meta; bf16 caches; out dtype bfloat16 or float32."""
+    st = lib().dlfp_attention_window(
+        dims, meta.c, d_work.data_ptr(), d_block_table.data_ptr(), d_block_table.size(1),
+        k_cache.size(0), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), float(scale),
+        out.data_ptr(), _out_code(out.dtype), workspace.data_ptr(), workspace.nbytes,
+        _stream(stream))
+    if st:
+        _check(st, "dlfp_attention_window")
+
+
+def dlfp_attention_kv8(dims: dlfp_dims, meta: Meta, d_work, d_block_table, q, k_cache, v_cache,
+                       k_exp, v_exp, scale: float, out, workspace, stream=None) -> None:
+    """The same over 8-bit caches with their exponents (uint8 [num_blocks][Hkv])."""
+    st = lib().dlfp_attention_kv8(
+        dims, meta.c, d_work.data_ptr(), d_block_table.data_ptr(), d_block_table.size(1),
+        k_cache.size(0), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_exp.data_ptr(),
+        v_exp.data_ptr(), float(scale), out.data_ptr(), _out_code(out.dtype), workspace.data_ptr(),
+        workspace.nbytes, _stream(stream))
+    if st:
+        _check(st, "dlfp_attention_kv8")
 
 
 def dlfp_linear_bf16(x, w, out, stream=None) -> None:

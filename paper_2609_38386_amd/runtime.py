@@ -40,8 +40,91 @@ class KVPool:
         self.num_blocks = num_blocks
         self.num_kv_heads = num_kv_heads
 
+    @classmethod
+    def of(cls, k: torch.Tensor, v: torch.Tensor) -> "KVPool":
+        """A pool over two tensors that are there already."""
+        if (k.dtype != torch.bfloat16 or v.dtype != torch.bfloat16 or
+                not _are_pages(k, v)):
+            raise ValueError("caches must be contiguous bf16 pages")
+        pool = cls.__new__(cls)
+        pool.k, pool.v, pool.num_blocks, pool.num_kv_heads = k, v, k.size(0), k.size(1)
+        return pool
+
     def host_bits(self):
         return device_to_bits(self.k), device_to_bits(self.v)
+
+
+def _are_pages(k: torch.Tensor, v: torch.Tensor) -> bool:
+    return (k.dim() == 4 and tuple(k.shape[2:]) == (_d.PAGE_SIZE, _d.HEAD_DIM) and
+            tuple(v.shape) == (*k.shape[:2], _d.HEAD_DIM, _d.PAGE_SIZE) and
+            k.is_contiguous() and v.is_contiguous())
+
+
+class KVPool8:
+    """Paged KV cache of one layer in 8 bits: e4m3 codes K [nb][Hkv][16][128], V
+    [nb][Hkv][128][16], and an exponent byte for each page and KV head of both (a code
+    c stands for c 2^(byte - 127)).  New pages hold zeros."""
+
+    def __init__(self, num_blocks: int, num_kv_heads: int, device):
+        shape_k = (num_blocks, num_kv_heads, _d.PAGE_SIZE, _d.HEAD_DIM)
+        shape_v = (num_blocks, num_kv_heads, _d.HEAD_DIM, _d.PAGE_SIZE)
+        self._set(*(torch.zeros(x, dtype=torch.uint8, device=device).view(torch.float8_e4m3fn)
+                    for x in (shape_k, shape_v)),
+                  *(torch.full((num_blocks, num_kv_heads), 127, dtype=torch.uint8, device=device)
+                    for _ in range(2)))
+
+    def _set(self, k, v, k_exp, v_exp):
+        self.k, self.v, self.k_exp, self.v_exp = k, v, k_exp, v_exp
+        self.num_blocks, self.num_kv_heads = k.size(0), k.size(1)
+
+    @classmethod
+    def of(cls, k: torch.Tensor, v: torch.Tensor, k_exp: torch.Tensor,
+           v_exp: torch.Tensor) -> "KVPool8":
+        """A pool over four tensors that are there already."""
+        if k.element_size() != 1 or v.element_size() != 1 or not _are_pages(k, v):
+            raise ValueError("caches must be contiguous pages of one byte a value")
+        for e in (k_exp, v_exp):
+            if e.dtype != torch.uint8 or e.shape != k.shape[:2] or not e.is_contiguous():
+                raise ValueError("exponents must be uint8 [num_blocks][Hkv]")
+        pool = cls.__new__(cls)
+        pool._set(k, v, k_exp, v_exp)
+        return pool
+
+
+class Rope:
+    """Rotary position embedding: the table of cosines and sines (computed in 64 bits) and
+    the C struct over it.  ``positions``: rows, the longest sequence."""
+
+    def __init__(self, positions: int, device, theta: float = 1.0e6, rotary_dim: int = _d.HEAD_DIM,
+                 interleaved: bool = False):
+        freq = float(theta) ** (-2.0 * torch.arange(rotary_dim // 2, dtype=torch.float64) /
+                                rotary_dim)
+        angle = torch.arange(positions, dtype=torch.float64)[:, None] * freq
+        self._set(torch.cat([angle.cos(), angle.sin()], 1).float().to(device), interleaved)
+
+    def _set(self, table, interleaved):
+        self.table = table
+        self.c = _d.make_rope(table, interleaved)
+
+    @classmethod
+    def of(cls, table: torch.Tensor, interleaved: bool = False) -> "Rope":
+        """A rope over a table that is there already."""
+        rope = cls.__new__(cls)
+        rope._set(table, interleaved)
+        return rope
+
+
+def rope_append(dims: _d.dlfp_dims, rope: Rope, pool, positions: torch.Tensor,
+                slots: torch.Tensor, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
+                q_out: torch.Tensor, stream=None):
+    """Rotate queries and keys to their positions and write keys and values into the pages
+    of a KVPool or KVPool8."""
+    if isinstance(pool, KVPool8):
+        _d.dlfp_rope_append_kv8(dims, rope.c, positions, slots, q, k_new, v_new, q_out, pool.k,
+                                pool.v, pool.k_exp, pool.v_exp, stream)
+    else:
+        _d.dlfp_rope_append(dims, rope.c, positions, slots, q, k_new, v_new, q_out, pool.k, pool.v,
+                            stream)
 
 
 class Workspace:
@@ -102,6 +185,48 @@ class Batch:
         ws = workspace.ensure(self.meta.workspace_bytes, self.meta.num_groups, stream)
         _d.dlfp_append_attention_mixed(self.dims, self.meta, self.d_work, self.d_block_table, q,
                                        k_new, v_new, pool.k, pool.v, scale, out, ws, stream)
+
+
+class WindowBatch:
+    """Metadata of one mixed iteration for the rotating append and windowed or 8-bit
+    attention, plus device copies of its arrays.  ``window`` None: every key up to a row's
+    own."""
+
+    def __init__(self, dims: _d.dlfp_dims, q_len: Sequence[int], kv_len: Sequence[int],
+                 block_table: np.ndarray, num_blocks: int, device, window: Optional[int] = None,
+                 sinks: int = 0, tuning: Optional[_d.dlfp_tuning] = None):
+        if window is None and sinks:
+            raise ValueError("sinks need a window")
+        self.dims = dims
+        self.q_len = np.asarray(q_len, dtype=np.int32)
+        self.kv_len = np.asarray(kv_len, dtype=np.int32)
+        table = np.ascontiguousarray(block_table, dtype=np.int32)
+        self.meta = m = _d.dlfp_build_window_meta(
+            dims, self.q_len, self.kv_len, table, num_blocks,
+            _d.dlfp_window(window, sinks) if window is not None else None, tuning)
+        self.num_tokens = t = m.num_tokens
+        seq = np.repeat(np.arange(len(self.q_len)), self.q_len)
+        positions = m.q_pos0[seq] + np.arange(t, dtype=np.int32) - m.cu_q[seq]
+        host = np.concatenate([m.slot_mapping[:t], positions, m.records.reshape(-1)]
+                              ).astype(np.int32)
+        dev = torch.from_numpy(host).to(device)
+        self.d_slots, self.d_positions, self.d_work = dev[:t], dev[t:2 * t], dev[2 * t:]
+        self.d_block_table = torch.from_numpy(table).to(device)
+
+    def append(self, rope: Rope, pool, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
+               q_out: torch.Tensor, stream=None):
+        rope_append(self.dims, rope, pool, self.d_positions, self.d_slots, q, k_new, v_new, q_out,
+                    stream)
+
+    def attention(self, pool, q: torch.Tensor, scale: float, out: torch.Tensor,
+                  workspace: Workspace, stream=None):
+        ws = workspace.ensure(self.meta.workspace_bytes, self.meta.num_groups, stream)
+        if isinstance(pool, KVPool8):
+            _d.dlfp_attention_kv8(self.dims, self.meta, self.d_work, self.d_block_table, q, pool.k,
+                                  pool.v, pool.k_exp, pool.v_exp, scale, out, ws, stream)
+        else:
+            _d.dlfp_attention_window(self.dims, self.meta, self.d_work, self.d_block_table, q,
+                                     pool.k, pool.v, scale, out, ws, stream)
 
 
 class Iteration:
