@@ -54,7 +54,8 @@ int check_rope_append(const dlfp_dims* dims, const dlfp_rope* rope, int32_t num_
     return DLFP_EUNSUPPORTED;
   if (rope->interleaved != 0 && rope->interleaved != 1) return DLFP_EINVAL;
   const int64_t hq = dims->num_q_heads, hkv = dims->num_kv_heads;
-  if (hkv + ceil_div(hq, 4) > 65535) return DLFP_EUNSUPPORTED;  // a grid's second dimension
+  // Workgroups and wavefronts of a launch are counted in 31 bits.
+  if (num_tokens * (hkv + ceil_div(hq, 16)) > I32_MAX / 4) return DLFP_ERANGE;
   if (!good_stride(ldq, hq) || !good_stride(ldo, hq) || !good_stride(ldk, hkv) ||
       !good_stride(ldv, hkv))
     return DLFP_EINVAL;

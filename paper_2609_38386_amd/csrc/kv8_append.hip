@@ -30,7 +30,6 @@ constexpr int PAGE = DLFP_PAGE_SIZE;
 constexpr int PAGE_BYTES = PAGE * D;
 constexpr int THREADS = 256;
 constexpr int WAVES = THREADS / 64;
-constexpr int QUERY_HEADS = 16;  // query heads of a token that a wavefront turns
 constexpr int EXP_MIN = -100, EXP_BIAS = 127;
 
 struct Args {
@@ -48,7 +47,8 @@ struct Args {
   int num_tokens;
   int hkv;
   int64_t num_slots;
-  int window;  // tokens of a workgroup
+  int window;   // tokens of a workgroup: 4 or 16
+  int blocks;   // workgroups of a KV head
 };
 
 // Position of token slot t inside a value page row (bits 2 and 3 swap).
@@ -95,6 +95,10 @@ __device__ __forceinline__ uint32_t moved(uint32_t w, int up) {
   const auto hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
   return codes(scaled(lo[0], -up), scaled(lo[1], -up), scaled(hi[0], -up), scaled(hi[1], -up));
 }
+
+// Where a value row (16 bytes) sits in LDS: rows 8 c + x of the 16 chunks c, which
+// the lanes write together, fall on different banks.
+__device__ __forceinline__ int lds_row(int d) { return d ^ ((d >> 4) & 7); }
 
 // Lanes of one wavefront hand data to each other through LDS (and, between the
 // runs of one page, through memory).
@@ -192,8 +196,8 @@ __device__ void append_run(const Args& a, int first, int n, int slot0, int h, ui
         }
       }
     }
-    reinterpret_cast<uint4*>(lds)[2 * lane] = rows[0];
-    reinterpret_cast<uint4*>(lds)[2 * lane + 1] = rows[1];
+    reinterpret_cast<uint4*>(lds)[lds_row(2 * lane)] = rows[0];
+    reinterpret_cast<uint4*>(lds)[lds_row(2 * lane + 1)] = rows[1];
   }
   wave_fence();
 #pragma unroll
@@ -209,15 +213,17 @@ __device__ void append_run(const Args& a, int first, int n, int slot0, int h, ui
                    held(scaled(__builtin_bit_cast(float, v[2 * w + 1] & 0xFFFF0000u), -v_e)));
     const int i = 4 * j + quarter;
     if (i < n) {
-      uint8_t* at = lds + 8 * chunk * PAGE + vt_pos(o0 + i);
+      uint8_t* at = lds + vt_pos(o0 + i);
 #pragma unroll
-      for (int x = 0; x < 8; ++x) at[x * PAGE] = (uint8_t)(c[x >> 2] >> (8 * (x & 3)));
+      for (int x = 0; x < 8; ++x)
+        at[lds_row(8 * chunk + x) * PAGE] = (uint8_t)(c[x >> 2] >> (8 * (x & 3)));
     }
   }
   wave_fence();
 #pragma unroll
   for (int r = 0; r < 2; ++r)
-    reinterpret_cast<uint4*>(vp)[64 * r + lane] = reinterpret_cast<const uint4*>(lds)[64 * r + lane];
+    reinterpret_cast<uint4*>(vp)[64 * r + lane] =
+        reinterpret_cast<const uint4*>(lds)[lds_row(64 * r + lane)];
   if (lane == 0) {
     a.k_exp[page] = (uint8_t)(k_e + EXP_BIAS);
     a.v_exp[page] = (uint8_t)(v_e + EXP_BIAS);
@@ -226,18 +232,20 @@ __device__ void append_run(const Args& a, int first, int n, int slot0, int h, ui
   wave_fence();
 }
 
-// Workgroup (x, y): y < hkv: the runs that begin among tokens x * window .. of KV
-// head y, in turn over the wavefronts; others: those tokens' queries.
+// Workgroups: for each KV head and window of tokens the runs that begin there, in
+// turn over the wavefronts; then the queries.
 __global__ __launch_bounds__(THREADS) void kv8_append_kernel(const Args a) {
   __shared__ __attribute__((aligned(16))) uint8_t lds[WAVES][PAGE_BYTES];
-  const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
-  const int t0 = blockIdx.x * a.window, t1 = min(t0 + a.window, a.num_tokens);
-  if ((int)blockIdx.y >= a.hkv) {
-    const int h0 = ((int)blockIdx.y - a.hkv) * QUERY_HEADS;
-    for (int t = t0 + wave; t < t1; t += WAVES)
-      rotate_queries(a.query, a.rope, a.positions, t, h0, min(h0 + QUERY_HEADS, a.query.hq));
+  const int wave = __builtin_amdgcn_readfirstlane((int)(threadIdx.x >> 6)), lane = threadIdx.x & 63;
+  int block = blockIdx.x;
+  if (block >= a.blocks * a.hkv) {
+    const int item = (block - a.blocks * a.hkv) * WAVES + wave;
+    if (item < a.num_tokens * a.query.chunks) rotate_queries(a.query, a.rope, a.positions, item);
     return;
   }
+  const int h = block / a.blocks;
+  block -= h * a.blocks;
+  const int t0 = block * a.window, t1 = min(t0 + a.window, a.num_tokens);
   // Lane l has the slot of token t0 - 16 + l: the 16 before the window's (at most
   // 16), and the 15 after.
   const int t = t0 - PAGE + lane;
@@ -262,7 +270,7 @@ __global__ __launch_bounds__(THREADS) void kv8_append_kernel(const Args a) {
     if (i % WAVES != wave) continue;
     for (int l = __builtin_ctzll(begins);;) {
       const int n = 1 + __builtin_ctzll(~(goes_on >> (l + 1)));
-      append_run(a, t0 - PAGE + l, n, __builtin_amdgcn_readlane(slot, l), blockIdx.y, lds[wave]);
+      append_run(a, t0 - PAGE + l, n, __builtin_amdgcn_readlane(slot, l), h, lds[wave]);
       const uint64_t rest = starts & ~((2ull << l) - 1);
       l = rest ? __builtin_ctzll(rest) : 0;
       if (!(joins >> l & 1) || !rest) break;
@@ -287,7 +295,7 @@ extern "C" int dlfp_rope_append_kv8(const dlfp_dims* dims, const dlfp_rope* rope
   Args a;
   a.rope = {rope->table, rope->positions, rope->rotary_dim, rope->interleaved};
   a.query = {static_cast<const uint16_t*>(q), static_cast<uint16_t*>(q_out), ldq, ldo,
-             dims->num_q_heads};
+             dims->num_q_heads, 0};
   a.positions = positions;
   a.slots = slot_mapping;
   a.k_new = static_cast<const uint16_t*>(k_new);
@@ -301,10 +309,11 @@ extern "C" int dlfp_rope_append_kv8(const dlfp_dims* dims, const dlfp_rope* rope
   a.num_tokens = num_tokens;
   a.hkv = dims->num_kv_heads;
   a.num_slots = (int64_t)num_blocks * PAGE;
-  a.window = 16;
+  a.query.chunks = query_chunks(dims->num_q_heads);
+  a.window = num_tokens <= 1024 ? 4 : 16;
+  a.blocks = (num_tokens + a.window - 1) / a.window;
+  const int64_t queries = ((int64_t)num_tokens * a.query.chunks + WAVES - 1) / WAVES;
   (void)hipGetLastError();
-  const dim3 grid((num_tokens + a.window - 1) / a.window,
-                  dims->num_kv_heads + (dims->num_q_heads + QUERY_HEADS - 1) / QUERY_HEADS);
-  kv8_append_kernel<<<grid, THREADS, 0, stream>>>(a);
+  kv8_append_kernel<<<(unsigned)((int64_t)a.blocks * a.hkv + queries), THREADS, 0, stream>>>(a);
   return hipGetLastError() == hipSuccess ? DLFP_OK : DLFP_EHIP;
 }

@@ -22,9 +22,8 @@
 // slot load per wavefront, contiguous stores of the value rows).
 //
 // With ROPE the same kernel turns the keys to their positions on the way (the
-// angles cost a round trip more, after the positions) and its workgroups past
-// the KV heads turn the queries: one wavefront for up to 16 heads of a token, so
-// that the angles are loaded once for them.
+// angles cost a round trip more, after the positions), and workgroups behind
+// those of the KV heads turn the queries.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>
@@ -48,15 +47,16 @@ constexpr int THREADS = 128;
 __device__ __forceinline__ int vt_pos(int t) { return (t & 3) | ((t & 4) << 1) | ((t & 8) >> 1); }
 
 // Arguments of a launch that rotates: the strides of the new tokens' rows, the
-// queries, the wavefronts that share a token's query heads.
+// queries.  Its grid has one dimension: blocks of tokens of each KV head, then
+// the queries.
 struct Rotation {
   RopeArgs rope;
   QueryArgs query;
   const int32_t* positions;
   int64_t ldk, ldv;
+  int blocks;  // of 16 tokens
 };
 struct NoRotation {};
-constexpr int QUERY_HEADS = 16;  // query heads of a token that a wavefront turns
 
 template <class R>
 __global__ __launch_bounds__(THREADS) void kv_append_kernel(
@@ -64,17 +64,20 @@ __global__ __launch_bounds__(THREADS) void kv_append_kernel(
     const int32_t* __restrict__ slots, uint16_t* __restrict__ k_cache,
     uint16_t* __restrict__ v_cache, int num_tokens, int hkv, int64_t num_slots, const R rot) {
   constexpr bool ROPE = std::is_same<R, Rotation>::value;
-  const int t0 = blockIdx.x * TOK;
+  int block = blockIdx.x, h = blockIdx.y;
   if constexpr (ROPE) {
-    if ((int)blockIdx.y >= hkv) {  // queries: a wavefront takes every other token of the block
-      const int h0 = ((int)blockIdx.y - hkv) * QUERY_HEADS;
-      for (int t = t0 + (int)(threadIdx.x >> 6); t < min(t0 + TOK, num_tokens); t += THREADS / 64)
-        rotate_queries(rot.query, rot.rope, rot.positions, t, h0,
-                       min(h0 + QUERY_HEADS, rot.query.hq));
+    const int kv = rot.blocks * hkv;
+    if (block >= kv) {
+      const int item = __builtin_amdgcn_readfirstlane((block - kv) * (THREADS / 64) +
+                                                      (int)(threadIdx.x >> 6));
+      if (item < num_tokens * rot.query.chunks)
+        rotate_queries(rot.query, rot.rope, rot.positions, item);
       return;
     }
+    h = block / rot.blocks;
+    block -= h * rot.blocks;
   }
-  const int h = blockIdx.y;
+  const int t0 = block * TOK;
   const int tid = threadIdx.x;
   const int nt = min(TOK, num_tokens - t0);
   // Rows of this head.
@@ -230,14 +233,15 @@ extern "C" int dlfp_rope_append(const dlfp_dims* dims, const dlfp_rope* rope, in
                                          k_new, ldk, v_new, ldv, q_out, ldo, k_cache, v_cache,
                                          num_blocks);
   if (st != DLFP_OK || num_tokens == 0) return st;
-  const Rotation rot = {
-      {rope->table, rope->positions, rope->rotary_dim, rope->interleaved},
-      {static_cast<const uint16_t*>(q), static_cast<uint16_t*>(q_out), ldq, ldo, dims->num_q_heads},
-      positions, ldk, ldv};
+  const int chunks = query_chunks(dims->num_q_heads), blocks = (num_tokens + TOK - 1) / TOK;
+  const Rotation rot = {{rope->table, rope->positions, rope->rotary_dim, rope->interleaved},
+                        {static_cast<const uint16_t*>(q), static_cast<uint16_t*>(q_out), ldq, ldo,
+                         dims->num_q_heads, chunks},
+                        positions, ldk, ldv, blocks};
+  const int64_t queries = ((int64_t)num_tokens * chunks + THREADS / 64 - 1) / (THREADS / 64);
+  const int64_t grid = (int64_t)blocks * dims->num_kv_heads + queries;
   (void)hipGetLastError();
-  const dim3 grid((num_tokens + TOK - 1) / TOK,
-                  dims->num_kv_heads + (dims->num_q_heads + QUERY_HEADS - 1) / QUERY_HEADS);
-  kv_append_kernel<<<grid, THREADS, 0, stream>>>(
+  kv_append_kernel<<<(unsigned)grid, THREADS, 0, stream>>>(
       static_cast<const uint16_t*>(k_new), static_cast<const uint16_t*>(v_new), slot_mapping,
       static_cast<uint16_t*>(k_cache), static_cast<uint16_t*>(v_cache), num_tokens,
       dims->num_kv_heads, (int64_t)num_blocks * PAGE, rot);

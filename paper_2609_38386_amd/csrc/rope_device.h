@@ -94,28 +94,37 @@ struct QueryArgs {
   const uint16_t* q;
   uint16_t* out;
   int64_t ldq, ldo;
-  int hq;
+  int hq, chunks;  // query heads, groups of QUERY_HEADS of them
 };
 
-// Rotates the queries of a launch's token `t`, heads h0 .. h1 - 1, by one
-// wavefront: four heads at a time, 16 lanes a head.  Every lane calls it.
+// Turns QUERY_HEADS heads of one token by one wavefront: four heads at a time, 16
+// lanes a head, every load issued before the angles' (whose address waits for
+// the position).  item: token * chunks + chunk of its heads.
+constexpr int QUERY_HEADS = 16;
+inline int query_chunks(int hq) { return (hq + QUERY_HEADS - 1) / QUERY_HEADS; }
 __device__ __forceinline__ void rotate_queries(const QueryArgs& a, const RopeArgs& r,
-                                               const int32_t* positions, int t, int h0, int h1) {
+                                               const int32_t* positions, int item) {
   const int lane = threadIdx.x & 63, chunk = lane & 15;
+  const int t = item / a.chunks, h0 = item % a.chunks * QUERY_HEADS;
+  const int n = min(QUERY_HEADS, a.hq - h0);
+  const uint16_t* src = a.q + t * a.ldq + h0 * DLFP_HEAD_DIM + 8 * chunk;
+  uint16_t* dst = a.out + t * a.ldo + h0 * DLFP_HEAD_DIM + 8 * chunk;
   const int pos = __builtin_amdgcn_readfirstlane(positions[t]);
+  uint4 v[QUERY_HEADS / 4];
+#pragma unroll
+  for (int i = 0; i < QUERY_HEADS / 4; ++i)
+    v[i] = *reinterpret_cast<const uint4*>(src + min(4 * i + (lane >> 4), n - 1) * DLFP_HEAD_DIM);
   if ((unsigned)pos >= (unsigned)r.positions) return;
   const Turn turn = load_turn(r, pos, chunk);
-  const uint16_t* src = a.q + t * a.ldq + 8 * chunk;
-  uint16_t* dst = a.out + t * a.ldo + 8 * chunk;
-  for (int h = h0; h < h1; h += 4) {
-    const int head = h + (lane >> 4), at = min(head, h1 - 1);
-    const uint4 v = *reinterpret_cast<const uint4*>(src + (int64_t)at * DLFP_HEAD_DIM);
-    const uint32_t x[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < QUERY_HEADS / 4; ++i) {
+    const int head = 4 * i + (lane >> 4);
+    const uint32_t x[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
     float y[8];
     rotate(r, turn, chunk, x, y);
     const uint4 o = {rope_pack(y[0], y[1]), rope_pack(y[2], y[3]), rope_pack(y[4], y[5]),
                      rope_pack(y[6], y[7])};
-    if (head < h1) *reinterpret_cast<uint4*>(dst + (int64_t)head * DLFP_HEAD_DIM) = o;
+    if (head < n) *reinterpret_cast<uint4*>(dst + head * DLFP_HEAD_DIM) = o;
   }
 }
 
