@@ -1817,20 +1817,6 @@ __global__ void fill_zero_kernel(int* p, int64_t n) {
   if (i < n) p[i] = 0;
 }
 
-// Compute units of the current device (queried once per device).
-int compute_units() {
-  static int cached[64] = {0};
-  int dev = 0;
-  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
-  if (!cached[dev]) {
-    int n = 0;
-    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0)
-      n = 256;
-    cached[dev] = n;
-  }
-  return cached[dev];
-}
-
 template <int G, bool APP>
 hipError_t launch(const Args& a, int grid, hipStream_t stream) {
   if (a.num_prefill == 0 && a.wide == 4)
@@ -1922,7 +1908,7 @@ int launch_mixed(const dlfp_dims* dims, const dlfp_meta* meta, const int32_t* d_
   // slots, fewer when there are fewer units; they drain the decode queue.  Only
   // those that find a slot left by the append and prefill workgroups from the
   // start (at least 64) get units by position.
-  const int cus = compute_units();
+  const int cus = dlfp::compute_units();
   const int decode_units = meta->num_units - meta->num_prefill_units;
   const int ahead = meta->num_prefill_units + a.app_wgs;
   a.wide = dlfp::decode_by_workgroup(*meta, cus) ? 4 : 0;
@@ -1987,6 +1973,24 @@ int static_workspace(void** ptr, hipStream_t stream) {
 }
 
 }  // namespace
+
+namespace dlfp {
+
+// Compute units of the current device (queried once per device).
+int compute_units() {
+  static int cached[64] = {0};
+  int dev = 0;
+  if (hipGetDevice(&dev) != hipSuccess || dev < 0 || dev >= 64) return 256;
+  if (!cached[dev]) {
+    int n = 0;
+    if (hipDeviceGetAttribute(&n, hipDeviceAttributeMultiprocessorCount, dev) != hipSuccess || n <= 0)
+      n = 256;
+    cached[dev] = n;
+  }
+  return cached[dev];
+}
+
+}  // namespace dlfp
 
 extern "C" int dlfp_attention_mixed(const dlfp_dims* dims, const dlfp_meta* meta,
                                     const int32_t* d_work,

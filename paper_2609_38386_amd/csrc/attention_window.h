@@ -60,8 +60,10 @@ struct Args {
   int32_t num_units;
   int32_t num_prefill;
   int32_t out_f32;
-  int32_t lead;         // prefill workgroups before the first decode workgroup
-  int32_t decode_lead;  // decode workgroups before the remaining prefill ones
+  // Grid of a launch with both shares: `lead` prefill workgroups, `decode_lead`
+  // decode ones, then groups of eight workgroups, prefill_groups and decode_groups
+  // of them evenly mixed, then what is left of each share.
+  int32_t lead, decode_lead, prefill_groups, decode_groups;
   float scale_log2;
 };
 
@@ -90,29 +92,43 @@ __device__ __forceinline__ float scale_of(int byte) {
   return __builtin_bit_cast(float, byte ? (uint32_t)byte << 23 : 0x00400000u);
 }
 
-// Which keys a unit's rows see.
+// Which keys a unit's rows see, in virtual keys: a row at position p those below
+// end(p) that are not below low(p), or are below `sinks`.  (The gap ends before
+// the window of every row of the unit, so the sink pages keep their positions and
+// all other keys move by the gap.)
 struct Span {
   int window, sinks;
   int sink_pages, gap;  // virtual pages from sink_pages on are `gap` pages further
   __device__ __forceinline__ int page(int vp) const { return vp >= sink_pages ? vp + gap : vp; }
-  __device__ __forceinline__ bool sees(int pos, int key) const {
-    return key <= pos && (pos - key < window || key < sinks);
+  __device__ __forceinline__ int low(int p) const { return max(p - window + 1 - PAGE * gap, 0); }
+  __device__ __forceinline__ int end(int p) const { return p + 1 - PAGE * gap; }
+  // Whether virtual keys [v0, v1) hold one that rows up to position p do not see
+  // because it lies before their window.
+  __device__ __forceinline__ bool below(int v0, int v1, int p) const {
+    return v0 < low(p) && v1 > sinks;
   }
-  // Whether virtual keys [v0, v1) hold one that a row among positions first ..
-  // last does not see (may say so of some that do not).
-  __device__ __forceinline__ bool edge(int v0, int v1, int first, int last) const {
-    const int k0 = page(v0 / PAGE) * PAGE, k1 = page((v1 - 1) / PAGE) * PAGE + PAGE - 1;
-    return k1 > first || (last - k0 >= window && k1 >= sinks);
+  // Bit i: the position of the value page from virtual key v on whose slot is seen
+  // by a row at p, keys from `stop` on left out.
+  __device__ __forceinline__ uint32_t seen(int v, int p, int stop) const {
+    auto first = [](int n) { return (1u << min(max(n, 0), PAGE)) - 1; };
+    const uint32_t m = (~first(low(p) - v) | first(sinks - v)) & first(stop - v);
+    return (m & 0xF00Fu) | ((m & 0x00F0u) << 4) | ((m & 0x0F00u) >> 4);
   }
 };
-template <class R>
-__device__ __forceinline__ Span span_of(const R& f) {
+__device__ __forceinline__ Span span_of(record_t f) {
   Span s;
   s.window = f[DLFP_W_WINDOW];
   s.sinks = f[DLFP_W_SINKS];
   s.gap = f[DLFP_W_GAP];
   s.sink_pages = s.gap ? (s.sinks + PAGE - 1) / PAGE : 0;
   return s;
+}
+// Masks of a pair of 16-bit values, of four bytes, from their bits.
+__device__ __forceinline__ uint32_t pair_mask(uint32_t bits) {
+  return (bits & 1 ? 0x0000FFFFu : 0u) | (bits & 2 ? 0xFFFF0000u : 0u);
+}
+__device__ __forceinline__ uint32_t byte_mask(uint32_t bits) {
+  return (((bits & 15) * 0x00204081u) & 0x01010101u) * 0xFFu;
 }
 
 // Probabilities of two keys as bf16 pairs, for the matrix products.  bf16 output:
@@ -140,8 +156,22 @@ struct PreLds {
   static constexpr int BYTES = ETAB + (KV8 ? 2 * PRE_PTAB : 0);
 };
 
+// Per wavefront of a decode unit: a key slot and a value slot of one block each
+// (32 keys of bf16 pages, 64 of 8-bit ones), ids and exponents of its pages.
+constexpr int SLOT = 8192;
+template <bool KV8, int NW>
+constexpr int decode_wave_lds() {
+  return 2 * SLOT + ((DEC_PTAB / NW + 4) * (KV8 ? 6 : 4) + 63) / 64 * 64;
+}
+
+template <bool KV8>
+constexpr int window_lds() {
+  constexpr int pre = PreLds<KV8>::BYTES, dec = 4 * decode_wave_lds<KV8, 4>();
+  return pre > dec ? pre : dec;
+}
+
 template <int G, bool KV8, bool OUT32>
-__device__ void prefill_unit(const Args& a, const record_t f, char* smem, int* flag) {
+__device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, char* smem, int* flag) {
   using L = PreLds<KV8>;
   constexpr int PB = page_bytes<KV8>();
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
@@ -157,11 +187,15 @@ __device__ void prefill_unit(const Args& a, const record_t f, char* smem, int* f
   const int r = wave * 32 + col;  // this lane's row within the tile
   const int tr = r / G, hh = r % G;
   const bool row_ok = tr < nt;
-  const int pos = row_ok ? pos0 + tr : -1;  // rows past the tile see nothing
+  // Virtual keys [v_low, v_end) and those below the sinks are this row's; rows past
+  // the tile see nothing.
+  const int v_end = row_ok ? min(sp.end(pos0 + tr), ve) : 0;
+  const int v_low = row_ok ? sp.low(pos0 + tr) : 0;
   const int wave_tok0 = uniform((wave * 32) / G);
   const bool wave_active = wave_tok0 < nt;
-  // Positions of the wavefront's first and last row.
-  const int wave_first = pos0 + wave_tok0;
+  // Keys from wave_end on some row of the wavefront does not see; the position of
+  // its last row.
+  const int wave_end = min(sp.end(pos0 + wave_tok0), ve);
   const int wave_last = pos0 + min(nt - 1, uniform((wave * 32 + 31) / G));
 
   // Q^T as the B operand.  Rows past the tile load its first one.
@@ -179,6 +213,7 @@ __device__ void prefill_unit(const Args& a, const record_t f, char* smem, int* f
   const int first_page = vb / PAGE, npages = (ve - 1) / PAGE - first_page + 1;
   int32_t* ptab = reinterpret_cast<int32_t*>(smem + L::PTAB);
   uint16_t* etab = reinterpret_cast<uint16_t*>(smem + L::ETAB);
+#pragma unroll 4
   for (int i = tid; i < npages; i += THREADS) {
     int id = bt[sp.page(first_page + i)];
     if ((unsigned)id >= (unsigned)a.num_blocks) {
@@ -186,10 +221,6 @@ __device__ void prefill_unit(const Args& a, const record_t f, char* smem, int* f
       id = 0;
     }
     ptab[i] = id;
-    if constexpr (KV8) {
-      const int64_t e = (int64_t)id * a.hkv + kh;
-      etab[i] = (uint16_t)(a.k_exp[e] | a.v_exp[e] << 8);
-    }
   }
   wait_memory_complete();
   __syncthreads();
@@ -213,10 +244,8 @@ __device__ void prefill_unit(const Args& a, const record_t f, char* smem, int* f
       voff[i] = d * 32 + (((ck & 1) ^ vt_swz(d)) << 4);
     }
   }
-  auto page_off = [&](int t) -> int64_t {
-    const int id = uniform(ptab[min(4 * t + wave, npages - 1)]);
-    return ((int64_t)id * a.hkv + kh) * PB;
-  };
+  auto page_id = [&](int t) { return ptab[min(4 * t + wave, npages - 1)]; };
+  auto page_off = [&](int id) -> int64_t { return ((int64_t)uniform(id) * a.hkv + kh) * PB; };
   const uint32_t lds_wave = lds_addr(smem) + uniform(wave) * PB;
   auto issue_k = [&](int64_t off, int slot) {
     const char* src = uniform_ptr(a.kc + off);
@@ -229,43 +258,33 @@ __device__ void prefill_unit(const Args& a, const record_t f, char* smem, int* f
     for (int i = 0; i < NC; ++i)
       lds_copy16(src, voff[i], lds_wave + L::V_BASE + slot * L::TILE + i * 1024);
   };
-  // Values that no row of the unit sees are zeroed in LDS (a probability of 0
-  // times a NaN would still be NaN).
-  auto unseen = [&](int vkey) {
-    const int key = sp.page(vkey / PAGE) * PAGE + vkey % PAGE;
-    return vkey >= ve || (pos0 - key >= sp.window && key >= sp.sinks);
-  };
-  auto zero_unseen = [&](int slot, int v0) {
-    const int pg = tid >> 6;
-    constexpr int CH = PB / 1024;  // 16-byte chunks of the page for this thread
-#pragma unroll
-    for (int c = 0; c < CH; ++c) {
-      if constexpr (KV8) {
-        u32x4_t* p = reinterpret_cast<u32x4_t*>(smem + L::V_BASE + slot * L::TILE + pg * PB) +
-                     64 * c + lane;
-        u32x4_t v = *p;
-#pragma unroll
-        for (int e = 0; e < 16; ++e)
-          if (unseen(v0 + pg * PAGE + vt_pos(e))) v[e >> 2] &= ~(0xFFu << (8 * (e & 3)));
-        *p = v;
-      } else {
-        const int d = 2 * lane + (c >> 1), h = c & 1, half = h ^ vt_swz(d);
-        u32x4_t* p = reinterpret_cast<u32x4_t*>(smem + L::V_BASE + slot * L::TILE + pg * PB +
-                                                d * 32 + (h << 4));
-        u32x4_t v = *p;
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (unseen(v0 + pg * PAGE + vt_pos(8 * half + e)))
-            v[e >> 1] &= e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
-        *p = v;
-      }
-    }
-  };
-  // Tiles with such values: where some key is past the end, or before the first
-  // row's window and no sink.
+  // Values that no row of the unit sees (before the first one's window and no
+  // sinks, or past the unit's end) are zeroed in LDS: a probability of 0 times a
+  // NaN would still be NaN.  Wavefront w does page w of the tile.
   auto has_unseen = [&](int t) {
     const int v0 = vb + t * KV_TILE;
-    return v0 + KV_TILE > ve || sp.edge(v0, v0 + KV_TILE, 0x7FFFFFFF, pos0);
+    return v0 + KV_TILE > ve || sp.below(v0, v0 + KV_TILE, pos0);
+  };
+  auto zero_unseen = [&](int slot, int v0) {
+    const int pg = uniform(wave);
+    const uint32_t seen = sp.seen(v0 + pg * PAGE, pos0, ve);
+    if (seen == 0xFFFFu) return;
+    u32x4_t* page = reinterpret_cast<u32x4_t*>(smem + L::V_BASE + slot * L::TILE + pg * PB);
+#pragma unroll
+    for (int c = 0; c < NC; ++c) {
+      const int ck = 64 * c + lane;
+      u32x4_t v = page[ck];
+      if constexpr (KV8) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) v[w] &= byte_mask(seen >> (4 * w));
+      } else {
+        const bool upper = (ck & 1) ^ vt_swz(ck >> 1);  // positions 8 .. 15
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          v[w] &= upper ? pair_mask(seen >> (8 + 2 * w)) : pair_mask(seen >> (2 * w));
+      }
+      page[ck] = v;
+    }
   };
 
   // Per-lane LDS offsets of the operands.
@@ -324,17 +343,31 @@ __device__ void prefill_unit(const Args& a, const record_t f, char* smem, int* f
       }
     }
   };
-  // Masks the scores of a tile starting at virtual key v0.
+  // Masks the scores of a tile starting at virtual key v0, where it has to be.
+  auto needs_mask = [&](int v0) {
+    return v0 + KV_TILE > wave_end || sp.below(v0, v0 + KV_TILE, wave_last);
+  };
   auto mask = [&](f32x16_t* sacc, int v0) {
+    // Register rr of accumulator j is key v0 + base + at(j, rr).
+    const int base = KV8 ? 16 * hi : 4 * hi;
+    auto at = [](int j, int rr) {
+      return 32 * j + (KV8 ? vt_pos(rr) : 8 * (rr >> 2) + (rr & 3));
+    };
+    const float none = -__builtin_inff();
+    if (v0 + KV_TILE > wave_end) {
+      const int n = v_end - v0 - base;
 #pragma unroll
-    for (int j = 0; j < 2; ++j)
+      for (int x = 0; x < 32; ++x)
+        sacc[x >> 4][x & 15] = at(x >> 4, x & 15) < n ? sacc[x >> 4][x & 15] : none;
+    }
+    if (sp.below(v0, v0 + KV_TILE, wave_last)) {
+      const int n = v_low - v0 - base, m = sp.sinks - v0 - base;
 #pragma unroll
-      for (int rr = 0; rr < 16; ++rr) {
-        const int pg = KV8 ? 2 * j + hi : 2 * j + (rr >> 3);
-        const int slot = KV8 ? vt_pos(rr) : 8 * ((rr >> 2) & 1) + 4 * hi + (rr & 3);
-        const int vkey = v0 + pg * PAGE + slot, key = sp.page(v0 / PAGE + pg) * PAGE + slot;
-        sacc[j][rr] = vkey < ve && sp.sees(pos, key) ? sacc[j][rr] : -__builtin_inff();
+      for (int x = 0; x < 32; ++x) {
+        const int k = at(x >> 4, x & 15);
+        sacc[x >> 4][x & 15] = k >= n || k < m ? sacc[x >> 4][x & 15] : none;
       }
+    }
   };
   auto rowmax = [&](const f32x16_t* sacc) {
     float m4[4];
@@ -435,12 +468,19 @@ __device__ void prefill_unit(const Args& a, const record_t f, char* smem, int* f
   };
 
   // Tiles 0 (K and V) and 1 (K) in flight, then S_0.
-  int64_t off_next = page_off(0);
+  int64_t off_next = page_off(page_id(0));
   issue_k(off_next, 0);
   issue_v(off_next, 0);
   if (ntiles > 1) {
-    off_next = page_off(1);
+    off_next = page_off(page_id(1));
     issue_k(off_next, 1);
+  }
+  if constexpr (KV8) {  // with the first tiles on their way
+#pragma unroll 4
+    for (int i = tid; i < npages; i += THREADS) {
+      const int64_t e = (int64_t)ptab[i] * a.hkv + kh;
+      etab[i] = (uint16_t)(a.k_exp[e] | a.v_exp[e] << 8);
+    }
   }
   wait_memory_complete();
   __syncthreads();
@@ -451,10 +491,11 @@ __device__ void prefill_unit(const Args& a, const record_t f, char* smem, int* f
   f32x16_t sa[2], sb[2];
   if (wave_active) {
     qk(sa, 0, 0);
-    if (vb + KV_TILE > ve || sp.edge(vb, vb + KV_TILE, wave_first, wave_last)) mask(sa, vb);
+    if (needs_mask(vb)) mask(sa, vb);
     rebase(rowmax(sa));
   }
   __syncthreads();  // K slot 0 is refilled below
+  int id2 = page_id(2);  // read a step before its use
 
   // Step j: loads of K_{j+2} and V_{j+1} go out; S_{j+1} = K_{j+1} Q^T beside the
   // first half of tile j's exponentials; the second half beside the first half of
@@ -464,17 +505,36 @@ __device__ void prefill_unit(const Args& a, const record_t f, char* smem, int* f
     const bool more = j + 1 < ntiles;
     if (more) issue_v(off_next, PAR ^ 1);
     if (j + 2 < ntiles) {
-      off_next = page_off(j + 2);
+      off_next = page_off(id2);
       issue_k(off_next, PAR);
     }
+    id2 = page_id(j + 3);
     if (wave_active) {
       bf16x8_t pf[4];
       // On the last tile this reads a stale slot; the result is not used.
       qk(nxt, PAR ^ 1, j + 1);
       probs(cur, pf, 0, 2);
+      if constexpr (!KV8) {
+        // Key operands four products ahead, exponentials between the products.
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+        }
+      }
       __builtin_amdgcn_s_setprio(1);
       probs(cur, pf, 2, 4);
       pv(pf, PAR, j, 0, 1);
+      if constexpr (!KV8) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 1);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 1);
+          __builtin_amdgcn_sched_group_barrier(0x002, 5, 1);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 1);
+        }
+      }
       __builtin_amdgcn_sched_barrier(0);
       pv(pf, PAR, j, 1, 2);
       rowsum(pf);
@@ -485,10 +545,19 @@ __device__ void prefill_unit(const Args& a, const record_t f, char* smem, int* f
         pv(pf, PAR, j, 0, 2);
       }
       float mx = rowmax(nxt);
+      if constexpr (!KV8 && !OUT32) {
+        __builtin_amdgcn_sched_group_barrier(0x100, 4, 2);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          __builtin_amdgcn_sched_group_barrier(0x008, 1, 2);
+          __builtin_amdgcn_sched_group_barrier(0x002, 5, 2);
+          __builtin_amdgcn_sched_group_barrier(0x100, 1, 2);
+        }
+      }
       __builtin_amdgcn_s_setprio(0);
       if (more) {
         const int v1 = vb + (j + 1) * KV_TILE;
-        if (v1 + KV_TILE > ve || sp.edge(v1, v1 + KV_TILE, wave_first, wave_last)) {
+        if (needs_mask(v1)) {
           mask(nxt, v1);
           mx = rowmax(nxt);
         }
@@ -513,15 +582,39 @@ __device__ void prefill_unit(const Args& a, const record_t f, char* smem, int* f
   const int rows = nt * G;
   // o[mb][rr] = O[row][32 mb + 8 (rr / 4) + 4 hi + rr % 4]
   if (nsplits == 1) {
-    if (row_ok) {
-      const float inv = 1.f / l_run;
-      const int64_t orow = ((int64_t)(row0 + tr) * a.hq + kh * G + hh) * D;
+    // Through the wavefront's part of the tiles' LDS, so that stores are whole
+    // rows: a row's 16-byte chunk x sits at x ^ row.
+    if (!wave_active) return;
+    constexpr int ROW = OUT32 ? 512 : 256, CHUNKS = ROW / 16;
+    static_assert(128 * ROW <= window_lds<KV8>(), "the tile's rows");
+    char* rows_lds = smem + wave * 32 * ROW;
+    const float inv = 1.f / l_run;
 #pragma unroll
-      for (int mb = 0; mb < 4; ++mb)
+    for (int mb = 0; mb < 4; ++mb)
 #pragma unroll
-        for (int g4 = 0; g4 < 4; ++g4)
-          store4(a, orow + mb * 32 + 8 * g4 + 4 * hi, o[mb][4 * g4] * inv,
-                 o[mb][4 * g4 + 1] * inv, o[mb][4 * g4 + 2] * inv, o[mb][4 * g4 + 3] * inv);
+      for (int g4 = 0; g4 < 4; ++g4) {
+        float x[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) x[i] = o[mb][4 * g4 + i] * inv;
+        char* row = rows_lds + col * ROW;
+        if constexpr (OUT32)
+          *reinterpret_cast<f32x4_t*>(row + (((8 * mb + 2 * g4 + hi) ^ col) << 4)) =
+              f32x4_t{x[0], x[1], x[2], x[3]};
+        else
+          *reinterpret_cast<u32x2_t*>(row + (((4 * mb + g4) ^ (col & 15)) << 4) + 8 * hi) =
+              u32x2_t{pack_bf16(x[0], x[1]), pack_bf16(x[2], x[3])};
+      }
+    wave_sync();
+    char* out = static_cast<char*>(a.out);
+#pragma unroll
+    for (int i = 0; i < 32 * CHUNKS / 64; ++i) {
+      const int at = 64 * i + lane, lr = at / CHUNKS, x = at % CHUNKS;
+      const int rr = wave * 32 + lr, t = rr / G;
+      const u32x4_t v =
+          *reinterpret_cast<const u32x4_t*>(rows_lds + lr * ROW + ((x ^ (lr & (CHUNKS - 1))) << 4));
+      if (t < nt)
+        *reinterpret_cast<u32x4_t*>(
+            out + ((int64_t)(row0 + t) * a.hq + kh * G + rr % G) * ROW + 16 * x) = v;
     }
     return;
   }
@@ -562,14 +655,6 @@ __device__ void prefill_unit(const Args& a, const record_t f, char* smem, int* f
 
 // ---------------------------------------------------------------- decode
 
-// Per wavefront of a decode unit: a key slot and a value slot of one block each
-// (32 keys of bf16 pages, 64 of 8-bit ones), ids and exponents of its pages.
-constexpr int SLOT = 8192;
-template <bool KV8, int NW>
-constexpr int decode_wave_lds() {
-  return 2 * SLOT + ((DEC_PTAB / NW + 4) * (KV8 ? 6 : 4) + 63) / 64 * 64;
-}
-
 // Decode unit of a workgroup of NW wavefronts: wavefront w takes blocks w, w + NW,
 // ... of the unit; their results meet in LDS, those of split ranges in memory.
 // The unit's g heads are columns 0-7 of 16x16 products and, with the second term
@@ -577,7 +662,7 @@ constexpr int decode_wave_lds() {
 // q = l / 16 owns, of 8-bit pages, the 16 keys of page q of the block, of bf16
 // pages the eight at positions 8 (q / 2) .. of page q % 2.
 template <int G, bool KV8, bool OUT32, int NW>
-__device__ void decode_unit(const Args& a, const int32_t* rec, char* smem, int* flag) {
+__device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, char* smem, int* flag) {
   static_assert(G >= 1 && G <= 8, "heads");
   constexpr int PB = page_bytes<KV8>();
   constexpr int BP = SLOT / PB;       // pages of a block
@@ -604,7 +689,7 @@ __device__ void decode_unit(const Args& a, const int32_t* rec, char* smem, int* 
   auto page_of = [&](int i, int h) { return min(BP * (wave + NW * i) + h, npages - 1); };
   auto pages_in = [&](int i) { return min(BP, npages - BP * (wave + NW * i)); };
 
-  // Ids (and exponents) of the wavefront's pages; the queries as the B operand.
+  // Ids of the wavefront's pages; the queries as the B operand.
   for (int x = lane; x < BP * mine; x += 64) {
     int id = bt[sp.page(first_page + page_of(x / BP, x % BP))];
     if ((unsigned)id >= (unsigned)a.num_blocks) {
@@ -612,10 +697,6 @@ __device__ void decode_unit(const Args& a, const int32_t* rec, char* smem, int* 
       id = 0;
     }
     ptab[x] = id;
-    if constexpr (KV8) {
-      const int64_t e = (int64_t)id * a.hkv + kh;
-      etab[x] = (uint16_t)(a.k_exp[e] | a.v_exp[e] << 8);
-    }
   }
   bf16x8_t qb[4];
   {
@@ -674,6 +755,13 @@ __device__ void decode_unit(const Args& a, const int32_t* rec, char* smem, int* 
     issue_k(0);
     issue_v(0);
   }
+  if constexpr (KV8) {  // with the first block on its way
+    for (int x = lane; x < BP * mine; x += 64) {
+      const int64_t e = (int64_t)ptab[x] * a.hkv + kh;
+      etab[x] = (uint16_t)(a.k_exp[e] | a.v_exp[e] << 8);
+    }
+    wave_sync();
+  }
 
   float m_run = NEG_BIG, l_run = 0.f;
   f32x4_t o[8];
@@ -700,7 +788,7 @@ __device__ void decode_unit(const Args& a, const int32_t* rec, char* smem, int* 
     const int v0 = vb + BP * PAGE * (wave + NW * i);  // first virtual key of the block
     const int n = pages_in(i);
     const bool more = i + 1 < mine, full = n == BP;
-    const bool edge = v0 + BP * PAGE > ve || sp.edge(v0, v0 + BP * PAGE, pos, pos);
+    const bool edge = v0 + BP * PAGE > ve || sp.below(v0, v0 + BP * PAGE, pos);
     // In flight, oldest first: this block's keys, its values (eight copies each
     // of a full block; others are the unit's last).
     if (full)
@@ -749,13 +837,13 @@ __device__ void decode_unit(const Args& a, const int32_t* rec, char* smem, int* 
     wait_lds();  // the key slot is free
     if (more) issue_k(i + 1);
     const bool next_full = more && pages_in(i + 1) == BP;
-    // Position and virtual key of slot 0 of this lane group's page.
-    const int base = sp.page(v0 / PAGE + vpage) * PAGE, vbase = v0 + vpage * PAGE;
     if (edge) {
+      const int base = v0 + vpage * PAGE + slot_of(0);
+      const int stop = ve - base, low = sp.low(pos) - base, sinks = sp.sinks - base;
 #pragma unroll
       for (int x = 0; x < 4 * NCH; ++x) {
-        const int slot = slot_of(x >> 2) + (x & 3);
-        sc[x] = vbase + slot < ve && sp.sees(pos, base + slot) ? sc[x] : -__builtin_inff();
+        const int k = (KV8 ? vt_pos(x & 12) : 8 * (x >> 2)) + (x & 3);
+        sc[x] = k < stop && (k >= low || k < sinks) ? sc[x] : -__builtin_inff();
       }
     }
     float mx = -__builtin_inff();
@@ -794,28 +882,25 @@ __device__ void decode_unit(const Args& a, const int32_t* rec, char* smem, int* 
       // Values that the token does not see are zeroed (a probability of 0 times
       // a NaN would still be NaN).
 #pragma unroll
-      for (int j = 0; j < 8; ++j) {
-        const int pg = j / NC, ck = 64 * (j % NC) + lane;
-        const int vkey = v0 + pg * PAGE, key = sp.page(v0 / PAGE + pg) * PAGE;
-        u32x4_t* p = reinterpret_cast<u32x4_t*>(wl + SLOT + pg * PB + ck * 16);
-        u32x4_t v = *p;
-        if constexpr (KV8) {
+      for (int pg = 0; pg < BP; ++pg) {
+        const uint32_t seen = sp.seen(v0 + pg * PAGE, pos, ve);
+        if (seen == 0xFFFFu) continue;
+        u32x4_t* page = reinterpret_cast<u32x4_t*>(wl + SLOT + pg * PB);
 #pragma unroll
-          for (int e = 0; e < 16; ++e) {
-            const int slot = vt_pos(e);
-            if (vkey + slot >= ve || !sp.sees(pos, key + slot))
-              v[e >> 2] &= ~(0xFFu << (8 * (e & 3)));
-          }
-        } else {
-          const int half = (ck & 1) ^ vt_swz(ck >> 1);
+        for (int j = 0; j < NC; ++j) {
+          const int ck = 64 * j + lane;
+          u32x4_t v = page[ck];
+          if constexpr (KV8) {
 #pragma unroll
-          for (int e = 0; e < 8; ++e) {
-            const int slot = vt_pos(8 * half + e);
-            if (vkey + slot >= ve || !sp.sees(pos, key + slot))
-              v[e >> 1] &= e & 1 ? 0x0000FFFFu : 0xFFFF0000u;
+            for (int w = 0; w < 4; ++w) v[w] &= byte_mask(seen >> (4 * w));
+          } else {
+            const bool upper = (ck & 1) ^ vt_swz(ck >> 1);  // positions 8 .. 15
+#pragma unroll
+            for (int w = 0; w < 4; ++w)
+              v[w] &= upper ? pair_mask(seen >> (8 + 2 * w)) : pair_mask(seen >> (2 * w));
           }
+          page[ck] = v;
         }
-        *p = v;
       }
       wave_sync();
     }
@@ -962,25 +1047,39 @@ __device__ void decode_unit(const Args& a, const int32_t* rec, char* smem, int* 
 
 // ---------------------------------------------------------------- kernels
 
-template <bool KV8>
-constexpr int window_lds() {
-  constexpr int pre = PreLds<KV8>::BYTES, dec = 4 * decode_wave_lds<KV8, 4>();
-  return pre > dec ? pre : dec;
+// The unit of workgroup b of a launch with prefill units.  The i-th prefill
+// workgroup takes unit xcd_remap(i); all parts of the grid but the last begin at a
+// multiple of eight, so it runs on XCD i % 8.
+__device__ __forceinline__ int unit_of(const Args& a, int b) {
+  const int np = a.num_prefill;
+  if (b < a.lead) return xcd_remap(b, np);
+  b -= a.lead;
+  if (b < a.decode_lead) return np + b;
+  b -= a.decode_lead;
+  const int gp = a.prefill_groups, g = gp + a.decode_groups;
+  const int group = b >> 3, lane = b & 7;
+  const int before = group < g ? (int)((uint64_t)group * gp / max(g, 1)) : gp;
+  if (group < g) {
+    const bool prefill = (int)((uint64_t)(group + 1) * gp / g) > before;
+    return prefill ? xcd_remap(a.lead + 8 * before + lane, np)
+                   : np + a.decode_lead + 8 * (group - before) + lane;
+  }
+  b -= 8 * g;
+  const int left = np - a.lead - 8 * gp;
+  return b < left ? xcd_remap(a.lead + 8 * gp + b, np)
+                  : np + a.decode_lead + 8 * a.decode_groups + b - left;
 }
 
-// Prefill units, then (with `lead`, from the middle on) decode units of a
-// workgroup each.
 template <int G, bool KV8, bool OUT32>
 __global__ __launch_bounds__(THREADS, 2) void window_kernel(Args a) {
   __shared__ __attribute__((aligned(16))) char smem[window_lds<KV8>()];
   __shared__ int flag;
-  const int b = blockIdx.x, np = a.num_prefill, L = a.lead, DL = a.decode_lead;
-  const int u = b < L ? xcd_remap(b, np)
-                      : b < L + DL ? L - 1 - b : b < np + DL ? xcd_remap(b - DL, np) : np - 1 - b;
-  if (u >= 0)
-    prefill_unit<G, KV8, OUT32>(a, load_record(a.work + (int64_t)u * DLFP_WORK_INTS), smem, &flag);
+  const int u = unit_of(a, blockIdx.x);
+  const int32_t* rec = a.work + (int64_t)u * DLFP_WORK_INTS;
+  if (u < a.num_prefill)
+    prefill_unit<G, KV8, OUT32>(a, load_record(rec), smem, &flag);
   else
-    decode_unit<G, KV8, OUT32, 4>(a, a.work + (int64_t)(np - 1 - u) * DLFP_WORK_INTS, smem, &flag);
+    decode_unit<G, KV8, OUT32, 4>(a, rec, smem, &flag);
 }
 
 template <int G, bool KV8, bool OUT32, int NW>
@@ -996,8 +1095,10 @@ hipError_t launch_window(const Args& a, int nw, hipStream_t stream) {
     window_kernel<G, KV8, OUT32><<<a.num_units, THREADS, 0, stream>>>(a);
   else if (nw == 8)
     window_decode_kernel<G, KV8, OUT32, 8><<<a.num_units, 8 * 64, 0, stream>>>(a);
-  else
+  else if (nw == 4)
     window_decode_kernel<G, KV8, OUT32, 4><<<a.num_units, 4 * 64, 0, stream>>>(a);
+  else
+    window_decode_kernel<G, KV8, OUT32, 1><<<a.num_units, 64, 0, stream>>>(a);
   return hipGetLastError();
 }
 
@@ -1055,13 +1156,31 @@ int attention_window(const dlfp_dims* dims, const dlfp_meta* meta, const int32_t
   a.num_prefill = meta->num_prefill_units;
   a.out_f32 = out_dtype;
   a.scale_log2 = scale * LOG2E;
-  // Beside more prefill units than compute units the decode units start after
-  // one prefill unit for each of those.
+  const int cus = dlfp::compute_units();
   const int decode_units = a.num_units - a.num_prefill;
-  a.lead = meta->prefill_lead_units;
-  a.decode_lead = a.lead < a.num_prefill ? std::min(decode_units, 256) / 8 * 8 : 0;
-  if (a.decode_lead == 0) a.lead = a.num_prefill;
-  const int nw = a.num_units > 4 * 256 ? 4 : 8;
+  // One prefill unit for each compute unit, one decode unit for each, then the
+  // rest of both in equal measure, so that a compute unit has one of each kind as
+  // long as there are both.
+  a.lead = a.num_prefill;
+  a.decode_lead = a.prefill_groups = a.decode_groups = 0;
+  if (meta->prefill_lead_units < a.num_prefill && decode_units >= 8) {
+    a.lead = meta->prefill_lead_units / 8 * 8;
+    a.decode_lead = std::min(decode_units, cus) / 8 * 8;
+    a.prefill_groups = (a.num_prefill - a.lead) / 8;
+    a.decode_groups = (decode_units - a.decode_lead) / 8;
+  }
+  // Wavefronts of a decode unit's workgroup in a launch of decode units alone.
+  // One, with units of up to 128 KiB of cache that are more than three for each
+  // compute unit: a workgroup is then mostly its start and its sum (2048 units of
+  // 64 keys, 8-bit pages 10.2 us, with four wavefronts 20.9; of 512 keys 45.9 and
+  // 48.8; bf16, 128 keys 23.9 and 27.2).  Eight, with long units on a quarter of
+  // the compute units: one lasts as long as its chain of steps (8 units of 2048
+  // keys 15.0 and 17.2 us).  Else four, two workgroups on a compute unit, one's
+  // start and sum behind the other (512 units of 1024 keys, 8 bits: 23.2 us, with
+  // eight 26.5, with one 31.5).
+  const int64_t unit_bytes = (int64_t)meta->decode_split_tokens * 2 * DLFP_HEAD_DIM * (KV8 ? 1 : 2);
+  const int nw = a.num_units > 3 * cus && unit_bytes <= 128 << 10 ? 1
+                 : a.num_units <= cus / 4 && meta->decode_split_tokens > 256 ? 8 : 4;
   (void)hipGetLastError();
   hipError_t e;
   switch (g) {

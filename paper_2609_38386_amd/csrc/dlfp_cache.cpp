@@ -160,16 +160,44 @@ int build(const dlfp_dims* dims, const dlfp_tuning* tuning, const dlfp_window* w
     const int64_t part = ceil_div(tile_keys * hkv, slots);
     split_p = std::clamp<int64_t>(round_up(part, 64), 512, DLFP_MAX_PREFILL_UNIT_KEYS);
   }
+  // A decoder's range is cut into n equal parts when it is longer than the split.
+  auto cut = [](int64_t keys, int64_t split, int64_t granule) {
+    const int64_t n = ceil_div(keys, split);
+    return round_up(ceil_div(keys, n), granule);
+  };
   int64_t split_d = tn.decode_split_tokens;
-  if (!split_d) {
-    const int64_t part = ceil_div(one_keys * hkv, slots);
-    split_d = std::clamp<int64_t>(round_up(part, 64), 256, DLFP_MAX_DECODE_UNIT_KEYS);
+  if (!split_d && !ones.empty()) {
+    // The split (an n-th of the longest range) that minimises an estimate of the
+    // decode share's time in us: full rounds of units and the rest of the last one
+    // stream at 6.2 TB/s (384 bytes a key, between the two kinds of pages), no unit
+    // faster than 6.3 ns a key; a merge takes 3 us and 0.05 for each part.
+    double best = 0.;
+    for (int64_t n = ceil_div(one_longest, DLFP_MAX_DECODE_UNIT_KEYS); n <= 256; ++n) {
+      const int64_t split = std::max<int64_t>(round_up(ceil_div(one_longest, n), 64), 128);
+      int64_t count = 0, longest = 0, parts = 1;
+      for (const Rows& r : ones) {
+        const int64_t part = cut(r.keys, split, 64), p = ceil_div(r.keys, part);
+        count += p;
+        longest = std::max(longest, std::min(part, r.keys));
+        parts = std::max(parts, p);
+      }
+      count *= hkv;
+      const double keys_us = 6.2e6 / 384, mean = (double)one_keys * hkv / count;
+      const int64_t full = count / slots, rest = count % slots;
+      const double est = full * slots * mean / keys_us + 0.7 * full +
+                         (rest ? std::max(longest * 6.3e-3, rest * mean / keys_us) : 0.) +
+                         (parts > 1 ? 3. + 0.05 * parts : 0.);
+      if (!split_d || est < best) {
+        best = est;
+        split_d = split;
+      }
+      if (split == 128) break;
+    }
   }
-
   std::vector<Unit> units;
   int64_t groups = 0, off = DLFP_WORKSPACE_PARTIALS / 4;
   auto emit = [&](const Rows& r, int64_t kh, int64_t split, int64_t granule, int32_t kind) {
-    const int64_t n = ceil_div(r.keys, split), part = round_up(ceil_div(r.keys, n), granule);
+    const int64_t part = cut(r.keys, split, granule);
     const int64_t parts = ceil_div(r.keys, part);
     const int64_t floats = slot_floats((int64_t)r.nt * g);
     for (int64_t j = 0; j < parts; ++j) {
@@ -209,6 +237,8 @@ int build(const dlfp_dims* dims, const dlfp_tuning* tuning, const dlfp_window* w
     return x.f[DLFP_W_KVEND] - x.f[DLFP_W_KVBEGIN] > y.f[DLFP_W_KVEND] - y.f[DLFP_W_KVBEGIN];
   });
   const int64_t n_units = (int64_t)units.size();
+  const int64_t longest_one =
+      n_units > num_prefill ? units[num_prefill].f[DLFP_W_KVEND] - units[num_prefill].f[DLFP_W_KVBEGIN] : 0;
   if (n_units > I32_MAX / DLFP_WORK_INTS || groups > DLFP_MAX_GROUPS || off > I32_MAX)
     return DLFP_ERANGE;
 
@@ -217,7 +247,7 @@ int build(const dlfp_dims* dims, const dlfp_tuning* tuning, const dlfp_window* w
   meta->num_units = (int32_t)n_units;
   meta->num_prefill_units = (int32_t)num_prefill;
   meta->num_groups = (int32_t)groups;
-  meta->decode_split_tokens = (int32_t)split_d;
+  meta->decode_split_tokens = (int32_t)longest_one;
   meta->prefill_split_tokens = (int32_t)split_p;
   meta->workspace_bytes = 4 * off;
   meta->num_append = 0;

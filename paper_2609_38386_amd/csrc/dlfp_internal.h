@@ -10,6 +10,9 @@ namespace dlfp {
 // DLFP_OK if dims are supported; *group receives Hq / Hkv.
 int check_dims(const dlfp_dims* dims, int* group);
 
+// Compute units of the current device.
+int compute_units();
+
 // The checks that the two rotating appends share (dlfp_cache.h).
 int check_rope_append(const dlfp_dims* dims, const dlfp_rope* rope, int32_t num_tokens,
                       const int32_t* positions, const int32_t* slot_mapping, const void* q,

@@ -341,14 +341,15 @@ def dlfp_append_attention_mixed_static(dims: dlfp_dims, meta: Meta, d_work, d_bl
         _check(st, "dlfp_append_attention_mixed_static")
 
 
-def _rows(t, heads: int, tokens: int) -> int:
+def _rows(t, shape) -> int:
     """Elements between the tokens' rows of a [tokens][heads][128] bf16 tensor whose heads
     are contiguous."""
-    if t.dim() != 3 or t.size(0) != tokens or t.size(1) != heads or t.size(2) != HEAD_DIM:
-        raise ValueError("shapes disagree")
-    if t.element_size() != 2 or t.stride(2) != 1 or (heads > 1 and t.stride(1) != HEAD_DIM):
-        raise ValueError("a token's heads must be contiguous bf16")
-    return t.stride(0) if tokens > 1 else heads * HEAD_DIM
+    if t.shape != shape or t.element_size() != 2:
+        raise ValueError("queries, keys and values must be bf16 [tokens][heads][128]")
+    token, head, dim = t.stride()
+    if dim != 1 or (head != HEAD_DIM and shape[1] > 1):
+        raise ValueError("a token's heads must be contiguous")
+    return token if shape[0] > 1 else shape[1] * HEAD_DIM
 
 
 def make_rope(table, interleaved: bool = False) -> dlfp_rope:
@@ -359,15 +360,15 @@ def make_rope(table, interleaved: bool = False) -> dlfp_rope:
 
 
 def _append_args(dims, rope, positions, slot_mapping, q, k_new, v_new, q_out, k_cache, v_cache):
-    n, hq, hkv = slot_mapping.size(0), dims.num_q_heads, dims.num_kv_heads
+    n = slot_mapping.size(0)
     if positions.size(0) != n:
         raise ValueError("shapes disagree")
     if positions.element_size() != 4 or slot_mapping.element_size() != 4:
         raise ValueError("positions and slots must be int32")
+    qs, ks = (n, dims.num_q_heads, HEAD_DIM), (n, dims.num_kv_heads, HEAD_DIM)
     return (dims, rope, n, positions.data_ptr(), slot_mapping.data_ptr(), q.data_ptr(),
-            _rows(q, hq, n), k_new.data_ptr(), _rows(k_new, hkv, n), v_new.data_ptr(),
-            _rows(v_new, hkv, n), q_out.data_ptr(), _rows(q_out, hq, n), k_cache.data_ptr(),
-            v_cache.data_ptr())
+            _rows(q, qs), k_new.data_ptr(), _rows(k_new, ks), v_new.data_ptr(), _rows(v_new, ks),
+            q_out.data_ptr(), _rows(q_out, qs), k_cache.data_ptr(), v_cache.data_ptr())
 
 
 def dlfp_rope_append(dims: dlfp_dims, rope: dlfp_rope, positions, slot_mapping, q, k_new, v_new,
