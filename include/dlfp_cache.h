@@ -121,16 +121,17 @@ enum {
 #define DLFP_WINDOW_META 3
 
 /* dlfp_build_varlen_meta for dlfp_attention_window and dlfp_attention_kv8: the
- * same arrays and counts (num_append and num_waiting_units are 0;
- * decode_split_tokens is the longest decode unit's key count).  window may
+ * same arrays and counts (num_append is 0, the two split counts are the
+ * keys of the longest unit of each kind, num_waiting_units is the decode share's
+ * keys over the prefill share's times 1024).  window may
  * be null: every key up to a row's own.  Only the pages that a row sees, and
  * those of the new tokens, need a block id in [0, num_blocks); other entries of
  * the block table are not read (a window's dropped pages may be -1).
  * prefill_tile_tokens, the two splits, target_units and prefill_lead_units of
  * the tuning act as in dlfp.h; splits are cut from the keys that are read.
- * Zero fields of the tuning split a prompt's keys so that its units are about two
- * for each compute unit, in parts of at least 512 keys, and the decoders' into
- * equal parts of at least 128 that minimise an estimate of their time.
+ * Zero fields of the tuning choose by estimates of the launch time: prompts in
+ * tiles of 128 rows or of 32 and in equal parts of at least 256 keys, decoders in
+ * equal parts of at least 128.
  * Errors: as dlfp_build_varlen_meta; DLFP_EINVAL for a window below 1 or sinks
  * below 0; DLFP_ENOSPC also when host memory runs out. */
 int dlfp_build_window_meta(const dlfp_dims* dims, const dlfp_tuning* tuning,

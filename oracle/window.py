@@ -141,7 +141,7 @@ def check_window_list(meta, q_len, kv_len, num_q_heads, num_kv_heads, window, si
         assert nt * g <= 128 and 0 <= t0 and t0 + nt <= q_len[s] and nt >= 1
         assert r[12] == cu[s] + t0 and r[13] == kv_len[s] - q_len[s] + t0
         assert vb % (64 if pre else 16) == 0 and vb < ve
-        assert ve - vb <= (32768 if pre else 4096)
+        assert ve - vb <= (32768 if pre and nt * g > 32 else 4096)
         assert r[9] == (window if window is not None else 2 ** 31 - 1)
         assert r[14] == min(sinks, 2 ** 31 - 17) and r[15] >= 0
         first, last = r[13], r[13] + nt - 1

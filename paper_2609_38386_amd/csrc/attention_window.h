@@ -40,6 +40,7 @@ namespace {
 
 constexpr int KV_TILE = 64;  // keys per prefill tile (4 pages)
 constexpr int THREADS = 256;
+constexpr int SMALL_ROWS = DLFP_SMALL_ROWS;  // units of at most so many rows split their keys
 constexpr int PRE_PTAB = DLFP_MAX_PREFILL_UNIT_KEYS / PAGE;
 constexpr int DEC_PTAB = DLFP_MAX_DECODE_UNIT_KEYS / PAGE;
 
@@ -61,8 +62,8 @@ struct Args {
   int32_t num_prefill;
   int32_t out_f32;
   // Grid of a launch with both shares: `lead` prefill workgroups, `decode_lead`
-  // decode ones, then groups of eight workgroups, prefill_groups and decode_groups
-  // of them evenly mixed, then what is left of each share.
+  // decode ones, then groups of GRID_GROUP workgroups, prefill_groups and
+  // decode_groups of them evenly mixed, then what is left of each share.
   int32_t lead, decode_lead, prefill_groups, decode_groups;
   float scale_log2;
 };
@@ -90,6 +91,71 @@ __device__ __forceinline__ void widen(codes_t c, float scale, bf16x8_t* lo, bf16
 // The scale of an exponent byte (0: 2^-127, a subnormal; 255: infinity, NaN out).
 __device__ __forceinline__ float scale_of(int byte) {
   return __builtin_bit_cast(float, byte ? (uint32_t)byte << 23 : 0x00400000u);
+}
+
+// Codes of 16-byte pieces as the operand of a product of 8-bit numbers.
+typedef int operand8_t __attribute__((ext_vector_type(8)));
+__device__ __forceinline__ operand8_t operand8(codes_t a, codes_t b) {
+  operand8_t x;
+#pragma unroll
+  for (int w = 0; w < 4; ++w) x[w] = (int)a[w], x[w + 4] = (int)b[w];
+  return x;
+}
+// Four numbers into the codes nearest to x / scale, and two codes back times scale.
+__device__ __forceinline__ uint32_t to_codes(float a, float b, float c, float d, float scale) {
+  typedef short s16x2_t __attribute__((ext_vector_type(2)));
+  s16x2_t x = {0, 0};
+  x = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(x, a, b, scale, false);
+  x = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(x, c, d, scale, true);
+  return __builtin_bit_cast(uint32_t, x);
+}
+
+// A query row for products with keys of codes: a bf16 number is a sum of two e4m3
+// codes (4 bits each) in scales 2^4 apart, exactly but for numbers below 2^-14 of
+// the row's largest, which lose what lies below 2^-22 of it.  x: the lane's dims
+// (eight to a word group), amax: the row's largest magnitude.  hi and lo: the
+// codes; returns the exponent byte of hi's scale, lo's is 4 less.
+__device__ __forceinline__ float largest(bf16x8_t x) {
+  float m = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) m = fmaxf(m, __builtin_fabsf((float)x[i]));
+  return m;
+}
+__device__ __forceinline__ int row_exponent(float amax) {  // amax <= 448 * 2^(e - 127)
+  return max(27, (int)(__builtin_bit_cast(uint32_t, amax) >> 23) - 7);
+}
+__device__ __forceinline__ void split_codes(bf16x8_t x, int e, uint32_t* hi, uint32_t* lo) {
+  const float s = scale_of(e), t = scale_of(e - 4);
+#pragma unroll
+  for (int w = 0; w < 2; ++w) {
+    float f[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) f[i] = (float)x[4 * w + i];
+    hi[w] = to_codes(f[0], f[1], f[2], f[3], s);
+    const auto a = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi[w], s, false);
+    const auto b = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(hi[w], s, true);
+    lo[w] = to_codes(f[0] - a[0], f[1] - a[1], f[2] - b[0], f[3] - b[1], t);
+  }
+}
+
+// The codes of a row of 32 x 32 products, whose dims two lanes hold 16 by 16:
+// q8[high, low term][dims 64 d .. + 63].  Returns the exponent byte.
+__device__ __forceinline__ int query_codes(const bf16x8_t* q, operand8_t (*q8)[2]) {
+  float m = 0.f;
+#pragma unroll
+  for (int kk = 0; kk < 8; ++kk) m = fmaxf(m, largest(q[kk]));
+  const int e = row_exponent(max_xor32(m));
+#pragma unroll
+  for (int kk = 0; kk < 8; ++kk) {
+    uint32_t hi[2], lo[2];
+    split_codes(q[kk], e, hi, lo);
+#pragma unroll
+    for (int w = 0; w < 2; ++w) {
+      q8[0][kk >> 2][2 * (kk & 3) + w] = (int)hi[w];
+      q8[1][kk >> 2][2 * (kk & 3) + w] = (int)lo[w];
+    }
+  }
+  return e;
 }
 
 // Which keys a unit's rows see, in virtual keys: a row at position p those below
@@ -131,6 +197,36 @@ __device__ __forceinline__ uint32_t byte_mask(uint32_t bits) {
   return (((bits & 15) * 0x00204081u) & 0x01010101u) * 0xFFu;
 }
 
+// Zeroes in LDS the values of BP pages from virtual key v0 on that a row at `pos`
+// does not see, or that lie at or past `stop` (one wavefront).
+template <bool KV8, int BP>
+__device__ __forceinline__ void zero_unseen_values(char* values, const Span& sp, int v0, int pos,
+                                                   int stop) {
+  constexpr int PB = page_bytes<KV8>();
+  const int lane = threadIdx.x & 63;
+#pragma unroll
+  for (int pg = 0; pg < BP; ++pg) {
+    const uint32_t seen = sp.seen(v0 + pg * PAGE, pos, stop);
+    if (seen == 0xFFFFu) continue;
+    u32x4_t* page = reinterpret_cast<u32x4_t*>(values + pg * PB);
+#pragma unroll
+    for (int c = 0; c < PB / 1024; ++c) {
+      const int ck = 64 * c + lane;
+      u32x4_t v = page[ck];
+      if constexpr (KV8) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) v[w] &= byte_mask(seen >> (4 * w));
+      } else {
+        const bool upper = (ck & 1) ^ vt_swz(ck >> 1);  // positions 8 .. 15
+#pragma unroll
+        for (int w = 0; w < 4; ++w)
+          v[w] &= upper ? pair_mask(seen >> (8 + 2 * w)) : pair_mask(seen >> (2 * w));
+      }
+      page[ck] = v;
+    }
+  }
+}
+
 // Probabilities of two keys as bf16 pairs, for the matrix products.  bf16 output:
 // one term, rounded to nearest: 1.1e-3 to 1.6e-3 of a row in the 2-norm, below
 // what rounding the output leaves (1.7e-3).  fp32 output: three terms, the first
@@ -167,6 +263,7 @@ constexpr int decode_wave_lds() {
 template <bool KV8>
 constexpr int window_lds() {
   constexpr int pre = PreLds<KV8>::BYTES, dec = 4 * decode_wave_lds<KV8, 4>();
+  static_assert(4 * 1024 * 16 + 2 * 4 * 32 * 4 <= (pre > dec ? pre : dec), "four partial results");
   return pre > dec ? pre : dec;
 }
 
@@ -199,6 +296,7 @@ __device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, ch
   const int wave_last = pos0 + min(nt - 1, uniform((wave * 32 + 31) / G));
 
   // Q^T as the B operand.  Rows past the tile load its first one.
+  constexpr bool CODES = KV8 && !OUT32;  // scores from products of codes
   bf16x8_t qf[8];
   {
     const int64_t qrow = ((int64_t)(row0 + (row_ok ? tr : 0)) * a.hq + kh * G + hh) * D;
@@ -208,6 +306,10 @@ __device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, ch
       qf[kk] = *reinterpret_cast<const bf16x8_t*>(a.q + qrow + d);
     }
   }
+
+  operand8_t q8[2][2];
+  int q_exp = 0;
+  if constexpr (CODES) q_exp = query_codes(qf, q8);
 
   const int ntiles = (ve - vb + KV_TILE - 1) / KV_TILE;
   const int first_page = vb / PAGE, npages = (ve - 1) / PAGE - first_page + 1;
@@ -266,25 +368,8 @@ __device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, ch
     return v0 + KV_TILE > ve || sp.below(v0, v0 + KV_TILE, pos0);
   };
   auto zero_unseen = [&](int slot, int v0) {
-    const int pg = uniform(wave);
-    const uint32_t seen = sp.seen(v0 + pg * PAGE, pos0, ve);
-    if (seen == 0xFFFFu) return;
-    u32x4_t* page = reinterpret_cast<u32x4_t*>(smem + L::V_BASE + slot * L::TILE + pg * PB);
-#pragma unroll
-    for (int c = 0; c < NC; ++c) {
-      const int ck = 64 * c + lane;
-      u32x4_t v = page[ck];
-      if constexpr (KV8) {
-#pragma unroll
-        for (int w = 0; w < 4; ++w) v[w] &= byte_mask(seen >> (4 * w));
-      } else {
-        const bool upper = (ck & 1) ^ vt_swz(ck >> 1);  // positions 8 .. 15
-#pragma unroll
-        for (int w = 0; w < 4; ++w)
-          v[w] &= upper ? pair_mask(seen >> (8 + 2 * w)) : pair_mask(seen >> (2 * w));
-      }
-      page[ck] = v;
-    }
+    zero_unseen_values<KV8, 1>(smem + L::V_BASE + slot * L::TILE + uniform(wave) * PB, sp,
+                               v0 + uniform(wave) * PAGE, pos0, ve);
   };
 
   // Per-lane LDS offsets of the operands.
@@ -310,15 +395,35 @@ __device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, ch
 
   // Scales of a tile's pages: keys' of this lane's row page, values' of page
   // 2 j + hi.
+  auto tile_exp = [&](int t, int j, int pg, int shift) {
+    return (etab[min(4 * t + 2 * j + pg, npages - 1)] >> shift) & 0xFF;
+  };
   auto tile_scale = [&](int t, int j, int pg, int shift) {
-    const int e = etab[min(4 * t + 2 * j + pg, npages - 1)];
-    return scale_of((e >> shift) & 0xFF);
+    return scale_of(tile_exp(t, j, pg, shift));
   };
   // S^T = K Q^T for the tile in K slot `slot`, two 32-key accumulators.
   auto qk = [&](f32x16_t* sacc, int slot, int t) {
     sacc[0] = f32x16_t{};
     sacc[1] = f32x16_t{};
-    if constexpr (KV8) {
+    if constexpr (CODES) {
+#pragma unroll
+      for (int d = 0; d < 2; ++d) {
+        operand8_t x[2];
+#pragma unroll
+        for (int j = 0; j < 2; ++j) {
+          const char* kp = smem + slot * L::TILE + kbase + 2 * j * PB;
+          x[j] = operand8(*reinterpret_cast<const codes_t*>(kp + (((4 * d + hi) ^ krow[0]) << 4)),
+                          *reinterpret_cast<const codes_t*>(kp + (((4 * d + 2 + hi) ^ krow[0]) << 4)));
+        }
+#pragma unroll
+        for (int term = 0; term < 2; ++term)
+#pragma unroll
+          for (int j = 0; j < 2; ++j)
+            sacc[j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                x[j], q8[term][d], sacc[j], 0, 0, 0, tile_exp(t, j, (col >> 2) & 1, 0), 0,
+                q_exp - 4 * term);
+      }
+    } else if constexpr (KV8) {
       const float s0 = tile_scale(t, 0, (col >> 2) & 1, 0), s1 = tile_scale(t, 1, (col >> 2) & 1, 0);
 #pragma unroll
       for (int kk = 0; kk < 8; kk += 2) {
@@ -653,6 +758,355 @@ __device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, ch
     __hip_atomic_store(group_counter(a.ws, grp), 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
 
+// Unit of at most 32 query rows: one wavefront holds all of them, so the four
+// split the keys instead: wavefront w takes blocks w, w + 4, ... of the unit, each
+// through a key slot and a value slot of its own, without a barrier until the
+// four results are added through LDS.  Block and slots as a decode unit's (32 keys
+// of bf16 pages, 64 of 8-bit ones), products, masks and layouts as a tile's.
+template <int G, bool KV8, bool OUT32>
+__device__ __forceinline__ void small_unit(const Args& a, const record_t f, char* smem, int* flag) {
+  constexpr int PB = page_bytes<KV8>();
+  constexpr int BP = SLOT / PB;     // pages of a block
+  constexpr int KEYS = BP * PAGE;
+  constexpr int NJ = BP / 2;        // 32-key products of a block
+  constexpr int NC = PB / 1024;     // copies of a page
+  constexpr bool CODES = KV8 && !OUT32;
+  const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
+  const int col = lane & 31, hi = lane >> 5;
+  char* wl = smem + wave * decode_wave_lds<KV8, 4>();
+  const int s = f[DLFP_W_SEQ], kh = f[DLFP_W_KVHEAD], nt = f[DLFP_W_QNTOK];
+  const int vb = f[DLFP_W_KVBEGIN], ve = f[DLFP_W_KVEND];
+  const int nsplits = f[DLFP_W_NSPLITS];
+  const int row0 = f[DLFP_W_QROW0], pos0 = f[DLFP_W_QPOS0];
+  const Span sp = span_of(f);
+  const int32_t* bt = a.block_table + (int64_t)s * a.max_blocks;
+  int32_t* ptab = reinterpret_cast<int32_t*>(wl + 2 * SLOT);
+  uint16_t* etab = reinterpret_cast<uint16_t*>(ptab + DEC_PTAB / 4 + 4);
+
+  const int tr = col / G, hh = col % G;
+  const bool row_ok = tr < nt;
+  const int v_end = row_ok ? min(sp.end(pos0 + tr), ve) : 0;
+  const int v_low = row_ok ? sp.low(pos0 + tr) : 0;
+  const int unit_end = min(sp.end(pos0), ve), last = pos0 + nt - 1;
+
+  const int first_page = vb / PAGE;
+  const int npages = (ve + PAGE - 1) / PAGE - first_page, nblocks = (npages + BP - 1) / BP;
+  const int mine = nblocks > wave ? (nblocks - wave + 3) / 4 : 0;
+  auto page_of = [&](int i, int h) { return min(BP * (wave + 4 * i) + h, npages - 1); };
+  auto pages_in = [&](int i) { return min(BP, npages - BP * (wave + 4 * i)); };
+  for (int x = lane; x < BP * mine; x += 64) {
+    int id = bt[sp.page(first_page + page_of(x / BP, x % BP))];
+    if ((unsigned)id >= (unsigned)a.num_blocks) {
+      raise_error(a.ws);
+      id = 0;
+    }
+    ptab[x] = id;
+  }
+  bf16x8_t qf[8];
+  {
+    const int64_t qrow = ((int64_t)(row0 + (row_ok ? tr : 0)) * a.hq + kh * G + hh) * D;
+#pragma unroll
+    for (int kk = 0; kk < 8; ++kk) {
+      const int d = KV8 ? 32 * (kk >> 1) + 16 * hi + 8 * (kk & 1) : 16 * kk + 8 * hi;
+      qf[kk] = *reinterpret_cast<const bf16x8_t*>(a.q + qrow + d);
+    }
+  }
+  wait_memory_complete();
+  wave_sync();
+
+  uint32_t kofs[NC], vofs[NC];
+#pragma unroll
+  for (int j = 0; j < NC; ++j) {
+    const int ck = 64 * j + lane;
+    if constexpr (KV8) {
+      const int R = ck >> 3;
+      kofs[j] = R * 128 + (((ck & 7) ^ ((R >> 1) & 7)) << 4);
+      vofs[j] = ck << 4;
+    } else {
+      const int R = ck >> 4, d = ck >> 1;
+      kofs[j] = R * 256 + (((ck & 15) ^ R) << 4);
+      vofs[j] = d * 32 + (((ck & 1) ^ vt_swz(d)) << 4);
+    }
+  }
+  const uint32_t lds_wave = (uint32_t)uniform((int)lds_addr(wl));
+  auto issue_k = [&](int i) {
+    const int n = pages_in(i);
+#pragma unroll
+    for (int h = 0; h < BP; ++h) {
+      if (h >= n) break;
+      const char* src = a.kc + ((int64_t)uniform(ptab[BP * i + h]) * a.hkv + kh) * PB;
+      const uint32_t x = KV8 ? (h & 1) << 5 : 0;
+#pragma unroll
+      for (int j = 0; j < NC; ++j) lds_copy16(src + (kofs[j] ^ x), lds_wave + h * PB + j * 1024);
+    }
+  };
+  auto issue_v = [&](int i) {
+    const int n = pages_in(i);
+#pragma unroll
+    for (int h = 0; h < BP; ++h) {
+      if (h >= n) break;
+      const char* src = a.vc + ((int64_t)uniform(ptab[BP * i + h]) * a.hkv + kh) * PB;
+#pragma unroll
+      for (int j = 0; j < NC; ++j) lds_copy16(src + vofs[j], lds_wave + SLOT + h * PB + j * 1024);
+    }
+  };
+  if (mine > 0) {
+    issue_k(0);
+    issue_v(0);
+  }
+  if constexpr (KV8) {
+    for (int x = lane; x < BP * mine; x += 64) {
+      const int64_t e = (int64_t)ptab[x] * a.hkv + kh;
+      etab[x] = (uint16_t)(a.k_exp[e] | a.v_exp[e] << 8);
+    }
+    wave_sync();
+  }
+  operand8_t q8[2][2];
+  int q_exp = 0;
+  if constexpr (CODES) q_exp = query_codes(qf, q8);
+
+  // Operand offsets, as in prefill_unit.
+  int kbase, vbase, kxor = 0;
+  const int kpg = (col >> 2) & 1;
+  if constexpr (KV8) {
+    const int slot = vt_pos(4 * (col >> 3) + (col & 3));
+    kbase = kpg * PB + slot * 128;
+    kxor = ((slot >> 1) & 7) ^ (kpg << 1);
+    vbase = SLOT + hi * PB + col * 16;
+  } else {
+    kbase = col * 256 + ((hi ^ (col & 15)) << 4);
+    vbase = SLOT + col * 32 + ((hi ^ vt_swz(col)) << 4);
+  }
+  float m_run = NEG_BIG, l_run = 0.f;
+  f32x16_t o[4];
+#pragma unroll
+  for (int mb = 0; mb < 4; ++mb) o[mb] = f32x16_t{};
+  const float c = a.scale_log2;
+
+  for (int i = 0; i < mine; ++i) {
+    const int v0 = vb + KEYS * (wave + 4 * i);
+    const bool more = i + 1 < mine;
+    if (pages_in(i) == BP)
+      wait_copies<8>();  // in flight, oldest first: this block's keys, its values
+    else
+      wait_copies<0>();
+    f32x16_t sacc[NJ];
+#pragma unroll
+    for (int j = 0; j < NJ; ++j) sacc[j] = f32x16_t{};
+    if constexpr (CODES) {
+#pragma unroll
+      for (int d = 0; d < 2; ++d)
+#pragma unroll
+        for (int j = 0; j < NJ; ++j) {
+          const char* kp = wl + kbase + 2 * j * PB;
+          const operand8_t x = operand8(
+              *reinterpret_cast<const codes_t*>(kp + (((4 * d + hi) ^ kxor) << 4)),
+              *reinterpret_cast<const codes_t*>(kp + (((4 * d + 2 + hi) ^ kxor) << 4)));
+          const int ke = etab[BP * i + 2 * j + kpg] & 0xFF;
+#pragma unroll
+          for (int term = 0; term < 2; ++term)
+            sacc[j] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(
+                x, q8[term][d], sacc[j], 0, 0, 0, ke, 0, q_exp - 4 * term);
+        }
+    } else if constexpr (KV8) {
+#pragma unroll
+      for (int j = 0; j < NJ; ++j) {
+        const float ks = scale_of(etab[BP * i + 2 * j + kpg] & 0xFF);
+#pragma unroll
+        for (int kk = 0; kk < 8; kk += 2) {
+          bf16x8_t x[2];
+          widen(*reinterpret_cast<const codes_t*>(wl + kbase + 2 * j * PB + (((kk + hi) ^ kxor) << 4)),
+                ks, &x[0], &x[1]);
+#pragma unroll
+          for (int h = 0; h < 2; ++h)
+            sacc[j] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[h], qf[kk + h], sacc[j], 0, 0, 0);
+        }
+      }
+    } else {
+      bf16x8_t kf[8];
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk)
+        kf[kk] = *reinterpret_cast<const bf16x8_t*>(wl + (kbase ^ (kk << 5)));
+#pragma unroll
+      for (int kk = 0; kk < 8; ++kk)
+        sacc[0] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kf[kk], qf[kk], sacc[0], 0, 0, 0);
+    }
+    wait_lds();  // the key slot is free
+    if (more) issue_k(i + 1);
+    const bool next_full = more && pages_in(i + 1) == BP;
+    // Masks, as in prefill_unit.
+    const int base = KV8 ? 16 * hi : 4 * hi;
+    auto at = [](int x) {
+      return 32 * (x >> 4) + (KV8 ? vt_pos(x & 15) : 8 * ((x & 15) >> 2) + (x & 3));
+    };
+    if (v0 + KEYS > unit_end) {
+      const int n = v_end - v0 - base;
+#pragma unroll
+      for (int x = 0; x < 16 * NJ; ++x)
+        sacc[x >> 4][x & 15] = at(x) < n ? sacc[x >> 4][x & 15] : -__builtin_inff();
+    }
+    if (sp.below(v0, v0 + KEYS, last)) {
+      const int n = v_low - v0 - base, m = sp.sinks - v0 - base;
+#pragma unroll
+      for (int x = 0; x < 16 * NJ; ++x)
+        sacc[x >> 4][x & 15] = at(x) >= n || at(x) < m ? sacc[x >> 4][x & 15] : -__builtin_inff();
+    }
+    float mx = -__builtin_inff();
+#pragma unroll
+    for (int x = 0; x < 16 * NJ; ++x) mx = fmaxf(mx, sacc[x >> 4][x & 15]);
+    const float m_tile = max_xor32(mx) * c;
+    if (__builtin_amdgcn_ballot_w64(m_tile > m_run + RESCALE_LOG2)) {
+      const float m_new = m_tile > m_run + RESCALE_LOG2 ? m_tile : m_run;
+      const float alpha = fexp2(m_run - m_new);
+      m_run = m_new;
+      l_run *= alpha;
+#pragma unroll
+      for (int mb = 0; mb < 4; ++mb) o[mb] *= alpha;
+    }
+    bf16x8_t pf[2 * NJ];
+#pragma unroll
+    for (int kk = 0; kk < 2 * NJ; ++kk) {
+      u32x4_t pk;
+#pragma unroll
+      for (int w = 0; w < 4; ++w) {
+        const int x = 8 * (kk & 1) + 2 * w;
+        float p0 = fexp2(__builtin_fmaf(sacc[kk >> 1][x], c, -m_run));
+        float p1 = fexp2(__builtin_fmaf(sacc[kk >> 1][x + 1], c, -m_run));
+        if constexpr (OUT32) {
+          l_run += p0 + p1;
+          pk[w] = cut(p0, p1);
+          sacc[kk >> 1][x] = p0;
+          sacc[kk >> 1][x + 1] = p1;
+        } else {
+          pk[w] = pack_bf16(p0, p1);
+          l_run = dot2(pk[w], 0x3F803F80u, l_run);  // two bf16 1.0
+        }
+      }
+      pf[kk] = __builtin_bit_cast(bf16x8_t, pk);
+    }
+    if (next_full)
+      wait_copies<8>();  // the values; behind them the next block's keys
+    else
+      wait_copies<0>();
+    if (v0 + KEYS > ve || sp.below(v0, v0 + KEYS, pos0)) {
+      zero_unseen_values<KV8, BP>(wl + SLOT, sp, v0, pos0, ve);
+      wave_sync();
+    }
+    auto pv = [&]() {
+#pragma unroll
+      for (int kk = 0; kk < 2 * NJ; kk += KV8 ? 2 : 1)
+#pragma unroll
+        for (int mb = 0; mb < 4; ++mb) {
+          if constexpr (KV8) {
+            bf16x8_t x[2];
+            widen(*reinterpret_cast<const codes_t*>(wl + vbase + kk * PB + mb * 512),
+                  scale_of(etab[BP * i + kk + hi] >> 8), &x[0], &x[1]);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+              o[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(x[h], pf[kk + h], o[mb], 0, 0, 0);
+          } else {
+            const bf16x8_t vf =
+                *reinterpret_cast<const bf16x8_t*>(wl + vbase + kk * PB + mb * 1024);
+            o[mb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vf, pf[kk], o[mb], 0, 0, 0);
+          }
+        }
+    };
+    pv();
+    if constexpr (OUT32) {
+#pragma unroll
+      for (int term = 0; term < 2; ++term) {
+#pragma unroll
+        for (int kk = 0; kk < 2 * NJ; ++kk) {
+          u32x4_t pk;
+#pragma unroll
+          for (int w = 0; w < 4; ++w) {
+            const int x = 8 * (kk & 1) + 2 * w;
+            float p0 = sacc[kk >> 1][x], p1 = sacc[kk >> 1][x + 1];
+            pk[w] = term ? pack_bf16(p0, p1) : cut(p0, p1);
+            sacc[kk >> 1][x] = p0;
+            sacc[kk >> 1][x + 1] = p1;
+          }
+          pf[kk] = __builtin_bit_cast(bf16x8_t, pk);
+        }
+        pv();
+      }
+    }
+    wait_lds();  // the value slot is free
+    if (more) issue_v(i + 1);
+  }
+
+  // Add the four wavefronts' results through LDS.  Piece (chunk, hi) of a row holds
+  // dims 32 (chunk / 4) + 8 (chunk % 4) + 4 hi .. + 3; thread (row, sub) takes chunks
+  // 2 sub and 2 sub + 1, 16 consecutive dims; the row is XORed with the chunk so that
+  // both sides spread over the banks.
+  l_run = sum_xor32(l_run);
+  wait_memory_complete();
+  __syncthreads();  // every wavefront is done with its slots
+  f32x4_t* red = reinterpret_cast<f32x4_t*>(smem);
+  float* stat = reinterpret_cast<float*>(smem + 4 * 1024 * 16);  // m[4][32], l[4][32]
+  auto at = [](int w, int ch, int h, int row) {
+    return w * 1024 + ch * 64 + h * 32 + (row ^ (((ch >> 1) & 7) << 1));
+  };
+#pragma unroll
+  for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+    for (int g4 = 0; g4 < 4; ++g4)
+      red[at(wave, 4 * mb + g4, hi, col)] = f32x4_t{o[mb][4 * g4], o[mb][4 * g4 + 1],
+                                                   o[mb][4 * g4 + 2], o[mb][4 * g4 + 3]};
+  if (hi == 0) {
+    stat[wave * 32 + col] = m_run;
+    stat[128 + wave * 32 + col] = l_run;
+  }
+  __syncthreads();
+  const int row = tid >> 3, sub = tid & 7, rows = nt * G;
+  float M = NEG_BIG, L = 0.f, wgt[4];
+#pragma unroll
+  for (int w = 0; w < 4; ++w) M = fmaxf(M, stat[w * 32 + row]);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    wgt[w] = fexp2(stat[w * 32 + row] - M);
+    L += wgt[w] * stat[128 + w * 32 + row];
+  }
+  f32x4_t acc[4];  // pieces (2 sub, 0), (2 sub, 1), (2 sub + 1, 0), (2 sub + 1, 1)
+#pragma unroll
+  for (int x = 0; x < 4; ++x) {
+    acc[x] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+    for (int w = 0; w < 4; ++w) acc[x] += wgt[w] * red[at(w, 2 * sub + (x >> 1), x & 1, row)];
+  }
+  if (nsplits == 1) {
+    if (row < rows) {
+      const float inv = 1.f / L;
+      const int64_t orow = ((int64_t)(row0 + row / G) * a.hq + kh * G + row % G) * D + 16 * sub;
+#pragma unroll
+      for (int x = 0; x < 4; ++x)
+        store4(a, orow + 4 * x, acc[x][0] * inv, acc[x][1] * inv, acc[x][2] * inv, acc[x][3] * inv);
+    }
+    return;
+  }
+  const int slot_floats = slot_floats_for(rows);
+  const Slots sl = group_slots(a.ws, f[DLFP_W_WSGROUP], nsplits, slot_floats);
+  const int my = f[DLFP_W_SPLIT] * slot_floats;
+  if (row < rows) {
+#pragma unroll
+    for (int x = 0; x < 4; ++x)
+      pstore4(sl, my + ((2 * sub + (x >> 1)) * rows + row) * 8 + 4 * (x & 1), acc[x]);
+    if (sub == 0) {
+      pstore1(sl, my + rows * D + row, M);
+      pstore1(sl, my + rows * D + rows + row, L);
+    }
+  }
+  wait_memory_complete();
+  __syncthreads();  // every wave of the unit has completed its stores
+  const int grp = f[DLFP_W_GROUP];
+  if (tid == 0) *flag = arrive(a.ws, grp) == nsplits - 1;
+  __syncthreads();
+  if (!*flag) return;
+  prefill_merge<G, 8>(a, sl, slot_floats, nsplits, rows, row0, kh);
+  if (tid == 0)
+    __hip_atomic_store(group_counter(a.ws, grp), 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+}
+
 // ---------------------------------------------------------------- decode
 
 // Decode unit of a workgroup of NW wavefronts: wavefront w takes blocks w, w + NW,
@@ -668,6 +1122,7 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
   constexpr int BP = SLOT / PB;       // pages of a block
   constexpr int NCH = KV8 ? 4 : 2;    // 16-key products of a block
   constexpr int NC = PB / 1024;       // copies of a page
+  constexpr bool CODES = KV8 && !OUT32;
   const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
   char* wl = smem + wave * decode_wave_lds<KV8, NW>();
   const int col = lane & 15, gq = lane >> 4, head = col & 7;
@@ -706,6 +1161,22 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
       const int d = KV8 ? 64 * (kk >> 1) + 16 * gq + 8 * (kk & 1) : 32 * kk + 8 * gq;
       const u32x4_t v = *reinterpret_cast<const u32x4_t*>(qp + d);
       qb[kk] = __builtin_bit_cast(bf16x8_t, head < G ? v : u32x4_t{0u, 0u, 0u, 0u});
+    }
+  }
+  operand8_t q8;
+  int q_exp = 0;
+  if constexpr (CODES) {  // the high terms in columns 0-7, the low ones in 8-15
+    float m = 0.f;
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) m = fmaxf(m, largest(qb[kk]));
+    const int e = row_exponent(max_xor32(max_xor16(m)));
+    q_exp = col >= 8 ? e - 4 : e;
+#pragma unroll
+    for (int kk = 0; kk < 4; ++kk) {
+      uint32_t hw[2], lw[2];
+      split_codes(qb[kk], e, hw, lw);
+#pragma unroll
+      for (int w = 0; w < 2; ++w) q8[2 * kk + w] = (int)(col >= 8 ? lw[w] : hw[w]);
     }
   }
   wait_memory_complete();
@@ -755,12 +1226,19 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
     issue_k(0);
     issue_v(0);
   }
+  int v_ref = 0;  // largest value exponent of the wavefront's pages
   if constexpr (KV8) {  // with the first block on its way
     for (int x = lane; x < BP * mine; x += 64) {
       const int64_t e = (int64_t)ptab[x] * a.hkv + kh;
-      etab[x] = (uint16_t)(a.k_exp[e] | a.v_exp[e] << 8);
+      const int v = a.v_exp[e];
+      etab[x] = (uint16_t)(a.k_exp[e] | v << 8);
+      v_ref = max(v_ref, v);
     }
     wave_sync();
+  }
+  if constexpr (CODES) {
+#pragma unroll
+    for (int m = 32; m > 0; m >>= 1) v_ref = max(v_ref, __shfl_xor(v_ref, m));
   }
 
   float m_run = NEG_BIG, l_run = 0.f;
@@ -801,13 +1279,20 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
 #pragma unroll
       for (int b = 0; b < NCH; ++b) sacc[b] = f32x4_t{0.f, 0.f, 0.f, 0.f};
       if constexpr (KV8) {
-        const float ks = scale_of(etab[BP * i + kpage] & 0xFF);
+        const int ke = etab[BP * i + kpage] & 0xFF;
+        const float ks = scale_of(ke);
         codes_t kc[NCH][2];
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
           for (int b = 0; b < NCH; ++b)
             kc[b][j] = *reinterpret_cast<const codes_t*>(wl + krow[b] + (((4 * j + gq) ^ kxor[b]) << 4));
+        if constexpr (CODES) {
+#pragma unroll
+          for (int b = 0; b < NCH; ++b)
+            sacc[b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(
+                operand8(kc[b][0], kc[b][1]), q8, sacc[b], 0, 0, 0, ke, 0, q_exp);
+        } else
 #pragma unroll
         for (int j = 0; j < 2; ++j)
 #pragma unroll
@@ -832,7 +1317,8 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
             sacc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(kf[b][kk], qb[kk], sacc[b], 0, 0, 0);
       }
 #pragma unroll
-      for (int x = 0; x < 4 * NCH; ++x) sc[x] = sacc[x >> 2][x & 3];
+      for (int x = 0; x < 4 * NCH; ++x)
+        sc[x] = CODES ? sum_xor8(sacc[x >> 2][x & 3]) : sacc[x >> 2][x & 3];
     }
     wait_lds();  // the key slot is free
     if (more) issue_k(i + 1);
@@ -849,7 +1335,10 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
     float mx = -__builtin_inff();
 #pragma unroll
     for (int x = 0; x < 4 * NCH; ++x) mx = fmaxf(mx, sc[x]);
-    const float m_tile = max_xor32(max_xor16(mx)) * c;
+    // Products of codes take a probability times its page's value scale (relative
+    // to the largest), so the reference maximum is that of both.
+    const int dv = CODES ? (etab[BP * i + vpage] >> 8) - v_ref : 0;
+    const float m_tile = max_xor32(max_xor16(__builtin_fmaf(mx, c, (float)dv)));
     if (__builtin_amdgcn_ballot_w64(m_tile > m_run + RESCALE_LOG2)) {
       const float m_new = m_tile > m_run + RESCALE_LOG2 ? m_tile : m_run;
       const float alpha = fexp2(m_run - m_new);
@@ -860,8 +1349,31 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
     }
     // P^T: this lane's keys of its column, its term of each, the B operands.
     u32x4_t pk[NCH / 2], third[NCH / 2];
+    if constexpr (CODES) {
+      // Two e4m3 terms, the second in a scale 2^5 smaller: its columns take the
+      // exponentials 2^5 larger.
+      const float low = col >= 8 ? 32.f : 1.f;
+      const float shift = (float)(dv + (col >= 8 ? 5 : 0)) - m_run;
+      float sum = 0.f;
 #pragma unroll
-    for (int w = 0; w < 2 * NCH; ++w) {
+      for (int w = 0; w < NCH; ++w) {
+        float e[4];
+#pragma unroll
+        for (int x = 0; x < 4; ++x) {
+          e[x] = fexp2(__builtin_fmaf(sc[4 * w + x], c, shift));
+          sum += e[x];
+        }
+        const uint32_t first = to_codes(e[0], e[1], e[2], e[3], low);
+        const auto f0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(first, low, false);
+        const auto f1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(first, low, true);
+        const uint32_t second =
+            to_codes(e[0] - f0[0], e[1] - f0[1], e[2] - f1[0], e[3] - f1[1], 1.f);
+        pk[0][w] = col >= 8 ? second : first;
+      }
+      l_run += __builtin_ldexpf(sum, -dv);  // of columns 0-7
+    }
+#pragma unroll
+    for (int w = 0; w < (CODES ? 0 : 2 * NCH); ++w) {
       float e0 = fexp2(__builtin_fmaf(sc[2 * w], c, -m_run));
       float e1 = fexp2(__builtin_fmaf(sc[2 * w + 1], c, -m_run));
       l_run += e0 + e1;
@@ -881,27 +1393,7 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
     if (edge) {
       // Values that the token does not see are zeroed (a probability of 0 times
       // a NaN would still be NaN).
-#pragma unroll
-      for (int pg = 0; pg < BP; ++pg) {
-        const uint32_t seen = sp.seen(v0 + pg * PAGE, pos, ve);
-        if (seen == 0xFFFFu) continue;
-        u32x4_t* page = reinterpret_cast<u32x4_t*>(wl + SLOT + pg * PB);
-#pragma unroll
-        for (int j = 0; j < NC; ++j) {
-          const int ck = 64 * j + lane;
-          u32x4_t v = page[ck];
-          if constexpr (KV8) {
-#pragma unroll
-            for (int w = 0; w < 4; ++w) v[w] &= byte_mask(seen >> (4 * w));
-          } else {
-            const bool upper = (ck & 1) ^ vt_swz(ck >> 1);  // positions 8 .. 15
-#pragma unroll
-            for (int w = 0; w < 4; ++w)
-              v[w] &= upper ? pair_mask(seen >> (8 + 2 * w)) : pair_mask(seen >> (2 * w));
-          }
-          page[ck] = v;
-        }
-      }
+      zero_unseen_values<KV8, BP>(wl + SLOT, sp, v0, pos, ve);
       wave_sync();
     }
     // O^T += V^T P^T, eight blocks of 16 dims.
@@ -913,6 +1405,15 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
         vc[mb] = *reinterpret_cast<const codes_t*>(wl + vbyte + mb * 256);
 #pragma unroll
       for (int mb = 0; mb < 8; ++mb) {
+        if constexpr (CODES) {
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            const u32x2_t v = {vc[mb][2 * h], vc[mb][2 * h + 1]}, p = {pk[0][2 * h], pk[0][2 * h + 1]};
+            o[mb] = __builtin_amdgcn_mfma_f32_16x16x32_fp8_fp8(
+                __builtin_bit_cast(long, v), __builtin_bit_cast(long, p), o[mb], 0, 0, 0);
+          }
+          continue;
+        }
         bf16x8_t x[2];
         widen(vc[mb], vs, &x[0], &x[1]);
 #pragma unroll
@@ -949,7 +1450,10 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
 #pragma unroll
   for (int mb = 0; mb < 8; ++mb)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) o[mb][i] = sum_xor8(o[mb][i]);
+    for (int i = 0; i < 4; ++i) {
+      const float x = CODES ? __builtin_ldexpf(o[mb][i], v_ref - 127 - (col >= 8 ? 5 : 0)) : o[mb][i];
+      o[mb][i] = sum_xor8(x);
+    }
   wait_memory_complete();
   __syncthreads();  // every wavefront is done with its slots
   f32x4_t* red = reinterpret_cast<f32x4_t*>(smem);
@@ -1049,7 +1553,11 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
 
 // The unit of workgroup b of a launch with prefill units.  The i-th prefill
 // workgroup takes unit xcd_remap(i); all parts of the grid but the last begin at a
-// multiple of eight, so it runs on XCD i % 8.
+// multiple of eight, so it runs on XCD i % 8.  Workgroups go to the XCDs and to the
+// four shader engines of each in turn, and wait for their own: groups of 32 give
+// all of them the same order of long and short ones (in groups of eight, one
+// engine got all of the prefill units, and of 512 slots 200 stood empty).
+constexpr int GRID_GROUP = 32;
 __device__ __forceinline__ int unit_of(const Args& a, int b) {
   const int np = a.num_prefill;
   if (b < a.lead) return xcd_remap(b, np);
@@ -1057,17 +1565,17 @@ __device__ __forceinline__ int unit_of(const Args& a, int b) {
   if (b < a.decode_lead) return np + b;
   b -= a.decode_lead;
   const int gp = a.prefill_groups, g = gp + a.decode_groups;
-  const int group = b >> 3, lane = b & 7;
+  const int group = b / GRID_GROUP, lane = b % GRID_GROUP;
   const int before = group < g ? (int)((uint64_t)group * gp / max(g, 1)) : gp;
   if (group < g) {
     const bool prefill = (int)((uint64_t)(group + 1) * gp / g) > before;
-    return prefill ? xcd_remap(a.lead + 8 * before + lane, np)
-                   : np + a.decode_lead + 8 * (group - before) + lane;
+    return prefill ? xcd_remap(a.lead + GRID_GROUP * before + lane, np)
+                   : np + a.decode_lead + GRID_GROUP * (group - before) + lane;
   }
-  b -= 8 * g;
-  const int left = np - a.lead - 8 * gp;
-  return b < left ? xcd_remap(a.lead + 8 * gp + b, np)
-                  : np + a.decode_lead + 8 * a.decode_groups + b - left;
+  b -= GRID_GROUP * g;
+  const int left = np - a.lead - GRID_GROUP * gp;
+  return b < left ? xcd_remap(a.lead + GRID_GROUP * gp + b, np)
+                  : np + a.decode_lead + GRID_GROUP * a.decode_groups + b - left;
 }
 
 template <int G, bool KV8, bool OUT32>
@@ -1076,10 +1584,15 @@ __global__ __launch_bounds__(THREADS, 2) void window_kernel(Args a) {
   __shared__ int flag;
   const int u = unit_of(a, blockIdx.x);
   const int32_t* rec = a.work + (int64_t)u * DLFP_WORK_INTS;
-  if (u < a.num_prefill)
-    prefill_unit<G, KV8, OUT32>(a, load_record(rec), smem, &flag);
-  else
+  if (u >= a.num_prefill) {
     decode_unit<G, KV8, OUT32, 4>(a, rec, smem, &flag);
+    return;
+  }
+  const record_t f = load_record(rec);
+  if (f[DLFP_W_QNTOK] * G <= SMALL_ROWS)
+    small_unit<G, KV8, OUT32>(a, f, smem, &flag);
+  else
+    prefill_unit<G, KV8, OUT32>(a, f, smem, &flag);
 }
 
 template <int G, bool KV8, bool OUT32, int NW>
@@ -1158,16 +1671,30 @@ int attention_window(const dlfp_dims* dims, const dlfp_meta* meta, const int32_t
   a.scale_log2 = scale * LOG2E;
   const int cus = dlfp::compute_units();
   const int decode_units = a.num_units - a.num_prefill;
-  // One prefill unit for each compute unit, one decode unit for each, then the
-  // rest of both in equal measure, so that a compute unit has one of each kind as
-  // long as there are both.
+  // One prefill unit for each compute unit, then one decode unit for each, so that
+  // both shares run from the start (beside each other each runs at 0.62 of its
+  // speed alone).  A decode share that takes as long as the prefill share goes on
+  // beside it: the rest of the prefill units come mixed with as many decode units
+  // as take the same time, the decode units left behind them (128 windowed decoders
+  // beside 1999 prompt tokens, 8-bit pages 128.6 us, without the mixture 143.5, all
+  // prefill units first 159; bf16 197.5, 208 and 243).  A shorter one would leave
+  // the last prefill units alone: they come first then (whole contexts, 8-bit
+  // pages: 403 us, mixed 475).
   a.lead = a.num_prefill;
   a.decode_lead = a.prefill_groups = a.decode_groups = 0;
-  if (meta->prefill_lead_units < a.num_prefill && decode_units >= 8) {
-    a.lead = meta->prefill_lead_units / 8 * 8;
-    a.decode_lead = std::min(decode_units, cus) / 8 * 8;
-    a.prefill_groups = (a.num_prefill - a.lead) / 8;
-    a.decode_groups = (decode_units - a.decode_lead) / 8;
+  if (meta->prefill_lead_units < a.num_prefill && decode_units >= GRID_GROUP) {
+    a.lead = meta->prefill_lead_units / GRID_GROUP * GRID_GROUP;
+    a.decode_lead = std::min(decode_units, cus) / GRID_GROUP * GRID_GROUP;
+    a.prefill_groups = (a.num_prefill - a.lead) / GRID_GROUP;
+    // Keys of the decode units for one of the prefill units, times what a key takes
+    // of the decode share alone (its bytes at 6.4 TB/s) over the prefill share alone
+    // (128 rows at 1.12 PFLOP/s).
+    const double key = (KV8 ? 256 : 512) / 6.4 / (128 * 512 / 1120.);
+    const double shares = meta->num_waiting_units / 1024. * key;
+    const double groups = shares >= 0.9 ? 0.85 * key * a.prefill_groups * meta->prefill_split_tokens /
+                                              std::max(meta->decode_split_tokens, 64)
+                                        : 0.;
+    a.decode_groups = (int)std::min<double>((decode_units - a.decode_lead) / GRID_GROUP, groups);
   }
   // Wavefronts of a decode unit's workgroup in a launch of decode units alone.
   // One, with units of up to 128 KiB of cache that are more than three for each

@@ -135,58 +135,58 @@ int build(const dlfp_dims* dims, const dlfp_tuning* tuning, const dlfp_window* w
   }
   if (tokens > I32_MAX) return DLFP_ERANGE;
 
-  // Tiles of a prompt's rows, as tall as one unit takes.
-  const int64_t tile_tokens = tn.prefill_tile_tokens ? tn.prefill_tile_tokens : DLFP_TILE_ROWS / g;
   std::vector<Rows> tiles, ones;
-  int64_t tile_keys = 0, tile_longest = 0, one_keys = 0, one_longest = 0;
-  for (int32_t s : prompts)
-    for (int64_t t0 = 0; t0 < q_len[s]; t0 += tile_tokens) {
-      tiles.push_back(rows_of(s, t0, std::min<int64_t>(tile_tokens, q_len[s] - t0)));
-      tile_keys += tiles.back().keys;
-      tile_longest = std::max(tile_longest, tiles.back().keys);
-    }
+  int64_t one_keys = 0, one_longest = 0;
   for (int32_t s : decoders) {
     ones.push_back(rows_of(s, 0, 1));
     one_keys += ones.back().keys;
     one_longest = std::max(one_longest, ones.back().keys);
   }
-  auto longest_first = [](const Rows& x, const Rows& y) { return x.keys > y.keys; };
-  std::stable_sort(tiles.begin(), tiles.end(), longest_first);
-  std::stable_sort(ones.begin(), ones.end(), longest_first);
-
-  // Splits: enough units to fill the device, parts not shorter than pays.
-  int64_t split_p = tn.prefill_split_tokens;
-  if (!split_p) {
-    const int64_t part = ceil_div(tile_keys * hkv, slots);
-    split_p = std::clamp<int64_t>(round_up(part, 64), 512, DLFP_MAX_PREFILL_UNIT_KEYS);
-  }
-  // A decoder's range is cut into n equal parts when it is longer than the split.
+  // A range longer than the split is cut into equal parts.
   auto cut = [](int64_t keys, int64_t split, int64_t granule) {
     const int64_t n = ceil_div(keys, split);
     return round_up(ceil_div(keys, n), granule);
   };
+  // Units of ranges cut at `split`: their count, keys of all, of the longest, parts
+  // of the longest range.
+  struct Cut {
+    int64_t units, keys, longest, parts;
+  };
+  auto cuts = [&](const std::vector<Rows>& ranges, int64_t split) {
+    Cut c = {0, 0, 0, 1};
+    for (const Rows& r : ranges) {
+      const int64_t part = cut(r.keys, split, 64), n = ceil_div(r.keys, part);
+      c.units += n * hkv;
+      c.keys += r.keys * hkv;
+      c.longest = std::max(c.longest, std::min(part, r.keys));
+      c.parts = std::max(c.parts, n);
+    }
+    return c;
+  };
+  auto split_tiles = [&](int64_t tokens_each) {
+    std::vector<Rows> t;
+    for (int32_t s : prompts)
+      for (int64_t t0 = 0; t0 < q_len[s]; t0 += tokens_each)
+        t.push_back(rows_of(s, t0, std::min<int64_t>(tokens_each, q_len[s] - t0)));
+    return t;
+  };
+
+  // Decode split: an n-th of the longest range, the n that minimises an estimate of
+  // the decode share's time in us: full rounds of units and the rest of the last one
+  // stream at 6.2 TB/s (256 bytes a key, those of 8-bit pages), no unit
+  // faster than 6.3 ns a key; a full round takes 3.5 us more, a merge 3 and 0.05 for
+  // each part.
   int64_t split_d = tn.decode_split_tokens;
   if (!split_d && !ones.empty()) {
-    // The split (an n-th of the longest range) that minimises an estimate of the
-    // decode share's time in us: full rounds of units and the rest of the last one
-    // stream at 6.2 TB/s (384 bytes a key, between the two kinds of pages), no unit
-    // faster than 6.3 ns a key; a merge takes 3 us and 0.05 for each part.
     double best = 0.;
     for (int64_t n = ceil_div(one_longest, DLFP_MAX_DECODE_UNIT_KEYS); n <= 256; ++n) {
       const int64_t split = std::max<int64_t>(round_up(ceil_div(one_longest, n), 64), 128);
-      int64_t count = 0, longest = 0, parts = 1;
-      for (const Rows& r : ones) {
-        const int64_t part = cut(r.keys, split, 64), p = ceil_div(r.keys, part);
-        count += p;
-        longest = std::max(longest, std::min(part, r.keys));
-        parts = std::max(parts, p);
-      }
-      count *= hkv;
-      const double keys_us = 6.2e6 / 384, mean = (double)one_keys * hkv / count;
-      const int64_t full = count / slots, rest = count % slots;
-      const double est = full * slots * mean / keys_us + 0.7 * full +
-                         (rest ? std::max(longest * 6.3e-3, rest * mean / keys_us) : 0.) +
-                         (parts > 1 ? 3. + 0.05 * parts : 0.);
+      const Cut c = cuts(ones, split);
+      const double keys_us = 6.2e6 / 256, mean = (double)c.keys / c.units;
+      const int64_t full = c.units / slots, rest = c.units % slots;
+      const double est = full * slots * mean / keys_us + 3.5 * full +
+                         (rest ? std::max(c.longest * 6.3e-3, rest * mean / keys_us) : 0.) +
+                         (c.parts > 1 ? 3. + 0.05 * c.parts : 0.);
       if (!split_d || est < best) {
         best = est;
         split_d = split;
@@ -194,9 +194,70 @@ int build(const dlfp_dims* dims, const dlfp_tuning* tuning, const dlfp_window* w
       if (split == 128) break;
     }
   }
+
+  // Prefill tiles and split: tiles of 128 rows, or of 32 whose units split their
+  // keys over the wavefronts, and a number of equal parts, by an estimate of the
+  // prefill share's time in us.  A unit of 128 rows takes 22.7 ns a key with a
+  // compute unit to itself and 30.5 beside another one, one of 32 rows 9.2 and 13.5;
+  // its start and end 4.5 and 8, 5 and 6; a further round 3 and 2, and 2 more for
+  // the partial results; a merge 5 and 3, and 0.9 and 0.4 for each part.  Beside a decode share that fills a workgroup slot of every
+  // compute unit the prefill units have the other one.
+  int64_t split_p = tn.prefill_split_tokens, tile_tokens = tn.prefill_tile_tokens;
+  if (!prompts.empty()) {
+    struct Height {
+      int64_t rows;
+      double alone, beside, start, start2, round, merge, part;
+    };
+    constexpr Height heights[] = {{DLFP_TILE_ROWS, 22.7e-3, 30.5e-3, 4.5, 8., 3., 5., 0.9},
+                                  {DLFP_SMALL_ROWS, 9.2e-3, 13.5e-3, 5., 6., 2., 3., 0.4}};
+    const int64_t fixed_tile = tile_tokens, fixed_split = split_p;
+    const bool shared = !ones.empty() && cuts(ones, split_d).units >= cus;
+    const int64_t room = shared ? slots - cus : slots;
+    double best = 0.;
+    bool found = false;
+    for (const Height& h : heights) {
+      const int64_t each = fixed_tile ? fixed_tile : std::max<int64_t>(1, h.rows / g);
+      if (fixed_tile && (each * g <= DLFP_SMALL_ROWS) != (h.rows == DLFP_SMALL_ROWS)) continue;
+      std::vector<Rows> t = split_tiles(each);
+      int64_t whole = 0;
+      for (const Rows& r : t) whole = std::max(whole, r.keys);
+      const int64_t most = each * g <= DLFP_SMALL_ROWS ? DLFP_MAX_DECODE_UNIT_KEYS
+                                                       : DLFP_MAX_PREFILL_UNIT_KEYS;
+      bool better = false;
+      for (int64_t n = ceil_div(whole, most); n <= ceil_div(whole, most) + 15; ++n) {
+        const int64_t split = fixed_split ? fixed_split
+                                          : std::max<int64_t>(round_up(ceil_div(whole, n), 64), 256);
+        const Cut c = cuts(t, split);
+        const double mean = (double)c.keys / c.units;
+        const int64_t full = c.units / room, rest = c.units % room;
+        const bool two = shared || c.units > cus;
+        double est = (two ? h.start2 : h.start) + full * (h.round + mean * h.beside) +
+                     (c.parts > 1 ? h.merge + h.part * c.parts + 2. * full : 0.);
+        if (rest)
+          est += (full ? mean : two ? 0.5 * (mean + c.longest) : (double)c.longest) *
+                 (shared || rest > cus ? h.beside : h.alone);
+        if (!found || est < best) {
+          best = est;
+          split_p = split;
+          found = better = true;
+        }
+        if (fixed_split || split == 256) break;
+      }
+      if (better) tiles = std::move(t);
+    }
+  }
+  int64_t tile_keys = 0;
+  for (const Rows& r : tiles) tile_keys += r.keys;
+  auto longest_first = [](const Rows& x, const Rows& y) { return x.keys > y.keys; };
+  std::stable_sort(tiles.begin(), tiles.end(), longest_first);
+  std::stable_sort(ones.begin(), ones.end(), longest_first);
+
   std::vector<Unit> units;
   int64_t groups = 0, off = DLFP_WORKSPACE_PARTIALS / 4;
   auto emit = [&](const Rows& r, int64_t kh, int64_t split, int64_t granule, int32_t kind) {
+    // Units of few rows keep their block ids where decode units do.
+    if ((int64_t)r.nt * g <= DLFP_SMALL_ROWS)
+      split = std::min<int64_t>(split, DLFP_MAX_DECODE_UNIT_KEYS);
     const int64_t part = cut(r.keys, split, granule);
     const int64_t parts = ceil_div(r.keys, part);
     const int64_t floats = slot_floats((int64_t)r.nt * g);
@@ -237,8 +298,11 @@ int build(const dlfp_dims* dims, const dlfp_tuning* tuning, const dlfp_window* w
     return x.f[DLFP_W_KVEND] - x.f[DLFP_W_KVBEGIN] > y.f[DLFP_W_KVEND] - y.f[DLFP_W_KVBEGIN];
   });
   const int64_t n_units = (int64_t)units.size();
-  const int64_t longest_one =
-      n_units > num_prefill ? units[num_prefill].f[DLFP_W_KVEND] - units[num_prefill].f[DLFP_W_KVBEGIN] : 0;
+  auto longest = [](auto first, auto last) {
+    int32_t n = 0;
+    for (; first != last; ++first) n = std::max(n, first->f[DLFP_W_KVEND] - first->f[DLFP_W_KVBEGIN]);
+    return n;
+  };
   if (n_units > I32_MAX / DLFP_WORK_INTS || groups > DLFP_MAX_GROUPS || off > I32_MAX)
     return DLFP_ERANGE;
 
@@ -247,11 +311,12 @@ int build(const dlfp_dims* dims, const dlfp_tuning* tuning, const dlfp_window* w
   meta->num_units = (int32_t)n_units;
   meta->num_prefill_units = (int32_t)num_prefill;
   meta->num_groups = (int32_t)groups;
-  meta->decode_split_tokens = (int32_t)longest_one;
-  meta->prefill_split_tokens = (int32_t)split_p;
+  meta->decode_split_tokens = longest(units.begin() + num_prefill, units.end());
+  meta->prefill_split_tokens = longest(units.begin(), units.begin() + num_prefill);
   meta->workspace_bytes = 4 * off;
   meta->num_append = 0;
-  meta->num_waiting_units = 0;
+  meta->num_waiting_units =
+      num_prefill ? (int32_t)std::min<int64_t>(1024 * one_keys / std::max<int64_t>(tile_keys, 1), I32_MAX) : 0;
   // With more prefill units than compute units, one for each of those leads and
   // the decode units follow, so that the two shares run side by side.
   int64_t lead = num_prefill;

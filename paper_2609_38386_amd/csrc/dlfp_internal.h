@@ -5,6 +5,10 @@
 #include "dlfp.h"
 #include "dlfp_cache.h"
 
+// A prefill unit of dlfp_build_window_meta with at most so many rows splits its
+// keys over the wavefronts, which limits them like a decode unit's.
+#define DLFP_SMALL_ROWS 32
+
 namespace dlfp {
 
 // DLFP_OK if dims are supported; *group receives Hq / Hkv.

@@ -78,7 +78,7 @@ class Mix:
             if kv8:
                 ke, ve = far(ke), far(ve)
             self.table[self.table >= 0] += first_block
-        self.blocks = first_block + blocks
+        self.blocks, self.v_exp = first_block + blocks, -5   # the largest exponent drawn
         self.pool = rt.KVPool8.of(k, v, ke, ve) if kv8 else rt.KVPool.of(k, v)
         self.dq = bf16(np.concatenate(self.q)).to(dev)
         self.dev = dev
@@ -101,7 +101,13 @@ class Mix:
         at most 128 steps of 2^-24 of sum |q k| scale; 2^-18 for the exponential (its
         argument, up to 2^5, rounded to 2^-24 of it, and its own last place) and the
         sums over keys; the weights' rounding: one bf16 term 2^-8 (prompts, bf16
-        output), two 2^-15, three 2^-21.  Then the output's half step."""
+        output), two 2^-15, three 2^-21.  Then the output's half step.
+
+        8-bit pages with bf16 output: a product of codes adds its 64 or 128 terms to
+        within 2^-15 of sum |q k| (2^-15.9 measured over random rows).  A decoder's
+        weights (times 2^e of the page's values, relative to the largest) are two e4m3
+        terms: 2^-8 of the weight, or, below 2^-6 of the largest such, half of the lesser
+        term's least step, 2^-15 of the largest, each times a value of at most 448 2^e."""
         got = out.double().cpu().numpy()
         assert np.isfinite(got).all()
         half = 2.0 ** -8 if out.dtype == torch.bfloat16 else 2.0 ** -24
@@ -124,11 +130,17 @@ class Mix:
                     spread = np.stack([(w[j][:, None] * np.abs(vv - o[j])).sum(0)
                                        for j in range(len(q))])
                     d = 128 * 2.0 ** -24 * scale * (np.abs(q) @ np.abs(kk).T).max() + 2.0 ** -18
+                    least = 0.0
                     if half < 2.0 ** -20:
                         d += 2.0 ** -21
                     else:
-                        d += 2.0 ** -8 if ql > 1 else 2.0 ** -15
-                    tol = half * np.abs(o) + 2 * d / (1 - d) * spread + 2.0 ** -22 * np.abs(o) + 1e-30
+                        d += 2.0 ** -8 if ql > 1 or self.kv8 else 2.0 ** -15
+                        if self.kv8:
+                            d += 2.0 ** -15 * scale * (np.abs(q) @ np.abs(kk).T).max()
+                            if ql == 1:
+                                least = 2.0 ** -15 * len(vv) * w.max(1, keepdims=True) * \
+                                    448 * 2.0 ** self.v_exp
+                    tol = least + half * np.abs(o) + 2 * d / (1 - d) * spread + 2.0 ** -22 * np.abs(o) + 1e-30
                     err = np.abs(got[at + r, hs] - o)
                     assert (err <= tol).all(), (s, r, h, float((err / tol).max()))
             at += ql
