@@ -147,18 +147,19 @@ int build(const dlfp_dims* dims, const dlfp_tuning* tuning, const dlfp_window* w
     const int64_t n = ceil_div(keys, split);
     return round_up(ceil_div(keys, n), granule);
   };
-  // Units of ranges cut at `split`: their count, keys of all, of the longest, parts
-  // of the longest range.
+  // Units of ranges cut at `split`: their count, keys of all, of the longest and of
+  // the range with the shortest, parts of the longest range.
   struct Cut {
-    int64_t units, keys, longest, parts;
+    int64_t units, keys, longest, shortest, parts;
   };
   auto cuts = [&](const std::vector<Rows>& ranges, int64_t split) {
-    Cut c = {0, 0, 0, 1};
+    Cut c = {0, 0, 0, I32_MAX, 1};
     for (const Rows& r : ranges) {
       const int64_t part = cut(r.keys, split, 64), n = ceil_div(r.keys, part);
       c.units += n * hkv;
       c.keys += r.keys * hkv;
       c.longest = std::max(c.longest, std::min(part, r.keys));
+      c.shortest = std::min(c.shortest, std::min(part, r.keys));
       c.parts = std::max(c.parts, n);
     }
     return c;
@@ -173,20 +174,30 @@ int build(const dlfp_dims* dims, const dlfp_tuning* tuning, const dlfp_window* w
 
   // Decode split: an n-th of the longest range, the n that minimises an estimate of
   // the decode share's time in us: full rounds of units and the rest of the last one
-  // stream at 6.2 TB/s (256 bytes a key, those of 8-bit pages), no unit
-  // faster than 6.3 ns a key; a full round takes 3.5 us more, a merge 3 and 0.05 for
-  // each part.
+  // stream at 6.2 TB/s (256 bytes a key, those of 8-bit pages), no unit faster
+  // than 6.3 ns a key (10.8 where some compute units have two); a full round
+  // takes 3.5 us more, a merge 3 and 0.1 for each part.
   int64_t split_d = tn.decode_split_tokens;
   if (!split_d && !ones.empty()) {
+    // Beside a prefill share for every compute unit: one slot of each, and a round
+    // costs more (whole 8-bit contexts beside 1999 tokens, 4096-key units 403 us,
+    // of 2752 keys 445).
+    const bool beside = (int64_t)split_tiles(std::max(1, DLFP_TILE_ROWS / g)).size() * hkv >= cus;
+    const int64_t room = beside ? slots - cus : slots;
+    const double round = beside ? 8. : 3.5;
     double best = 0.;
     for (int64_t n = ceil_div(one_longest, DLFP_MAX_DECODE_UNIT_KEYS); n <= 256; ++n) {
       const int64_t split = std::max<int64_t>(round_up(ceil_div(one_longest, n), 64), 128);
       const Cut c = cuts(ones, split);
       const double keys_us = 6.2e6 / 256, mean = (double)c.keys / c.units;
-      const int64_t full = c.units / slots, rest = c.units % slots;
-      const double est = full * slots * mean / keys_us + 3.5 * full +
-                         (rest ? std::max(c.longest * 6.3e-3, rest * mean / keys_us) : 0.) +
-                         (c.parts > 1 ? 3. + 0.05 * c.parts : 0.);
+      const int64_t full = c.units / room, rest = c.units % room;
+      // The longest units come first, so a last round after full ones has the short
+      // ones.
+      const double least = full ? c.shortest * 6.3e-3
+                                : c.longest * (rest > cus ? 10.8e-3 : 6.3e-3);
+      const double est = full * room * mean / keys_us + round * full +
+                         (rest ? std::max(least, rest * mean / keys_us) : 0.) +
+                         (c.parts > 1 ? 3. + 0.1 * c.parts : 0.);
       if (!split_d || est < best) {
         best = est;
         split_d = split;
