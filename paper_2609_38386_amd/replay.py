@@ -116,6 +116,19 @@ class ReplayConfig:
     layer_proxy: bool = False
     hidden: int = 1024
     mlp: int = 3072
+    # The layer's cache and mask.  kv_bits 8 keeps it in e4m3 pages; a window lets a
+    # row see its last `window` keys and the first `sinks`; rotary turns queries and
+    # keys to their positions on the way to the cache.  With none of them the layer is
+    # the one-launch append and attention, else a rotating append (rotary_dim 128) and
+    # an attention launch.
+    kv_bits: int = 16
+    window: Optional[int] = None
+    sinks: int = 0
+    rotary: bool = False
+
+    @property
+    def windowed(self) -> bool:
+        return self.kv_bits != 16 or self.window is not None or self.rotary
 
     @property
     def max_blocks(self) -> int:
@@ -391,11 +404,17 @@ class GpuExecutor:
         self.torch, self.D = torch, D
         self.dims = D.make_dims(cfg.num_q_heads, cfg.num_kv_heads)
         self.num_blocks = cfg.num_blocks()
-        self.pool = rt.KVPool(self.num_blocks, cfg.num_kv_heads, device)
+        if cfg.kv_bits not in (8, 16):
+            raise ValueError("kv_bits must be 8 or 16")
         gen = torch.Generator(device=device)
         gen.manual_seed(cfg.seed + seed)
-        self.pool.k.normal_(generator=gen)
-        self.pool.v.normal_(generator=gen)
+        self.windowed = cfg.windowed
+        if cfg.kv_bits == 8:   # every page is begun by the append of its first token
+            self.pool = rt.KVPool8(self.num_blocks, cfg.num_kv_heads, device)
+        else:
+            self.pool = rt.KVPool(self.num_blocks, cfg.num_kv_heads, device)
+            self.pool.k.normal_(generator=gen)
+            self.pool.v.normal_(generator=gen)
         rows = cfg.budget + cfg.max_seqs
         self.q = torch.empty((rows, cfg.num_q_heads, 128), dtype=torch.bfloat16, device=device)
         self.k = torch.empty((rows, cfg.num_kv_heads, 128), dtype=torch.bfloat16, device=device)
@@ -419,7 +438,17 @@ class GpuExecutor:
             self.gu = torch.empty((rows, 2 * cfg.mlp), dtype=torch.bfloat16, device=device)
             self.y2 = torch.empty_like(self.y)
             self.mlp = cfg.mlp
-        self.stage = rt.StagedBatch(self.dims, cfg.max_seqs + 1, rows, 65536, device)
+        if self.windowed:
+            self.rt = rt
+            self.stage = rt.WindowStagedBatch(self.dims, cfg.max_seqs + 1, rows, 65536, device,
+                                              cfg.window, cfg.sinks)
+            self.rope = rt.Rope(cfg.prompt_hi + cfg.out_len, device)
+            if not cfg.rotary:
+                self.rope.table[:, :64] = 1.0
+                self.rope.table[:, 64:] = 0.0
+            self.q_turned = torch.empty_like(self.q)
+        else:
+            self.stage = rt.StagedBatch(self.dims, cfg.max_seqs + 1, rows, 65536, device)
         bt_cap = (cfg.max_seqs + 1) * cfg.max_blocks
         self.bt_host = torch.empty(bt_cap, dtype=torch.int32, pin_memory=True)
         self.bt_dev = torch.empty(bt_cap, dtype=torch.int32, device=device)
@@ -483,9 +512,15 @@ class GpuExecutor:
             D.dlfp_linear_bf16(x, self.w_q, self.q[:T].view(T, -1))
             D.dlfp_linear_bf16(x, self.w_k, self.k[:T].view(T, -1))
             D.dlfp_linear_bf16(x, self.w_v, self.v[:T].view(T, -1))
-        D.dlfp_append_attention_mixed(self.dims, st.meta, st.d_work, d_bt, self.q[:T],
-                                      self.k[:T], self.v[:T], self.pool.k, self.pool.v,
-                                      self.scale, self.out[:T], ws)
+        if self.windowed:
+            self.rt.rope_append(self.dims, self.rope, self.pool, st.d_positions, st.d_slots,
+                                self.q[:T], self.k[:T], self.v[:T], self.q_turned[:T])
+            self.rt.window_attention(self.dims, st.meta, st.d_work, d_bt, self.pool,
+                                     self.q_turned[:T], self.scale, self.out[:T], ws)
+        else:
+            D.dlfp_append_attention_mixed(self.dims, st.meta, st.d_work, d_bt, self.q[:T],
+                                          self.k[:T], self.v[:T], self.pool.k, self.pool.v,
+                                          self.scale, self.out[:T], ws)
         if self.proxy:
             D.dlfp_linear_bf16(self.out[:T].view(T, -1), self.w_o, self.y[:T])
             D.dlfp_linear_bf16(self.y[:T], self.w_gu, self.gu[:T])

@@ -187,6 +187,24 @@ class Batch:
                                        k_new, v_new, pool.k, pool.v, scale, out, ws, stream)
 
 
+def window_attention(dims: _d.dlfp_dims, meta: _d.Meta, d_work: torch.Tensor,
+                     d_block_table: torch.Tensor, pool, q: torch.Tensor, scale: float,
+                     out: torch.Tensor, workspace: torch.Tensor, stream=None):
+    """Attention over the pages of a KVPool or KVPool8, metadata of dlfp_build_window_meta."""
+    if isinstance(pool, KVPool8):
+        _d.dlfp_attention_kv8(dims, meta, d_work, d_block_table, q, pool.k, pool.v, pool.k_exp,
+                              pool.v_exp, scale, out, workspace, stream)
+    else:
+        _d.dlfp_attention_window(dims, meta, d_work, d_block_table, q, pool.k, pool.v, scale, out,
+                                 workspace, stream)
+
+
+def new_positions(meta: _d.Meta, q_len: np.ndarray) -> np.ndarray:
+    """Positions of a batch's new tokens, in packed order."""
+    seq = np.repeat(np.arange(len(q_len)), q_len)
+    return meta.q_pos0[seq] + np.arange(len(seq), dtype=np.int32) - meta.cu_q[seq]
+
+
 class WindowBatch:
     """Metadata of one mixed iteration for the rotating append and windowed or 8-bit
     attention, plus device copies of its arrays.  ``window`` None: every key up to a row's
@@ -205,9 +223,8 @@ class WindowBatch:
             dims, self.q_len, self.kv_len, table, num_blocks,
             _d.dlfp_window(window, sinks) if window is not None else None, tuning)
         self.num_tokens = t = m.num_tokens
-        seq = np.repeat(np.arange(len(self.q_len)), self.q_len)
-        positions = m.q_pos0[seq] + np.arange(t, dtype=np.int32) - m.cu_q[seq]
-        host = np.concatenate([m.slot_mapping[:t], positions, m.records.reshape(-1)]
+        host = np.concatenate([m.slot_mapping[:t], new_positions(m, self.q_len),
+                               m.records.reshape(-1)]
                               ).astype(np.int32)
         dev = torch.from_numpy(host).to(device)
         self.d_slots, self.d_positions, self.d_work = dev[:t], dev[t:2 * t], dev[2 * t:]
@@ -221,12 +238,8 @@ class WindowBatch:
     def attention(self, pool, q: torch.Tensor, scale: float, out: torch.Tensor,
                   workspace: Workspace, stream=None):
         ws = workspace.ensure(self.meta.workspace_bytes, self.meta.num_groups, stream)
-        if isinstance(pool, KVPool8):
-            _d.dlfp_attention_kv8(self.dims, self.meta, self.d_work, self.d_block_table, q, pool.k,
-                                  pool.v, pool.k_exp, pool.v_exp, scale, out, ws, stream)
-        else:
-            _d.dlfp_attention_window(self.dims, self.meta, self.d_work, self.d_block_table, q,
-                                     pool.k, pool.v, scale, out, ws, stream)
+        window_attention(self.dims, self.meta, self.d_work, self.d_block_table, pool, q, scale, out,
+                         ws, stream)
 
 
 class Iteration:
@@ -298,6 +311,7 @@ class StagedBatch:
                  tuning: Optional[_d.dlfp_tuning] = None):
         import ctypes
         self._ct = ctypes
+        self.pieces = ()   # further int32 arrays that go along, after the slots and records
         self.dims = dims
         self.tuning = tuning if tuning is not None else _d.dlfp_tuning(0, 0, 0)
         self.meta = _d.Meta(cap_seqs, cap_tokens, cap_work)
@@ -311,22 +325,54 @@ class StagedBatch:
               num_blocks: int, stream=None):
         ct = self._ct
         m = self.meta
+        self._build(ct, m, q_len, kv_len, block_table, num_blocks)
+        T, U = m.c.num_tokens, m.c.num_units + m.c.num_append
+        h = self.host_np
+        o = 0
+        offs = []
+        for arr, cnt in ((m.slot_mapping, T), (m.work_buf.reshape(-1), U * _d.WORK_INTS),
+                         *self.pieces):
+            h[o:o + cnt] = arr[:cnt]
+            offs.append((o, cnt))
+            o += cnt
+        self.dev[:o].copy_(self.host[:o], non_blocking=True)
+        (d, nd), (e, ne) = offs[:2]
+        self.d_slots = self.dev[d:d + nd]
+        self.d_work = self.dev[e:e + ne]
+        self.d_pieces = [self.dev[p:p + n] for p, n in offs[2:]]
+        self.num_tokens = T
+        return self
+
+    def _build(self, ct, m, q_len, kv_len, block_table, num_blocks):
         st = self.lib.dlfp_build_varlen_meta(
             ct.byref(self.dims), ct.byref(self.tuning), len(q_len), _d._ptr32(q_len),
             _d._ptr32(kv_len), _d._ptr32(block_table), block_table.shape[1], int(num_blocks),
             ct.byref(m.c))
         _d._check(st, "dlfp_build_varlen_meta")
-        T, U = m.c.num_tokens, m.c.num_units + m.c.num_append
-        h = self.host_np
-        o = 0
-        offs = []
-        for arr, cnt in ((m.slot_mapping, T), (m.work_buf.reshape(-1), U * _d.WORK_INTS)):
-            h[o:o + cnt] = arr[:cnt]
-            offs.append((o, cnt))
-            o += cnt
-        self.dev[:o].copy_(self.host[:o], non_blocking=True)
-        (d, nd), (e, ne) = offs
-        self.d_slots = self.dev[d:d + nd]
-        self.d_work = self.dev[e:e + ne]
-        self.num_tokens = T
-        return self
+
+
+class WindowStagedBatch(StagedBatch):
+    """The same for the rotating append and windowed or 8-bit attention: metadata of
+    dlfp_build_window_meta, and the new tokens' positions.  ``window`` None: every key up
+    to a row's own."""
+
+    def __init__(self, dims: _d.dlfp_dims, cap_seqs: int, cap_tokens: int, cap_work: int, device,
+                 window: Optional[int] = None, sinks: int = 0,
+                 tuning: Optional[_d.dlfp_tuning] = None):
+        if window is None and sinks:
+            raise ValueError("sinks need a window")
+        super().__init__(dims, cap_seqs, 2 * cap_tokens, cap_work, device, tuning)
+        self.window = _d.dlfp_window(window, sinks) if window is not None else None
+
+    def _build(self, ct, m, q_len, kv_len, block_table, num_blocks):
+        st = self.lib.dlfp_build_window_meta(
+            ct.byref(self.dims), ct.byref(self.tuning),
+            ct.byref(self.window) if self.window is not None else None, len(q_len),
+            _d._ptr32(q_len), _d._ptr32(kv_len), _d._ptr32(block_table), block_table.shape[1],
+            int(num_blocks), ct.byref(m.c))
+        _d._check(st, "dlfp_build_window_meta")
+        self.pieces = ((new_positions(m, q_len), m.c.num_tokens),)
+
+    @property
+    def d_positions(self) -> torch.Tensor:
+        return self.d_pieces[0]

@@ -103,6 +103,13 @@ class Mix:
         sums over keys; the weights' rounding: one bf16 term 2^-8 (prompts, bf16
         output), two 2^-15, three 2^-21.  Then the output's half step.
 
+        What does not fall with the spread, where one key has all the weight: roundings of
+        the sum itself, each at most 2^-24 of B = sum_j p_j |v_j|.  A matrix product adds
+        16 keys or more, so n keys take n / 16; the three terms of a weight leave 2^-22 of
+        it (two cut to 8 bits, the third rounded to 8: 2^-7 2^-7 2^-8), four such; the
+        exponentials of the wavefronts' and splits' maxima, their sums, the division and
+        the product with it, up to 12 more.
+
         8-bit pages with bf16 output: a product of codes adds its 64 or 128 terms to
         within 2^-15 of sum |q k| (2^-15.9 measured over random rows).  A decoder's
         weights (times 2^e of the page's values, relative to the largest) are two e4m3
@@ -140,7 +147,8 @@ class Mix:
                             if ql == 1:
                                 least = 2.0 ** -15 * len(vv) * w.max(1, keepdims=True) * \
                                     448 * 2.0 ** self.v_exp
-                    tol = least + half * np.abs(o) + 2 * d / (1 - d) * spread + 2.0 ** -22 * np.abs(o) + 1e-30
+                    sums = (len(vv) / 16 + 16) * 2.0 ** -24 * (w @ np.abs(vv))
+                    tol = least + half * np.abs(o) + 2 * d / (1 - d) * spread + sums + 1e-30
                     err = np.abs(got[at + r, hs] - o)
                     assert (err <= tol).all(), (s, r, h, float((err / tol).max()))
             at += ql
