@@ -144,10 +144,11 @@ int dlfp_build_window_meta(const dlfp_dims* dims, const dlfp_tuning* tuning,
  * sequence s at position p = q_pos0[s] + i and query head h with KV head h / g,
  * out = softmax_j(scale * q.k_j) v_j over the keys j that the row sees.
  * Arguments as for dlfp_attention_mixed, with a metadata of
- * dlfp_build_window_meta.  Scores, statistics and sums are fp32.  With bf16
- * output the probabilities of a prompt's rows are rounded to bf16 for the
- * product with the values; with fp32 output, and a decoder's always, they are
- * taken in terms that keep 16 (decoder, bf16 output) to 24 bits.
+ * dlfp_build_window_meta; q, caches, out and workspace are 16-byte aligned.
+ * Scores, statistics and sums are fp32.  With bf16 output the probabilities of a
+ * prompt's rows are rounded to bf16 for the product with the values (1.1e-3 to
+ * 1.6e-3 of a row in the 2-norm, below the output's own rounding) and a decoder's
+ * taken in two bf16 terms; with fp32 output they are three terms, 24 bits.
  * Keys and values that no row of the batch sees are not used, whatever they
  * hold.  A NaN or infinite value that some rows of a prompt see and others of
  * the same 128 / g tokens do not can make the latter NaN too.
@@ -158,7 +159,12 @@ int dlfp_attention_window(const dlfp_dims* dims, const dlfp_meta* meta, const in
                           void* out, int32_t out_dtype, void* workspace, size_t workspace_bytes,
                           hipStream_t stream);
 
-/* The same over 8-bit pages and their exponents, with or without a window. */
+/* The same over 8-bit pages and their exponents, with or without a window.  With
+ * bf16 output the scores come from products of 8-bit numbers: a query is the sum
+ * of two e4m3 codes in scales 2^4 apart (what lies below 2^-22 of its row's
+ * largest is lost) and the matrix cores add a product's terms to within 2^-15 of
+ * the sum of their magnitudes (2e-6 on average); a decoder's probabilities are two
+ * e4m3 terms (2^-8, or 2^-15 of the largest), a prompt's one bf16 term. */
 int dlfp_attention_kv8(const dlfp_dims* dims, const dlfp_meta* meta, const int32_t* d_work,
                        const int32_t* d_block_table, int32_t max_blocks, int32_t num_blocks,
                        const void* q, const void* k_cache, const void* v_cache,

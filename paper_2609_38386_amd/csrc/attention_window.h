@@ -1647,6 +1647,9 @@ int attention_window(const dlfp_dims* dims, const dlfp_meta* meta, const int32_t
   if (!d_work || !d_block_table || !q || !k_cache || !v_cache || !out || !workspace)
     return DLFP_EINVAL;
   if (KV8 && (!k_exp || !v_exp)) return DLFP_EINVAL;
+  for (const void* p : {q, k_cache, v_cache, static_cast<const void*>(out),
+                        static_cast<const void*>(workspace)})
+    if (reinterpret_cast<uintptr_t>(p) % 16) return DLFP_EINVAL;
   if (max_blocks <= 0 || num_blocks <= 0) return DLFP_EINVAL;
   if ((int64_t)workspace_bytes < meta->workspace_bytes ||
       workspace_bytes < (size_t)DLFP_WORKSPACE_PARTIALS)

@@ -359,12 +359,26 @@ def make_rope(table, interleaved: bool = False) -> dlfp_rope:
     return dlfp_rope(table.data_ptr(), table.size(0), table.size(1), 1 if interleaved else 0)
 
 
+def _on_one_device(*tensors) -> None:
+    """Refuses tensors on the host or on different devices, whose addresses a kernel would
+    follow all the same."""
+    device = tensors[0].get_device()
+    for t in tensors:
+        if t.get_device() != device:
+            raise ValueError("tensors are on different devices")
+    if device < 0 and tensors[0].numel():
+        raise ValueError("tensors must be on a device")
+
+
 def _append_args(dims, rope, positions, slot_mapping, q, k_new, v_new, q_out, k_cache, v_cache):
     n = slot_mapping.size(0)
     if positions.size(0) != n:
         raise ValueError("shapes disagree")
     if positions.element_size() != 4 or slot_mapping.element_size() != 4:
         raise ValueError("positions and slots must be int32")
+    if n > 1 and (positions.stride(0) != 1 or slot_mapping.stride(0) != 1):
+        raise ValueError("positions and slots must be contiguous")
+    _on_one_device(q, positions, slot_mapping, k_new, v_new, q_out, k_cache, v_cache)
     qs, ks = (n, dims.num_q_heads, HEAD_DIM), (n, dims.num_kv_heads, HEAD_DIM)
     return (dims, rope, n, positions.data_ptr(), slot_mapping.data_ptr(), q.data_ptr(),
             _rows(q, qs), k_new.data_ptr(), _rows(k_new, ks), v_new.data_ptr(), _rows(v_new, ks),
@@ -393,9 +407,19 @@ def dlfp_rope_append_kv8(dims: dlfp_dims, rope: dlfp_rope, positions, slot_mappi
         _check(st, "dlfp_rope_append_kv8")
 
 
+def _check_attention(dims, meta, d_work, d_block_table, q, k_cache, v_cache, out, workspace):
+    shape = (meta.c.num_tokens, dims.num_q_heads, HEAD_DIM)
+    if q.shape != shape or out.shape != shape or q.element_size() != 2:
+        raise ValueError("q and out must be [tokens][Hq][128], q bf16")
+    if not (q.is_contiguous() and out.is_contiguous() and d_block_table.is_contiguous()):
+        raise ValueError("q, out and the block table must be contiguous")
+    _on_one_device(q, d_work, d_block_table, k_cache, v_cache, out, workspace)
+
+
 def dlfp_attention_window(dims: dlfp_dims, meta: Meta, d_work, d_block_table, q, k_cache, v_cache,
                           scale: float, out, workspace, stream=None) -> None:
     """meta: of dlfp_build_window_meta; bf16 caches; out dtype bfloat16 or float32."""
+    _check_attention(dims, meta, d_work, d_block_table, q, k_cache, v_cache, out, workspace)
     st = lib().dlfp_attention_window(
         dims, meta.c, d_work.data_ptr(), d_block_table.data_ptr(), d_block_table.size(1),
         k_cache.size(0), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), float(scale),
@@ -408,6 +432,7 @@ def dlfp_attention_window(dims: dlfp_dims, meta: Meta, d_work, d_block_table, q,
 def dlfp_attention_kv8(dims: dlfp_dims, meta: Meta, d_work, d_block_table, q, k_cache, v_cache,
                        k_exp, v_exp, scale: float, out, workspace, stream=None) -> None:
     """The same over 8-bit caches with their exponents (uint8 [num_blocks][Hkv])."""
+    _check_attention(dims, meta, d_work, d_block_table, q, k_cache, v_cache, out, workspace)
     st = lib().dlfp_attention_kv8(
         dims, meta.c, d_work.data_ptr(), d_block_table.data_ptr(), d_block_table.size(1),
         k_cache.size(0), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_exp.data_ptr(),

@@ -8,6 +8,7 @@ numbers, its windowed rows by the full mask of oracle.attention.
 import ctypes
 import os
 import re
+from types import SimpleNamespace
 
 import numpy as np
 import pytest
@@ -120,7 +121,9 @@ def test_metadata_kinds_are_refused_where_the_other_belongs():
     assert L.dlfp_attention_kv8(DIMS, windowed.c, *args, none, one, *rest) == -1
     for bad, want in [((0.0, one, 0, one, 1 << 24, none), -1), ((0.1, one, 2, one, 1 << 24, none), -1),
                       ((0.1, one, 0, one, 1000, none), -3), ((float("nan"), one, 0, one, 1 << 24, none), -1),
-                      ((0.1, none, 0, one, 1 << 24, none), -1)]:
+                      ((0.1, none, 0, one, 1 << 24, none), -1),
+                      ((0.1, ctypes.c_void_p(24), 0, one, 1 << 24, none), -1),
+                      ((0.1, one, 0, ctypes.c_void_p(8), 1 << 24, none), -1)]:
         assert L.dlfp_attention_window(DIMS, windowed.c, *args, *bad) == want
         assert L.dlfp_attention_kv8(DIMS, windowed.c, *args, one, one, *bad) == want
     empty = D.dlfp_build_window_meta(DIMS, [], [], np.zeros((0, 1), np.int32), 1)
@@ -171,6 +174,15 @@ def test_binding_refusals():
             rt.rope_append(DIMS, rope, pool, at, at, *bad)
     with pytest.raises(ValueError):
         rt.rope_append(DIMS, rope, pool, at.long(), at, q, k, k, q)
+    with pytest.raises(ValueError):   # on the host
+        rt.rope_append(DIMS, rope, pool, at, at, q, k, k, q)
+    with pytest.raises(ValueError):   # every other position
+        rt.rope_append(DIMS, rope, pool, torch.zeros(6, dtype=torch.int32)[::2], at, q, k, k, q)
+    batch = rt.WindowBatch(DIMS, [3], [3], np.zeros((1, 1), np.int32), 1, "cpu")
+    ws = SimpleNamespace(ensure=lambda *a: torch.zeros(1 << 20, dtype=torch.uint8))
+    for bad in [(q, q), (q[:2], q), (q, q.float()[:, :8]), (q.transpose(0, 1), q)]:
+        with pytest.raises(ValueError):
+            batch.attention(pool, bad[0], 0.1, bad[1], ws)
     with pytest.raises(ValueError):
         rt.KVPool8.of(pool.k, pool.v, pool.k_exp[:2], pool.v_exp)
     with pytest.raises(ValueError):
