@@ -65,6 +65,7 @@ struct Args {
   // decode ones, then groups of GRID_GROUP workgroups, prefill_groups and
   // decode_groups of them evenly mixed, then what is left of each share.
   int32_t lead, decode_lead, prefill_groups, decode_groups;
+  int32_t solo;  // a decode workgroup has four units, a wavefront each
   float scale_log2;
 };
 
@@ -262,7 +263,7 @@ constexpr int decode_wave_lds() {
 
 template <bool KV8>
 constexpr int window_lds() {
-  constexpr int pre = PreLds<KV8>::BYTES, dec = 4 * decode_wave_lds<KV8, 4>();
+  constexpr int pre = PreLds<KV8>::BYTES, dec = 4 * decode_wave_lds<KV8, 1>();
   static_assert(4 * 1024 * 16 + 2 * 4 * 32 * 4 <= (pre > dec ? pre : dec), "four partial results");
   return pre > dec ? pre : dec;
 }
@@ -616,10 +617,12 @@ __device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, ch
     id2 = page_id(j + 3);
     if (wave_active) {
       bf16x8_t pf[4];
-      // On the last tile this reads a stale slot; the result is not used.
-      qk(nxt, PAR ^ 1, j + 1);
+      // On the last tile this reads a stale slot; the result is not used.  With
+      // fp32 output the probabilities stay in registers for their three terms, and
+      // the next scores come after them.
+      if constexpr (!OUT32) qk(nxt, PAR ^ 1, j + 1);
       probs(cur, pf, 0, 2);
-      if constexpr (!KV8) {
+      if constexpr (!KV8 && !OUT32) {
         // Key operands four products ahead, exponentials between the products.
         __builtin_amdgcn_sched_group_barrier(0x100, 4, 0);
 #pragma unroll
@@ -631,7 +634,7 @@ __device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, ch
       __builtin_amdgcn_s_setprio(1);
       probs(cur, pf, 2, 4);
       pv(pf, PAR, j, 0, 1);
-      if constexpr (!KV8) {
+      if constexpr (!KV8 && !OUT32) {
         __builtin_amdgcn_sched_group_barrier(0x100, 4, 1);
 #pragma unroll
         for (int i = 0; i < 8; ++i) {
@@ -648,6 +651,7 @@ __device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, ch
         pv(pf, PAR, j, 0, 2);
         next_term(cur, pf, true);
         pv(pf, PAR, j, 0, 2);
+        qk(nxt, PAR ^ 1, j + 1);
       }
       float mx = rowmax(nxt);
       if constexpr (!KV8 && !OUT32) {
@@ -1109,8 +1113,9 @@ __device__ __forceinline__ void small_unit(const Args& a, const record_t f, char
 
 // ---------------------------------------------------------------- decode
 
-// Decode unit of a workgroup of NW wavefronts: wavefront w takes blocks w, w + NW,
-// ... of the unit; their results meet in LDS, those of split ranges in memory.
+// Decode unit of NW wavefronts: wavefront w takes blocks w, w + NW, ... of the unit;
+// their results meet in LDS, those of split ranges in memory.  NW 1: the wavefront
+// has no others to wait for, whatever the workgroup.
 // The unit's g heads are columns 0-7 of 16x16 products and, with the second term
 // of the probabilities, columns 8-15.  Lane l owns column l % 16; its group
 // q = l / 16 owns, of 8-bit pages, the 16 keys of page q of the block, of bf16
@@ -1123,7 +1128,14 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
   constexpr int NCH = KV8 ? 4 : 2;    // 16-key products of a block
   constexpr int NC = PB / 1024;       // copies of a page
   constexpr bool CODES = KV8 && !OUT32;
-  const int tid = threadIdx.x, wave = uniform(tid >> 6), lane = tid & 63;
+  const int tid = NW == 1 ? threadIdx.x & 63 : threadIdx.x, wave = uniform(tid >> 6);
+  const int lane = tid & 63;
+  auto meet = [] {
+    if constexpr (NW == 1)
+      wave_sync();
+    else
+      __syncthreads();
+  };
   char* wl = smem + wave * decode_wave_lds<KV8, NW>();
   const int col = lane & 15, gq = lane >> 4, head = col & 7;
   const record_t f = load_record(rec);
@@ -1455,7 +1467,7 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
       o[mb][i] = sum_xor8(x);
     }
   wait_memory_complete();
-  __syncthreads();  // every wavefront is done with its slots
+  meet();  // every wavefront is done with its slots
   f32x4_t* red = reinterpret_cast<f32x4_t*>(smem);
   float* stat = reinterpret_cast<float*>(smem + NW * G * 512);  // m[NW][G], l[NW][G]
   auto at = [](int w, int h, int q) { return (w * G + h) * 32 + (q ^ ((h & 7) << 2)); };
@@ -1467,7 +1479,7 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
       stat[NW * G + wave * G + col] = l_tot;
     }
   }
-  __syncthreads();
+  meet();
   const int slot_floats = slot_floats_for(G);
   const Slots sl = group_slots(a.ws, f[DLFP_W_WSGROUP], nsplits, slot_floats);
   const int my = f[DLFP_W_SPLIT] * slot_floats;
@@ -1504,10 +1516,16 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
   // The last arriver merges the splits in order.
   const int grp = f[DLFP_W_GROUP];
   wait_memory_complete();
-  __syncthreads();  // every wave of the unit has completed its stores
-  if (tid == 0) *flag = arrive(a.ws, grp) == nsplits - 1;
-  __syncthreads();
-  if (!*flag) return;
+  meet();  // every wave of the unit has completed its stores
+  if constexpr (NW == 1) {
+    int order = 0;
+    if (lane == 0) order = arrive(a.ws, grp);
+    if (uniform(order) != nsplits - 1) return;
+  } else {
+    if (tid == 0) *flag = arrive(a.ws, grp) == nsplits - 1;
+    __syncthreads();
+    if (!*flag) return;
+  }
 #pragma unroll
   for (int h0 = 0; h0 < G; h0 += 2 * NW) {
     const int h = h0 + (tid >> 5);
@@ -1582,10 +1600,17 @@ template <int G, bool KV8, bool OUT32>
 __global__ __launch_bounds__(THREADS, 2) void window_kernel(Args a) {
   __shared__ __attribute__((aligned(16))) char smem[window_lds<KV8>()];
   __shared__ int flag;
-  const int u = unit_of(a, blockIdx.x);
+  const int u = unit_of(a, blockIdx.x);  // prefill unit, or num_prefill + decode workgroup
   const int32_t* rec = a.work + (int64_t)u * DLFP_WORK_INTS;
   if (u >= a.num_prefill) {
-    decode_unit<G, KV8, OUT32, 4>(a, rec, smem, &flag);
+    if (a.solo) {
+      const int wave = uniform(threadIdx.x >> 6), d = 4 * (u - a.num_prefill) + wave;
+      if (d < a.num_units - a.num_prefill)
+        decode_unit<G, KV8, OUT32, 1>(a, a.work + (int64_t)(a.num_prefill + d) * DLFP_WORK_INTS,
+                                      smem + wave * decode_wave_lds<KV8, 1>(), nullptr);
+    } else {
+      decode_unit<G, KV8, OUT32, 4>(a, rec, smem, &flag);
+    }
     return;
   }
   const record_t f = load_record(rec);
@@ -1603,9 +1628,9 @@ __global__ __launch_bounds__(NW * 64, 2) void window_decode_kernel(Args a) {
 }
 
 template <int G, bool KV8, bool OUT32>
-hipError_t launch_window(const Args& a, int nw, hipStream_t stream) {
+hipError_t launch_window(const Args& a, int grid, int nw, hipStream_t stream) {
   if (a.num_prefill > 0)
-    window_kernel<G, KV8, OUT32><<<a.num_units, THREADS, 0, stream>>>(a);
+    window_kernel<G, KV8, OUT32><<<grid, THREADS, 0, stream>>>(a);
   else if (nw == 8)
     window_decode_kernel<G, KV8, OUT32, 8><<<a.num_units, 8 * 64, 0, stream>>>(a);
   else if (nw == 4)
@@ -1616,9 +1641,9 @@ hipError_t launch_window(const Args& a, int nw, hipStream_t stream) {
 }
 
 template <int G, bool KV8>
-hipError_t launch_window(const Args& a, int nw, hipStream_t stream) {
-  return a.out_f32 ? launch_window<G, KV8, true>(a, nw, stream)
-                   : launch_window<G, KV8, false>(a, nw, stream);
+hipError_t launch_window(const Args& a, int grid, int nw, hipStream_t stream) {
+  return a.out_f32 ? launch_window<G, KV8, true>(a, grid, nw, stream)
+                   : launch_window<G, KV8, false>(a, grid, nw, stream);
 }
 
 // Validation and launch shared by the two entry points.
@@ -1674,6 +1699,23 @@ int attention_window(const dlfp_dims* dims, const dlfp_meta* meta, const int32_t
   a.scale_log2 = scale * LOG2E;
   const int cus = dlfp::compute_units();
   const int decode_units = a.num_units - a.num_prefill;
+  // Decode units of a wavefront each spend no workgroup on their start and sum, but
+  // last four times as long: 29 ns a key of bf16 pages, 25 of 8-bit ones.  Alone they
+  // are those of up to 128 KiB of cache that are more than three for each compute
+  // unit (2048 units of 64 keys, 8-bit pages: 10.2 us, of four wavefronts 20.9; of 512
+  // keys 45.9 and 48.8; bf16, 128 keys: 23.9 and 27.2).  Beside prefill units, those
+  // that last up to a quarter of the launch, by its operations at 1120 TFLOP/s and
+  // its bytes at 6.4 TB/s: 8-bit pages, 500 decoders of 64 keys beside 512 tokens
+  // 33.4 us, of four wavefronts 59.4, of 256 keys 63.5 and 79.5; 70 of 500 keys,
+  // which last longer, 33.3 and 28.9.
+  const double key_us = (KV8 ? 256 : 512) / 6.4e6, tile_key_us = 128 * 512 / 1120e6;
+  const double unit_us = meta->decode_split_tokens * (KV8 ? 25e-3 : 29e-3);
+  const double prefill_us = 0.75 * a.num_prefill * meta->prefill_split_tokens * tile_key_us;
+  const double decode_us = 0.75 * decode_units * (double)meta->decode_split_tokens * key_us;
+  const int64_t unit_bytes = (int64_t)meta->decode_split_tokens * 2 * DLFP_HEAD_DIM * (KV8 ? 1 : 2);
+  a.solo = a.num_prefill ? 4. * unit_us <= prefill_us + decode_us
+                         : decode_units > 3 * cus && unit_bytes <= 128 << 10;
+  const int decode_wgs = a.solo ? (decode_units + 3) / 4 : decode_units;
   // One prefill unit for each compute unit, then one decode unit for each, so that
   // both shares run from the start (beside each other each runs at 0.62 of its
   // speed alone).  A decode share that takes as long as the prefill share goes on
@@ -1685,39 +1727,35 @@ int attention_window(const dlfp_dims* dims, const dlfp_meta* meta, const int32_t
   // pages: 403 us, mixed 475).
   a.lead = a.num_prefill;
   a.decode_lead = a.prefill_groups = a.decode_groups = 0;
-  if (meta->prefill_lead_units < a.num_prefill && decode_units >= GRID_GROUP) {
+  if (meta->prefill_lead_units < a.num_prefill && decode_wgs >= GRID_GROUP) {
     a.lead = meta->prefill_lead_units / GRID_GROUP * GRID_GROUP;
-    a.decode_lead = std::min(decode_units, cus) / GRID_GROUP * GRID_GROUP;
+    a.decode_lead = std::min(decode_wgs, cus) / GRID_GROUP * GRID_GROUP;
     a.prefill_groups = (a.num_prefill - a.lead) / GRID_GROUP;
     // Keys of the decode units for one of the prefill units, times what a key takes
     // of the decode share alone (its bytes at 6.4 TB/s) over the prefill share alone
     // (128 rows at 1.12 PFLOP/s).
-    const double key = (KV8 ? 256 : 512) / 6.4 / (128 * 512 / 1120.);
+    const double key = key_us / tile_key_us;
     const double shares = meta->num_waiting_units / 1024. * key;
     const double groups = shares >= 0.9 ? 0.85 * key * a.prefill_groups * meta->prefill_split_tokens /
-                                              std::max(meta->decode_split_tokens, 64)
+                                              std::max(meta->decode_split_tokens, 64) /
+                                              (a.solo ? 4 : 1)
                                         : 0.;
-    a.decode_groups = (int)std::min<double>((decode_units - a.decode_lead) / GRID_GROUP, groups);
+    a.decode_groups = (int)std::min<double>((decode_wgs - a.decode_lead) / GRID_GROUP, groups);
   }
-  // Wavefronts of a decode unit's workgroup in a launch of decode units alone.
-  // One, with units of up to 128 KiB of cache that are more than three for each
-  // compute unit: a workgroup is then mostly its start and its sum (2048 units of
-  // 64 keys, 8-bit pages 10.2 us, with four wavefronts 20.9; of 512 keys 45.9 and
-  // 48.8; bf16, 128 keys 23.9 and 27.2).  Eight, with long units on a quarter of
-  // the compute units: one lasts as long as its chain of steps (8 units of 2048
-  // keys 15.0 and 17.2 us).  Else four, two workgroups on a compute unit, one's
-  // start and sum behind the other (512 units of 1024 keys, 8 bits: 23.2 us, with
-  // eight 26.5, with one 31.5).
-  const int64_t unit_bytes = (int64_t)meta->decode_split_tokens * 2 * DLFP_HEAD_DIM * (KV8 ? 1 : 2);
-  const int nw = a.num_units > 3 * cus && unit_bytes <= 128 << 10 ? 1
-                 : a.num_units <= cus / 4 && meta->decode_split_tokens > 256 ? 8 : 4;
+  // Wavefronts of a decode unit in a launch of decode units alone.  Eight, with long
+  // units on a quarter of the compute units: one lasts as long as its chain of steps
+  // (8 units of 2048 keys 15.0 us, with four 17.2).  Else four, two workgroups on a
+  // compute unit, one's start and sum behind the other (512 units of 1024 keys, 8
+  // bits: 23.2 us, with eight 26.5, with one 31.5).
+  const int nw = a.solo ? 1 : a.num_units <= cus / 4 && meta->decode_split_tokens > 256 ? 8 : 4;
+  const int grid = a.num_prefill + decode_wgs;
   (void)hipGetLastError();
   hipError_t e;
   switch (g) {
-    case 1: e = launch_window<1, KV8>(a, nw, stream); break;
-    case 2: e = launch_window<2, KV8>(a, nw, stream); break;
-    case 4: e = launch_window<4, KV8>(a, nw, stream); break;
-    default: e = launch_window<8, KV8>(a, nw, stream); break;
+    case 1: e = launch_window<1, KV8>(a, grid, nw, stream); break;
+    case 2: e = launch_window<2, KV8>(a, grid, nw, stream); break;
+    case 4: e = launch_window<4, KV8>(a, grid, nw, stream); break;
+    default: e = launch_window<8, KV8>(a, grid, nw, stream); break;
   }
   return e == hipSuccess ? DLFP_OK : DLFP_EHIP;
 }

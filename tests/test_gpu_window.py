@@ -77,3 +77,25 @@ def test_mixed(dev, ws, case, kv8):
         for tn in (None, D.dlfp_tuning(32, 64), D.dlfp_tuning(0, 0, 0, 1, 1)):
             m.check(m.run(ws, dtype, SCALE, tn), SCALE)
     assert D.dlfp_workspace_error(ws.buf) == 0
+
+
+# Decode units of a wavefront each: many short ones, alone and beside a prompt, whole
+# and split, in numbers that leave the last workgroup with one, two and three.
+SHORT = [
+    (8, 1, [1] * 37 + [400], [1 + 5 * i % 6 for i in range(37)] + [1200], None, 0, None),
+    (16, 2, [1] * 61 + [800], [1 + 37 * i % 200 for i in range(61)] + [2200], None, 0, 64),
+    (4, 2, [800] + [1] * 43, [2200] + [3 + 37 * i % 190 for i in range(43)], 150, 20, 64),
+    (16, 2, [1] * 389, [1 + 31 * i % 97 for i in range(389)], None, 0, 64),
+    (4, 2, [1] * 391, [1 + 31 * i % 211 for i in range(391)], 90, 20, 64),
+]
+
+
+@pytest.mark.parametrize("kv8", [False, True])
+@pytest.mark.parametrize("case", range(len(SHORT)))
+def test_short_decoders(dev, ws, case, kv8):
+    hq, hkv, q_len, kv_len, window, sinks, split = SHORT[case]
+    m = Mix(dev, hq, hkv, q_len, kv_len, window, sinks, kv8, seed=case)
+    for dtype in (BF16, FP32):
+        for tn in (None, D.dlfp_tuning(split or 0)):
+            m.check(m.run(ws, dtype, SCALE, tn), SCALE, rows=[0, 399, 795, 799])
+    assert D.dlfp_workspace_error(ws.buf) == 0
