@@ -187,6 +187,16 @@ def _bind_current_handle():
     return handle
 
 
+_current_device = None
+
+
+def _bind_current_device():
+    global _current_device
+    import torch
+    _current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
+    return _current_device
+
+
 def _stream(stream) -> int:
     if stream is None:
         return _current_handle() if _current_handle is not None else _bind_current_handle()
@@ -346,6 +356,8 @@ def _rows(t, shape) -> int:
     are contiguous."""
     if t.shape != shape or t.element_size() != 2:
         raise ValueError("queries, keys and values must be bf16 [tokens][heads][128]")
+    if t.is_contiguous():
+        return shape[1] * HEAD_DIM
     token, head, dim = t.stride()
     if dim != 1 or (head != HEAD_DIM and shape[1] > 1):
         raise ValueError("a token's heads must be contiguous")
@@ -360,14 +372,17 @@ def make_rope(table, interleaved: bool = False) -> dlfp_rope:
 
 
 def _on_one_device(*tensors) -> None:
-    """Refuses tensors on the host or on different devices, whose addresses a kernel would
-    follow all the same."""
+    """Refuses tensors on the host, on different devices or on one that is not the current
+    one, whose addresses a kernel would follow all the same."""
     device = tensors[0].get_device()
     for t in tensors:
         if t.get_device() != device:
             raise ValueError("tensors are on different devices")
-    if device < 0 and tensors[0].numel():
-        raise ValueError("tensors must be on a device")
+    if device < 0:
+        if tensors[0].numel():
+            raise ValueError("tensors must be on a device")
+    elif device != (_current_device or _bind_current_device())():
+        raise ValueError("tensors must be on the current device")
 
 
 def _append_args(dims, rope, positions, slot_mapping, q, k_new, v_new, q_out, k_cache, v_cache):
@@ -376,7 +391,7 @@ def _append_args(dims, rope, positions, slot_mapping, q, k_new, v_new, q_out, k_
         raise ValueError("shapes disagree")
     if positions.element_size() != 4 or slot_mapping.element_size() != 4:
         raise ValueError("positions and slots must be int32")
-    if n > 1 and (positions.stride(0) != 1 or slot_mapping.stride(0) != 1):
+    if not (positions.is_contiguous() and slot_mapping.is_contiguous()):
         raise ValueError("positions and slots must be contiguous")
     _on_one_device(q, positions, slot_mapping, k_new, v_new, q_out, k_cache, v_cache)
     qs, ks = (n, dims.num_q_heads, HEAD_DIM), (n, dims.num_kv_heads, HEAD_DIM)

@@ -270,3 +270,16 @@ def test_replay(dev, bits, window, rotary):
     assert all(0.0 < it["layer_ms"] < 50.0 for it in trace)
     assert torch.isfinite(ex.out[:4].float()).all()
     assert D.dlfp_workspace_error(ex.ws.buf) == 0
+
+
+def test_tensors_of_another_device_than_the_current_one(dev, ws, monkeypatch):
+    m = Mix(dev, 4, 2, [1], [20], None, 0, False)
+    batch, out = m.batch(), torch.empty(m.dq.shape, dtype=torch.bfloat16, device=dev)
+    rope = rt.Rope(32, dev)
+    at = torch.zeros(1, dtype=torch.int32, device=dev)
+    k = torch.zeros(1, 2, 128, dtype=torch.bfloat16, device=dev)
+    monkeypatch.setattr(D, "_current_device", lambda: dev.index + 1)
+    with pytest.raises(ValueError, match="current device"):
+        batch.attention(m.pool, m.dq, SCALE, out, ws)
+    with pytest.raises(ValueError, match="current device"):
+        rt.rope_append(m.dims, rope, m.pool, at, at, m.dq, k, k, torch.empty_like(m.dq))
