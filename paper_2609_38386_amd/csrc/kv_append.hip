@@ -23,7 +23,10 @@
 //
 // With ROPE the same kernel turns the keys to their positions on the way (the
 // angles cost a round trip more, after the positions), and workgroups behind
-// those of the KV heads turn the queries.
+// those of the KV heads turn the queries.  With 64 and 8 heads: up to 64 decoders
+// 4.1 to 5.6 us, 256 7.7, a chunk of 2048 tokens 18.0 us (85 MB, 4.7 TB/s, the rate
+// of a copy) and of 8192 69 (340 MB, 4.9 TB/s); 2048 decoders 49, twice their bytes'
+// time: each of their values is a 2-byte store.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>

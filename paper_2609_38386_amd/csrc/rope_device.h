@@ -99,7 +99,9 @@ struct QueryArgs {
 
 // Turns QUERY_HEADS heads of one token by one wavefront: four heads at a time, 16
 // lanes a head, every load issued before the angles' (whose address waits for
-// the position).  item: token * chunks + chunk of its heads.
+// the position): an append of 2048 tokens, 16 and 8 heads, 11.5 us, 27.3 with
+// eight tokens of a wavefront one after the other.  item: token * chunks + chunk of
+// its heads.
 constexpr int QUERY_HEADS = 16;
 inline int query_chunks(int hq) { return (hq + QUERY_HEADS - 1) / QUERY_HEADS; }
 __device__ __forceinline__ void rotate_queries(const QueryArgs& a, const RopeArgs& r,

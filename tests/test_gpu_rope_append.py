@@ -287,3 +287,22 @@ def test_no_tokens(dev, kv8):
     at = torch.empty(0, dtype=torch.int32, device=dev)
     rt.rope_append(D.make_dims(16, 8), rt.Rope(4, dev), pool, at, at, none, none[:, :8],
                    none[:, :8], none)
+
+
+LONG = [
+    [(1, 1 + 7 * i % 50) for i in range(521)] + [(90, 300)],
+    [(517, 1003)] + [(1, 1 + 5 * i % 40) for i in range(19)] + [(3, 33), (20, 30)],
+    [(1100, 1100)], [(2, 2 + 5 * i % 40) for i in range(300)],
+]
+
+
+@pytest.mark.parametrize("kv8", [False, True])
+@pytest.mark.parametrize("left_out", [False, True])
+@pytest.mark.parametrize("seqs", range(len(LONG)))
+def test_many_tokens(dev, seqs, left_out, kv8):
+    """More tokens than the launches for few take; with slots outside the pool, the runs of
+    a page that a token left out makes two of."""
+    a = Append(dev, 4, 2, LONG[seqs], seed=seqs)
+    if left_out:
+        a.slots[np.arange(5, a.n, 37)] = -1
+    _run(a, kv8)
