@@ -10,15 +10,19 @@
 // [KVBEGIN, KVEND) of them whatever the mask, and a unit's table of block ids in
 // LDS lists its pages in that order; only masks go back to positions.
 //
-// 8-bit pages: with a power of two as a page's scale, v_cvt_scalef32_pk_bf16_fp8
-// turns two codes into the two bf16 numbers that they stand for, so that from the
-// operands on both kinds are the same kernel.  The pages travel to LDS as they
-// are stored, by direct copies, half the bytes; operands are converted as they
-// are read, 16 codes (one 16-byte LDS read) into two operands of eight.  Which
-// dims and keys a lane's eight are is free as long as both factors of a product
-// agree, so a lane takes 16 codes that are next to each other: of a key row, dims
-// 32 j + 16 hi .. + 15 (of 32 x 32 products; of 16 x 16 ones 64 j + 16 q ..); of a
-// value row, all 16 slots of one page.
+// 8-bit pages travel to LDS as they are stored, by direct copies, half the bytes.
+// With a power of two as a page's scale, v_cvt_scalef32_pk_bf16_fp8 turns two codes
+// into the two bf16 numbers that they stand for, so that values, and with fp32
+// output keys, are operands of the same bf16 products from there on: 16 codes (one
+// 16-byte LDS read) make two operands of eight.  Which dims and keys a lane's eight
+// are is free as long as both factors of a product agree, so a lane takes 16 codes
+// that are next to each other: of a key row, dims 32 j + 16 hi .. + 15 (of 32 x 32
+// products; of 16 x 16 ones 64 j + 16 q ..); of a value row, all 16 slots of one page.
+// With bf16 output keys are not converted: a query is a sum of two rows of codes, and
+// scores are products of codes with the pages' exponents as their block scales, twice
+// the bf16 rate for twice the products, without the conversions (prompts of 1999
+// tokens over 8144 keys 445 -> 396 us); a decoder's values are not either, its
+// probabilities being two rows of codes.
 //
 // Everything else is as in attention_mixed.hip: S^T = K Q^T and O^T += V^T P^T
 // with row statistics in a lane, a lazily raised reference maximum in the exp2
@@ -268,6 +272,16 @@ constexpr int window_lds() {
   return pre > dec ? pre : dec;
 }
 
+// Unit of a tile of 128 query rows (128 / G tokens of G heads): 32 rows a wavefront,
+// their keys in tiles of 64 through two slots of LDS that the four share, each key and
+// value read from memory once for 128 rows.  32x32 products: the scores of a row are in
+// two lanes, so its maximum and sum take one exchange.  Bound by the matrix products
+// and the exponentials between them at the clock that their power allows: 4096 tokens
+// of 64 heads in a window of 4000 keys, bf16 pages, 538 GFLOP in 495 to 517 us (1.04 to
+// 1.09 PFLOP/s; a library product of 8192^3 1.23); 2 x 1999 tokens of 32 heads over
+// 8144 keys, 8-bit pages, 457 GFLOP in 395 to 421 us (1.09 to 1.16).  fp32 output has
+// three products for one with the values: 1450 tokens of 16 heads over 8533 keys 175 us,
+// with bf16 output 118.
 template <int G, bool KV8, bool OUT32>
 __device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, char* smem, int* flag) {
   using L = PreLds<KV8>;
@@ -766,7 +780,11 @@ __device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, ch
 // split the keys instead: wavefront w takes blocks w, w + 4, ... of the unit, each
 // through a key slot and a value slot of its own, without a barrier until the
 // four results are added through LDS.  Block and slots as a decode unit's (32 keys
-// of bf16 pages, 64 of 8-bit ones), products, masks and layouts as a tile's.
+// of bf16 pages, 64 of 8-bit ones), products, masks and layouts as a tile's.  Bound by
+// a wavefront's chain of steps: a quarter of the keys each, where a tile of as many
+// rows has one wavefront for all.  64 tokens of 16 heads over 264 keys 8.7 us, as a
+// tile 12.2; 256 over 1256 15.4 and 20.1; 2048 over 4048, where the rows fill the
+// chip, 86 and 68, each key being read four times as often.
 template <int G, bool KV8, bool OUT32>
 __device__ __forceinline__ void small_unit(const Args& a, const record_t f, char* smem, int* flag) {
   constexpr int PB = page_bytes<KV8>();
@@ -1119,7 +1137,10 @@ __device__ __forceinline__ void small_unit(const Args& a, const record_t f, char
 // The unit's g heads are columns 0-7 of 16x16 products and, with the second term
 // of the probabilities, columns 8-15.  Lane l owns column l % 16; its group
 // q = l / 16 owns, of 8-bit pages, the 16 keys of page q of the block, of bf16
-// pages the eight at positions 8 (q / 2) .. of page q % 2.
+// pages the eight at positions 8 (q / 2) .. of page q % 2.  Every key and value is
+// read once, straight to LDS, for its g heads, and bounds the unit: 256 decoders of a
+// 4096-key window, bf16 pages, 4.24 GB in 665 us (6.4 TB/s), 128 of 1024 to 8192 keys,
+// 8-bit pages, 1.21 GB in 194 us (6.2 TB/s).
 template <int G, bool KV8, bool OUT32, int NW>
 __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, char* smem, int* flag) {
   static_assert(G >= 1 && G <= 8, "heads");
