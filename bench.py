@@ -292,7 +292,8 @@ TRAFFIC_PROFILE = os.path.join(ROOT, "profiles", "attention_mixed_qwen3-32b_swee
 # work-list policy that shapes it, and the headers they share.
 KERNEL_SOURCES = ("paper_2609_38386_amd/csrc/attention_mixed.hip",
                   "paper_2609_38386_amd/csrc/dlfp_host.cpp", "include/dlfp.h",
-                  "paper_2609_38386_amd/csrc/dlfp_internal.h")
+                  "paper_2609_38386_amd/csrc/dlfp_internal.h",
+                  "paper_2609_38386_amd/csrc/attention_device.h")
 
 
 def source_hash():
