@@ -1369,8 +1369,10 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
 #pragma unroll
     for (int x = 0; x < 4 * NCH; ++x) mx = fmaxf(mx, sc[x]);
     // Products of codes take a probability times its page's value scale (relative
-    // to the largest), so the reference maximum is that of both.
-    const int dv = CODES ? (etab[BP * i + vpage] >> 8) - v_ref : 0;
+    // to the largest), so the reference maximum is that of both.  A page counts as at
+    // most 2^96 below the largest (its values are then 2^-87 of the largest's or less),
+    // which keeps the sum of 2^-dv times the probabilities in range.
+    const int dv = CODES ? max((etab[BP * i + vpage] >> 8) - v_ref, -96) : 0;
     const float m_tile = max_xor32(max_xor16(__builtin_fmaf(mx, c, (float)dv)));
     if (__builtin_amdgcn_ballot_w64(m_tile > m_run + RESCALE_LOG2)) {
       const float m_new = m_tile > m_run + RESCALE_LOG2 ? m_tile : m_run;

@@ -114,11 +114,17 @@ class Rope:
         return rope
 
 
+def _check_heads(dims: _d.dlfp_dims, pool):
+    if pool.num_kv_heads != dims.num_kv_heads:
+        raise ValueError("the pool has other KV heads than the dims")
+
+
 def rope_append(dims: _d.dlfp_dims, rope: Rope, pool, positions: torch.Tensor,
                 slots: torch.Tensor, q: torch.Tensor, k_new: torch.Tensor, v_new: torch.Tensor,
                 q_out: torch.Tensor, stream=None):
     """Rotate queries and keys to their positions and write keys and values into the pages
     of a KVPool or KVPool8."""
+    _check_heads(dims, pool)
     if isinstance(pool, KVPool8):
         _d.dlfp_rope_append_kv8(dims, rope.c, positions, slots, q, k_new, v_new, q_out, pool.k,
                                 pool.v, pool.k_exp, pool.v_exp, stream)
@@ -191,6 +197,7 @@ def window_attention(dims: _d.dlfp_dims, meta: _d.Meta, d_work: torch.Tensor,
                      d_block_table: torch.Tensor, pool, q: torch.Tensor, scale: float,
                      out: torch.Tensor, workspace: torch.Tensor, stream=None):
     """Attention over the pages of a KVPool or KVPool8, metadata of dlfp_build_window_meta."""
+    _check_heads(dims, pool)
     if isinstance(pool, KVPool8):
         _d.dlfp_attention_kv8(dims, meta, d_work, d_block_table, q, pool.k, pool.v, pool.k_exp,
                               pool.v_exp, scale, out, workspace, stream)
@@ -307,15 +314,17 @@ class StagedBatch:
     single stream-ordered transfer.  Reuse requires the previous iteration's copy
     to have completed (callers synchronise on iteration completion anyway)."""
 
+    token_ints = 1   # of a token in the buffer
+    pieces = ()      # further int32 arrays that go along, after the slots and records
+
     def __init__(self, dims: _d.dlfp_dims, cap_seqs: int, cap_tokens: int, cap_work: int, device,
                  tuning: Optional[_d.dlfp_tuning] = None):
         import ctypes
         self._ct = ctypes
-        self.pieces = ()   # further int32 arrays that go along, after the slots and records
         self.dims = dims
         self.tuning = tuning if tuning is not None else _d.dlfp_tuning(0, 0, 0)
         self.meta = _d.Meta(cap_seqs, cap_tokens, cap_work)
-        total = cap_tokens + cap_work * _d.WORK_INTS
+        total = self.token_ints * cap_tokens + cap_work * _d.WORK_INTS
         self.host = torch.empty(total, dtype=torch.int32, pin_memory=True)
         self.host_np = self.host.numpy()
         self.dev = torch.empty(total, dtype=torch.int32, device=device)
@@ -356,12 +365,14 @@ class WindowStagedBatch(StagedBatch):
     dlfp_build_window_meta, and the new tokens' positions.  ``window`` None: every key up
     to a row's own."""
 
+    token_ints = 2   # its slot and its position
+
     def __init__(self, dims: _d.dlfp_dims, cap_seqs: int, cap_tokens: int, cap_work: int, device,
                  window: Optional[int] = None, sinks: int = 0,
                  tuning: Optional[_d.dlfp_tuning] = None):
         if window is None and sinks:
             raise ValueError("sinks need a window")
-        super().__init__(dims, cap_seqs, 2 * cap_tokens, cap_work, device, tuning)
+        super().__init__(dims, cap_seqs, cap_tokens, cap_work, device, tuning)
         self.window = _d.dlfp_window(window, sinks) if window is not None else None
 
     def _build(self, ct, m, q_len, kv_len, block_table, num_blocks):

@@ -21,7 +21,7 @@ def bf16(x):
 
 class Mix:
     def __init__(self, dev, hq, hkv, q_len, kv_len, window, sinks, kv8, seed=0, spread=1.0,
-                 spare=3, first_block=0):
+                 spare=3, first_block=0, v_exps=None):
         rng = np.random.default_rng(seed)
         self.hq, self.hkv, self.window, self.sinks, self.kv8 = hq, hkv, window, sinks, kv8
         self.q_len, self.kv_len = list(q_len), list(kv_len)
@@ -47,6 +47,9 @@ class Mix:
                 data = rng.normal(size=(kl, hkv, 128))
                 if kv8:
                     e = rng.integers(-9, -4, size=(pages[s], hkv))
+                    if name == "v" and v_exps:   # pages of far scales, all of them full
+                        e = rng.choice(v_exps, size=(pages[s], hkv))
+                        data *= np.repeat(2.0 ** (e + 7), 16, 0)[:kl, :, None]
                     scale = np.repeat(2.0 ** e, 16, 0)[:kl, :, None]
                     codes = ow.e4m3_encode(np.clip(data / scale, -448, 448))
                     data = ow.E4M3[codes] * scale
@@ -78,7 +81,8 @@ class Mix:
             if kv8:
                 ke, ve = far(ke), far(ve)
             self.table[self.table >= 0] += first_block
-        self.blocks, self.v_exp = first_block + blocks, -5   # the largest exponent drawn
+        self.blocks = first_block + blocks
+        self.v_exp = max(v_exps) if v_exps else -5   # the largest exponent drawn
         self.pool = rt.KVPool8.of(k, v, ke, ve) if kv8 else rt.KVPool.of(k, v)
         self.dq = bf16(np.concatenate(self.q)).to(dev)
         self.dev = dev
@@ -109,6 +113,12 @@ class Mix:
         it (two cut to 8 bits, the third rounded to 8: 2^-7 2^-7 2^-8), four such; the
         exponentials of the wavefronts' and splits' maxima, their sums, the division and
         the product with it, up to 12 more.
+
+        Weights are 32-bit numbers: an exponential below 2^-126 is 0, of the weight itself or
+        of a wavefront's or split's maximum against the others'.  A reference is at most 2^8
+        below its maximum, so weights up to 2^-118 of the row's largest may be lost, and of
+        three terms each another 2^-126: n 2^-117 of the largest weight times the largest
+        value in all.
 
         8-bit pages with bf16 output: a product of codes adds its 64 or 128 terms to
         within 2^-15 of sum |q k| (2^-15.9 measured over random rows).  A decoder's
@@ -148,7 +158,8 @@ class Mix:
                                 least = 2.0 ** -15 * len(vv) * w.max(1, keepdims=True) * \
                                     448 * 2.0 ** self.v_exp
                     sums = (len(vv) / 16 + 16) * 2.0 ** -24 * (w @ np.abs(vv))
-                    tol = least + half * np.abs(o) + 2 * d / (1 - d) * spread + sums + 1e-30
+                    lost = len(vv) * 2.0 ** -117 * w.max(1, keepdims=True) * np.abs(vv).max()
+                    tol = least + half * np.abs(o) + 2 * d / (1 - d) * spread + sums + lost + 1e-30
                     err = np.abs(got[at + r, hs] - o)
                     assert (err <= tol).all(), (s, r, h, float((err / tol).max()))
             at += ql

@@ -283,3 +283,37 @@ def test_tensors_of_another_device_than_the_current_one(dev, ws, monkeypatch):
         batch.attention(m.pool, m.dq, SCALE, out, ws)
     with pytest.raises(ValueError, match="current device"):
         rt.rope_append(m.dims, rope, m.pool, at, at, m.dq, k, k, torch.empty_like(m.dq))
+
+
+@pytest.mark.parametrize("window,sinks", [(None, 0), (300, 20)])
+def test_value_pages_of_far_scales(dev, ws, window, sinks):
+    """Value scales up to 2^140 apart beside scores that leave either kind of page all of
+    a row's weight."""
+    m = Mix(dev, 16, 2, [1, 1, 1, 9], [1000, 700, 333, 200], window, sinks, True, seed=6,
+            spread=60.0, v_exps=[-100, -40, 40])
+    for dtype in (torch.bfloat16, torch.float32):
+        for tn in (None, D.dlfp_tuning(64)):
+            m.check(m.run(ws, dtype, SCALE, tn), SCALE)
+
+
+def test_pool_of_other_heads(dev, ws):
+    m = Mix(dev, 4, 2, [1], [20], None, 0, False)
+    pool = rt.KVPool(4, 1, dev)
+    with pytest.raises(ValueError, match="heads"):
+        m.batch().attention(pool, m.dq, SCALE, torch.empty_like(m.dq), ws)
+    at = torch.zeros(1, dtype=torch.int32, device=dev)
+    k = torch.zeros(1, 2, 128, dtype=torch.bfloat16, device=dev)
+    with pytest.raises(ValueError, match="heads"):
+        rt.rope_append(m.dims, rt.Rope(4, dev), pool, at, at, m.dq, k, k, torch.empty_like(m.dq))
+
+
+def test_staged_batch_over_its_capacity(dev):
+    stage = rt.WindowStagedBatch(D.make_dims(4, 2), 2, 8, 64, dev, 16, 2)
+    table = np.arange(4, dtype=np.int32).reshape(2, 2)
+    lens = [np.array(x, np.int32) for x in ([7, 2], [7, 20])]
+    with pytest.raises(D.DlfpError):
+        stage.build(*lens, table, 4)
+    stage.build(np.array([6, 2], np.int32), np.array([7, 20], np.int32), table, 4)
+    torch.cuda.synchronize()
+    assert stage.d_positions.tolist() == [1, 2, 3, 4, 5, 6, 18, 19]
+    assert stage.d_slots.tolist() == [1, 2, 3, 4, 5, 6, 50, 51]
