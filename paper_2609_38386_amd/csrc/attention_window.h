@@ -1723,10 +1723,11 @@ int attention_window(const dlfp_dims* dims, const dlfp_meta* meta, const int32_t
   const int cus = dlfp::compute_units();
   const int decode_units = a.num_units - a.num_prefill;
   // Decode units of a wavefront each spend no workgroup on their start and sum, but
-  // last four times as long: 29 ns a key of bf16 pages, 25 of 8-bit ones.  Alone they
-  // are those of up to 128 KiB of cache that are more than three for each compute
-  // unit (2048 units of 64 keys, 8-bit pages: 10.2 us, of four wavefronts 20.9; of 512
-  // keys 45.9 and 48.8; bf16, 128 keys: 23.9 and 27.2).  Beside prefill units, those
+  // last four times as long: 29 ns a key of bf16 pages, 25 of 8-bit ones.  They are
+  // those of up to 128 KiB of cache that are more than two for each compute unit, a
+  // further round of workgroups (8-bit pages: 640 units of 64 keys 6.9 us, of four
+  // wavefronts 11.1, 2048 10.2 and 20.9, 2048 of 512 keys 45.7 and 49.6; bf16: 640 of
+  // 256 keys 15.4 and 16.4, 2048 of 128 23.9 and 27.2), and, beside prefill units, those
   // that last up to a quarter of the launch, by its operations at 1120 TFLOP/s and
   // its bytes at 6.4 TB/s: 8-bit pages, 500 decoders of 64 keys beside 512 tokens
   // 33.4 us, of four wavefronts 59.4, of 256 keys 63.5 and 79.5; 70 of 500 keys,
@@ -1736,8 +1737,8 @@ int attention_window(const dlfp_dims* dims, const dlfp_meta* meta, const int32_t
   const double prefill_us = 0.75 * a.num_prefill * meta->prefill_split_tokens * tile_key_us;
   const double decode_us = 0.75 * decode_units * (double)meta->decode_split_tokens * key_us;
   const int64_t unit_bytes = (int64_t)meta->decode_split_tokens * 2 * DLFP_HEAD_DIM * (KV8 ? 1 : 2);
-  a.solo = a.num_prefill ? 4. * unit_us <= prefill_us + decode_us
-                         : decode_units > 3 * cus && unit_bytes <= 128 << 10;
+  a.solo = (decode_units > 2 * cus && unit_bytes <= 128 << 10) ||
+           (a.num_prefill > 0 && 4. * unit_us <= prefill_us + decode_us);
   const int decode_wgs = a.solo ? (decode_units + 3) / 4 : decode_units;
   // One prefill unit for each compute unit, then one decode unit for each, so that
   // both shares run from the start (beside each other each runs at 0.62 of its
