@@ -386,8 +386,8 @@ def _on_one_device(*tensors) -> None:
 
 
 def _append_args(dims, rope, positions, slot_mapping, q, k_new, v_new, q_out, k_cache, v_cache):
-    n = slot_mapping.size(0)
-    if positions.size(0) != n:
+    n = slot_mapping.numel()
+    if positions.numel() != n:
         raise ValueError("shapes disagree")
     if positions.element_size() != 4 or slot_mapping.element_size() != 4:
         raise ValueError("positions and slots must be int32")
