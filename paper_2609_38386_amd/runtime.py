@@ -57,7 +57,7 @@ class KVPool:
 def _are_pages(k: torch.Tensor, v: torch.Tensor) -> bool:
     return (k.dim() == 4 and tuple(k.shape[2:]) == (_d.PAGE_SIZE, _d.HEAD_DIM) and
             tuple(v.shape) == (*k.shape[:2], _d.HEAD_DIM, _d.PAGE_SIZE) and
-            k.is_contiguous() and v.is_contiguous())
+            k.is_contiguous() and v.is_contiguous() and k.device == v.device)
 
 
 class KVPool8:
@@ -84,8 +84,9 @@ class KVPool8:
         if k.element_size() != 1 or v.element_size() != 1 or not _are_pages(k, v):
             raise ValueError("caches must be contiguous pages of one byte a value")
         for e in (k_exp, v_exp):
-            if e.dtype != torch.uint8 or e.shape != k.shape[:2] or not e.is_contiguous():
-                raise ValueError("exponents must be uint8 [num_blocks][Hkv]")
+            if (e.dtype != torch.uint8 or e.shape != k.shape[:2] or not e.is_contiguous() or
+                    e.device != k.device):
+                raise ValueError("exponents must be uint8 [num_blocks][Hkv] beside the caches")
         pool = cls.__new__(cls)
         pool._set(k, v, k_exp, v_exp)
         return pool
@@ -125,6 +126,8 @@ def rope_append(dims: _d.dlfp_dims, rope: Rope, pool, positions: torch.Tensor,
     """Rotate queries and keys to their positions and write keys and values into the pages
     of a KVPool or KVPool8."""
     _check_heads(dims, pool)
+    if rope.table.get_device() != q.get_device():
+        raise ValueError("the rope's table is on another device")
     if isinstance(pool, KVPool8):
         _d.dlfp_rope_append_kv8(dims, rope.c, positions, slots, q, k_new, v_new, q_out, pool.k,
                                 pool.v, pool.k_exp, pool.v_exp, stream)

@@ -317,3 +317,17 @@ def test_staged_batch_over_its_capacity(dev):
     torch.cuda.synchronize()
     assert stage.d_positions.tolist() == [1, 2, 3, 4, 5, 6, 18, 19]
     assert stage.d_slots.tolist() == [1, 2, 3, 4, 5, 6, 50, 51]
+
+
+def test_parts_on_the_host(dev):
+    """A rope or a pool of which a part is on the host is refused."""
+    dims, at = D.make_dims(4, 2), torch.zeros(1, dtype=torch.int32, device=dev)
+    k = torch.zeros(1, 2, 128, dtype=torch.bfloat16, device=dev)
+    q = torch.zeros(1, 4, 128, dtype=torch.bfloat16, device=dev)
+    pool = rt.KVPool8(2, 2, dev)
+    with pytest.raises(ValueError, match="another device"):
+        rt.rope_append(dims, rt.Rope.of(torch.zeros(4, 128)), pool, at, at, q, k, k, q.clone())
+    with pytest.raises(ValueError):
+        rt.KVPool8.of(pool.k, pool.v.cpu(), pool.k_exp, pool.v_exp)
+    with pytest.raises(ValueError):
+        rt.KVPool8.of(pool.k, pool.v, pool.k_exp.cpu(), pool.v_exp)
