@@ -371,15 +371,13 @@ def make_rope(table, interleaved: bool = False) -> dlfp_rope:
     return dlfp_rope(table.data_ptr(), table.size(0), table.size(1), 1 if interleaved else 0)
 
 
-def _on_one_device(*tensors) -> None:
+def _check_device(same: bool, device: int, tokens: int) -> None:
     """Refuses tensors on the host, on different devices or on one that is not the current
     one, whose addresses a kernel would follow all the same."""
-    device = tensors[0].get_device()
-    for t in tensors:
-        if t.get_device() != device:
-            raise ValueError("tensors are on different devices")
+    if not same:
+        raise ValueError("tensors are on different devices")
     if device < 0:
-        if tensors[0].numel():
+        if tokens:
             raise ValueError("tensors must be on a device")
     elif device != (_current_device or _bind_current_device())():
         raise ValueError("tensors must be on the current device")
@@ -393,7 +391,10 @@ def _append_args(dims, rope, positions, slot_mapping, q, k_new, v_new, q_out, k_
         raise ValueError("positions and slots must be int32")
     if not (positions.is_contiguous() and slot_mapping.is_contiguous()):
         raise ValueError("positions and slots must be contiguous")
-    _on_one_device(q, positions, slot_mapping, k_new, v_new, q_out, k_cache, v_cache)
+    device = q.get_device()
+    _check_device(device == positions.get_device() == slot_mapping.get_device() ==
+                  k_new.get_device() == v_new.get_device() == q_out.get_device() ==
+                  k_cache.get_device() == v_cache.get_device(), device, n)
     qs, ks = (n, dims.num_q_heads, HEAD_DIM), (n, dims.num_kv_heads, HEAD_DIM)
     return (dims, rope, n, positions.data_ptr(), slot_mapping.data_ptr(), q.data_ptr(),
             _rows(q, qs), k_new.data_ptr(), _rows(k_new, ks), v_new.data_ptr(), _rows(v_new, ks),
@@ -428,7 +429,10 @@ def _check_attention(dims, meta, d_work, d_block_table, q, k_cache, v_cache, out
         raise ValueError("q and out must be [tokens][Hq][128], q bf16")
     if not (q.is_contiguous() and out.is_contiguous() and d_block_table.is_contiguous()):
         raise ValueError("q, out and the block table must be contiguous")
-    _on_one_device(q, d_work, d_block_table, k_cache, v_cache, out, workspace)
+    device = q.get_device()
+    _check_device(device == d_work.get_device() == d_block_table.get_device() ==
+                  k_cache.get_device() == v_cache.get_device() == out.get_device() ==
+                  workspace.get_device(), device, shape[0])
 
 
 def dlfp_attention_window(dims: dlfp_dims, meta: Meta, d_work, d_block_table, q, k_cache, v_cache,
