@@ -1729,16 +1729,21 @@ int attention_window(const dlfp_dims* dims, const dlfp_meta* meta, const int32_t
   // wavefronts 11.1, 2048 10.2 and 20.9, 2048 of 512 keys 45.7 and 49.6; bf16: 640 of
   // 256 keys 15.4 and 16.4, 2048 of 128 23.9 and 27.2), and, beside prefill units, those
   // that last up to a quarter of the launch, by its operations at 1120 TFLOP/s and
-  // its bytes at 6.4 TB/s: 8-bit pages, 500 decoders of 64 keys beside 512 tokens
-  // 33.4 us, of four wavefronts 59.4, of 256 keys 63.5 and 79.5; 70 of 500 keys,
-  // which last longer, 33.3 and 28.9.
+  // its bytes at 6.4 TB/s, or 0.45 of it where the prompts are a third of it or more
+  // and hide the last of them, and every compute unit gets some: 8-bit pages, 500 decoders of 64 keys beside 512 tokens
+  // 33.4 us, of four wavefronts 59.4, of 256 keys 63.5 and 79.5; 128 windowed ones of
+  // 2048 keys beside 1999 tokens 128 and 138, of 1024 to 8192 keys 384 and 427 (bf16
+  // 188 and 200, 522 and 522); 70 of 500 keys beside 512 tokens, which last longer,
+  // 33.3 and 28.9, 32 of 2000 beside 1024 76 and 58; bf16, 16 of 9 to 37 thousand in
+  // 792 units beside 328 396 and 357.
   const double key_us = (KV8 ? 256 : 512) / 6.4e6, tile_key_us = 128 * 512 / 1120e6;
   const double unit_us = meta->decode_split_tokens * (KV8 ? 25e-3 : 29e-3);
-  const double prefill_us = 0.75 * a.num_prefill * meta->prefill_split_tokens * tile_key_us;
-  const double decode_us = 0.75 * decode_units * (double)meta->decode_split_tokens * key_us;
+  const double prefill_us = 0.85 * a.num_prefill * meta->prefill_split_tokens * tile_key_us;
+  const double decode_us = 0.85 * decode_units * (double)meta->decode_split_tokens * key_us;
   const int64_t unit_bytes = (int64_t)meta->decode_split_tokens * 2 * DLFP_HEAD_DIM * (KV8 ? 1 : 2);
+  const bool hidden = 2. * prefill_us >= decode_us && decode_units >= 4 * cus;
   a.solo = (decode_units > 2 * cus && unit_bytes <= 128 << 10) ||
-           (a.num_prefill > 0 && 4. * unit_us <= prefill_us + decode_us);
+           (a.num_prefill > 0 && unit_us <= (prefill_us + decode_us) * (hidden ? 0.45 : 0.25));
   const int decode_wgs = a.solo ? (decode_units + 3) / 4 : decode_units;
   // One prefill unit for each compute unit, then one decode unit for each, so that
   // both shares run from the start (beside each other each runs at 0.62 of its
