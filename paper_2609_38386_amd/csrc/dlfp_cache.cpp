@@ -211,24 +211,27 @@ int build(const dlfp_dims* dims, const dlfp_tuning* tuning, const dlfp_window* w
   // keys over the wavefronts, and a number of equal parts, by an estimate of the
   // prefill share's time in us.  A unit of 128 rows takes 22.7 ns a key with a
   // compute unit to itself and 30.5 beside another one, one of 32 rows 9.2 and 13.5;
-  // its start and end 4.5 and 8, 5 and 6; a further round 6 and 4, and 2 more for
-  // the partial results; a merge 5 and 3, and 0.9 and 0.4 for each part.  The units
-  // of a decode share have a slot each, up to one on every compute unit, for 6 us and
-  // 16 ns a key, and prefill units that find none left wait so long.  (Tiles of 128 and of 32 rows, 8 KV heads, bf16 pages: 64 tokens
-  // of 16 heads over 264 keys 12.2 and 8.7 us, 1024 over 2024 33.6 and 27.3, 2048 over
-  // 4048 68 and 86; of 64 heads, 256 over 1256 25.7 and 21.3, 1024 over 2024 64 and 93.)
+  // its start and end 4.5 and 8, 5 and 6; a further round 6 and 4, with partial
+  // results 7 and 2 more; a merge 5 and 3, and 0.9 and 0.4 for each part, twice that
+  // where a decode share leaves few slots.  The units of a decode share have a slot
+  // each, up to one on every compute unit, for 6 us and 16 ns a key, and prefill units
+  // that find none left wait so long.  (Tiles of 128 and of 32 rows, 8 KV heads, bf16
+  // pages: 64 tokens of 16 heads over 264 keys 12.2 and 8.7 us, 1024 over 2024 33.6 and
+  // 27.3, 2048 over 4048 68 and 86; of 64 heads, 256 over 1256 25.7 and 21.3, 1024 over
+  // 2024 64 and 93.  Whole and in two parts: 2 x 1365 tokens of 32 heads over windows
+  // of 1870 keys 115 and 144.)
   int64_t split_p = tn.prefill_split_tokens, tile_tokens = tn.prefill_tile_tokens;
   if (!prompts.empty()) {
     struct Height {
       int64_t rows;
-      double alone, beside, start, start2, round, merge, part;
+      double alone, beside, start, start2, round, merge, part, partial;
     };
-    constexpr Height heights[] = {{DLFP_TILE_ROWS, 22.7e-3, 30.5e-3, 4.5, 8., 6., 5., 0.9},
-                                  {DLFP_SMALL_ROWS, 9.2e-3, 13.5e-3, 5., 6., 4., 3., 0.4}};
+    constexpr Height heights[] = {{DLFP_TILE_ROWS, 22.7e-3, 30.5e-3, 4.5, 8., 6., 5., 0.9, 7.},
+                                  {DLFP_SMALL_ROWS, 9.2e-3, 13.5e-3, 5., 6., 4., 3., 0.4, 2.}};
     const int64_t fixed_tile = tile_tokens, fixed_split = split_p;
     const Cut d = cuts(ones, split_d);
     const int64_t taken = std::min(d.units, cus);
-    const double held = (6. + 16e-3 * d.longest) * ceil_div(d.units, cus);
+    const double held = taken ? 6. * ceil_div(d.units, cus) + 16e-3 * d.keys / taken : 0.;
     double best = 0.;
     bool found = false;
     for (const Height& h : heights) {
@@ -247,11 +250,14 @@ int build(const dlfp_dims* dims, const dlfp_tuning* tuning, const dlfp_window* w
         const double mean = (double)c.keys / c.units;
         const int64_t full = (c.units - 1) / slots, rest = c.units - full * slots;
         const bool two = taken + c.units > cus;
-        const double est = (two ? h.start2 : h.start) + full * (h.round + mean * h.beside) +
-                           (full ? mean : two ? 0.5 * (mean + c.longest) : (double)c.longest) *
-                               (taken + rest > cus ? h.beside : h.alone) +
+        const double crowd = taken > 0 && taken + c.units > slots * 3 / 4 ? 2. : 1.;
+        // Keys of the busiest slot: longest units first, the shortest fill the end.
+        const double keys = full ? (double)c.keys / slots + c.shortest * (1. - (double)rest / slots)
+                                 : two ? 0.5 * (mean + c.longest) : (double)c.longest;
+        const double est = (two ? h.start2 : h.start) + h.round * full +
+                           keys * (two ? h.beside : h.alone) +
                            (taken + c.units > slots ? held : 0.) +
-                           (c.parts > 1 ? h.merge + h.part * c.parts + 2. * full : 0.);
+                           (c.parts > 1 ? crowd * (h.merge + h.part * c.parts) + h.partial * full : 0.);
         if (!found || est < best) {
           best = est;
           split_p = split;
