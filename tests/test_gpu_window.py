@@ -99,3 +99,16 @@ def test_short_decoders(dev, ws, case, kv8):
         for tn in (None, D.dlfp_tuning(split or 0)):
             m.check(m.run(ws, dtype, SCALE, tn), SCALE, rows=[0, 399, 795, 799])
     assert D.dlfp_workspace_error(ws.buf) == 0
+
+
+@pytest.mark.parametrize("kv8", [False, True])
+@pytest.mark.parametrize("kv_len", [[700, 5, 1, 20], [300, 700, 31, 290], [20, 700, 3, 17, 9, 1, 2]])
+def test_few_decoders_beside_many_prefill_units(dev, ws, kv_len, kv8):
+    """More prefill units than lead the grid, and fewer decode workgroups than a group of it."""
+    q_len = [600 if n == 700 else 1 for n in kv_len]
+    m = Mix(dev, 16, 2, q_len, kv_len, None, 0, kv8, seed=len(kv_len))
+    for dtype in (BF16, FP32):
+        b = m.batch(D.dlfp_tuning(64, 64, 0, 16))
+        assert b.meta.num_prefill_units > 256
+        m.check(m.run(ws, dtype, SCALE, batch=b), SCALE, rows=[0, 255, 599])
+    assert D.dlfp_workspace_error(ws.buf) == 0
