@@ -279,9 +279,9 @@ constexpr int window_lds() {
 // and the exponentials between them at the clock that their power allows: 4096 tokens
 // of 64 heads in a window of 4000 keys, bf16 pages, 538 GFLOP in 495 to 517 us (1.04 to
 // 1.09 PFLOP/s; a library product of 8192^3 1.23); 2 x 1999 tokens of 32 heads over
-// 8144 keys, 8-bit pages, 457 GFLOP in 395 to 421 us (1.09 to 1.16).  fp32 output has
-// three products for one with the values: 1450 tokens of 16 heads over 8533 keys 175 us,
-// with bf16 output 118.
+// 8144 keys, 8-bit pages, 457 GFLOP in 392 to 421 us (1.09 to 1.17).  fp32 output has
+// three products for one with the values: 1450 tokens of 64 heads over 8533 keys 607 us,
+// with bf16 output 371; of products that is 1.22 PFLOP/s.
 template <int G, bool KV8, bool OUT32>
 __device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, char* smem, int* flag) {
   using L = PreLds<KV8>;
