@@ -66,9 +66,10 @@ struct Args {
   int32_t num_prefill;
   int32_t out_f32;
   // Grid of a launch with both shares: `lead` prefill workgroups, `decode_lead`
-  // decode ones, then groups of GRID_GROUP workgroups, prefill_groups and
-  // decode_groups of them evenly mixed, then what is left of each share.
-  int32_t lead, decode_lead, prefill_groups, decode_groups;
+  // decode ones, then either `decode_rest` more and the other prefill ones, or groups
+  // of GRID_GROUP workgroups, prefill_groups and decode_groups of them evenly mixed,
+  // and what is left of each share.
+  int32_t lead, decode_lead, decode_rest, prefill_groups, decode_groups;
   int32_t solo;  // a decode workgroup has four units, a wavefront each
   float scale_log2;
 };
@@ -1605,6 +1606,10 @@ __device__ __forceinline__ int unit_of(const Args& a, int b) {
   b -= a.lead;
   if (b < a.decode_lead) return np + b;
   b -= a.decode_lead;
+  // (The prefill units behind decode_rest workgroups keep their XCDs together, others
+  // than those of the lead where the rest is no multiple of eight.)
+  if (a.decode_rest > 0)
+    return b < a.decode_rest ? np + a.decode_lead + b : xcd_remap(a.lead + b - a.decode_rest, np);
   const int gp = a.prefill_groups, g = gp + a.decode_groups;
   const int group = b / GRID_GROUP, lane = b % GRID_GROUP;
   const int before = group < g ? (int)((uint64_t)group * gp / max(g, 1)) : gp;
@@ -1623,17 +1628,15 @@ template <int G, bool KV8, bool OUT32>
 __global__ __launch_bounds__(THREADS, 2) void window_kernel(Args a) {
   __shared__ __attribute__((aligned(16))) char smem[window_lds<KV8>()];
   __shared__ int flag;
-  // Prefill unit, or num_prefill + decode workgroup (none: at the lead's end).
-  const int u = unit_of(a, blockIdx.x);
+  const int u = unit_of(a, blockIdx.x);  // prefill unit, or num_prefill + decode workgroup
   const int32_t* rec = a.work + (int64_t)u * DLFP_WORK_INTS;
   if (u >= a.num_prefill) {
-    const int units = a.num_units - a.num_prefill;
     if (a.solo) {
       const int wave = uniform(threadIdx.x >> 6), d = 4 * (u - a.num_prefill) + wave;
-      if (d < units)
+      if (d < a.num_units - a.num_prefill)
         decode_unit<G, KV8, OUT32, 1>(a, a.work + (int64_t)(a.num_prefill + d) * DLFP_WORK_INTS,
                                       smem + wave * decode_wave_lds<KV8, 1>(), nullptr);
-    } else if (u - a.num_prefill < units) {
+    } else {
       decode_unit<G, KV8, OUT32, 4>(a, rec, smem, &flag);
     }
     return;
@@ -1755,14 +1758,15 @@ int attention_window(const dlfp_dims* dims, const dlfp_meta* meta, const int32_t
   // beside 1999 prompt tokens, 8-bit pages 128.6 us, without the mixture 143.5, all
   // prefill units first 159; bf16 197.5, 208 and 243).  A shorter one would leave
   // the last prefill units alone: they come first then (whole contexts, 8-bit
-  // pages: 403 us, mixed 475).  The first decode workgroups are filled up to whole
-  // groups by ones without a unit, so that a few are not left to the end (2 decoders
+  // pages: 403 us, mixed 475).  The last of up to `cus` decode workgroups, less than a
+  // group, go in front of them too, so that a few are not left to the end (2 decoders
   // beside 1408 tokens of 64 heads, bf16: 48 us, behind them 58).
   a.lead = a.num_prefill;
-  a.decode_lead = a.prefill_groups = a.decode_groups = 0;
+  a.decode_lead = a.decode_rest = a.prefill_groups = a.decode_groups = 0;
   if (meta->prefill_lead_units < a.num_prefill && decode_wgs > 0) {
     a.lead = meta->prefill_lead_units / GRID_GROUP * GRID_GROUP;
-    a.decode_lead = (std::min(decode_wgs, cus) + GRID_GROUP - 1) / GRID_GROUP * GRID_GROUP;
+    a.decode_lead = std::min(decode_wgs, cus) / GRID_GROUP * GRID_GROUP;
+    if (decode_wgs <= cus) a.decode_rest = decode_wgs % GRID_GROUP;
     a.prefill_groups = (a.num_prefill - a.lead) / GRID_GROUP;
     // Keys of the decode units for one of the prefill units, times what a key takes
     // of the decode share alone (its bytes at 6.4 TB/s) over the prefill share alone
@@ -1773,8 +1777,7 @@ int attention_window(const dlfp_dims* dims, const dlfp_meta* meta, const int32_t
                                               std::max(meta->decode_split_tokens, 64) /
                                               (a.solo ? 4 : 1)
                                         : 0.;
-    a.decode_groups =
-        (int)std::min<double>(std::max(decode_wgs - a.decode_lead, 0) / GRID_GROUP, groups);
+    a.decode_groups = (int)std::min<double>((decode_wgs - a.decode_lead) / GRID_GROUP, groups);
   }
   // Wavefronts of a decode unit in a launch of decode units alone.  Eight, with long
   // units on a quarter of the compute units: one lasts as long as its chain of steps
@@ -1782,7 +1785,7 @@ int attention_window(const dlfp_dims* dims, const dlfp_meta* meta, const int32_t
   // compute unit, one's start and sum behind the other (512 units of 1024 keys, 8
   // bits: 23.2 us, with eight 26.5, with one 31.5).
   const int nw = a.solo ? 1 : a.num_units <= cus / 4 && meta->decode_split_tokens > 256 ? 8 : 4;
-  const int grid = a.num_prefill + std::max(decode_wgs, a.decode_lead);
+  const int grid = a.num_prefill + decode_wgs;
   (void)hipGetLastError();
   hipError_t e;
   switch (g) {
