@@ -407,7 +407,7 @@ def dlfp_rope_append(dims: dlfp_dims, rope: dlfp_rope, positions, slot_mapping, 
     positions, slot_mapping: int32 [T]; bf16 caches per the pool layout."""
     st = lib().dlfp_rope_append(*_append_args(dims, rope, positions, slot_mapping, q, k_new, v_new,
                                               q_out, k_cache, v_cache),
-                                k_cache.size(0), _stream(stream))
+                                k_cache.shape[0], _stream(stream))
     if st:
         _check(st, "dlfp_rope_append")
 
@@ -417,7 +417,7 @@ def dlfp_rope_append_kv8(dims: dlfp_dims, rope: dlfp_rope, positions, slot_mappi
     """The same into 8-bit caches with their exponents (uint8 [num_blocks][Hkv])."""
     st = lib().dlfp_rope_append_kv8(*_append_args(dims, rope, positions, slot_mapping, q, k_new,
                                                   v_new, q_out, k_cache, v_cache),
-                                    k_exp.data_ptr(), v_exp.data_ptr(), k_cache.size(0),
+                                    k_exp.data_ptr(), v_exp.data_ptr(), k_cache.shape[0],
                                     _stream(stream))
     if st:
         _check(st, "dlfp_rope_append_kv8")
@@ -440,8 +440,8 @@ def dlfp_attention_window(dims: dlfp_dims, meta: Meta, d_work, d_block_table, q,
     """meta: of dlfp_build_window_meta; bf16 caches; out dtype bfloat16 or float32."""
     _check_attention(dims, meta, d_work, d_block_table, q, k_cache, v_cache, out, workspace)
     st = lib().dlfp_attention_window(
-        dims, meta.c, d_work.data_ptr(), d_block_table.data_ptr(), d_block_table.size(1),
-        k_cache.size(0), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), float(scale),
+        dims, meta.c, d_work.data_ptr(), d_block_table.data_ptr(), d_block_table.shape[1],
+        k_cache.shape[0], q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), float(scale),
         out.data_ptr(), _out_code(out.dtype), workspace.data_ptr(), workspace.nbytes,
         _stream(stream))
     if st:
@@ -453,8 +453,8 @@ def dlfp_attention_kv8(dims: dlfp_dims, meta: Meta, d_work, d_block_table, q, k_
     """The same over 8-bit caches with their exponents (uint8 [num_blocks][Hkv])."""
     _check_attention(dims, meta, d_work, d_block_table, q, k_cache, v_cache, out, workspace)
     st = lib().dlfp_attention_kv8(
-        dims, meta.c, d_work.data_ptr(), d_block_table.data_ptr(), d_block_table.size(1),
-        k_cache.size(0), q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_exp.data_ptr(),
+        dims, meta.c, d_work.data_ptr(), d_block_table.data_ptr(), d_block_table.shape[1],
+        k_cache.shape[0], q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_exp.data_ptr(),
         v_exp.data_ptr(), float(scale), out.data_ptr(), _out_code(out.dtype), workspace.data_ptr(),
         workspace.nbytes, _stream(stream))
     if st:

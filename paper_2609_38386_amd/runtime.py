@@ -247,7 +247,8 @@ class WindowBatch:
 
     def attention(self, pool, q: torch.Tensor, scale: float, out: torch.Tensor,
                   workspace: Workspace, stream=None):
-        ws = workspace.ensure(self.meta.workspace_bytes, self.meta.num_groups, stream)
+        counts = self.meta.c   # (a field through the meta itself costs 0.4 us)
+        ws = workspace.ensure(counts.workspace_bytes, counts.num_groups, stream)
         window_attention(self.dims, self.meta, self.d_work, self.d_block_table, pool, q, scale, out,
                          ws, stream)
 
