@@ -351,17 +351,21 @@ def dlfp_append_attention_mixed_static(dims: dlfp_dims, meta: Meta, d_work, d_bl
         _check(st, "dlfp_append_attention_mixed_static")
 
 
-def _rows(t, shape) -> int:
-    """Elements between the tokens' rows of a [tokens][heads][128] bf16 tensor whose heads
-    are contiguous."""
-    if t.shape != shape or t.element_size() != 2:
+def _row_strides(n, hq, hkv, q, k, v, out):
+    """Elements between the tokens' rows of q, k, v and out: [n][heads][128] bf16, a token's
+    heads contiguous."""
+    qs, ks = (n, hq, HEAD_DIM), (n, hkv, HEAD_DIM)
+    if (q.shape != qs or out.shape != qs or k.shape != ks or v.shape != ks or
+            not q.element_size() == k.element_size() == v.element_size() == out.element_size() == 2):
         raise ValueError("queries, keys and values must be bf16 [tokens][heads][128]")
-    if t.is_contiguous():
-        return shape[1] * HEAD_DIM
-    token, head, dim = t.stride()
-    if dim != 1 or (head != HEAD_DIM and shape[1] > 1):
+    sq, sk, sv, so = q.stride(), k.stride(), v.stride(), out.stride()
+    if (not sq[2] == sk[2] == sv[2] == so[2] == 1 or
+            (hq > 1 and not sq[1] == so[1] == HEAD_DIM) or
+            (hkv > 1 and not sk[1] == sv[1] == HEAD_DIM)):
         raise ValueError("a token's heads must be contiguous")
-    return token if shape[0] > 1 else shape[1] * HEAD_DIM
+    if n > 1:
+        return sq[0], sk[0], sv[0], so[0]
+    return hq * HEAD_DIM, hkv * HEAD_DIM, hkv * HEAD_DIM, hq * HEAD_DIM
 
 
 def make_rope(table, interleaved: bool = False) -> dlfp_rope:
@@ -395,10 +399,10 @@ def _append_args(dims, rope, positions, slot_mapping, q, k_new, v_new, q_out, k_
     _check_device(device == positions.get_device() == slot_mapping.get_device() ==
                   k_new.get_device() == v_new.get_device() == q_out.get_device() ==
                   k_cache.get_device() == v_cache.get_device(), device, n)
-    qs, ks = (n, dims.num_q_heads, HEAD_DIM), (n, dims.num_kv_heads, HEAD_DIM)
-    return (dims, rope, n, positions.data_ptr(), slot_mapping.data_ptr(), q.data_ptr(),
-            _rows(q, qs), k_new.data_ptr(), _rows(k_new, ks), v_new.data_ptr(), _rows(v_new, ks),
-            q_out.data_ptr(), _rows(q_out, qs), k_cache.data_ptr(), v_cache.data_ptr())
+    ldq, ldk, ldv, ldo = _row_strides(n, dims.num_q_heads, dims.num_kv_heads, q, k_new, v_new, q_out)
+    return (dims, rope, n, positions.data_ptr(), slot_mapping.data_ptr(), q.data_ptr(), ldq,
+            k_new.data_ptr(), ldk, v_new.data_ptr(), ldv, q_out.data_ptr(), ldo, k_cache.data_ptr(),
+            v_cache.data_ptr())
 
 
 def dlfp_rope_append(dims: dlfp_dims, rope: dlfp_rope, positions, slot_mapping, q, k_new, v_new,
