@@ -1729,18 +1729,19 @@ int attention_window(const dlfp_dims* dims, const dlfp_meta* meta, const int32_t
   const int decode_units = a.num_units - a.num_prefill;
   // Decode units of a wavefront each spend no workgroup on their start and sum, but
   // last four times as long: 29 ns a key of bf16 pages, 25 of 8-bit ones.  They are
-  // those of up to 128 KiB of cache that are more than two for each compute unit, a
-  // further round of workgroups (8-bit pages: 640 units of 64 keys 6.9 us, of four
-  // wavefronts 11.1, 2048 10.2 and 20.9, 2048 of 512 keys 45.7 and 49.6; bf16: 640 of
-  // 256 keys 15.4 and 16.4, 2048 of 128 23.9 and 27.2), and, beside prefill units, those
-  // that last up to a quarter of the launch, by its operations at 1120 TFLOP/s and
-  // its bytes at 6.4 TB/s, or 0.45 of it where the prompts are a third of it or more
-  // and hide the last of them, and every compute unit gets some: 8-bit pages, 500 decoders of 64 keys beside 512 tokens
-  // 33.4 us, of four wavefronts 59.4, of 256 keys 63.5 and 79.5; 128 windowed ones of
-  // 2048 keys beside 1999 tokens 128 and 138, of 1024 to 8192 keys 384 and 427 (bf16
-  // 188 and 200, 522 and 522); 70 of 500 keys beside 512 tokens, which last longer,
-  // 33.3 and 28.9, 32 of 2000 beside 1024 76 and 58; bf16, 16 of 9 to 37 thousand in
-  // 792 units beside 328 396 and 357.
+  // - those of up to 128 KiB of cache that are more than two for each compute unit, a
+  //   further round of workgroups (8-bit pages: 640 units of 64 keys 6.9 us, of four
+  //   wavefronts 11.1, 2048 10.2 and 20.9, 2048 of 512 keys 45.7 and 49.6; bf16: 640
+  //   of 256 keys 15.4 and 16.4, 2048 of 128 23.9 and 27.2);
+  // - beside prefill units those that last up to a quarter of the launch, by its
+  //   operations at 1120 TFLOP/s and its bytes at 6.4 TB/s, or 0.45 of it where the
+  //   prompts are a third of it or more and hide the last of them, and every compute
+  //   unit gets some (8-bit pages: 500 decoders of 64 keys beside 512 tokens 33.4 us,
+  //   of four wavefronts 59.4, of 256 keys 63.5 and 79.5; 128 windowed ones of 2048
+  //   keys beside 1999 tokens 128 and 138, of 1024 to 8192 keys 384 and 427, bf16 188
+  //   and 200, 522 and 522; not 70 of 500 keys beside 512 tokens, which last longer,
+  //   33.3 and 28.9, 32 of 2000 beside 1024, 76 and 58, nor bf16, 16 of 9 to 37
+  //   thousand in 792 units beside 328, 396 and 357).
   const double key_us = (KV8 ? 256 : 512) / 6.4e6, tile_key_us = 128 * 512 / 1120e6;
   const double unit_us = meta->decode_split_tokens * (KV8 ? 25e-3 : 29e-3);
   const double prefill_us = 0.85 * a.num_prefill * meta->prefill_split_tokens * tile_key_us;
@@ -1751,8 +1752,8 @@ int attention_window(const dlfp_dims* dims, const dlfp_meta* meta, const int32_t
            (a.num_prefill > 0 && unit_us <= (prefill_us + decode_us) * (hidden ? 0.45 : 0.25));
   const int decode_wgs = a.solo ? (decode_units + 3) / 4 : decode_units;
   // One prefill unit for each compute unit, then one decode unit for each, so that
-  // both shares run from the start (beside each other each runs at 0.62 of its
-  // speed alone).  A decode share that takes as long as the prefill share goes on
+  // both shares run from the start (beside each other each runs at 0.62 to 0.65 of
+  // its speed alone).  A decode share that takes as long as the prefill share goes on
   // beside it: the rest of the prefill units come mixed with as many decode units
   // as take the same time, the decode units left behind them (128 windowed decoders
   // beside 1999 prompt tokens, 8-bit pages 128.6 us, without the mixture 143.5, all
