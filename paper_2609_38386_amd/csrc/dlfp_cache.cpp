@@ -186,7 +186,9 @@ int build(const dlfp_dims* dims, const dlfp_tuning* tuning, const dlfp_window* w
     const int64_t room = beside ? slots - cus : slots;
     const double round = beside ? 8. : 3.5;
     double best = 0.;
-    for (int64_t n = ceil_div(one_longest, DLFP_MAX_DECODE_UNIT_KEYS); n <= 256; ++n) {
+    // (A range that takes more than 256 units at the longest unit is cut into those.)
+    const int64_t fewest = ceil_div(one_longest, DLFP_MAX_DECODE_UNIT_KEYS);
+    for (int64_t n = fewest; n <= std::max<int64_t>(fewest, 256); ++n) {
       const int64_t split = std::max<int64_t>(round_up(ceil_div(one_longest, n), 64), 128);
       const Cut c = cuts(ones, split);
       const double keys_us = 6.2e6 / 256, mean = (double)c.keys / c.units;

@@ -1,0 +1,67 @@
+"""Single calls of dlfp_build_window_meta at the ends of what it takes, each in a process
+of its own, built with AddressSanitizer and UndefinedBehaviorSanitizer."""
+import json
+import os
+import shutil
+import subprocess
+
+import pytest
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+@pytest.fixture(scope="module")
+def driver(tmp_path_factory):
+    gxx = shutil.which("g++")
+    if gxx is None:
+        pytest.skip("no host C++ compiler")
+    out = str(tmp_path_factory.mktemp("native") / "window_call")
+    csrc = os.path.join(ROOT, "paper_2609_38386_amd", "csrc")
+    cmd = [gxx, "-std=c++17", "-O1", "-g", "-fsanitize=address,undefined",
+           "-fno-sanitize-recover=all", "-fno-omit-frame-pointer", "-D__HIP_PLATFORM_AMD__",
+           "-I/opt/rocm/include", f"-I{ROOT}/include", f"-I{csrc}",
+           os.path.join(ROOT, "tests", "native", "window_call.cpp"),
+           os.path.join(csrc, "dlfp_cache.cpp"), os.path.join(csrc, "dlfp_host.cpp"), "-o", out]
+    subprocess.run(cmd, check=True, capture_output=True, text=True)
+    return out
+
+
+def _call(driver, seqs, hq=1, hkv=1, window=0, sinks=0, decode_split=0, prefill_split=0, target=0,
+          tile=0):
+    env = dict(os.environ, ASAN_OPTIONS="detect_leaks=1:abort_on_error=1",
+               UBSAN_OPTIONS="print_stacktrace=1:halt_on_error=1")
+    env.pop("LD_PRELOAD", None)
+    args = [hq, hkv, window, sinks, decode_split, prefill_split, target, tile,
+            *(x for s in seqs for x in s)]
+    r = subprocess.run([driver, *map(str, args)], capture_output=True, text=True, env=env,
+                       timeout=300)
+    assert r.returncode == 0, r.stderr[-4000:]
+    return json.loads(r.stdout)
+
+
+def _covers(got, seqs, hkv, keys):
+    """Every token of every KV head once, its units' ranges end to end over `keys`."""
+    assert got["status"] == 0
+    rows = {}
+    for u in got["units"]:
+        assert 0 < u[5] - u[4] <= (32768 if u[11] == 0 else 4096)
+        rows.setdefault((u[0], u[1], u[2], u[3]), []).append((u[4], u[5]))
+    tokens = {}
+    for (s, h, t0, nt), spans in rows.items():
+        spans.sort()
+        assert spans[0][0] == 0 and all(a[1] == b[0] for a, b in zip(spans, spans[1:]))
+        assert spans[-1][1] == keys(*seqs[s], t0, nt)
+        tokens[s, h] = tokens.get((s, h), 0) + nt
+    assert tokens == {(s, h): q for s, (q, _) in enumerate(seqs) for h in range(hkv)}
+
+
+def _all_keys(q, kv, t0, nt):
+    return kv - q + t0 + nt
+
+
+# 256 units of 4096 keys are 1048576.
+@pytest.mark.parametrize("seqs,hkv,window", [
+    ([(1, 1048576)], 1, 0), ([(1, 1048577)], 1, 0), ([(1, 3000001), (1, 5)], 2, 0),
+    ([(1, 1048577), (40, 90)], 1, 2 ** 31 - 1), ([(1, 20), (100, 1300000)], 1, 0)])
+def test_contexts_past_a_million_keys(driver, seqs, hkv, window):
+    _covers(_call(driver, seqs, 2 * hkv, hkv, window), seqs, hkv, _all_keys)
