@@ -183,7 +183,7 @@ int build(const dlfp_dims* dims, const dlfp_tuning* tuning, const dlfp_window* w
     // costs more (whole 8-bit contexts beside 1999 tokens, 4096-key units 403 us,
     // of 2752 keys 445).
     const bool beside = (int64_t)split_tiles(std::max(1, DLFP_TILE_ROWS / g)).size() * hkv >= cus;
-    const int64_t room = beside ? slots - cus : slots;
+    const int64_t room = beside ? std::max<int64_t>(1, slots - cus) : slots;
     const double round = beside ? 8. : 3.5;
     double best = 0.;
     // (A range that takes more than 256 units at the longest unit is cut into those.)

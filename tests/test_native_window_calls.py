@@ -65,3 +65,20 @@ def _all_keys(q, kv, t0, nt):
     ([(1, 1048577), (40, 90)], 1, 2 ** 31 - 1), ([(1, 20), (100, 1300000)], 1, 0)])
 def test_contexts_past_a_million_keys(driver, seqs, hkv, window):
     _covers(_call(driver, seqs, 2 * hkv, hkv, window), seqs, hkv, _all_keys)
+
+
+@pytest.mark.parametrize("target", [1, 2, 3, 4, 5, 6, 7, 8, 9, 15, 16, 64])
+def test_few_target_units_beside_a_prompt(driver, target):
+    seqs = [(1, 300), (40, 90), (1, 7)]
+    _covers(_call(driver, seqs, 8, 8, target=target), seqs, 8, _all_keys)
+    _covers(_call(driver, seqs, 8, 1, 30, 5, target=target), seqs, 1, _in_window(30, 5))
+    _covers(_call(driver, [(1, 9000)], 8, 2, target=target), [(1, 9000)], 2, _all_keys)
+
+
+def _in_window(window, sinks):
+    """Keys that the rows of a tile read: whole pages left out of the others."""
+    def keys(q, kv, t0, nt):
+        first = kv - q + t0
+        low = max(0, first - window + 1) // 16
+        return first + nt - 16 * max(0, low - -(-min(sinks, first + nt) // 16))
+    return keys
