@@ -163,10 +163,8 @@ int dlfp_attention_window(const dlfp_dims* dims, const dlfp_meta* meta, const in
  * bf16 output the scores come from products of 8-bit numbers: a query is the sum
  * of two e4m3 codes in scales 2^4 apart (what lies below 2^-22 of its row's
  * largest is lost) and the matrix cores add a product's terms to within 2^-15 of
- * the sum of their magnitudes (2e-6 on average); a decoder's probabilities are two
- * e4m3 terms (2^-8, or 2^-15 of the largest, probabilities times their pages' value
- * scales), and a value page more than 2^96 below another of the decoder's counts as
- * 2^96 below it; a prompt's are one bf16 term. */
+ * the sum of their magnitudes (2e-6 on average).  Probabilities are those of
+ * dlfp_attention_window. */
 int dlfp_attention_kv8(const dlfp_dims* dims, const dlfp_meta* meta, const int32_t* d_work,
                        const int32_t* d_block_table, int32_t max_blocks, int32_t num_blocks,
                        const void* q, const void* k_cache, const void* v_cache,

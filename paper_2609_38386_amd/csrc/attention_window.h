@@ -21,8 +21,7 @@
 // With bf16 output keys are not converted: a query is a sum of two rows of codes, and
 // scores are products of codes with the pages' exponents as their block scales, twice
 // the bf16 rate for twice the products, without the conversions (prompts of 1999
-// tokens over 8144 keys 445 -> 396 us); a decoder's values are not either, its
-// probabilities being two rows of codes.
+// tokens over 8144 keys 445 -> 396 us).
 //
 // Everything else is as in attention_mixed.hip: S^T = K Q^T and O^T += V^T P^T
 // with row statistics in a lane, a lazily raised reference maximum in the exp2
@@ -1260,19 +1259,12 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
     issue_k(0);
     issue_v(0);
   }
-  int v_ref = 0;  // largest value exponent of the wavefront's pages
   if constexpr (KV8) {  // with the first block on its way
     for (int x = lane; x < BP * mine; x += 64) {
       const int64_t e = (int64_t)ptab[x] * a.hkv + kh;
-      const int v = a.v_exp[e];
-      etab[x] = (uint16_t)(a.k_exp[e] | v << 8);
-      v_ref = max(v_ref, v);
+      etab[x] = (uint16_t)(a.k_exp[e] | a.v_exp[e] << 8);
     }
     wave_sync();
-  }
-  if constexpr (CODES) {
-#pragma unroll
-    for (int m = 32; m > 0; m >>= 1) v_ref = max(v_ref, __shfl_xor(v_ref, m));
   }
 
   float m_run = NEG_BIG, l_run = 0.f;
@@ -1369,12 +1361,7 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
     float mx = -__builtin_inff();
 #pragma unroll
     for (int x = 0; x < 4 * NCH; ++x) mx = fmaxf(mx, sc[x]);
-    // Products of codes take a probability times its page's value scale (relative
-    // to the largest), so the reference maximum is that of both.  A page counts as at
-    // most 2^96 below the largest (its values are then 2^-87 of the largest's or less),
-    // which keeps the sum of 2^-dv times the probabilities in range.
-    const int dv = CODES ? max((etab[BP * i + vpage] >> 8) - v_ref, -96) : 0;
-    const float m_tile = max_xor32(max_xor16(__builtin_fmaf(mx, c, (float)dv)));
+    const float m_tile = max_xor32(max_xor16(mx)) * c;
     if (__builtin_amdgcn_ballot_w64(m_tile > m_run + RESCALE_LOG2)) {
       const float m_new = m_tile > m_run + RESCALE_LOG2 ? m_tile : m_run;
       const float alpha = fexp2(m_run - m_new);
@@ -1383,33 +1370,14 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
 #pragma unroll
       for (int mb = 0; mb < 8; ++mb) o[mb] *= alpha;
     }
-    // P^T: this lane's keys of its column, its term of each, the B operands.
+    // P^T: this lane's keys of its column, its term of each, the B operands.  Terms
+    // of bf16 over 8-bit pages too: many small weights together may be the output, so
+    // each keeps its own precision (e4m3 ones step by 2^-15 of the largest; the
+    // widened values cost 2% of 128 decoders beside 1999 tokens, 125.4 -> 128.0 us,
+    // and nothing of decoders alone, 193.6 us).
     u32x4_t pk[NCH / 2], third[NCH / 2];
-    if constexpr (CODES) {
-      // Two e4m3 terms, the second in a scale 2^5 smaller: its columns take the
-      // exponentials 2^5 larger.
-      const float low = col >= 8 ? 32.f : 1.f;
-      const float shift = (float)(dv + (col >= 8 ? 5 : 0)) - m_run;
-      float sum = 0.f;
 #pragma unroll
-      for (int w = 0; w < NCH; ++w) {
-        float e[4];
-#pragma unroll
-        for (int x = 0; x < 4; ++x) {
-          e[x] = fexp2(__builtin_fmaf(sc[4 * w + x], c, shift));
-          sum += e[x];
-        }
-        const uint32_t first = to_codes(e[0], e[1], e[2], e[3], low);
-        const auto f0 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(first, low, false);
-        const auto f1 = __builtin_amdgcn_cvt_scalef32_pk_f32_fp8(first, low, true);
-        const uint32_t second =
-            to_codes(e[0] - f0[0], e[1] - f0[1], e[2] - f1[0], e[3] - f1[1], 1.f);
-        pk[0][w] = col >= 8 ? second : first;
-      }
-      l_run += __builtin_ldexpf(sum, -dv);  // of columns 0-7
-    }
-#pragma unroll
-    for (int w = 0; w < (CODES ? 0 : 2 * NCH); ++w) {
+    for (int w = 0; w < 2 * NCH; ++w) {
       float e0 = fexp2(__builtin_fmaf(sc[2 * w], c, -m_run));
       float e1 = fexp2(__builtin_fmaf(sc[2 * w + 1], c, -m_run));
       l_run += e0 + e1;
@@ -1441,15 +1409,6 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
         vc[mb] = *reinterpret_cast<const codes_t*>(wl + vbyte + mb * 256);
 #pragma unroll
       for (int mb = 0; mb < 8; ++mb) {
-        if constexpr (CODES) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const u32x2_t v = {vc[mb][2 * h], vc[mb][2 * h + 1]}, p = {pk[0][2 * h], pk[0][2 * h + 1]};
-            o[mb] = __builtin_amdgcn_mfma_f32_16x16x32_fp8_fp8(
-                __builtin_bit_cast(long, v), __builtin_bit_cast(long, p), o[mb], 0, 0, 0);
-          }
-          continue;
-        }
         bf16x8_t x[2];
         widen(vc[mb], vs, &x[0], &x[1]);
 #pragma unroll
@@ -1486,10 +1445,7 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
 #pragma unroll
   for (int mb = 0; mb < 8; ++mb)
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const float x = CODES ? __builtin_ldexpf(o[mb][i], v_ref - 127 - (col >= 8 ? 5 : 0)) : o[mb][i];
-      o[mb][i] = sum_xor8(x);
-    }
+    for (int i = 0; i < 4; ++i) o[mb][i] = sum_xor8(o[mb][i]);
   wait_memory_complete();
   meet();  // every wavefront is done with its slots
   f32x4_t* red = reinterpret_cast<f32x4_t*>(smem);

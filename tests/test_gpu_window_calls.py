@@ -6,6 +6,7 @@ import pytest
 import torch
 
 from _paged_mixes import bf16
+from _rows import far_scales, one_dominates
 from paper_2609_38386_amd import dlfp as D
 from paper_2609_38386_amd import runtime as rt
 
@@ -60,3 +61,40 @@ def test_context_past_a_million_keys(dev, ws):
         err = np.abs(out[0].double().cpu().numpy() - want)
         assert (err <= tol).all(), float((err / tol).max())
     assert D.dlfp_workspace_error(ws.buf) == 0
+
+
+# rows, hq, hkv, keys, decode split, rows of a prompt beside: units of eight wavefronts,
+# of four, of one, and of one beside a prompt.
+DOMINATED = [(2, 8, 1, 4096, 4096, 0), (40, 8, 2, 4096, 2048, 0), (530, 4, 1, 512, 512, 0),
+             (300, 4, 2, 2048, 2048, 1500), (3, 2, 1, 1024, 1024, 0), (520, 1, 1, 300, 304, 0)]
+
+
+@pytest.mark.parametrize("spread", [0.0, 1.0])
+@pytest.mark.parametrize("weight", [0.5, 0.9, 0.99, 0.9999])
+@pytest.mark.parametrize("case", range(len(DOMINATED)))
+def test_one_key_has_most_of_the_weight(dev, ws, case, weight, spread):
+    """The others' weights, each far below the largest, together make the output, whatever
+    the number of wavefronts."""
+    rows, hq, hkv, n, split, prompt = DOMINATED[case]
+    m = one_dominates(case, rows, hq, hkv, n, weight, spread, dev)
+    want, bounds = m.expected(SCALE)
+    before = m.dq[:1].expand(prompt, -1, -1).contiguous() if prompt else None
+    for dtype, tol in zip((BF16, FP32), bounds):
+        got, units, prefill = m.run(ws, dtype, SCALE, D.dlfp_tuning(split), before)
+        assert (units > 512) == (rows >= 300) and (prefill > 0) == (prompt > 0)
+        err = np.abs(got.double().cpu().numpy() - want)
+        print(dtype, float(np.linalg.norm(err) / np.linalg.norm(want)), float((err / tol).max()))
+        assert (err <= tol).all()
+    assert D.dlfp_workspace_error(ws.buf) == 0
+
+
+@pytest.mark.parametrize("sharp", [40.0, 600.0])
+@pytest.mark.parametrize("rows,hq,hkv,n,split", [(6, 8, 4, 900, 0), (3, 8, 1, 4000, 4096),
+                                                 (530, 2, 1, 400, 400), (40, 16, 2, 700, 0)])
+def test_each_row_by_its_own_scales(dev, ws, rows, hq, hkv, n, split, sharp):
+    """Rows whose weight is on value pages of small scales, beside others' of large ones."""
+    m = far_scales(rows, rows, hq, hkv, n, dev, sharp)
+    want, bounds = m.expected(SCALE)
+    for dtype, tol in zip((BF16, FP32), bounds):
+        got, _, _ = m.run(ws, dtype, SCALE, D.dlfp_tuning(split))
+        assert (np.abs(got.double().cpu().numpy() - want) <= tol).all()
