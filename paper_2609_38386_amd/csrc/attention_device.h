@@ -321,7 +321,9 @@ __device__ __forceinline__ u32x4_t mask_elems(u32x4_t v, int limit, F key_of) {
 // before any is consumed, so a batch costs about one memory round trip; NB is
 // chosen so that a batch holds about 136 registers.  Every load instruction
 // of a wavefront reads whole contiguous runs of the partial layout.
-template <int G, int TPR, class A>
+// A batch that reaches past the last split takes that one again with a weight of
+// zero, which makes a NaN of an infinite partial value; with EXACT it leaves it out.
+template <int G, int TPR, class A, bool EXACT = false>
 __device__ __forceinline__ void prefill_merge(const A& a, const Slots sl, int slot_floats,
                                               int nsplits, int rows, int row0, int kh) {
   constexpr int NP = 32 / TPR;             // pieces per thread
@@ -362,6 +364,7 @@ __device__ __forceinline__ void prefill_merge(const A& a, const Slots sl, int sl
       for (int i = 0; i < PP; ++i) acc[i] *= rs;
 #pragma unroll
       for (int u = 0; u < NB; ++u) {
+        if (EXACT && j + u >= nsplits) break;
         const float w = j + u < nsplits ? fexp2(mj[u] - mn) : 0.f;
         lsum += w * lj[u];
 #pragma unroll

@@ -767,11 +767,11 @@ __device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, ch
   __syncthreads();
   if (!*flag) return;
   if (rows > 64)
-    prefill_merge<G, 2>(a, sl, slot_floats, nsplits, rows, row0, kh);
+    prefill_merge<G, 2, Args, true>(a, sl, slot_floats, nsplits, rows, row0, kh);
   else if (rows > 32)
-    prefill_merge<G, 4>(a, sl, slot_floats, nsplits, rows, row0, kh);
+    prefill_merge<G, 4, Args, true>(a, sl, slot_floats, nsplits, rows, row0, kh);
   else
-    prefill_merge<G, 8>(a, sl, slot_floats, nsplits, rows, row0, kh);
+    prefill_merge<G, 8, Args, true>(a, sl, slot_floats, nsplits, rows, row0, kh);
   if (tid == 0)
     __hip_atomic_store(group_counter(a.ws, grp), 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
@@ -1124,7 +1124,7 @@ __device__ __forceinline__ void small_unit(const Args& a, const record_t f, char
   if (tid == 0) *flag = arrive(a.ws, grp) == nsplits - 1;
   __syncthreads();
   if (!*flag) return;
-  prefill_merge<G, 8>(a, sl, slot_floats, nsplits, rows, row0, kh);
+  prefill_merge<G, 8, Args, true>(a, sl, slot_floats, nsplits, rows, row0, kh);
   if (tid == 0)
     __hip_atomic_store(group_counter(a.ws, grp), 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }

@@ -5,7 +5,7 @@ import numpy as np
 import pytest
 import torch
 
-from _paged_mixes import bf16
+from _paged_mixes import Mix, bf16
 from _rows import far_scales, one_dominates
 from paper_2609_38386_amd import dlfp as D
 from paper_2609_38386_amd import runtime as rt
@@ -98,3 +98,44 @@ def test_each_row_by_its_own_scales(dev, ws, rows, hq, hkv, n, split, sharp):
     for dtype, tol in zip((BF16, FP32), bounds):
         got, _, _ = m.run(ws, dtype, SCALE, D.dlfp_tuning(split))
         assert (np.abs(got.double().cpu().numpy() - want) <= tol).all()
+
+
+# hq, hkv, q_len, kv_len, window, sinks, tuning: decode units of eight, four and one
+# wavefronts, whole and split, alone and beside a prompt; prompts' tiles of 128 and of 32
+# rows, whole and in parts of which the last batch of a merge has one to three.
+INFINITE = [
+    (8, 2, [1, 1], [1500, 900], None, 0, None), (2, 2, [1, 1], [700, 40], None, 0, (64,)),
+    (16, 2, [1] * 40, [30 + 25 * i for i in range(40)], None, 0, (2048,)),
+    (8, 1, [1] * 530, [1 + i % 90 for i in range(530)], None, 0, None),
+    (4, 2, [40, 1, 1], [300, 500, 33], None, 0, None), (4, 1, [1, 1], [800, 90], 200, 20, None),
+    (8, 2, [1] * 300 + [1500], [100] * 300 + [1500], None, 0, None),
+    (8, 2, [100], [700], None, 0, (0, 0, 0, 32)), (8, 2, [100], [700], None, 0, (0, 128, 0, 32)),
+    (2, 2, [100], [900], None, 0, (0, 192, 0, 40)), (2, 2, [60], [900], 800, 16, (0, 64, 0, 60)),
+    (8, 2, [9], [900], None, 0, (0, 0, 0, 8)), (16, 2, [9], [900], None, 0, (0, 192, 0, 4)),
+    (4, 2, [70], [500], 400, 0, (0, 64, 0, 2)), (8, 2, [33, 2], [300, 80], None, 0, (0, 64)),
+]
+
+
+@pytest.mark.parametrize("dtype", [BF16])
+@pytest.mark.parametrize("case", range(len(INFINITE)))
+def test_infinite_values(dev, ws, case, dtype):
+    """An infinite value that all rows of a sequence see makes that dim of its heads that
+    infinity and leaves every other output as it was."""
+    hq, hkv, q_len, kv_len, window, sinks, tn = INFINITE[case]
+    m = Mix(dev, hq, hkv, q_len, kv_len, window, sinks, False, seed=case)
+    batch, g = m.batch(D.dlfp_tuning(*tn) if tn else None), hq // hkv
+    want = m.run(ws, dtype, SCALE, batch=batch)
+    assert want.isfinite().all()
+    at = 0
+    for s, (ql, kl) in enumerate(zip(q_len, kv_len)):
+        head, dim, sign = s % hkv, (11 * s + 3) % 128, 1.0 - 2.0 * (s % 2)
+        seen = min(kl - ql + 1, window or kl)            # by every row, up to the first one's
+        key = kl - ql - (7 * s) % max(1, seen - ql)
+        page = m.pool.v[int(m.table[s, key // 16]), head, dim]
+        page[SWAP[key % 16]] = sign * math.inf
+        want[at:at + ql, head * g:(head + 1) * g, dim] = sign * math.inf
+        at += ql
+    got = m.run(ws, dtype, SCALE, batch=batch)
+    wrong = (got != want).nonzero()[:4].tolist()
+    assert not wrong
+    assert D.dlfp_workspace_error(ws.buf) == 0
