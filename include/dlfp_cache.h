@@ -150,7 +150,8 @@ int dlfp_build_window_meta(const dlfp_dims* dims, const dlfp_tuning* tuning,
  * 1.6e-3 of a row in the 2-norm, below the output's own rounding) and a decoder's
  * taken in two bf16 terms; with fp32 output they are three terms, 24 bits.
  * Keys and values that no row of the batch sees are not used, whatever they
- * hold.  A NaN or infinite value that some rows of a prompt see and others of
+ * hold.  An infinite value that a row sees makes that dim of its heads that
+ * infinity (NaN if its weight is below 2^-126 of the largest).  A NaN or infinite value that some rows of a prompt see and others of
  * the same 128 / g tokens do not can make the latter NaN too.
  * Errors: as dlfp_attention_mixed; DLFP_EINVAL for the other kind of metadata. */
 int dlfp_attention_window(const dlfp_dims* dims, const dlfp_meta* meta, const int32_t* d_work,

@@ -235,13 +235,24 @@ __device__ __forceinline__ void zero_unseen_values(char* values, const Span& sp,
 // Probabilities of two keys as bf16 pairs, for the matrix products.  bf16 output:
 // one term, rounded to nearest: 1.1e-3 to 1.6e-3 of a row in the 2-norm, below
 // what rounding the output leaves (1.7e-3).  fp32 output: three terms, the first
-// two cut off so that all are positive (an infinite value then stays one), 24
-// bits together.
+// two cut off so that none is negative, 24 bits together.
 __device__ __forceinline__ uint32_t cut(float& a, float& b) {
   const uint32_t x = __builtin_bit_cast(uint32_t, a), y = __builtin_bit_cast(uint32_t, b);
   a -= __builtin_bit_cast(float, x & 0xFFFF0000u);
   b -= __builtin_bit_cast(float, y & 0xFFFF0000u);
   return __builtin_amdgcn_perm(y, x, 0x07060302u);
+}
+// A later term, at least the least normal number where the term before is one too
+// (8-bit pages hold no infinity): a term of 0 would make a NaN of an infinite value
+// that the row sees, and one above 0 would give a masked key a weight.
+template <bool KV8>
+__device__ __forceinline__ uint32_t above_zero(uint32_t term, uint32_t before) {
+  if constexpr (KV8) return term;
+  typedef uint16_t u16x2_t __attribute__((ext_vector_type(2)));
+  const u16x2_t least = {0x0080, 0x0080};
+  const u16x2_t floor = __builtin_elementwise_min(__builtin_bit_cast(u16x2_t, before), least);
+  return __builtin_bit_cast(
+      uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, term), floor));
 }
 
 // ---------------------------------------------------------------- prefill
@@ -537,12 +548,12 @@ __device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, ch
   auto next_term = [&](f32x16_t* sacc, bf16x8_t* pf, bool last) {
 #pragma unroll
     for (int kk = 0; kk < 4; ++kk) {
-      u32x4_t pk;
+      u32x4_t pk = __builtin_bit_cast(u32x4_t, pf[kk]);
 #pragma unroll
       for (int w = 0; w < 4; ++w) {
         const int x = 8 * (kk & 1) + 2 * w;
         float p0 = sacc[kk >> 1][x], p1 = sacc[kk >> 1][x + 1];
-        pk[w] = last ? pack_bf16(p0, p1) : cut(p0, p1);
+        pk[w] = above_zero<KV8>(last ? pack_bf16(p0, p1) : cut(p0, p1), pk[w]);
         sacc[kk >> 1][x] = p0;
         sacc[kk >> 1][x + 1] = p1;
       }
@@ -1039,12 +1050,12 @@ __device__ __forceinline__ void small_unit(const Args& a, const record_t f, char
       for (int term = 0; term < 2; ++term) {
 #pragma unroll
         for (int kk = 0; kk < 2 * NJ; ++kk) {
-          u32x4_t pk;
+          u32x4_t pk = __builtin_bit_cast(u32x4_t, pf[kk]);
 #pragma unroll
           for (int w = 0; w < 4; ++w) {
             const int x = 8 * (kk & 1) + 2 * w;
             float p0 = sacc[kk >> 1][x], p1 = sacc[kk >> 1][x + 1];
-            pk[w] = term ? pack_bf16(p0, p1) : cut(p0, p1);
+            pk[w] = above_zero<KV8>(term ? pack_bf16(p0, p1) : cut(p0, p1), pk[w]);
             sacc[kk >> 1][x] = p0;
             sacc[kk >> 1][x + 1] = p1;
           }
@@ -1382,9 +1393,10 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
       float e1 = fexp2(__builtin_fmaf(sc[2 * w + 1], c, -m_run));
       l_run += e0 + e1;
       if constexpr (OUT32) {
-        const uint32_t t0 = cut(e0, e1), t1 = cut(e0, e1);
+        // (Columns 8-15 have no third term: the least weight of the second.)
+        const uint32_t t0 = cut(e0, e1), t1 = above_zero<KV8>(cut(e0, e1), t0);
         pk[w >> 2][w & 3] = col >= 8 ? t1 : t0;
-        third[w >> 2][w & 3] = col >= 8 ? 0u : pack_bf16(e0, e1);
+        third[w >> 2][w & 3] = above_zero<KV8>(col >= 8 ? 0u : pack_bf16(e0, e1), t1);
       } else {
         pk[w >> 2][w & 3] = pack_term(e0, e1, col >= 8);
       }

@@ -116,7 +116,7 @@ INFINITE = [
 ]
 
 
-@pytest.mark.parametrize("dtype", [BF16])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
 @pytest.mark.parametrize("case", range(len(INFINITE)))
 def test_infinite_values(dev, ws, case, dtype):
     """An infinite value that all rows of a sequence see makes that dim of its heads that
