@@ -351,12 +351,23 @@ def dlfp_append_attention_mixed_static(dims: dlfp_dims, meta: Meta, d_work, d_bl
         _check(st, "dlfp_append_attention_mixed_static")
 
 
+_types = None
+
+
+def _bind_types():
+    """(bfloat16, float32, int32): types are compared, as a size alone would let others pass."""
+    global _types
+    import torch
+    _types = torch.bfloat16, torch.float32, torch.int32
+    return _types
+
+
 def _row_strides(n, hq, hkv, q, k, v, out):
     """Elements between the tokens' rows of q, k, v and out: [n][heads][128] bf16, a token's
     heads contiguous."""
     qs, ks = (n, hq, HEAD_DIM), (n, hkv, HEAD_DIM)
     if (q.shape != qs or out.shape != qs or k.shape != ks or v.shape != ks or
-            not q.element_size() == k.element_size() == v.element_size() == out.element_size() == 2):
+            not q.dtype is k.dtype is v.dtype is out.dtype is (_types or _bind_types())[0]):
         raise ValueError("queries, keys and values must be bf16 [tokens][heads][128]")
     sq, sk, sv, so = q.stride(), k.stride(), v.stride(), out.stride()
     if (not sq[2] == sk[2] == sv[2] == so[2] == 1 or
@@ -370,7 +381,8 @@ def _row_strides(n, hq, hkv, q, k, v, out):
 
 def make_rope(table, interleaved: bool = False) -> dlfp_rope:
     """table: float32 [positions][rotary_dim], cosines then sines; it has to outlive the rope."""
-    if table.dim() != 2 or table.element_size() != 4 or not table.is_contiguous():
+    if (table.dim() != 2 or table.dtype is not (_types or _bind_types())[1] or
+            not table.is_contiguous()):
         raise ValueError("the table must be contiguous float32 [positions][rotary_dim]")
     return dlfp_rope(table.data_ptr(), table.size(0), table.size(1), 1 if interleaved else 0)
 
@@ -391,15 +403,15 @@ def _append_args(dims, rope, positions, slot_mapping, q, k_new, v_new, q_out, k_
     n = slot_mapping.numel()
     if positions.numel() != n:
         raise ValueError("shapes disagree")
-    if positions.element_size() != 4 or slot_mapping.element_size() != 4:
+    if not positions.dtype is slot_mapping.dtype is (_types or _bind_types())[2]:
         raise ValueError("positions and slots must be int32")
     if not (positions.is_contiguous() and slot_mapping.is_contiguous()):
         raise ValueError("positions and slots must be contiguous")
+    ldq, ldk, ldv, ldo = _row_strides(n, dims.num_q_heads, dims.num_kv_heads, q, k_new, v_new, q_out)
     device = q.get_device()
     _check_device(device == positions.get_device() == slot_mapping.get_device() ==
                   k_new.get_device() == v_new.get_device() == q_out.get_device() ==
                   k_cache.get_device() == v_cache.get_device(), device, n)
-    ldq, ldk, ldv, ldo = _row_strides(n, dims.num_q_heads, dims.num_kv_heads, q, k_new, v_new, q_out)
     return (dims, rope, n, positions.data_ptr(), slot_mapping.data_ptr(), q.data_ptr(), ldq,
             k_new.data_ptr(), ldk, v_new.data_ptr(), ldv, q_out.data_ptr(), ldo, k_cache.data_ptr(),
             v_cache.data_ptr())
@@ -429,8 +441,11 @@ def dlfp_rope_append_kv8(dims: dlfp_dims, rope: dlfp_rope, positions, slot_mappi
 
 def _check_attention(dims, meta, d_work, d_block_table, q, k_cache, v_cache, out, workspace):
     shape = (meta.c.num_tokens, dims.num_q_heads, HEAD_DIM)
-    if q.shape != shape or out.shape != shape or q.element_size() != 2:
+    bf16, _, int32 = _types or _bind_types()
+    if q.shape != shape or out.shape != shape or q.dtype is not bf16:
         raise ValueError("q and out must be [tokens][Hq][128], q bf16")
+    if not d_work.dtype is d_block_table.dtype is int32:
+        raise ValueError("the work list and the block table must be int32")
     if not (q.is_contiguous() and out.is_contiguous() and d_block_table.is_contiguous()):
         raise ValueError("q, out and the block table must be contiguous")
     device = q.get_device()

@@ -81,8 +81,11 @@ class KVPool8:
     def of(cls, k: torch.Tensor, v: torch.Tensor, k_exp: torch.Tensor,
            v_exp: torch.Tensor) -> "KVPool8":
         """A pool over four tensors that are there already."""
-        if k.element_size() != 1 or v.element_size() != 1 or not _are_pages(k, v):
-            raise ValueError("caches must be contiguous pages of one byte a value")
+        for x in (k, v):   # (uint8: the codes themselves)
+            if x.dtype not in (torch.float8_e4m3fn, torch.uint8):
+                raise ValueError("caches must hold e4m3 codes (float8_e4m3fn or uint8)")
+        if not _are_pages(k, v):
+            raise ValueError("caches must be contiguous pages")
         for e in (k_exp, v_exp):
             if (e.dtype != torch.uint8 or e.shape != k.shape[:2] or not e.is_contiguous() or
                     e.device != k.device):

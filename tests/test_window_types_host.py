@@ -1,0 +1,76 @@
+"""Types that the calls of dlfp_cache.h would read as others are refused (no GPU needed)."""
+from types import SimpleNamespace
+
+import numpy as np
+import pytest
+import torch
+
+from paper_2609_38386_amd import dlfp as D
+from paper_2609_38386_amd import runtime as rt
+
+DIMS = D.make_dims(16, 8)
+
+
+def _append(pool, q=torch.bfloat16, k=torch.bfloat16, v=torch.bfloat16, out=torch.bfloat16,
+            at=torch.int32, slots=torch.int32, rope=None):
+    rt.rope_append(DIMS, rope or rt.Rope(10, "cpu"), pool, torch.zeros(3, dtype=at),
+                   torch.zeros(3, dtype=slots), torch.zeros((3, 16, 128), dtype=q),
+                   torch.zeros((3, 8, 128), dtype=k), torch.zeros((3, 8, 128), dtype=v),
+                   torch.zeros((3, 16, 128), dtype=out))
+
+
+@pytest.mark.parametrize("pool", [rt.KVPool8(4, 8, "cpu"), rt.KVPool(4, 8, "cpu")])
+def test_appends(pool):
+    with pytest.raises(ValueError, match="on a device"):   # all types right, on the host
+        _append(pool)
+    for name in ("q", "k", "v", "out"):
+        for bad in (torch.float16, torch.int16, torch.uint16, torch.float32):
+            with pytest.raises(ValueError, match="bf16"):
+                _append(pool, **{name: bad})
+    for name in ("at", "slots"):
+        for bad in (torch.float32, torch.uint32, torch.int64):
+            with pytest.raises(ValueError, match="int32"):
+                _append(pool, **{name: bad})
+
+
+def test_rope_tables():
+    rt.Rope.of(torch.zeros(4, 128))
+    for bad in (torch.int32, torch.float64, torch.bfloat16):
+        with pytest.raises(ValueError, match="float32"):
+            rt.Rope.of(torch.zeros((4, 128), dtype=bad))
+
+
+def test_attention():
+    pool = rt.KVPool(1, 8, "cpu")
+    batch = rt.WindowBatch(DIMS, [3], [3], np.zeros((1, 1), np.int32), 1, "cpu")
+    ws = SimpleNamespace(ensure=lambda *a: torch.zeros(1 << 20, dtype=torch.uint8))
+
+    def call(pool=pool, q=torch.bfloat16, out=torch.bfloat16):
+        batch.attention(pool, torch.zeros((3, 16, 128), dtype=q), 0.1,
+                        torch.zeros((3, 16, 128), dtype=out), ws)
+    for p in (pool, rt.KVPool8(1, 8, "cpu")):
+        with pytest.raises(ValueError, match="on a device"):
+            call(p)
+        for bad in (torch.float16, torch.int16):
+            with pytest.raises(ValueError, match="bf16"):
+                call(p, q=bad)
+    for name in ("d_work", "d_block_table"):
+        kept = getattr(batch, name)
+        for bad in (torch.float32, torch.int64):
+            setattr(batch, name, kept.to(bad))
+            with pytest.raises(ValueError, match="int32"):
+                call()
+        setattr(batch, name, kept)
+
+
+def test_pools():
+    pool = rt.KVPool8(4, 8, "cpu")
+    parts = (pool.k, pool.v, pool.k_exp, pool.v_exp)
+    rt.KVPool8.of(*parts)
+    rt.KVPool8.of(pool.k.view(torch.uint8), pool.v.view(torch.uint8), *parts[2:])   # the codes
+    for bad in (torch.float8_e4m3fnuz, torch.float8_e5m2, torch.int8, torch.bool):
+        for i in range(2):
+            x = list(parts)
+            x[i] = x[i].view(torch.uint8).view(bad)
+            with pytest.raises(ValueError, match="e4m3"):
+                rt.KVPool8.of(*x)
