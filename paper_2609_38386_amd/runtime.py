@@ -218,6 +218,16 @@ def new_positions(meta: _d.Meta, q_len: np.ndarray) -> np.ndarray:
     return meta.q_pos0[seq] + np.arange(len(seq), dtype=np.int32) - meta.cu_q[seq]
 
 
+def _window(window: Optional[int], sinks: int) -> Optional[_d.dlfp_window]:
+    if window is None:
+        if sinks:
+            raise ValueError("sinks need a window")
+        return None
+    if not (-2 ** 31 <= window < 2 ** 31 and -2 ** 31 <= sinks < 2 ** 31):
+        raise ValueError("window and sinks must be of 32 bits")
+    return _d.dlfp_window(window, sinks)
+
+
 class WindowBatch:
     """Metadata of one mixed iteration for the rotating append and windowed or 8-bit
     attention, plus device copies of its arrays.  ``window`` None: every key up to a row's
@@ -226,15 +236,13 @@ class WindowBatch:
     def __init__(self, dims: _d.dlfp_dims, q_len: Sequence[int], kv_len: Sequence[int],
                  block_table: np.ndarray, num_blocks: int, device, window: Optional[int] = None,
                  sinks: int = 0, tuning: Optional[_d.dlfp_tuning] = None):
-        if window is None and sinks:
-            raise ValueError("sinks need a window")
+        w = _window(window, sinks)
         self.dims = dims
         self.q_len = np.asarray(q_len, dtype=np.int32)
         self.kv_len = np.asarray(kv_len, dtype=np.int32)
         table = np.ascontiguousarray(block_table, dtype=np.int32)
         self.meta = m = _d.dlfp_build_window_meta(
-            dims, self.q_len, self.kv_len, table, num_blocks,
-            _d.dlfp_window(window, sinks) if window is not None else None, tuning)
+            dims, self.q_len, self.kv_len, table, num_blocks, w, tuning)
         self.num_tokens = t = m.num_tokens
         host = np.concatenate([m.slot_mapping[:t], new_positions(m, self.q_len),
                                m.records.reshape(-1)]
@@ -377,10 +385,8 @@ class WindowStagedBatch(StagedBatch):
     def __init__(self, dims: _d.dlfp_dims, cap_seqs: int, cap_tokens: int, cap_work: int, device,
                  window: Optional[int] = None, sinks: int = 0,
                  tuning: Optional[_d.dlfp_tuning] = None):
-        if window is None and sinks:
-            raise ValueError("sinks need a window")
+        self.window = _window(window, sinks)
         super().__init__(dims, cap_seqs, cap_tokens, cap_work, device, tuning)
-        self.window = _d.dlfp_window(window, sinks) if window is not None else None
 
     def _build(self, ct, m, q_len, kv_len, block_table, num_blocks):
         st = self.lib.dlfp_build_window_meta(

@@ -74,3 +74,15 @@ def test_pools():
             x[i] = x[i].view(torch.uint8).view(bad)
             with pytest.raises(ValueError, match="e4m3"):
                 rt.KVPool8.of(*x)
+
+
+@pytest.mark.parametrize("window,sinks", [(2 ** 31, 0), (2 ** 32 + 5, 0), (5, 2 ** 32 + 1), (5, 2 ** 31),
+                                          (-2 ** 32 + 1, 0)])
+def test_windows_past_32_bits(window, sinks):
+    """Not the number that 32 bits keep of them."""
+    for batch in (lambda: rt.WindowBatch(DIMS, [1], [60], np.zeros((1, 4), np.int32), 1, "cpu", window,
+                                         sinks),
+                  lambda: rt.WindowStagedBatch(DIMS, 1, 1, 8, "cpu", window, sinks)):
+        with pytest.raises(ValueError, match="32 bits"):
+            batch()
+    rt.WindowBatch(DIMS, [1], [60], np.zeros((1, 4), np.int32), 1, "cpu", 2 ** 31 - 1, 2 ** 31 - 1)
