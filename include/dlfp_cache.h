@@ -68,8 +68,9 @@ typedef struct {
  * [0, num_blocks * 16) leaves the pages as they are (the query is still
  * rotated); a token whose position is outside [0, positions) is left out
  * altogether.  Of two tokens with one slot, either may be kept.
- * Errors: DLFP_EINVAL, DLFP_EUNSUPPORTED (dims, rotary_dim), DLFP_ERANGE (more
- * than 2^29 tokens times KV heads and groups of 16 query heads), DLFP_EHIP. */
+ * Errors: DLFP_EINVAL, DLFP_EUNSUPPORTED (dims, rotary_dim), DLFP_ERANGE (2^32
+ * threads or more, of which a token has 16 for each KV head and 64 for each group of
+ * 16 query heads), DLFP_EHIP. */
 int dlfp_rope_append(const dlfp_dims* dims, const dlfp_rope* rope, int32_t num_tokens,
                      const int32_t* positions, const int32_t* slot_mapping, const void* q,
                      int64_t ldq, const void* k_new, int64_t ldk, const void* v_new, int64_t ldv,

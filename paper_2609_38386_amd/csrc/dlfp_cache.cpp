@@ -54,8 +54,13 @@ int check_rope_append(const dlfp_dims* dims, const dlfp_rope* rope, int32_t num_
     return DLFP_EUNSUPPORTED;
   if (rope->interleaved != 0 && rope->interleaved != 1) return DLFP_EINVAL;
   const int64_t hq = dims->num_q_heads, hkv = dims->num_kv_heads;
-  // Workgroups and wavefronts of a launch are counted in 31 bits.
-  if (num_tokens * (hkv + ceil_div(hq, 16)) > I32_MAX / 4) return DLFP_ERANGE;
+  // A launch has fewer than 2^32 threads: workgroups of 256 for 16 tokens (4 of up to 512)
+  // of a KV head and for 4 tokens' group of 16 query heads, the most of either append.
+  const int64_t chunks = ceil_div(hq, 16);
+  if (num_tokens * (hkv + chunks) > I32_MAX / 4 ||
+      ceil_div(num_tokens, num_tokens <= 512 ? 4 : 16) * hkv + ceil_div(num_tokens * chunks, 4) >=
+          1 << 24)
+    return DLFP_ERANGE;
   if (!good_stride(ldq, hq) || !good_stride(ldo, hq) || !good_stride(ldk, hkv) ||
       !good_stride(ldv, hkv))
     return DLFP_EINVAL;
