@@ -283,6 +283,7 @@ int build(const dlfp_dims* dims, const dlfp_tuning* tuning, const dlfp_window* w
 
   std::vector<Unit> units;
   int64_t groups = 0, off = DLFP_WORKSPACE_PARTIALS / 4;
+  int64_t group_bytes = 0;  // of the largest group's partial results
   auto emit = [&](const Rows& r, int64_t kh, int64_t split, int64_t granule, int32_t kind) {
     // Units of few rows keep their block ids where decode units do.
     if ((int64_t)r.nt * g <= DLFP_SMALL_ROWS)
@@ -314,6 +315,7 @@ int build(const dlfp_dims* dims, const dlfp_tuning* tuning, const dlfp_window* w
     if (parts > 1) {
       ++groups;
       off += parts * floats;
+      group_bytes = std::max(group_bytes, 4 * parts * floats);
     }
   };
   // Prefill units of one KV head together: the launch gives each XCD a contiguous
@@ -332,7 +334,9 @@ int build(const dlfp_dims* dims, const dlfp_tuning* tuning, const dlfp_window* w
     for (; first != last; ++first) n = std::max(n, first->f[DLFP_W_KVEND] - first->f[DLFP_W_KVBEGIN]);
     return n;
   };
-  if (n_units > I32_MAX / DLFP_WORK_INTS || groups > DLFP_MAX_GROUPS || off > I32_MAX)
+  // (A launch addresses the partial results of a group in 31 bits.)
+  if (n_units > I32_MAX / DLFP_WORK_INTS || groups > DLFP_MAX_GROUPS || off > I32_MAX ||
+      group_bytes > I32_MAX)
     return DLFP_ERANGE;
 
   meta->num_seqs = num_seqs;

@@ -82,3 +82,15 @@ def _in_window(window, sinks):
         low = max(0, first - window + 1) // 16
         return first + nt - 16 * max(0, low - -(-min(sinks, first + nt) // 16))
     return keys
+
+
+def test_partial_results_of_a_group_below_two_gib(driver):
+    """The kernels address a group's partial results in 31 bits: of 128 rows 66560 bytes."""
+    fits = 64 * ((2 ** 31 - 1) // 66560)
+    got = _call(driver, [(16, fits)], 8, 1, prefill_split=64, tile=16)
+    _covers(got, [(16, fits)], 1, _all_keys)
+    assert got["groups"] == 1 and got["workspace"] < 2 ** 31 + (1 << 20)
+    assert _call(driver, [(16, fits + 64)], 8, 1, prefill_split=64, tile=16)["status"] == -2
+    # A group of more than 4 GiB, whose offsets would meet others'.
+    assert _call(driver, [(16, 4200000)], 8, 1, prefill_split=64, tile=16)["status"] == -2
+    assert _call(driver, [(16, 4200000)], 8, 1)["status"] == 0
