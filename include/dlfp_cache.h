@@ -134,9 +134,9 @@ enum {
  * tiles of 128 rows or of 32 and in equal parts of at least 256 keys, decoders in
  * equal parts of at least 128.
  * Errors: as dlfp_build_varlen_meta; DLFP_EINVAL for a window below 1 or sinks
- * below 0; DLFP_ERANGE also for rows whose splits leave partial results of 2 GiB or
- * more (a tuning of short splits over millions of keys); DLFP_ENOSPC also when host
- * memory runs out. */
+ * below 0; DLFP_ERANGE also for a sequence that reads more than 2^31 - 65 keys, or
+ * whose splits leave a group 2 GiB of partial results or more (a tuning of short
+ * splits over millions of keys); DLFP_ENOSPC also when host memory runs out. */
 int dlfp_build_window_meta(const dlfp_dims* dims, const dlfp_tuning* tuning,
                            const dlfp_window* window, int32_t num_seqs, const int32_t* q_len,
                            const int32_t* kv_len, const int32_t* block_table, int32_t max_blocks,

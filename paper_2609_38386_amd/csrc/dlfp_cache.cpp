@@ -128,6 +128,7 @@ int build(const dlfp_dims* dims, const dlfp_tuning* tuning, const dlfp_window* w
     if (pages > max_blocks) return DLFP_ERANGE;
     const int32_t* row = block_table + (int64_t)s * max_blocks;
     const Rows r = rows_of(s, 0, ql);
+    if (r.keys > I32_MAX - 64) return DLFP_ERANGE;  // kernels look 64 keys past a unit's end
     // Pages before and past the gap of the sequence's first row.
     const int64_t sunk = r.gap ? ceil_div(sinks, PAGE) : 0;
     int32_t lo = std::numeric_limits<int32_t>::max(), hi = std::numeric_limits<int32_t>::min();

@@ -94,3 +94,13 @@ def test_partial_results_of_a_group_below_two_gib(driver):
     # A group of more than 4 GiB, whose offsets would meet others'.
     assert _call(driver, [(16, 4200000)], 8, 1, prefill_split=64, tile=16)["status"] == -2
     assert _call(driver, [(16, 4200000)], 8, 1)["status"] == 0
+
+
+def test_keys_up_to_the_end_of_31_bits(driver):
+    """The kernels look at most 64 keys past a unit's end: those are counted in 31 bits too.
+    A window's keys count without those left out."""
+    most = 2 ** 31 - 65
+    assert _call(driver, [(1, most + 1)])["status"] == -2
+    assert _call(driver, [(2, most + 1)], tile=2)["status"] == -2
+    seqs = [(1, 2 ** 31 - 1)]
+    _covers(_call(driver, seqs, window=100, sinks=5), seqs, 1, _in_window(100, 5))
