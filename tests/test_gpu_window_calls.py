@@ -7,6 +7,7 @@ import torch
 
 from _paged_mixes import Mix, bf16
 from _rows import far_scales, one_dominates
+from oracle import window as ow
 from paper_2609_38386_amd import dlfp as D
 from paper_2609_38386_amd import runtime as rt
 
@@ -139,3 +140,79 @@ def test_infinite_values(dev, ws, case, dtype):
     wrong = (got != want).nonzero()[:4].tolist()
     assert not wrong
     assert D.dlfp_workspace_error(ws.buf) == 0
+
+
+def test_append_of_far_8_bit_pages(dev):
+    """Codes and exponents of keys and values in pages past 32 bits of bytes, a run that
+    begins inside a page and one that begins the next."""
+    hkv, blocks = 8, (1 << 32) // (8 * 2048) + 50
+    rng = np.random.default_rng(8)
+    sizes = (blocks, hkv, 16, 128), (blocks, hkv, 128, 16), (blocks, hkv), (blocks, hkv)
+    pool = rt.KVPool8.of(*(torch.empty(x, dtype=torch.uint8, device=dev) for x in sizes))
+    pages = [blocks - 3, blocks - 1]
+    codes = rng.integers(0, 120, size=(2, 2, hkv, 16, 128)).astype(np.uint8)
+    exps = rng.integers(112, 118, size=(2, 2, hkv)).astype(np.uint8)   # the new tokens' are larger
+    for i, b in enumerate(pages):
+        pool.k[b] = torch.from_numpy(codes[0, i]).to(dev)
+        pool.v[b] = torch.from_numpy(codes[1, i][:, SWAP].swapaxes(1, 2).copy()).to(dev)
+        pool.k_exp[b], pool.v_exp[b] = (torch.from_numpy(exps[x, i]).to(dev) for x in range(2))
+    n, first = 9, 11                                  # slots 11 .. 15, then 0 .. 3
+    qkv = bf16(rng.normal(size=(n, 16 + 2 * hkv, 128)))
+    rope = rt.Rope(40, dev)
+    pos = np.arange(first, first + n)
+    slots = [16 * pages[p // 16] + p % 16 for p in pos]
+    d, out = qkv.to(dev), torch.empty((n, 16, 128), dtype=BF16, device=dev)
+    ints = [torch.tensor(list(x), dtype=torch.int32, device=dev) for x in (pos, slots)]
+    rt.rope_append(D.make_dims(16, hkv), rope, pool, *ints, d[:, :16], d[:, 16:16 + hkv],
+                   d[:, 16 + hkv:], out)
+    new = [ow.rotate(qkv[:, 16:16 + hkv].float().numpy(), rope.table.cpu().numpy(), pos),
+           qkv[:, 16 + hkv:].float().numpy()]
+    for i, (b, rows, slot) in enumerate([(pages[0], slice(0, 5), 11), (pages[1], slice(5, 9), 0)]):
+        for x, name in enumerate("kv"):
+            got = getattr(pool, name)[b].cpu().numpy()
+            got = got.swapaxes(1, 2)[:, SWAP] if name == "v" else got
+            for h in range(hkv):
+                want, e = ow.append_page(codes[x, i, h], exps[x, i, h],
+                                         new[x][rows, h].astype(np.float64), slot)
+                assert np.array_equal(got[h], want), (name, i, h)
+                assert int(getattr(pool, name + "_exp")[b, h]) == e
+
+
+# q_len, kv_len, window, sinks
+NORMS = [([1] * 40, [1000 + 7 * i for i in range(40)], None, 0), ([1] * 9, [4000] * 9, 1500, 20),
+         ([1] * 600, [1100] * 600, None, 0), ([90], [1100], None, 0), ([200, 40], [1300, 1000], 900, 7),
+         ([40, 1, 1], [1500, 1200, 1300], None, 0)]
+
+
+@pytest.mark.parametrize("kv8", [False, True])
+@pytest.mark.parametrize("case", range(len(NORMS)))
+def test_rows_in_the_two_norm(dev, ws, case, kv8):
+    """Heads of rows over about a thousand keys: the error in the 2-norm.
+
+    A rounding to bf16 is within 2^-8 of a value, 2^-8 / sqrt(3) in the mean square; with bf16
+    output that is the output's, and, of a prompt, as much again from its weights (each
+    key's part of the output has its own, and the parts add up in squares as the outputs
+    do).  Twice 128 of them together stay within 1.3 of their mean (5 standard deviations of a
+    sum of squares).  Scores of products of codes are within 2^-15 of sum |q k|, 11 here at
+    most, which moves a weight by 2^-11.5.  fp32 output: 2^-15 for all.  A key left out is
+    2^-5 of a row over a thousand."""
+    q_len, kv_len, window, sinks = NORMS[case]
+    m = Mix(dev, 8, 2, q_len, kv_len, window, sinks, kv8, seed=case)
+    for dtype in (BF16, FP32):
+        got = m.run(ws, dtype, SCALE).double().cpu().numpy()
+        at = 0
+        for s, (ql, kl) in enumerate(zip(q_len, kv_len)):
+            pick = np.unique(np.linspace(0, ql - 1, 12).astype(int))
+            if ql == 1 and s % max(1, len(q_len) // 20):
+                at += 1
+                continue
+            k, v = (np.nan_to_num(x) for x in (m.k[s], m.v[s]))
+            want = ow.attention_rows(m.q[s][pick], k, v, SCALE, kl - ql + pick, window, sinks)
+            err = np.linalg.norm(got[at + pick] - want, axis=2) / np.linalg.norm(want, axis=2)
+            if dtype is FP32:
+                bound = 2.0 ** -15
+            else:
+                bound = 1.3 * 2.0 ** -8 / 3 ** 0.5 * (2 if ql > 1 else 1) ** 0.5
+                bound += 2.0 ** -11.5 if kv8 else 0.0
+            assert (err <= bound).all(), float((err / bound).max())
+            at += ql

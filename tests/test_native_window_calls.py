@@ -2,10 +2,15 @@
 of its own, built with AddressSanitizer and UndefinedBehaviorSanitizer."""
 import json
 import os
+import random
 import shutil
 import subprocess
+from types import SimpleNamespace
 
+import numpy as np
 import pytest
+
+from oracle import window as ow
 
 ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 
@@ -104,3 +109,24 @@ def test_keys_up_to_the_end_of_31_bits(driver):
     assert _call(driver, [(2, most + 1)], tile=2)["status"] == -2
     seqs = [(1, 2 ** 31 - 1)]
     _covers(_call(driver, seqs, window=100, sinks=5), seqs, 1, _in_window(100, 5))
+
+
+@pytest.mark.parametrize("seed", range(24))
+def test_random_batches_with_nothing_else_in_the_table(driver, seed):
+    """Entries of pages that no row sees are -1, which a builder that looked at them would
+    refuse; the list against the mask's definition."""
+    rng = random.Random(seed)
+    g, hkv = rng.choice([1, 2, 4, 8]), rng.choice([1, 2, 3])
+    window, sinks = rng.choice([1, 2, 16, 17, 33, 100, 640]), rng.choice([0, 0, 1, 15, 16, 17, 70])
+    seqs = []
+    for _ in range(rng.randint(1, 5)):
+        q = 1 if rng.random() < 0.5 else rng.randint(1, 200)
+        seqs.append((q, q + rng.choice([0, rng.randint(0, 900)])))
+    tuned = dict(decode_split=16 * rng.randint(0, 20), prefill_split=64 * rng.randint(0, 6),
+                 target=rng.choice([0, 5, 600]), tile=rng.randint(0, 128 // g)) if seed % 2 else {}
+    got = _call(driver, seqs, g * hkv, hkv, window, sinks, **tuned)
+    assert got["status"] == 0
+    meta = SimpleNamespace(work=np.array(got["units"], np.int32), num_prefill_units=got["prefill"],
+                           num_groups=got["groups"], workspace_bytes=got["workspace"])
+    q_len, kv_len = zip(*seqs)
+    ow.check_window_list(meta, q_len, kv_len, g * hkv, hkv, window, sinks)
