@@ -152,10 +152,10 @@ int dlfp_build_window_meta(const dlfp_dims* dims, const dlfp_tuning* tuning,
  * prompt's rows are rounded to bf16 for the product with the values (1.1e-3 to
  * 1.6e-3 of a row in the 2-norm, below the output's own rounding) and a decoder's
  * taken in two bf16 terms; with fp32 output they are three terms, 24 bits.
- * Keys and values that no row of the batch sees are not used, whatever they
- * hold.  An infinite value that a row sees makes that dim of its heads that
- * infinity (NaN if its weight is below 2^-126 of the largest).  A NaN or infinite value that some rows of a prompt see and others of
- * the same 128 / g tokens do not can make the latter NaN too.
+ * What a row does not see changes none of its outputs, whatever it holds.  An
+ * infinite value that a row sees makes that dim of its heads that infinity (or NaN,
+ * if its weight is below 2^-126 of the largest), a NaN a NaN.  The units of a prompt
+ * that meet one do their work twice.
  * Errors: as dlfp_attention_mixed; DLFP_EINVAL for the other kind of metadata. */
 int dlfp_attention_window(const dlfp_dims* dims, const dlfp_meta* meta, const int32_t* d_work,
                           const int32_t* d_block_table, int32_t max_blocks, int32_t num_blocks,

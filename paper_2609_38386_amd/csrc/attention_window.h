@@ -202,17 +202,25 @@ __device__ __forceinline__ uint32_t byte_mask(uint32_t bits) {
   return (((bits & 15) * 0x00204081u) & 0x01010101u) * 0xFFu;
 }
 
+// The values of a word (four codes, two bf16 numbers) that are infinite or NaN.
+template <bool KV8>
+__device__ __forceinline__ uint32_t not_finite(uint32_t w) {
+  if constexpr (KV8) return ((((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u) >> 7) * 0xFFu;
+  return ((((w & 0x7F807F80u) + 0x00800080u) & 0x80008000u) >> 15) * 0xFFFFu;
+}
+
 // Zeroes in LDS the values of BP pages from virtual key v0 on that a row at `pos`
-// does not see, or that lie at or past `stop` (one wavefront).
-template <bool KV8, int BP>
-__device__ __forceinline__ void zero_unseen_values(char* values, const Span& sp, int v0, int pos,
-                                                   int stop) {
+// does not see, or that lie at or past `stop` (one wavefront).  FINITE: also those
+// that are infinite or NaN.
+template <bool KV8, int BP, bool FINITE>
+__device__ __forceinline__ void zero_values(char* values, const Span& sp, int v0, int pos,
+                                            int stop) {
   constexpr int PB = page_bytes<KV8>();
   const int lane = threadIdx.x & 63;
 #pragma unroll
   for (int pg = 0; pg < BP; ++pg) {
     const uint32_t seen = sp.seen(v0 + pg * PAGE, pos, stop);
-    if (seen == 0xFFFFu) continue;
+    if (!FINITE && seen == 0xFFFFu) continue;
     u32x4_t* page = reinterpret_cast<u32x4_t*>(values + pg * PB);
 #pragma unroll
     for (int c = 0; c < PB / 1024; ++c) {
@@ -226,6 +234,10 @@ __device__ __forceinline__ void zero_unseen_values(char* values, const Span& sp,
 #pragma unroll
         for (int w = 0; w < 4; ++w)
           v[w] &= upper ? pair_mask(seen >> (8 + 2 * w)) : pair_mask(seen >> (2 * w));
+      }
+      if constexpr (FINITE) {
+#pragma unroll
+        for (int w = 0; w < 4; ++w) v[w] &= ~not_finite<KV8>(v[w]);
       }
       page[ck] = v;
     }
@@ -253,6 +265,129 @@ __device__ __forceinline__ uint32_t above_zero(uint32_t term, uint32_t before) {
   const u16x2_t floor = __builtin_elementwise_min(__builtin_bit_cast(u16x2_t, before), least);
   return __builtin_bit_cast(
       uint32_t, __builtin_elementwise_max(__builtin_bit_cast(u16x2_t, term), floor));
+}
+
+// Values that are not finite of keys that some rows of a unit see and others do not: a
+// probability of 0 times one is NaN.  A prompt's unit whose sums are not all finite does
+// its work again with such values as zero in the tiles that not all rows see whole, and
+// then adds what they are to the results that one reaches: for each 32 rows (`first`
+// and on) and such a tile of `tile` keys, it multiplies what a value is, a digit of a
+// count for each kind, with 1 where a row sees the key, else 0.  (Zeroed as tiles come
+// in, the same costs all prompts 1% to 6%; so it is a look at a unit's sums, 0.2% of long
+// prompts and 1% of short ones, and up to twice the time where all units meet one.)
+__device__ __forceinline__ bool all_finite(const f32x16_t* o) {
+  uint32_t most = 0;
+#pragma unroll
+  for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+      const float y = o[mb][x];  // (a bit cast of the element itself reads element 0)
+      most = max(most, __builtin_bit_cast(uint32_t, y) & 0x7FFFFFFFu);
+    }
+  return most < 0x7F800000u;
+}
+__device__ __forceinline__ bf16x8_t kinds_of(bf16x8_t values) {
+  u32x4_t v = __builtin_bit_cast(u32x4_t, values);
+#pragma unroll
+  for (int w = 0; w < 4; ++w) {
+    uint32_t kind = 0;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const uint32_t x = v[w] >> (16 * h) & 0xFFFFu;
+      const uint32_t k = (x & 0x7FFFu) > 0x7F80u ? 0x4980u    // NaN: 2^20
+                         : x == 0x7F80u          ? 0x3F80u    // infinity: 1
+                         : x == 0xFF80u          ? 0x4480u    // -infinity: 2^10
+                                                 : 0u;
+      kind |= k << (16 * h);
+    }
+    v[w] = kind;
+  }
+  return __builtin_bit_cast(bf16x8_t, v);
+}
+template <int G, bool KV8>
+__device__ __forceinline__ void add_special(const Args& a, const record_t f, int first, int tile) {
+  constexpr int PB = page_bytes<KV8>();
+  const int lane = threadIdx.x & 63, col = lane & 31, hi = lane >> 5;
+  const int kh = f[DLFP_W_KVHEAD], nt = f[DLFP_W_QNTOK];
+  const int vb = f[DLFP_W_KVBEGIN], ve = f[DLFP_W_KVEND], nsplits = f[DLFP_W_NSPLITS];
+  const Span sp = span_of(f);
+  const int32_t* bt = a.block_table + (int64_t)f[DLFP_W_SEQ] * a.max_blocks;
+  const int r = first + col, tr = r / G;
+  const bool row_ok = tr < nt;
+  const int end = row_ok ? min(sp.end(f[DLFP_W_QPOS0] + tr), ve) : 0;
+  const int low = row_ok ? sp.low(f[DLFP_W_QPOS0] + tr) : 0;
+  const int last_page = (ve - 1) / PAGE;
+  const int unit_end = min(sp.end(f[DLFP_W_QPOS0]), ve), last = f[DLFP_W_QPOS0] + nt - 1;
+
+  f32x16_t o[4];
+#pragma unroll
+  for (int mb = 0; mb < 4; ++mb) o[mb] = f32x16_t{};
+  for (int v0 = vb; v0 < ve; v0 += 2 * PAGE) {
+    const int t0 = v0 - (v0 - vb) % tile;
+    if (t0 + tile <= unit_end && !sp.below(t0, t0 + tile, last)) continue;
+    // Step h: 16 keys, in the order of the probabilities of the units (of 8-bit pages
+    // this lane has eight of page hi).
+    bf16x8_t sees[2];
+    const char* page[2];
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      u32x4_t w = {0u, 0u, 0u, 0u};
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int x = 8 * h + e;
+        const int key = v0 + (KV8 ? 16 * hi + vt_pos(x) : 4 * hi + 8 * (x >> 2) + (x & 3));
+        if (key < end && (key >= low || key < sp.sinks)) w[e >> 1] |= 0x3F80u << (16 * (e & 1));
+      }
+      sees[h] = __builtin_bit_cast(bf16x8_t, w);
+      const int id = bt[sp.page(min(v0 / PAGE + (KV8 ? hi : h), last_page))];
+      const int64_t block = (unsigned)id < (unsigned)a.num_blocks ? id : 0;
+      page[h] = a.vc + (block * a.hkv + kh) * PB + (KV8 ? 0 : 16 * hi);
+    }
+#pragma unroll
+    for (int mb = 0; mb < 4; ++mb) {
+      const int d = (32 * mb + col) * (PB / D);
+      bf16x8_t v[2];
+      if constexpr (KV8) {
+        widen(*reinterpret_cast<const codes_t*>(page[0] + d), 1.f, &v[0], &v[1]);
+      } else {
+        v[0] = *reinterpret_cast<const bf16x8_t*>(page[0] + d);
+        v[1] = *reinterpret_cast<const bf16x8_t*>(page[1] + d);
+      }
+      f32x16_t sum = f32x16_t{};
+#pragma unroll
+      for (int h = 0; h < 2; ++h)
+        sum = __builtin_amdgcn_mfma_f32_32x32x16_bf16(kinds_of(v[h]), sees[h], sum, 0, 0, 0);
+#pragma unroll
+      for (int x = 0; x < 16; ++x) {
+        const int n = (int)sum[x], plus = n & 1023, minus = n >> 10 & 1023;
+        const float y = n >> 20 || (plus && minus) ? __builtin_nanf("") : __builtin_inff();
+        o[mb][x] += n == 0 ? 0.f : plus ? y : -y;
+      }
+    }
+  }
+  if (!row_ok) return;
+  const int rows = nt * G, slot_floats = slot_floats_for(rows);
+  const Slots sl = group_slots(a.ws, f[DLFP_W_WSGROUP], nsplits, slot_floats);
+  const int my = f[DLFP_W_SPLIT] * slot_floats;
+  const int64_t orow = ((int64_t)(f[DLFP_W_QROW0] + tr) * a.hq + kh * G + r % G) * D;
+#pragma unroll
+  for (int mb = 0; mb < 4; ++mb)
+#pragma unroll
+    for (int x = 0; x < 16; ++x) {
+      const float y = o[mb][x];
+      if (y == 0.f) continue;
+      const int chunk = 4 * mb + (x >> 2), dim = 8 * chunk + 4 * hi + (x & 3);
+      if (nsplits > 1) {
+        const int at = my + (chunk * rows + r) * 8 + 4 * hi + (x & 3);
+        pstore1(sl, at, pload1(sl, at) + y);
+      } else if (a.out_f32) {
+        static_cast<float*>(a.out)[orow + dim] += y;
+      } else {
+        uint16_t* at = static_cast<uint16_t*>(a.out) + orow + dim;
+        const float z = __builtin_bit_cast(float, (uint32_t)*at << 16) + y;
+        *at = (uint16_t)pack_bf16(z, z);
+      }
+    }
 }
 
 // ---------------------------------------------------------------- prefill
@@ -293,8 +428,9 @@ constexpr int window_lds() {
 // 8144 keys, 8-bit pages, 457 GFLOP in 392 to 421 us (1.09 to 1.17).  fp32 output has
 // three products for one with the values: 1450 tokens of 64 heads over 8533 keys 607 us,
 // with bf16 output 371; of products that is 1.22 PFLOP/s.
-template <int G, bool KV8, bool OUT32>
-__device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, char* smem, int* flag) {
+template <int G, bool KV8, bool OUT32, bool CAREFUL>
+__device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, char* smem,
+                                             volatile int* special) {
   using L = PreLds<KV8>;
   constexpr int PB = page_bytes<KV8>();
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
@@ -341,6 +477,7 @@ __device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, ch
   const int first_page = vb / PAGE, npages = (ve - 1) / PAGE - first_page + 1;
   int32_t* ptab = reinterpret_cast<int32_t*>(smem + L::PTAB);
   uint16_t* etab = reinterpret_cast<uint16_t*>(smem + L::ETAB);
+  if (!CAREFUL && tid == 0) *special = 0;
 #pragma unroll 4
   for (int i = tid; i < npages; i += THREADS) {
     int id = bt[sp.page(first_page + i)];
@@ -388,14 +525,16 @@ __device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, ch
   };
   // Values that no row of the unit sees (before the first one's window and no
   // sinks, or past the unit's end) are zeroed in LDS: a probability of 0 times a
-  // NaN would still be NaN.  Wavefront w does page w of the tile.
+  // NaN would still be NaN.  CAREFUL: also those that are not finite, of tiles with
+  // keys that not all rows see.  Wavefront w does page w of the tile.
+  const int unit_end = CAREFUL ? min(sp.end(pos0), ve) : ve, last = pos0 + (CAREFUL ? nt - 1 : 0);
   auto has_unseen = [&](int t) {
     const int v0 = vb + t * KV_TILE;
-    return v0 + KV_TILE > ve || sp.below(v0, v0 + KV_TILE, pos0);
+    return v0 + KV_TILE > unit_end || sp.below(v0, v0 + KV_TILE, last);
   };
   auto zero_unseen = [&](int slot, int v0) {
-    zero_unseen_values<KV8, 1>(smem + L::V_BASE + slot * L::TILE + uniform(wave) * PB, sp,
-                               v0 + uniform(wave) * PAGE, pos0, ve);
+    zero_values<KV8, 1, CAREFUL>(smem + L::V_BASE + slot * L::TILE + uniform(wave) * PB, sp,
+                                 v0 + uniform(wave) * PAGE, pos0, ve);
   };
 
   // Per-lane LDS offsets of the operands.
@@ -712,6 +851,7 @@ __device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, ch
     if (j + 1 < ntiles) step(j + 1, sb, sa, odd);
   }
 
+  if (!CAREFUL && row_ok && !all_finite(o)) *special = 1;
   l_run = sum_xor32(l_run);
   const int rows = nt * G;
   // o[mb][rr] = O[row][32 mb + 8 (rr / 4) + 4 hi + rr % 4]
@@ -771,21 +911,11 @@ __device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, ch
       pstore1(sl, my + rows * D + rows + r, l_run);
     }
   }
-  wait_memory_complete();
-  __syncthreads();  // every wave of the unit has completed its stores
-  const int grp = f[DLFP_W_GROUP];
-  if (tid == 0) *flag = arrive(a.ws, grp) == nsplits - 1;
-  __syncthreads();
-  if (!*flag) return;
-  if (rows > 64)
-    prefill_merge<G, 2, Args, true>(a, sl, slot_floats, nsplits, rows, row0, kh);
-  else if (rows > 32)
-    prefill_merge<G, 4, Args, true>(a, sl, slot_floats, nsplits, rows, row0, kh);
-  else
-    prefill_merge<G, 8, Args, true>(a, sl, slot_floats, nsplits, rows, row0, kh);
-  if (tid == 0)
-    __hip_atomic_store(group_counter(a.ws, grp), 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
+
+// Keys of a block of a unit of few rows.
+template <bool KV8>
+constexpr int SMALL_KEYS = SLOT / page_bytes<KV8>() * PAGE;
 
 // Unit of at most 32 query rows: one wavefront holds all of them, so the four
 // split the keys instead: wavefront w takes blocks w, w + 4, ... of the unit, each
@@ -796,11 +926,12 @@ __device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, ch
 // rows has one wavefront for all.  64 tokens of 16 heads over 264 keys 8.7 us, as a
 // tile 12.2; 256 over 1256 15.4 and 20.1; 2048 over 4048, where the rows fill the
 // chip, 86 and 68, each key being read four times as often.
-template <int G, bool KV8, bool OUT32>
-__device__ __forceinline__ void small_unit(const Args& a, const record_t f, char* smem, int* flag) {
+template <int G, bool KV8, bool OUT32, bool CAREFUL>
+__device__ __forceinline__ void small_unit(const Args& a, const record_t f, char* smem,
+                                           volatile int* special) {
   constexpr int PB = page_bytes<KV8>();
   constexpr int BP = SLOT / PB;     // pages of a block
-  constexpr int KEYS = BP * PAGE;
+  constexpr int KEYS = SMALL_KEYS<KV8>;
   constexpr int NJ = BP / 2;        // 32-key products of a block
   constexpr int NC = PB / 1024;     // copies of a page
   constexpr bool CODES = KV8 && !OUT32;
@@ -915,6 +1046,7 @@ __device__ __forceinline__ void small_unit(const Args& a, const record_t f, char
 #pragma unroll
   for (int mb = 0; mb < 4; ++mb) o[mb] = f32x16_t{};
   const float c = a.scale_log2;
+  if (!CAREFUL && tid == 0) *special = 0;
 
   for (int i = 0; i < mine; ++i) {
     const int v0 = vb + KEYS * (wave + 4 * i);
@@ -1021,8 +1153,9 @@ __device__ __forceinline__ void small_unit(const Args& a, const record_t f, char
       wait_copies<8>();  // the values; behind them the next block's keys
     else
       wait_copies<0>();
-    if (v0 + KEYS > ve || sp.below(v0, v0 + KEYS, pos0)) {
-      zero_unseen_values<KV8, BP>(wl + SLOT, sp, v0, pos0, ve);
+    if (CAREFUL ? v0 + KEYS > unit_end || sp.below(v0, v0 + KEYS, last)
+                : v0 + KEYS > ve || sp.below(v0, v0 + KEYS, pos0)) {
+      zero_values<KV8, BP, CAREFUL>(wl + SLOT, sp, v0, pos0, ve);
       wave_sync();
     }
     auto pv = [&]() {
@@ -1075,6 +1208,7 @@ __device__ __forceinline__ void small_unit(const Args& a, const record_t f, char
   l_run = sum_xor32(l_run);
   wait_memory_complete();
   __syncthreads();  // every wavefront is done with its slots
+  if (!CAREFUL && row_ok && !all_finite(o)) *special = 1;
   f32x4_t* red = reinterpret_cast<f32x4_t*>(smem);
   float* stat = reinterpret_cast<float*>(smem + 4 * 1024 * 16);  // m[4][32], l[4][32]
   auto at = [](int w, int ch, int h, int row) {
@@ -1129,13 +1263,45 @@ __device__ __forceinline__ void small_unit(const Args& a, const record_t f, char
       pstore1(sl, my + rows * D + rows + row, L);
     }
   }
+}
+
+// A prompt's unit: its rows, stored as results or as partial ones, and, by the
+// unit of a split group that comes so far last, the merge.
+template <int G, bool KV8, bool OUT32>
+__device__ __forceinline__ void prompt_unit(const Args& a, const record_t f, char* smem, int* flag,
+                                            volatile int* special) {
+  const int tid = threadIdx.x, wave = uniform(tid >> 6);
+  const int rows = f[DLFP_W_QNTOK] * G, nsplits = f[DLFP_W_NSPLITS];
+  if (rows <= SMALL_ROWS)
+    small_unit<G, KV8, OUT32, false>(a, f, smem, special);
+  else
+    prefill_unit<G, KV8, OUT32, false>(a, f, smem, special);
+  __syncthreads();
+  if (uniform(*special)) {
+    if (rows <= SMALL_ROWS)
+      small_unit<G, KV8, OUT32, true>(a, f, smem, special);
+    else
+      prefill_unit<G, KV8, OUT32, true>(a, f, smem, special);
+    wait_memory_complete();  // the rows that it adds to
+    __syncthreads();
+    if (32 * wave < rows)
+      add_special<G, KV8>(a, f, 32 * wave, rows <= SMALL_ROWS ? SMALL_KEYS<KV8> : KV_TILE);
+  }
+  if (nsplits == 1) return;
   wait_memory_complete();
   __syncthreads();  // every wave of the unit has completed its stores
-  const int grp = f[DLFP_W_GROUP];
+  const int grp = f[DLFP_W_GROUP], slot_floats = slot_floats_for(rows);
   if (tid == 0) *flag = arrive(a.ws, grp) == nsplits - 1;
   __syncthreads();
   if (!*flag) return;
-  prefill_merge<G, 8, Args, true>(a, sl, slot_floats, nsplits, rows, row0, kh);
+  const Slots sl = group_slots(a.ws, f[DLFP_W_WSGROUP], nsplits, slot_floats);
+  const int row0 = f[DLFP_W_QROW0], kh = f[DLFP_W_KVHEAD];
+  if (rows > 64)
+    prefill_merge<G, 2, Args, true>(a, sl, slot_floats, nsplits, rows, row0, kh);
+  else if (rows > 32)
+    prefill_merge<G, 4, Args, true>(a, sl, slot_floats, nsplits, rows, row0, kh);
+  else
+    prefill_merge<G, 8, Args, true>(a, sl, slot_floats, nsplits, rows, row0, kh);
   if (tid == 0)
     __hip_atomic_store(group_counter(a.ws, grp), 0, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
 }
@@ -1409,7 +1575,7 @@ __device__ __forceinline__ void decode_unit(const Args& a, const int32_t* rec, c
     if (edge) {
       // Values that the token does not see are zeroed (a probability of 0 times
       // a NaN would still be NaN).
-      zero_unseen_values<KV8, BP>(wl + SLOT, sp, v0, pos, ve);
+      zero_values<KV8, BP, false>(wl + SLOT, sp, v0, pos, ve);
       wave_sync();
     }
     // O^T += V^T P^T, eight blocks of 16 dims.
@@ -1595,7 +1761,7 @@ __device__ __forceinline__ int unit_of(const Args& a, int b) {
 template <int G, bool KV8, bool OUT32>
 __global__ __launch_bounds__(THREADS, 2) void window_kernel(Args a) {
   __shared__ __attribute__((aligned(16))) char smem[window_lds<KV8>()];
-  __shared__ int flag;
+  __shared__ int flag, special;
   const int u = unit_of(a, blockIdx.x);  // prefill unit, or num_prefill + decode workgroup
   const int32_t* rec = a.work + (int64_t)u * DLFP_WORK_INTS;
   if (u >= a.num_prefill) {
@@ -1609,11 +1775,7 @@ __global__ __launch_bounds__(THREADS, 2) void window_kernel(Args a) {
     }
     return;
   }
-  const record_t f = load_record(rec);
-  if (f[DLFP_W_QNTOK] * G <= SMALL_ROWS)
-    small_unit<G, KV8, OUT32>(a, f, smem, &flag);
-  else
-    prefill_unit<G, KV8, OUT32>(a, f, smem, &flag);
+  prompt_unit<G, KV8, OUT32>(a, load_record(rec), smem, &flag, &special);
 }
 
 template <int G, bool KV8, bool OUT32, int NW>

@@ -216,3 +216,75 @@ def test_rows_in_the_two_norm(dev, ws, case, kv8):
                 bound += 2.0 ** -11.5 if kv8 else 0.0
             assert (err <= bound).all(), float((err / bound).max())
             at += ql
+
+
+# hq, hkv, q_len, kv_len, window, sinks, tuning: tiles of 128 rows, of few, whole and split,
+# without a window, with one, with sinks.
+PARTLY = [
+    (8, 2, 100, 400, None, 0, (0, 0, 0, 32)), (8, 2, 100, 400, 90, 0, (0, 0, 0, 32)),
+    (2, 2, 300, 300, None, 0, (0, 0, 0, 128)), (2, 2, 300, 700, 40, 37, (0, 128, 0, 100)),
+    (16, 2, 50, 200, 33, 5, (0, 64, 0, 16)), (8, 2, 40, 400, 70, 0, (0, 0, 0, 8)),
+    (2, 2, 90, 200, 21, 18, (0, 64, 0, 32)), (4, 2, 64, 64, None, 0, (0, 0, 0, 1)),
+]
+
+
+@pytest.mark.parametrize("kv8", [False, True])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("case", range(len(PARTLY)))
+def test_values_that_some_rows_of_a_prompt_see(dev, ws, case, dtype, kv8):
+    """A NaN or infinite value reaches its dim of the rows that see its key and no other
+    output, be the others' tokens earlier or later in the same tile."""
+    hq, hkv, ql, kl, window, sinks, tn = PARTLY[case]
+    m = Mix(dev, hq, hkv, [ql], [kl], window, sinks, kv8, seed=case)
+    batch, g = m.batch(D.dlfp_tuning(*tn)), hq // hkv
+    plain = m.run(ws, dtype, SCALE, batch=batch)
+    pos = np.arange(kl - ql, kl)
+    kept = m.pool.v.view(torch.uint8).clone()
+    seen_by_some = np.flatnonzero(ow.sees(pos[:, None], np.arange(kl)[None], window, sinks).any(0))
+    rng = np.random.default_rng(case)
+    for turn in range(3):
+        m.pool.v.view(torch.uint8).copy_(kept)
+        hits = np.zeros((3, ql, hkv, 128), bool)       # of +inf, -inf, NaN
+        for key in rng.choice(seen_by_some, size=6, replace=False):
+            head, dim, kind = rng.integers(hkv), rng.integers(128), 2 if kv8 else rng.integers(3)
+            page = m.pool.v.view(torch.uint8) if kv8 else m.pool.v
+            page[int(m.table[0, key // 16]), head, dim, SWAP[key % 16]] = \
+                0xFF if kv8 else (math.inf, -math.inf, math.nan)[kind]
+            hits[kind, ow.sees(pos, key, window, sinks), head, dim] = True
+        hits = [torch.from_numpy(np.repeat(h, g, axis=1)).to(dev) for h in hits]
+        want = plain.clone()
+        want[hits[0]] = math.inf
+        want[hits[1]] = -math.inf
+        want[hits[2] | (hits[0] & hits[1])] = math.nan
+        got = m.run(ws, dtype, SCALE, batch=batch)
+        wrong = ~((got == want) | (got.isnan() & want.isnan()))
+        where = wrong.nonzero()[:4].tolist()
+        assert not where
+    assert D.dlfp_workspace_error(ws.buf) == 0
+
+
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("tn", [(0, 0, 0, 32), (0, 64, 0, 32), (0, 64, 0, 4)])
+def test_rows_that_are_not_numbers_beside_infinite_values(dev, ws, tn, dtype):
+    """A NaN query's row stays NaN where a value that it sees is infinite, and changes no
+    other row; a NaN key those of the rows that see it."""
+    ql, kl = 100, 400
+    m = Mix(dev, 8, 2, [ql], [kl], None, 0, False, seed=3)
+    batch = m.batch(D.dlfp_tuning(*tn))
+    want = m.run(ws, dtype, SCALE, batch=batch)
+
+    def put(page, key, head, dim, x):
+        at = (key % 16, dim) if page is m.pool.k else (dim, SWAP[key % 16])
+        page[(int(m.table[0, key // 16]), head, *at)] = x
+    put(m.pool.v, 340, 0, 5, math.inf)
+    put(m.pool.v, 100, 1, 7, -math.inf)
+    put(m.pool.k, 370, 1, 9, math.nan)
+    m.dq[60, 1, 3] = math.nan                           # its token at 360
+    want[40:, :4, 5] = math.inf
+    want[:, 4:, 7] = -math.inf
+    want[60, 1] = math.nan
+    want[70:, 4:] = math.nan
+    got = m.run(ws, dtype, SCALE, batch=batch)
+    wrong = ~((got == want) | (got.isnan() & want.isnan()))
+    where = wrong.nonzero()[:4].tolist()
+    assert not where
