@@ -417,6 +417,15 @@ def _append_args(dims, rope, positions, slot_mapping, q, k_new, v_new, q_out, k_
             v_cache.data_ptr())
 
 
+def _check_exponents(dims, k_cache, k_exp, v_exp) -> None:
+    shape = (k_cache.size(0), dims.num_kv_heads)
+    if (k_exp.shape != shape or v_exp.shape != shape or
+            not k_exp.element_size() == v_exp.element_size() == 1 or
+            not (k_exp.is_contiguous() and v_exp.is_contiguous()) or
+            not k_exp.get_device() == v_exp.get_device() == k_cache.get_device()):
+        raise ValueError("exponents must be uint8 [num_blocks][Hkv] beside the caches")
+
+
 def dlfp_rope_append(dims: dlfp_dims, rope: dlfp_rope, positions, slot_mapping, q, k_new, v_new,
                      q_out, k_cache, v_cache, stream=None) -> None:
     """q, q_out: bf16 [T][Hq][128], k_new, v_new: bf16 [T][Hkv][128] (tokens may be strided);
@@ -431,6 +440,14 @@ def dlfp_rope_append(dims: dlfp_dims, rope: dlfp_rope, positions, slot_mapping, 
 def dlfp_rope_append_kv8(dims: dlfp_dims, rope: dlfp_rope, positions, slot_mapping, q, k_new,
                          v_new, q_out, k_cache, v_cache, k_exp, v_exp, stream=None) -> None:
     """The same into 8-bit caches with their exponents (uint8 [num_blocks][Hkv])."""
+    _check_exponents(dims, k_cache, k_exp, v_exp)
+    _rope_append_kv8(dims, rope, positions, slot_mapping, q, k_new, v_new, q_out, k_cache, v_cache,
+                     k_exp, v_exp, stream)
+
+
+def _rope_append_kv8(dims, rope, positions, slot_mapping, q, k_new, v_new, q_out, k_cache, v_cache,
+                     k_exp, v_exp, stream):
+    """The call with exponents that are a pool's."""
     st = lib().dlfp_rope_append_kv8(*_append_args(dims, rope, positions, slot_mapping, q, k_new,
                                                   v_new, q_out, k_cache, v_cache),
                                     k_exp.data_ptr(), v_exp.data_ptr(), k_cache.shape[0],
@@ -440,7 +457,9 @@ def dlfp_rope_append_kv8(dims: dlfp_dims, rope: dlfp_rope, positions, slot_mappi
 
 
 def _check_attention(dims, meta, d_work, d_block_table, q, k_cache, v_cache, out, workspace):
-    shape = (meta.c.num_tokens, dims.num_q_heads, HEAD_DIM)
+    """Returns the block table's width."""
+    counts = meta.c
+    shape = (counts.num_tokens, dims.num_q_heads, HEAD_DIM)
     bf16, _, int32 = _types or _bind_types()
     if q.shape != shape or out.shape != shape or q.dtype is not bf16:
         raise ValueError("q and out must be [tokens][Hq][128], q bf16")
@@ -448,18 +467,22 @@ def _check_attention(dims, meta, d_work, d_block_table, q, k_cache, v_cache, out
         raise ValueError("the work list and the block table must be int32")
     if not (q.is_contiguous() and out.is_contiguous() and d_block_table.is_contiguous()):
         raise ValueError("q, out and the block table must be contiguous")
+    rows, max_blocks = d_block_table.shape
+    if d_work.numel() < WORK_INTS * counts.num_units or rows < counts.num_seqs:
+        raise ValueError("the work list or the block table is not the metadata's")
     device = q.get_device()
     _check_device(device == d_work.get_device() == d_block_table.get_device() ==
                   k_cache.get_device() == v_cache.get_device() == out.get_device() ==
                   workspace.get_device(), device, shape[0])
+    return max_blocks
 
 
 def dlfp_attention_window(dims: dlfp_dims, meta: Meta, d_work, d_block_table, q, k_cache, v_cache,
                           scale: float, out, workspace, stream=None) -> None:
     """meta: of dlfp_build_window_meta; bf16 caches; out dtype bfloat16 or float32."""
-    _check_attention(dims, meta, d_work, d_block_table, q, k_cache, v_cache, out, workspace)
+    max_blocks = _check_attention(dims, meta, d_work, d_block_table, q, k_cache, v_cache, out, workspace)
     st = lib().dlfp_attention_window(
-        dims, meta.c, d_work.data_ptr(), d_block_table.data_ptr(), d_block_table.shape[1],
+        dims, meta.c, d_work.data_ptr(), d_block_table.data_ptr(), max_blocks,
         k_cache.shape[0], q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), float(scale),
         out.data_ptr(), _out_code(out.dtype), workspace.data_ptr(), workspace.nbytes,
         _stream(stream))
@@ -470,9 +493,17 @@ def dlfp_attention_window(dims: dlfp_dims, meta: Meta, d_work, d_block_table, q,
 def dlfp_attention_kv8(dims: dlfp_dims, meta: Meta, d_work, d_block_table, q, k_cache, v_cache,
                        k_exp, v_exp, scale: float, out, workspace, stream=None) -> None:
     """The same over 8-bit caches with their exponents (uint8 [num_blocks][Hkv])."""
-    _check_attention(dims, meta, d_work, d_block_table, q, k_cache, v_cache, out, workspace)
+    _check_exponents(dims, k_cache, k_exp, v_exp)
+    _attention_kv8(dims, meta, d_work, d_block_table, q, k_cache, v_cache, k_exp, v_exp, scale, out,
+                   workspace, stream)
+
+
+def _attention_kv8(dims, meta, d_work, d_block_table, q, k_cache, v_cache, k_exp, v_exp, scale, out,
+                   workspace, stream):
+    """The call with exponents that are a pool's."""
+    max_blocks = _check_attention(dims, meta, d_work, d_block_table, q, k_cache, v_cache, out, workspace)
     st = lib().dlfp_attention_kv8(
-        dims, meta.c, d_work.data_ptr(), d_block_table.data_ptr(), d_block_table.shape[1],
+        dims, meta.c, d_work.data_ptr(), d_block_table.data_ptr(), max_blocks,
         k_cache.shape[0], q.data_ptr(), k_cache.data_ptr(), v_cache.data_ptr(), k_exp.data_ptr(),
         v_exp.data_ptr(), float(scale), out.data_ptr(), _out_code(out.dtype), workspace.data_ptr(),
         workspace.nbytes, _stream(stream))

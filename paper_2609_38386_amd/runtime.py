@@ -118,9 +118,7 @@ class Rope:
         return rope
 
 
-def _check_heads(dims: _d.dlfp_dims, pool):
-    if pool.num_kv_heads != dims.num_kv_heads:
-        raise ValueError("the pool has other KV heads than the dims")
+_OTHER_HEADS = "the pool has other KV heads than the dims"
 
 
 def rope_append(dims: _d.dlfp_dims, rope: Rope, pool, positions: torch.Tensor,
@@ -128,12 +126,13 @@ def rope_append(dims: _d.dlfp_dims, rope: Rope, pool, positions: torch.Tensor,
                 q_out: torch.Tensor, stream=None):
     """Rotate queries and keys to their positions and write keys and values into the pages
     of a KVPool or KVPool8."""
-    _check_heads(dims, pool)
+    if pool.num_kv_heads != dims.num_kv_heads:
+        raise ValueError(_OTHER_HEADS)
     if rope.table.get_device() != q.get_device():
         raise ValueError("the rope's table is on another device")
     if isinstance(pool, KVPool8):
-        _d.dlfp_rope_append_kv8(dims, rope.c, positions, slots, q, k_new, v_new, q_out, pool.k,
-                                pool.v, pool.k_exp, pool.v_exp, stream)
+        _d._rope_append_kv8(dims, rope.c, positions, slots, q, k_new, v_new, q_out, pool.k, pool.v,
+                            pool.k_exp, pool.v_exp, stream)
     else:
         _d.dlfp_rope_append(dims, rope.c, positions, slots, q, k_new, v_new, q_out, pool.k, pool.v,
                             stream)
@@ -203,10 +202,11 @@ def window_attention(dims: _d.dlfp_dims, meta: _d.Meta, d_work: torch.Tensor,
                      d_block_table: torch.Tensor, pool, q: torch.Tensor, scale: float,
                      out: torch.Tensor, workspace: torch.Tensor, stream=None):
     """Attention over the pages of a KVPool or KVPool8, metadata of dlfp_build_window_meta."""
-    _check_heads(dims, pool)
+    if pool.num_kv_heads != dims.num_kv_heads:
+        raise ValueError(_OTHER_HEADS)
     if isinstance(pool, KVPool8):
-        _d.dlfp_attention_kv8(dims, meta, d_work, d_block_table, q, pool.k, pool.v, pool.k_exp,
-                              pool.v_exp, scale, out, workspace, stream)
+        _d._attention_kv8(dims, meta, d_work, d_block_table, q, pool.k, pool.v, pool.k_exp,
+                          pool.v_exp, scale, out, workspace, stream)
     else:
         _d.dlfp_attention_window(dims, meta, d_work, d_block_table, q, pool.k, pool.v, scale, out,
                                  workspace, stream)

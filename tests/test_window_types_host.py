@@ -86,3 +86,33 @@ def test_windows_past_32_bits(window, sinks):
         with pytest.raises(ValueError, match="32 bits"):
             batch()
     rt.WindowBatch(DIMS, [1], [60], np.zeros((1, 4), np.int32), 1, "cpu", 2 ** 31 - 1, 2 ** 31 - 1)
+
+
+def test_lists_and_tables_shorter_than_the_metadata():
+    """A work list or block table that does not hold what the metadata counts."""
+    pool = rt.KVPool(4, 8, "cpu")
+    batch = rt.WindowBatch(DIMS, [3, 1], [3, 40], np.arange(6, dtype=np.int32).reshape(2, 3) % 4, 4, "cpu")
+    ws = SimpleNamespace(ensure=lambda *a: torch.zeros(1 << 20, dtype=torch.uint8))
+    q = torch.zeros((4, 16, 128), dtype=torch.bfloat16)
+    for name, short in (("d_work", batch.d_work[:-1]), ("d_block_table", batch.d_block_table[:1]),
+                        ("d_work", batch.d_work[::2])):
+        kept = getattr(batch, name)
+        setattr(batch, name, short)
+        with pytest.raises(ValueError, match="metadata|contiguous"):
+            batch.attention(pool, q, 0.1, q.clone(), ws)
+        setattr(batch, name, kept)
+
+
+def test_exponents_of_the_binding():
+    """The calls under a pool's take its four tensors apart."""
+    pool = rt.KVPool8(4, 8, "cpu")
+    q, k = torch.zeros((3, 16, 128), dtype=torch.bfloat16), torch.zeros((3, 8, 128), dtype=torch.bfloat16)
+    at = torch.zeros(3, dtype=torch.int32)
+    meta = rt.WindowBatch(DIMS, [3], [3], np.zeros((1, 1), np.int32), 4, "cpu")
+    for bad in (pool.k_exp[:3], pool.k_exp[:, :7], pool.k_exp.to(torch.int32), pool.k_exp.t()):
+        for exps in ((bad, pool.v_exp), (pool.k_exp, bad)):
+            with pytest.raises(ValueError, match="exponents"):
+                D.dlfp_rope_append_kv8(DIMS, rt.Rope(4, "cpu").c, at, at, q, k, k, q, pool.k, pool.v, *exps)
+            with pytest.raises(ValueError, match="exponents"):
+                D.dlfp_attention_kv8(DIMS, meta.meta, meta.d_work, meta.d_block_table, q, pool.k,
+                                     pool.v, *exps, 0.1, q.clone(), torch.zeros(1 << 20, dtype=torch.uint8))
