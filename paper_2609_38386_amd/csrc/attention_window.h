@@ -1860,18 +1860,19 @@ int attention_window(const dlfp_dims* dims, const dlfp_meta* meta, const int32_t
   // Decode units of a wavefront each spend no workgroup on their start and sum, but
   // last four times as long: 29 ns a key of bf16 pages, 25 of 8-bit ones.  They are
   // - those of up to 128 KiB of cache that are more than two for each compute unit, a
-  //   further round of workgroups (8-bit pages: 640 units of 64 keys 6.9 us, of four
-  //   wavefronts 11.1, 2048 10.2 and 20.9, 2048 of 512 keys 45.7 and 49.6; bf16: 640
-  //   of 256 keys 15.4 and 16.4, 2048 of 128 23.9 and 27.2);
+  //   further round of workgroups (8-bit pages: 640 units of 64 keys 6.1 us, of four
+  //   wavefronts 10.0, 2048 10.1 and 21.3, 2048 of 512 keys 44.4 and 48.3; bf16: 640
+  //   of 256 keys 16.1 and 17.2, 2048 of 128 23.8 and 27.1);
   // - beside prefill units those that last up to a quarter of the launch, by its
   //   operations at 1120 TFLOP/s and its bytes at 6.4 TB/s, or 0.45 of it where the
   //   prompts are a third of it or more and hide the last of them, and every compute
-  //   unit gets some (8-bit pages: 500 decoders of 64 keys beside 512 tokens 33.4 us,
-  //   of four wavefronts 59.4, of 256 keys 63.5 and 79.5; 128 windowed ones of 2048
-  //   keys beside 1999 tokens 128 and 138, of 1024 to 8192 keys 384 and 427, bf16 188
-  //   and 200, 522 and 522; not 70 of 500 keys beside 512 tokens, which last longer,
-  //   33.3 and 28.9, 32 of 2000 beside 1024, 76 and 58, nor bf16, 16 of 9 to 37
-  //   thousand in 792 units beside 328, 396 and 357).
+  //   unit gets some (8-bit pages: 500 decoders of 64 keys beside 512 tokens 32.4 us,
+  //   of four wavefronts 57.1, of 256 keys 61.4 and 77.5; 128 windowed ones of 2048
+  //   keys beside 1999 tokens 128 and 140, of 1024 to 8192 keys 388 and 428; not 70 of
+  //   500 keys beside 512 tokens, which last longer, 32.5 and 27.7, 32 of 2000 beside
+  //   1024, 86 and 43, nor bf16, 16 of 9 to 37 thousand in 792 units beside 328, 396 and
+  //   357.  The estimate leaves four wavefronts to bf16 pages of the 128 windowed ones
+  //   too, 187 and 200; those of 1024 to 8192 keys are equal, 523 and 520).
   const double key_us = (KV8 ? 256 : 512) / 6.4e6, tile_key_us = 128 * 512 / 1120e6;
   const double unit_us = meta->decode_split_tokens * (KV8 ? 25e-3 : 29e-3);
   const double prefill_us = 0.85 * a.num_prefill * meta->prefill_split_tokens * tile_key_us;
@@ -1912,9 +1913,9 @@ int attention_window(const dlfp_dims* dims, const dlfp_meta* meta, const int32_t
   }
   // Wavefronts of a decode unit in a launch of decode units alone.  Eight, with long
   // units on a quarter of the compute units: one lasts as long as its chain of steps
-  // (8 units of 2048 keys 15.0 us, with four 17.2).  Else four, two workgroups on a
-  // compute unit, one's start and sum behind the other (512 units of 1024 keys, 8
-  // bits: 23.2 us, with eight 26.5, with one 31.5).
+  // (8 units of 2048 keys, 8 bits: 14.7 us, with four 16.6; bf16 13.2 and 18.3).  Else
+  // four, two workgroups on a compute unit, one's start and sum behind the other (512
+  // units of 1024 keys, 8 bits: 24.8 us, with eight 27.6, with one 29.4).
   const int nw = a.solo ? 1 : a.num_units <= cus / 4 && meta->decode_split_tokens > 256 ? 8 : 4;
   const int grid = a.num_prefill + decode_wgs;
   (void)hipGetLastError();
