@@ -288,3 +288,17 @@ def test_rows_that_are_not_numbers_beside_infinite_values(dev, ws, tn, dtype):
     wrong = ~((got == want) | (got.isnan() & want.isnan()))
     where = wrong.nonzero()[:4].tolist()
     assert not where
+
+
+@pytest.mark.parametrize("kv8", [False, True])
+def test_batches_without_sequences(dev, ws, kv8):
+    """Nothing to do: nothing is launched, and a later call finds the workspace as it was."""
+    dims = D.make_dims(8, 2)
+    pool = rt.KVPool8(3, 2, dev) if kv8 else rt.KVPool(3, 2, dev, 0)
+    batch = rt.WindowBatch(dims, [], [], np.zeros((0, 2), np.int32), 3, dev, 16, 2)
+    q, k = (torch.empty((0, h, 128), dtype=BF16, device=dev) for h in (8, 2))
+    batch.append(rt.Rope(4, dev), pool, q, k, k, q)
+    batch.attention(pool, q, SCALE, q, ws)
+    m = Mix(dev, 8, 2, [20, 1], [200, 77], 40, 3, kv8)
+    m.check(m.run(ws, BF16, SCALE, D.dlfp_tuning(64, 64)), SCALE)
+    assert D.dlfp_workspace_error(ws.buf) == 0
