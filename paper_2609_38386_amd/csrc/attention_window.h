@@ -426,8 +426,8 @@ constexpr int window_lds() {
 // of 64 heads in a window of 4000 keys, bf16 pages, 538 GFLOP in 495 to 517 us (1.04 to
 // 1.09 PFLOP/s; a library product of 8192^3 1.23); 2 x 1999 tokens of 32 heads over
 // 8144 keys, 8-bit pages, 457 GFLOP in 392 to 421 us (1.09 to 1.17).  fp32 output has
-// three products for one with the values: 1450 tokens of 64 heads over 8533 keys 607 us,
-// with bf16 output 371; of products that is 1.22 PFLOP/s.
+// three products for one with the values: 1450 tokens of 64 heads over 8533 keys 612 to
+// 630 us, with bf16 output 371; of products that is 1.18 to 1.21 PFLOP/s.
 template <int G, bool KV8, bool OUT32, bool CAREFUL>
 __device__ __forceinline__ void prefill_unit(const Args& a, const record_t f, char* smem,
                                              volatile int* special) {

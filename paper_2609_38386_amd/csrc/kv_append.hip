@@ -14,7 +14,8 @@
 // read-modify-write of its line.  A prompt's chunk rarely starts at a page, so
 // the page that a block writes is the full one that begins in it, wherever that
 // is: it ends in the next block, whose workgroup finds it by the same rule and
-// leaves its tokens out.  The launch is bound by its round trips (slots, tokens,
+// leaves its tokens out.  (Its values are read after the slots, the block's own having
+// been read beside them: twice in all.)  The launch is bound by its round trips (slots, tokens,
 // stores) up to about 2000 tokens and by its bytes from there.  Against pages
 // only where a block is one, with 8 heads: 2048 tokens from position 4099 9.9 ->
 // 6.7 us, 8192 from 1001 28.3 -> 15.7; from 4096, where a page's values are
