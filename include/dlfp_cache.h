@@ -67,7 +67,8 @@ typedef struct {
  * rounded once to bf16; values are copied.  A slot outside
  * [0, num_blocks * 16) leaves the pages as they are (the query is still
  * rotated); a token whose position is outside [0, positions) is left out
- * altogether.  Of two tokens with one slot, either may be kept.
+ * altogether.  Of two tokens with one slot, the key of either and the value of either
+ * may be kept.
  * Errors: DLFP_EINVAL, DLFP_EUNSUPPORTED (dims, rotary_dim), DLFP_ERANGE (2^32
  * threads or more, of which a token has 16 for each KV head and 64 for each group of
  * 16 query heads), DLFP_EHIP. */

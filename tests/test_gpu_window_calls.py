@@ -302,3 +302,26 @@ def test_batches_without_sequences(dev, ws, kv8):
     m = Mix(dev, 8, 2, [20, 1], [200, 77], 40, 3, kv8)
     m.check(m.run(ws, BF16, SCALE, D.dlfp_tuning(64, 64)), SCALE)
     assert D.dlfp_workspace_error(ws.buf) == 0
+
+
+@pytest.mark.parametrize("kv8", [False, True])
+@pytest.mark.parametrize("dtype", [BF16, FP32])
+@pytest.mark.parametrize("q_len,kv_len,tn", [
+    ([1, 1, 1], [700, 33, 1500], None), ([1, 1, 1], [700, 33, 1500], (128,)),
+    ([1] * 70, [40 + i for i in range(70)], None), ([100, 1], [300, 200], (0, 0, 0, 16)),
+    ([100, 20], [300, 200], (0, 64, 0, 8)), ([1] * 300 + [1500], [100] * 300 + [1500], None)])
+def test_queries_that_are_not_finite(dev, ws, q_len, kv_len, tn, dtype, kv8):
+    """A row's head whose query holds a NaN or an infinity is NaN, every other as it was."""
+    m = Mix(dev, 16, 2, q_len, kv_len, None, 0, kv8, seed=9)
+    batch = m.batch(D.dlfp_tuning(*tn) if tn else None)
+    want = m.run(ws, dtype, SCALE, batch=batch)
+    n = sum(q_len)
+    for row, head, dim, x in ((0, 3, 7, math.nan), (n // 2, 9, 100, math.inf), (n - 1, 15, 0, -math.inf),
+                              (n - 1, 8, 127, math.nan)):
+        m.dq[row, head, dim] = x
+        want[row, head] = math.nan
+    got = m.run(ws, dtype, SCALE, batch=batch)
+    wrong = ~((got == want) | (got.isnan() & want.isnan()))
+    where = wrong.nonzero()[:4].tolist()
+    assert not where
+    assert D.dlfp_workspace_error(ws.buf) == 0
