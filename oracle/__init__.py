@@ -22,6 +22,8 @@ Contents, each written from the definition it cites:
   positions, slot mapping) and a validity checker for work lists.
 * ``controller`` -- the proportional chunk controller, Eq. 2 (Sec. 3.1), with
   its guard and reset rules.
+* ``ffn``        -- 4-bit weights (values, nearest codes) and the gated feed-forward
+  projection.
 * ``stats``      -- paired Student-t confidence intervals (Sec. 4.3, Table 1).
 
 Parity status: every function here is pinned by ``tests/test_oracle_*.py``

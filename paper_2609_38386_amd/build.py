@@ -20,7 +20,7 @@ ARCH = "gfx950"
 
 SOURCES = ["attention_window.hip", "attention_kv8.hip", "attention_mixed.hip", "dlfp_host.cpp",
            "dlfp_cache.cpp", "dlfp_timer.cpp", "kv_append.hip", "kv8_append.hip", "stream_hold.hip",
-           "linear.hip"]
+           "linear.hip", "linear4.hip", "gated_linear.hip", "weights4.hip"]
 
 # Packed FP32 instructions are kept out of device code.
 DEVICE_FLAGS = ["-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops"]

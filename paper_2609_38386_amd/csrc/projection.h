@@ -1,0 +1,23 @@
+// What the projection entry points of dlfp_ffn.h share: arguments, their checks and launches.
+#pragma once
+
+#include <hip/hip_runtime.h>
+
+#include <cstdint>
+
+namespace dlfp {
+
+// out = x W^T, or act(x G^T) * (x U^T): weights [0] are W or G, [1] are U.
+struct ProjectionArgs {
+  const uint16_t* x;
+  const void* weights[2];        // bf16, or codes
+  const uint8_t* exps[2];        // of codes
+  void* out;
+  int64_t ldx, ldo;
+  int32_t m, n, k, act, out_f32;
+  int32_t wide;  // bf16 output rows take 16-byte stores
+};
+
+int check_projection(const ProjectionArgs& a, bool gated, bool codes, int32_t out_dtype);
+
+}  // namespace dlfp

@@ -82,6 +82,12 @@ EXPORTS = ["dlfp_build_varlen_meta", "dlfp_kv_append", "dlfp_attention_mixed",
 CACHE_EXPORTS = ["dlfp_rope_append", "dlfp_rope_append_kv8", "dlfp_build_window_meta",
                  "dlfp_attention_window", "dlfp_attention_kv8"]
 
+# Declared in dlfp_ffn.h.
+FFN_EXPORTS = ["dlfp_quantize_w4", "dlfp_dequantize_w4", "dlfp_linear_w4",
+               "dlfp_gated_linear_bf16", "dlfp_gated_linear_w4"]
+W4_GROUP = 32
+ACTIVATIONS = {"silu": 0, "gelu": 1}
+
 
 class dlfp_rope(ctypes.Structure):
     _fields_ = [("table", ctypes.c_void_p), ("positions", ctypes.c_int32),
@@ -148,7 +154,13 @@ def lib():
     rest = [ctypes.c_float, vp, i32, vp, sz, vp]
     L.dlfp_attention_window.argtypes = attention + rest
     L.dlfp_attention_kv8.argtypes = attention + [vp, vp] + rest
-    for name in EXPORTS + CACHE_EXPORTS:
+    L.dlfp_quantize_w4.argtypes = [i32, i32, vp, i64, vp, vp, vp]
+    L.dlfp_dequantize_w4.argtypes = [i32, i32, vp, vp, vp, i64, vp]
+    L.dlfp_linear_w4.argtypes = [i32, i32, i32, vp, i64, vp, vp, vp, i64, i32, vp]
+    L.dlfp_gated_linear_bf16.argtypes = [i32, i32, i32, vp, i64, vp, vp, i32, vp, i64, i32, vp]
+    L.dlfp_gated_linear_w4.argtypes = [i32, i32, i32, vp, i64, vp, vp, vp, vp, i32, vp, i64, i32,
+                                       vp]
+    for name in EXPORTS + CACHE_EXPORTS + FFN_EXPORTS:
         if name != "dlfp_status_string":
             getattr(L, name).restype = ctypes.c_int
     _lib = L
@@ -523,6 +535,142 @@ def dlfp_linear_bf16(x, w, out, stream=None) -> None:
                                 out.stride(0), _out_code(out.dtype), _stream(stream))
     if st:
         _check(st, "dlfp_linear_bf16")
+
+
+def _check_codes(codes, exps):
+    """(n, k) of 4-bit weights: uint8 codes [n][k / 2], exponents [n][k / 32]."""
+    n, half = codes.shape
+    if exps.shape != (n, half // (W4_GROUP // 2)) or half % (W4_GROUP // 2):
+        raise ValueError("codes are [n][k / 2] and exponents [n][k / 32]")
+    uint8 = _byte or _bind_byte()
+    if not codes.dtype is exps.dtype is uint8:
+        raise ValueError("codes and exponents must be uint8")
+    if not (codes.is_contiguous() and exps.is_contiguous()):
+        raise ValueError("codes and exponents must be contiguous")
+    return n, 2 * half
+
+
+_byte = None
+
+
+def _bind_byte():
+    global _byte
+    import torch
+    _byte = torch.uint8
+    return _byte
+
+
+def _row_stride(t, rows, columns, what):
+    """Elements between the rows of a [rows][columns] tensor whose rows are contiguous."""
+    if t.shape != (rows, columns):
+        raise ValueError(f"{what} must be [{rows}][{columns}]")
+    step, one = t.stride()
+    if one != 1 and columns > 1:
+        raise ValueError(f"rows of {what} must be contiguous")
+    return step if rows > 1 else columns + -columns % 8
+
+
+def _projection_rows(x, n, k, out):
+    """(m, row strides of x and out, code of out's type)."""
+    m = x.size(0)
+    if x.dtype is not (_types or _bind_types())[0]:
+        raise ValueError("x must be bf16")
+    return m, _row_stride(x, m, k, "x"), _row_stride(out, m, n, "out"), _out_code(out.dtype)
+
+
+def _convert_args(w, codes, exps):
+    n, k = _check_codes(codes, exps)
+    if w.dtype is not (_types or _bind_types())[0]:
+        raise ValueError("w must be bf16")
+    ldw = _row_stride(w, n, k, "w")
+    device = w.get_device()
+    _check_device(device == codes.get_device() == exps.get_device(), device, n)
+    return n, k, ldw
+
+
+def dlfp_quantize_w4(w, codes, exps, stream=None) -> None:
+    """w: bf16 [n][k] (rows may be strided) to codes uint8 [n][k / 2] and exponents uint8
+    [n][k / 32]."""
+    n, k, ldw = _convert_args(w, codes, exps)
+    st = lib().dlfp_quantize_w4(n, k, w.data_ptr(), ldw, codes.data_ptr(), exps.data_ptr(),
+                                _stream(stream))
+    if st:
+        _check(st, "dlfp_quantize_w4")
+
+
+def dlfp_dequantize_w4(codes, exps, w, stream=None) -> None:
+    """The values of 4-bit weights into w: bf16 [n][k] (rows may be strided)."""
+    n, k, ldw = _convert_args(w, codes, exps)
+    st = lib().dlfp_dequantize_w4(n, k, codes.data_ptr(), exps.data_ptr(), w.data_ptr(), ldw,
+                                  _stream(stream))
+    if st:
+        _check(st, "dlfp_dequantize_w4")
+
+
+def dlfp_linear_w4(x, codes, exps, out, stream=None) -> None:
+    """out[i][j] = sum_l x[i][l] W[j][l]; x: bf16 [m][k] (rows may be strided), W in 4 bits, out:
+    bf16 or float32 [m][n] (rows may be strided)."""
+    n, k = _check_codes(codes, exps)
+    _linear_w4(x, codes, exps, n, k, out, stream)
+
+
+def _linear_w4(x, codes, exps, n, k, out, stream):
+    """The call with codes and exponents that are a Weights4's."""
+    m, ldx, ldo, code = _projection_rows(x, n, k, out)
+    device = x.get_device()
+    _check_device(device == codes.get_device() == exps.get_device() == out.get_device(), device, m)
+    st = lib().dlfp_linear_w4(m, n, k, x.data_ptr(), ldx, codes.data_ptr(), exps.data_ptr(),
+                              out.data_ptr(), ldo, code, _stream(stream))
+    if st:
+        _check(st, "dlfp_linear_w4")
+
+
+def _activation(name) -> int:
+    code = ACTIVATIONS.get(name)
+    if code is None:
+        raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}")
+    return code
+
+
+def dlfp_gated_linear_bf16(x, w_gate, w_up, out, activation: str = "silu", stream=None) -> None:
+    """out = act(x G^T) * (x U^T); x: bf16 [m][k] (rows may be strided), w_gate, w_up: bf16 [n][k],
+    out: bf16 or float32 [m][n] (rows may be strided)."""
+    n, k = w_gate.shape
+    bf16 = (_types or _bind_types())[0]
+    if w_up.shape != (n, k) or not w_gate.dtype is w_up.dtype is bf16:
+        raise ValueError("gate and up must be bf16 [n][k] both")
+    if not (w_gate.is_contiguous() and w_up.is_contiguous()):
+        raise ValueError("gate and up must be contiguous")
+    m, ldx, ldo, code = _projection_rows(x, n, k, out)
+    device = x.get_device()
+    _check_device(device == w_gate.get_device() == w_up.get_device() == out.get_device(), device, m)
+    st = lib().dlfp_gated_linear_bf16(m, n, k, x.data_ptr(), ldx, w_gate.data_ptr(),
+                                      w_up.data_ptr(), _activation(activation), out.data_ptr(),
+                                      ldo, code, _stream(stream))
+    if st:
+        _check(st, "dlfp_gated_linear_bf16")
+
+
+def dlfp_gated_linear_w4(x, gate_codes, gate_exps, up_codes, up_exps, out,
+                         activation: str = "silu", stream=None) -> None:
+    """The same with both weights in 4 bits."""
+    n, k = _check_codes(gate_codes, gate_exps)
+    if _check_codes(up_codes, up_exps) != (n, k):
+        raise ValueError("gate and up must be [n][k] both")
+    _gated_linear_w4(x, gate_codes, gate_exps, up_codes, up_exps, n, k, out, activation, stream)
+
+
+def _gated_linear_w4(x, gate_codes, gate_exps, up_codes, up_exps, n, k, out, activation, stream):
+    m, ldx, ldo, code = _projection_rows(x, n, k, out)
+    device = x.get_device()
+    _check_device(device == gate_codes.get_device() == gate_exps.get_device() ==
+                  up_codes.get_device() == up_exps.get_device() == out.get_device(), device, m)
+    st = lib().dlfp_gated_linear_w4(m, n, k, x.data_ptr(), ldx, gate_codes.data_ptr(),
+                                    gate_exps.data_ptr(), up_codes.data_ptr(), up_exps.data_ptr(),
+                                    _activation(activation), out.data_ptr(), ldo, code,
+                                    _stream(stream))
+    if st:
+        _check(st, "dlfp_gated_linear_w4")
 
 
 def dlfp_workspace_init(workspace, stream=None) -> None:

@@ -138,6 +138,69 @@ def rope_append(dims: _d.dlfp_dims, rope: Rope, pool, positions: torch.Tensor,
                             stream)
 
 
+class Weights4:
+    """Weights of a linear layer in 4 bits: e2m1 codes uint8 [n][k / 2] (a row for each output
+    feature, the even column in a byte's low half) and exponent bytes uint8 [n][k / 32] (a code
+    c stands for c 2^(byte - 127)).  New weights are zeros."""
+
+    def __init__(self, n: int, k: int, device):
+        if k % _d.W4_GROUP:
+            raise ValueError("k must be a multiple of 32")
+        self._set(torch.zeros((n, k // 2), dtype=torch.uint8, device=device),
+                  torch.full((n, k // _d.W4_GROUP), 127, dtype=torch.uint8, device=device))
+
+    def _set(self, codes, exps):
+        self.codes, self.exps = codes, exps
+        self.n, self.k = _d._check_codes(codes, exps)
+        if codes.device != exps.device:
+            raise ValueError("codes and exponents are on different devices")
+
+    @classmethod
+    def of(cls, codes: torch.Tensor, exps: torch.Tensor) -> "Weights4":
+        """Weights over two tensors that are there already."""
+        weights = cls.__new__(cls)
+        weights._set(codes, exps)
+        return weights
+
+    @classmethod
+    def from_bf16(cls, w: torch.Tensor, stream=None) -> "Weights4":
+        """New weights nearest to w: bf16 [n][k]."""
+        weights = cls(w.size(0), w.size(1), w.device)
+        weights.quantize(w, stream)
+        return weights
+
+    def quantize(self, w: torch.Tensor, stream=None):
+        """Take the values nearest to w: bf16 [n][k] (rows may be strided)."""
+        _d.dlfp_quantize_w4(w, self.codes, self.exps, stream)
+
+    def dequantize(self, w: torch.Tensor, stream=None):
+        """Write the values into w: bf16 [n][k] (rows may be strided)."""
+        _d.dlfp_dequantize_w4(self.codes, self.exps, w, stream)
+
+
+def linear(x: torch.Tensor, w, out: torch.Tensor, stream=None):
+    """out = x W^T: x bf16 [m][k], w a Weights4 or bf16 [n][k], out bf16 or float32 [m][n]."""
+    if isinstance(w, Weights4):
+        _d._linear_w4(x, w.codes, w.exps, w.n, w.k, out, stream)
+    else:
+        _d.dlfp_linear_bf16(x, w, out, stream)
+
+
+def gated_linear(x: torch.Tensor, gate, up, out: torch.Tensor, activation: str = "silu",
+                 stream=None):
+    """out = act(x G^T) * (x U^T), both weights a Weights4 or both bf16 [n][k]; activation "silu"
+    or "gelu" (the tanh form)."""
+    four = isinstance(gate, Weights4)
+    if four != isinstance(up, Weights4):
+        raise ValueError("gate and up must be of one kind")
+    if not four:
+        return _d.dlfp_gated_linear_bf16(x, gate, up, out, activation, stream)
+    if (gate.n, gate.k) != (up.n, up.k):
+        raise ValueError("gate and up must be [n][k] both")
+    _d._gated_linear_w4(x, gate.codes, gate.exps, up.codes, up.exps, gate.n, gate.k, out,
+                        activation, stream)
+
+
 class Workspace:
     """Caller-owned split-K workspace, grown on demand; header and counters zeroed
     once per allocation (every launch leaves the counters zero again)."""

@@ -1,0 +1,210 @@
+"""Host side of 4-bit weights and the gated projection (no GPU): the oracle's pins, the exports,
+and every refusal."""
+import math
+import os
+import re
+
+import numpy as np
+import pytest
+import torch
+
+import _projections as pj
+from oracle import ffn as of
+from paper_2609_38386_amd import dlfp as D
+from paper_2609_38386_amd import runtime as rt
+
+ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
+
+
+def test_library_exports_every_declared_symbol():
+    txt = open(os.path.join(ROOT, "include", "dlfp_ffn.h")).read()
+    txt = re.sub(r"/\*.*?\*/", "", txt, flags=re.S)
+    declared = sorted(re.findall(r"\bint\s+(dlfp_\w+)\s*\(", txt))
+    assert declared == sorted(D.FFN_EXPORTS)
+    for name in declared:
+        assert hasattr(D.lib(), name)
+
+
+# ------------------------------------------------------------------- the oracle
+
+def test_code_values():
+    assert of.VALUES[:8].tolist() == [0, 0.5, 1, 1.5, 2, 3, 4, 6]
+    assert of.VALUES[8:].tolist() == [-0.0, -0.5, -1, -1.5, -2, -3, -4, -6]
+
+
+def test_values_of_a_row_by_hand():
+    codes = np.zeros((1, 16), np.uint8)
+    codes[0, 0], codes[0, 15] = 0x91, 0x70     # columns 0, 1 and 31
+    v = of.values(codes, np.array([[129]], np.uint8))
+    assert v[0, 0] == 2.0 and v[0, 1] == -2.0 and v[0, 31] == 24.0 and not v[0, 2:31].any()
+
+
+def test_quantize_by_hand():
+    w = np.zeros((1, 64))
+    w[0, :5] = [12.0, -1.0, 0.5, 1.5, -11.0]   # exponent 1: 6, -0.5, 0.25 -> 0, 0.75 -> 1, -5.5 -> -6
+    w[0, 32] = 6.5                             # past 6: the next exponent, 3.25 -> 3
+    codes, exps = of.quantize(w)
+    assert exps.tolist() == [[128, 128]]
+    assert codes[0, :5].tolist() == [7, 9, 0, 2, 15] and codes[0, 32] == 5
+
+
+def test_quantize_is_the_nearest_of_all_values():
+    rng = np.random.default_rng(3)
+    w = rng.standard_normal((6, 96)) * 2.0 ** rng.integers(-20, 20, (6, 1))
+    codes, exps = of.quantize(w)
+    scale = np.repeat(2.0 ** (exps.astype(float) - 127), 32, axis=1)
+    every = of.VALUES[None, None] * scale[..., None]
+    best = np.abs(every - w[..., None]).min(-1)
+    assert np.array_equal(np.abs(of.VALUES[codes] * scale - w), best)
+    most = np.abs(w).reshape(6, 3, 32).max(-1)
+    assert (most <= 6 * 2.0 ** (exps.astype(float) - 127)).all()
+    assert (most > 6 * 2.0 ** (exps.astype(float) - 128)).all()
+
+
+def test_activations_by_closed_forms():
+    g = np.linspace(-30, 30, 101)
+    assert np.allclose(of.activate(g, "silu"), g * 0.5 * (1 + np.tanh(g / 2)), rtol=1e-12, atol=1e-15)
+    t = np.tanh(math.sqrt(2 / math.pi) * (g + 0.044715 * g ** 3))
+    assert np.allclose(of.activate(g, "gelu"), 0.5 * g * (1 + t), rtol=1e-9, atol=1e-14)
+    slope = max(np.abs(np.diff(of.activate(x, a)) / np.diff(x)).max()
+                for a in ("silu", "gelu") for x in (np.linspace(-8, 8, 100001),))
+    assert slope < pj.SLOPE
+
+
+def test_bounds_reject_what_is_wrong():
+    """A dropped column, gate and up exchanged, neighbouring codes exchanged, a group's scale
+    doubled: each is far outside the bounds."""
+    rng = np.random.default_rng(8)
+    x = rng.standard_normal((4, 256))
+    gen = torch.Generator().manual_seed(1)
+    codes, exps = (t.numpy() for t in pj.random_codes(gen, 16, 256))
+    w = of.values(codes, exps)
+    want, bound = pj.linear(x, w, torch.bfloat16)
+    other = [of.values((codes >> 4 | codes << 4).astype(np.uint8), exps)]
+    bumped = exps.copy()
+    bumped[:, 3] += 1
+    other.append(of.values(codes, bumped))
+    short = w.copy()
+    short[:, 17] = 0
+    other.append(short)
+    for v in other:
+        assert (np.abs(x @ v.T - want) > bound).mean() > 0.5
+    up = rng.standard_normal((16, 256)) / 16
+    want, bound = pj.gated(x, w, up, "silu", torch.bfloat16)
+    assert (np.abs(of.gated_linear(x, up, w) - want) > bound).mean() > 0.9
+    assert (np.abs(of.gated_linear(x, w, up, "gelu") - want) > bound).mean() > 0.5
+
+
+# ------------------------------------------------------------------- refusals of the C calls
+
+P = 1 << 20        # an address: nothing is launched
+
+
+def _linear(m=4, n=32, k=64, x=P, ldx=64, codes=P, exps=P, out=P, ldo=32, dtype=0):
+    return D.lib().dlfp_linear_w4(m, n, k, x, ldx, codes, exps, out, ldo, dtype, None)
+
+
+def _gated4(m=4, n=32, k=64, x=P, ldx=64, gc=P, ge=P, uc=P, ue=P, act=0, out=P, ldo=32, dtype=0):
+    return D.lib().dlfp_gated_linear_w4(m, n, k, x, ldx, gc, ge, uc, ue, act, out, ldo, dtype, None)
+
+
+def _gated(m=4, n=32, k=64, x=P, ldx=64, gate=P, up=P, act=0, out=P, ldo=32, dtype=0):
+    return D.lib().dlfp_gated_linear_bf16(m, n, k, x, ldx, gate, up, act, out, ldo, dtype, None)
+
+
+COMMON = [(dict(m=-1), -1), (dict(n=0), -1), (dict(n=-16), -1), (dict(k=0), -1), (dict(k=-64), -1),
+          (dict(n=24), -5), (dict(k=96, ldx=96), -5), (dict(n=8, ldo=8), -5), (dict(k=32), -5),
+          (dict(ldx=56), -1), (dict(ldx=68), -1), (dict(ldo=28), -1), (dict(ldo=34), -1),
+          (dict(ldx=0), -1), (dict(ldo=-32), -1), (dict(dtype=2), -1), (dict(dtype=-1), -1),
+          (dict(x=None), -1), (dict(out=None), -1), (dict(x=P + 8), -1), (dict(out=P + 4), -1),
+          (dict(out=P + 8, dtype=1), -1)]
+
+
+@pytest.mark.parametrize("change,status", COMMON + [(dict(codes=None), -1), (dict(exps=None), -1),
+                                                    (dict(codes=P + 8), -1)])
+def test_linear_w4_refusals(change, status):
+    assert _linear(**change) == status
+
+
+@pytest.mark.parametrize("change,status", COMMON + [(dict(gc=None), -1), (dict(ge=None), -1),
+                                                    (dict(uc=None), -1), (dict(ue=None), -1),
+                                                    (dict(gc=P + 4), -1), (dict(uc=P + 8), -1),
+                                                    (dict(act=2), -1), (dict(act=-1), -1)])
+def test_gated_linear_w4_refusals(change, status):
+    assert _gated4(**change) == status
+
+
+@pytest.mark.parametrize("change,status", COMMON + [(dict(gate=None), -1), (dict(up=None), -1),
+                                                    (dict(gate=P + 8), -1), (dict(up=P + 2), -1),
+                                                    (dict(act=2), -1)])
+def test_gated_linear_bf16_refusals(change, status):
+    assert _gated(**change) == status
+
+
+def test_no_tokens_need_no_addresses():
+    assert _linear(m=0, x=None, codes=None, exps=None, out=None) == 0
+    assert _gated4(m=0, x=None, gc=None, ge=None, uc=None, ue=None, out=None) == 0
+    assert _gated(m=0, x=None, gate=None, up=None, out=None) == 0
+    assert _linear(m=0, n=24) == -5 and _gated(m=0, act=7) == -1
+
+
+@pytest.mark.parametrize("change,status", [
+    (dict(n=-1), -1), (dict(k=0), -1), (dict(k=48, ldw=48), -5), (dict(ldw=56), -1),
+    (dict(ldw=68), -1), (dict(w=None), -1), (dict(codes=None), -1), (dict(exps=None), -1),
+    (dict(w=P + 8), -1), (dict(codes=P + 8), -1), (dict(n=1 << 20, k=1 << 14, ldw=1 << 14), -2),
+    (dict(n=0, w=None, codes=None, exps=None), 0)])
+def test_conversion_refusals(change, status):
+    a = dict(n=4, k=64, w=P, ldw=64, codes=P, exps=P)
+    a.update(change)
+    L = D.lib()
+    assert L.dlfp_quantize_w4(a["n"], a["k"], a["w"], a["ldw"], a["codes"], a["exps"], None) == status
+    assert L.dlfp_dequantize_w4(a["n"], a["k"], a["codes"], a["exps"], a["w"], a["ldw"],
+                                None) == status
+
+
+# ------------------------------------------------------------------- refusals from Python
+
+def _bf16(*shape):
+    return torch.zeros(shape, dtype=torch.bfloat16)
+
+
+def test_python_refusals():
+    w = rt.Weights4(32, 64, "cpu")
+    x, out = _bf16(2, 64), _bf16(2, 32)
+    bad = [lambda: rt.linear(x, w, out),                                   # on the host
+           lambda: rt.linear(x.float(), w, out),
+           lambda: rt.linear(x[:, :32], w, out),
+           lambda: rt.linear(x, w, out[:, :16]),
+           lambda: rt.linear(x, w, _bf16(3, 32)),
+           lambda: rt.linear(_bf16(2, 128)[:, ::2], w, out),
+           lambda: rt.linear(x, w, _bf16(32, 2).T),
+           lambda: rt.gated_linear(x, w, w, out, activation="relu"),
+           lambda: rt.gated_linear(x, w, rt.Weights4(16, 64, "cpu"), out),
+           lambda: rt.gated_linear(x, w, _bf16(32, 64), out),
+           lambda: rt.gated_linear(x, _bf16(32, 64), w, out),
+           lambda: rt.gated_linear(x, _bf16(32, 64), _bf16(16, 64), out),
+           lambda: rt.gated_linear(x, _bf16(32, 64), _bf16(32, 64).float(), out),
+           lambda: rt.gated_linear(x, _bf16(32, 128)[:, :64], _bf16(32, 64), out),
+           lambda: rt.Weights4(4, 48, "cpu"),
+           lambda: rt.Weights4.of(w.codes, w.exps[:, :1]),
+           lambda: rt.Weights4.of(w.codes.int(), w.exps),
+           lambda: rt.Weights4.of(w.codes[:, :24], w.exps),
+           lambda: rt.Weights4.of(torch.zeros((32, 64), dtype=torch.uint8)[:, ::2], w.exps),
+           lambda: w.quantize(_bf16(32, 64).float()),
+           lambda: w.quantize(_bf16(32, 96)),
+           lambda: w.quantize(_bf16(32, 64)),                              # on the host
+           lambda: w.dequantize(_bf16(32, 64))]
+    for i, call in enumerate(bad):
+        with pytest.raises(ValueError):
+            call()
+            pytest.fail(f"call {i} was taken")
+    with pytest.raises(KeyError):
+        rt.linear(x, w, torch.zeros((2, 32), dtype=torch.float16))
+
+
+def test_python_takes_empty_batches():
+    w = rt.Weights4(32, 64, "cpu")
+    rt.linear(_bf16(0, 64), w, _bf16(0, 32), stream=0)
+    rt.gated_linear(_bf16(0, 64), w, w, _bf16(0, 32), stream=0)
+    rt.gated_linear(_bf16(0, 64), _bf16(32, 64), _bf16(32, 64), _bf16(0, 32), stream=0)
+    rt.Weights4(0, 64, "cpu").quantize(_bf16(0, 64), stream=0)
