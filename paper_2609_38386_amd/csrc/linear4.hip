@@ -4,7 +4,7 @@
 
 namespace dlfp {
 
-int check_projection(const ProjectionArgs& a, bool gated, bool codes, int32_t out_dtype) {
+int check_projection(ProjectionArgs& a, bool gated, bool codes, int32_t out_dtype) {
   if (a.m < 0 || a.n <= 0 || a.k <= 0) return DLFP_EINVAL;
   if (out_dtype != 0 && out_dtype != 1) return DLFP_EINVAL;
   if (gated && a.act != DLFP_SILU && a.act != DLFP_GELU) return DLFP_EINVAL;
@@ -17,6 +17,7 @@ int check_projection(const ProjectionArgs& a, bool gated, bool codes, int32_t ou
     if (!a.weights[i] || (reinterpret_cast<uintptr_t>(a.weights[i]) & 15)) return DLFP_EINVAL;
     if (codes && !a.exps[i]) return DLFP_EINVAL;
   }
+  a.wide = (reinterpret_cast<uintptr_t>(a.out) & 15) == 0 && a.ldo % 8 == 0;
   return DLFP_OK;
 }
 
@@ -34,7 +35,7 @@ int launch(const dlfp::ProjectionArgs& a, hipStream_t stream) {
 extern "C" int dlfp_linear_w4(int32_t m, int32_t n, int32_t k, const void* x, int64_t ldx,
                               const void* codes, const void* exps, void* out, int64_t ldo,
                               int32_t out_dtype, hipStream_t stream) {
-  const dlfp::ProjectionArgs a{static_cast<const uint16_t*>(x),
+  dlfp::ProjectionArgs a{static_cast<const uint16_t*>(x),
                                {codes, nullptr},
                                {static_cast<const uint8_t*>(exps), nullptr},
                                out, ldx, ldo, m, n, k, 0, out_dtype, 0};
@@ -47,7 +48,7 @@ extern "C" int dlfp_gated_linear_w4(int32_t m, int32_t n, int32_t k, const void*
                                     const void* up_codes, const void* up_exps, int32_t activation,
                                     void* out, int64_t ldo, int32_t out_dtype,
                                     hipStream_t stream) {
-  const dlfp::ProjectionArgs a{
+  dlfp::ProjectionArgs a{
       static_cast<const uint16_t*>(x),
       {gate_codes, up_codes},
       {static_cast<const uint8_t*>(gate_exps), static_cast<const uint8_t*>(up_exps)},

@@ -18,6 +18,7 @@ struct ProjectionArgs {
   int32_t wide;  // bf16 output rows take 16-byte stores
 };
 
-int check_projection(const ProjectionArgs& a, bool gated, bool codes, int32_t out_dtype);
+// DLFP_OK, or what is wrong with them; sets wide.
+int check_projection(ProjectionArgs& a, bool gated, bool codes, int32_t out_dtype);
 
 }  // namespace dlfp
