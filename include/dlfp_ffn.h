@@ -60,16 +60,23 @@ int dlfp_dequantize_w4(int32_t n, int32_t k, const void* codes, const void* exps
 /* Projection with 4-bit weights W:
  *   out[i][j] = sum_l x[i][l] * W[j][l],  i < m, j < n, l < k
  * x: device bf16, row i at x + i * ldx (ldx >= k, a multiple of 8, x 16-byte
- * aligned); codes (16-byte aligned), exps: device, as above; out: device, row i
+ * aligned); codes, exps (16-byte aligned): device, as above; out: device, row i
  * at out + i * ldo (ldo >= n, a multiple of 4), out_dtype 0 = bf16 (8-byte
  * aligned), 1 = fp32 (16-byte aligned).  Products are exact, sums are fp32 in an
- * order that depends on m, n and k, and are rounded once.  n must be a multiple
- * of 16 and k of 64 (DLFP_EUNSUPPORTED otherwise); m = 0 launches nothing.
- * Errors: DLFP_EINVAL, DLFP_EUNSUPPORTED, DLFP_ERANGE (2^32 threads or more, of
- * which 16 rows of out take up to 32 for each 16 features), DLFP_EHIP. */
+ * order that depends on m, n, k and the workspace, and are rounded once.  n must be a
+ * multiple of 16 and k of 64 (DLFP_EUNSUPPORTED otherwise); m = 0 launches nothing.
+ *
+ * workspace: device, 16-byte aligned, or null: where there are few tiles, K is split over
+ * workgroups, whose partial sums pass through it into a second launch.  How many bytes the
+ * fastest form takes dlfp_projection_workspace says; with fewer (0 with null) a form that
+ * fits is taken.  Its contents matter neither before nor after; calls that may overlap (on
+ * two streams, or as parts of graphs that may) need workspaces of their own.
+ * Errors: DLFP_EINVAL, DLFP_EUNSUPPORTED, DLFP_ERANGE (2^32 threads or more: a launch of
+ * many tokens has up to 512 for each 256 of them and 256 features, one with rows 2^22
+ * elements or more apart 512 for each 16 and 16), DLFP_EHIP. */
 int dlfp_linear_w4(int32_t m, int32_t n, int32_t k, const void* x, int64_t ldx, const void* codes,
-                   const void* exps, void* out, int64_t ldo, int32_t out_dtype,
-                   hipStream_t stream);
+                   const void* exps, void* out, int64_t ldo, int32_t out_dtype, void* workspace,
+                   size_t workspace_bytes, hipStream_t stream);
 
 /* Activations of the gated projection. */
 #define DLFP_SILU 0 /* g / (1 + e^-g) */
@@ -82,13 +89,22 @@ int dlfp_linear_w4(int32_t m, int32_t n, int32_t k, const void* x, int64_t ldx, 
  * are fp32 and are rounded once.  The rest as dlfp_linear_w4. */
 int dlfp_gated_linear_bf16(int32_t m, int32_t n, int32_t k, const void* x, int64_t ldx,
                            const void* w_gate, const void* w_up, int32_t activation, void* out,
-                           int64_t ldo, int32_t out_dtype, hipStream_t stream);
+                           int64_t ldo, int32_t out_dtype, void* workspace,
+                           size_t workspace_bytes, hipStream_t stream);
 
 /* The same with 4-bit weights. */
 int dlfp_gated_linear_w4(int32_t m, int32_t n, int32_t k, const void* x, int64_t ldx,
                          const void* gate_codes, const void* gate_exps, const void* up_codes,
                          const void* up_exps, int32_t activation, void* out, int64_t ldo,
-                         int32_t out_dtype, hipStream_t stream);
+                         int32_t out_dtype, void* workspace, size_t workspace_bytes,
+                         hipStream_t stream);
+
+/* Bytes of workspace that the fastest form of a projection takes (at most 32 MiB; 0 if it needs
+ * none, and for sizes that the call refuses). */
+#define DLFP_LINEAR_W4 0
+#define DLFP_GATED_LINEAR_BF16 1
+#define DLFP_GATED_LINEAR_W4 2
+int64_t dlfp_projection_workspace(int32_t kind, int32_t m, int32_t n, int32_t k);
 
 #ifdef __cplusplus
 }

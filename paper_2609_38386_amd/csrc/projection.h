@@ -18,7 +18,15 @@ struct ProjectionArgs {
   int32_t wide;  // bf16 output rows take 16-byte stores
 };
 
+// A launch whose K is split over `splits` workgroups a tile: the partial sums go to `part`,
+// [split][tile][unit of four features of a token] fp32, and a second launch adds them.
+struct Split {
+  float* part;
+  int32_t splits;
+};
+
 // DLFP_OK, or what is wrong with them; sets wide.
-int check_projection(ProjectionArgs& a, bool gated, bool codes, int32_t out_dtype);
+int check_projection(ProjectionArgs& a, bool gated, bool codes, int32_t out_dtype,
+                     const void* workspace);
 
 }  // namespace dlfp

@@ -162,6 +162,57 @@ __device__ __forceinline__ f32x4_t gated4(f32x4_t g, f32x4_t u, int act) {
   return v;
 }
 
+// The end of a tile whose K steps are split over the wavefronts: their sum, in wave order,
+// for the first TOKENS tokens.  Every wave is done with LDS.
+// A wave's accumulators are groups of four features: group (q, t, g) of lane l holds
+// features 32 q + 8 g + 4 (l / 32) .. + 3 of token 32 t + l % 32.  A thread sums and stores
+// eight consecutive features, neighbouring threads the next ones of the same token; the lane
+// index is XORed with g and q so that both the writes and these reads spread over the banks.
+template <int BN, int BM, int WAVES, int TOKENS, bool GATED>
+__device__ __forceinline__ void store_sums(const dlfp::ProjectionArgs& a, f32x16_t (&acc)[BN][BM],
+                                           char* smem, int tid, int wave, int n0, int m0) {
+  constexpr int GROUPS = BN * BM * 256;
+  const int lane = tid & 63;
+  f32x4_t* res = reinterpret_cast<f32x4_t*>(smem);
+  auto at = [](int q, int t, int g, int l) {
+    return ((q * BM + t) * 4 + g) * 64 + (l ^ (g << 2) ^ ((q & 1) << 1));
+  };
+#pragma unroll
+  for (int q = 0; q < BN; ++q)
+#pragma unroll
+    for (int t = 0; t < BM; ++t)
+#pragma unroll
+      for (int g = 0; g < 4; ++g)
+        res[wave * GROUPS + at(q, t, g, lane)] =
+            f32x4_t{acc[q][t][4 * g], acc[q][t][4 * g + 1], acc[q][t][4 * g + 2],
+                    acc[q][t][4 * g + 3]};
+  __syncthreads();
+  constexpr int EIGHTS = GATED ? 2 : 4;  // of features of a block
+  for (int u = tid; u < EIGHTS * BN * TOKENS; u += 64 * WAVES) {
+    const int g = u % EIGHTS, q = u / EIGHTS % BN, tok = u / EIGHTS / BN;
+    auto sum = [&](int g, f32x4_t& lo, f32x4_t& hi) {
+      const int ilo = at(q, tok >> 5, g, tok & 31), ihi = at(q, tok >> 5, g, 32 + (tok & 31));
+      lo = res[ilo];
+      hi = res[ihi];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) {
+        lo += res[w * GROUPS + ilo];
+        hi += res[w * GROUPS + ihi];
+      }
+    };
+    f32x4_t lo, hi;
+    sum(g, lo, hi);
+    if constexpr (GATED) {
+      f32x4_t ulo, uhi;
+      sum(g + 2, ulo, uhi);
+      lo = gated4(lo, ulo, a.act);
+      hi = gated4(hi, uhi, a.act);
+    }
+    const int n = n0 + 8 * EIGHTS * q + 8 * g;
+    if (m0 + tok < a.m && n < a.n) store8(a, m0 + tok, n, lo, hi);
+  }
+}
+
 // ---------------------------------------------------------------- split K
 
 // One TN x TM tile per workgroup; wave w computes K steps w, w + WAVES, ...
@@ -237,52 +288,49 @@ __global__ __launch_bounds__(64 * WAVES) void split_kernel(dlfp::ProjectionArgs 
     slot = slot + 1 == STAGES ? 0 : slot + 1;
   }
 
-  // Sum over the waves, in wave order.  A wave's accumulators are groups of
-  // four features: group (q, t, g) of lane l holds features
-  // 32 q + 8 g + 4 (l / 32) .. + 3 of token 32 t + l % 32.  A thread then sums
-  // and stores eight consecutive features, neighbouring threads the next ones
-  // of the same token; the lane index is XORed with g and q so that both the
-  // writes and these reads spread over the banks.
   wait_copies_barrier<0>();  // every wave is done with its ring
-  constexpr int GROUPS = TN * TM / 4;
-  f32x4_t* res = reinterpret_cast<f32x4_t*>(smem);
-  auto at = [](int q, int t, int g, int l) {
-    return ((q * BM + t) * 4 + g) * 64 + (l ^ (g << 2) ^ ((q & 1) << 1));
-  };
+  store_sums<BN, BM, WAVES, TM, GATED>(a, acc, smem, tid, wave, n0, m0);
+}
+
+// The end of a tile: through the wave's slice of LDS (`bytes` of them), so that whole
+// runs of a row are stored (straight from the accumulators a store covers 16 bytes of 32
+// rows; on m = 8192, n = 6144, k = 1024 the launch took 13% longer with those).  The
+// wave's part of the tile starts at feature n0 and token m0; every wave is done with LDS.
+template <int BN, int BM, int SLICE, bool GATED>
+__device__ __forceinline__ void store_tile(const dlfp::ProjectionArgs& a, f32x16_t (&acc)[BN][BM],
+                                           char* mine, int lane, int n0, int m0) {
+  const int lr = lane & 31, lh = lane >> 5;
+  constexpr int OF = GATED ? 16 : 32;      // features of a block
+  constexpr int FB = GATED ? 4 : 2;        // blocks per pass
+  static_assert(BN % FB == 0 || BN < FB, "passes");
+  constexpr int B = BN < FB ? BN : FB;
+  constexpr int RB = B * OF * 4 + 16;      // fp32 row of a pass, padded off the banks
+  static_assert(SLICE >= 32 * RB, "epilogue slice");
 #pragma unroll
-  for (int q = 0; q < BN; ++q)
+  for (int j = 0; j < BM; ++j)
 #pragma unroll
-    for (int t = 0; t < BM; ++t)
+    for (int p = 0; p < BN / B; ++p) {
 #pragma unroll
-      for (int g = 0; g < 4; ++g)
-        res[wave * GROUPS + at(q, t, g, lane)] =
-            f32x4_t{acc[q][t][4 * g], acc[q][t][4 * g + 1], acc[q][t][4 * g + 2],
-                    acc[q][t][4 * g + 3]};
-  __syncthreads();
-  constexpr int EIGHTS = GATED ? 2 : 4;  // of features of a block
-  for (int u = tid; u < GROUPS / 8 * EIGHTS; u += 64 * WAVES) {
-    const int g = u % EIGHTS, q = u / EIGHTS % BN, tok = u / EIGHTS / BN;
-    auto sum = [&](int g, f32x4_t& lo, f32x4_t& hi) {
-      const int ilo = at(q, tok >> 5, g, tok & 31), ihi = at(q, tok >> 5, g, 32 + (tok & 31));
-      lo = res[ilo];
-      hi = res[ihi];
+      for (int i = 0; i < B; ++i)
 #pragma unroll
-      for (int w = 1; w < WAVES; ++w) {
-        lo += res[w * GROUPS + ilo];
-        hi += res[w * GROUPS + ihi];
+        for (int g = 0; g < OF / 8; ++g) {
+          const f32x16_t& c = acc[p * B + i][j];
+          f32x4_t v = {c[4 * g], c[4 * g + 1], c[4 * g + 2], c[4 * g + 3]};
+          if constexpr (GATED)
+            v = gated4(v, f32x4_t{c[8 + 4 * g], c[9 + 4 * g], c[10 + 4 * g], c[11 + 4 * g]}, a.act);
+          *reinterpret_cast<f32x4_t*>(mine + lr * RB + (OF * i + 8 * g + 4 * lh) * 4) = v;
+        }
+      wait_lds();
+      constexpr int PER_ROW = B * OF / 8, ROWS = 64 / PER_ROW;  // lanes per row, rows per store
+#pragma unroll
+      for (int r0 = 0; r0 < 32; r0 += ROWS) {
+        const int r = r0 + lane / PER_ROW, f = 8 * (lane % PER_ROW);
+        const f32x4_t* v = reinterpret_cast<const f32x4_t*>(mine + r * RB + f * 4);
+        const int m = m0 + 32 * j + r, n = n0 + OF * p * B + f;
+        if (m < a.m && n < a.n) store8(a, m, n, v[0], v[1]);
       }
-    };
-    f32x4_t lo, hi;
-    sum(g, lo, hi);
-    if constexpr (GATED) {
-      f32x4_t ulo, uhi;
-      sum(g + 2, ulo, uhi);
-      lo = gated4(lo, ulo, a.act);
-      hi = gated4(hi, uhi, a.act);
+      wait_lds();
     }
-    const int n = n0 + 8 * EIGHTS * q + 8 * g;
-    if (m0 + tok < a.m && (!GATED || n < a.n)) store8(a, m0 + tok, n, lo, hi);
-  }
 }
 
 // ---------------------------------------------------------------- tiles
@@ -398,43 +446,10 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(dlfp::ProjectionA
     }
   }
 
-  // Through the wave's slice of LDS, so that whole runs of a row are stored
-  // (straight from the accumulators a store covers 16 bytes of 32 rows; on
-  // m = 8192, n = 6144, k = 1024 the launch took 13% longer with those).
   constexpr int SLICE = STAGES * STAGE / WAVES / 16 * 16;
-  constexpr int OF = GATED ? 16 : 32;      // features of a block
-  constexpr int FB = GATED ? 4 : 2;        // blocks per pass
-  constexpr int RB = FB * OF * 4 + 16;     // fp32 row of a pass, padded off the banks
-  static_assert(BN % FB == 0 || BN < FB, "passes");
-  constexpr int B = BN < FB ? BN : FB;
-  static_assert(SLICE >= 32 * RB, "epilogue slice");
   wait_copies_barrier<0>();
-  char* mine = smem + wave * SLICE;
-#pragma unroll
-  for (int j = 0; j < BM; ++j)
-#pragma unroll
-    for (int p = 0; p < BN / B; ++p) {
-#pragma unroll
-      for (int i = 0; i < B; ++i)
-#pragma unroll
-        for (int g = 0; g < OF / 8; ++g) {
-          const f32x16_t& c = acc[p * B + i][j];
-          f32x4_t v = {c[4 * g], c[4 * g + 1], c[4 * g + 2], c[4 * g + 3]};
-          if constexpr (GATED)
-            v = gated4(v, f32x4_t{c[8 + 4 * g], c[9 + 4 * g], c[10 + 4 * g], c[11 + 4 * g]}, a.act);
-          *reinterpret_cast<f32x4_t*>(mine + lr * RB + (OF * i + 8 * g + 4 * lh) * 4) = v;
-        }
-      wait_lds();
-      constexpr int PER_ROW = B * OF / 8, ROWS = 64 / PER_ROW;  // lanes per row, rows per store
-#pragma unroll
-      for (int r0 = 0; r0 < 32; r0 += ROWS) {
-        const int r = r0 + lane / PER_ROW, f = 8 * (lane % PER_ROW);
-        const f32x4_t* v = reinterpret_cast<const f32x4_t*>(mine + r * RB + f * 4);
-        const int m = m0 + 32 * (wm * BM + j) + r, n = n0 + OF * (wn * BN + p * B) + f;
-        if (m < a.m && (!GATED || n < a.n)) store8(a, m, n, v[0], v[1]);
-      }
-      wait_lds();
-    }
+  store_tile<BN, BM, SLICE, GATED>(a, acc, smem + wave * SLICE, lane,
+                                   n0 + (GATED ? 16 : 32) * wn * BN, m0 + 32 * wm * BM);
 }
 
 }  // namespace

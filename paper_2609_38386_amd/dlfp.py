@@ -84,9 +84,10 @@ CACHE_EXPORTS = ["dlfp_rope_append", "dlfp_rope_append_kv8", "dlfp_build_window_
 
 # Declared in dlfp_ffn.h.
 FFN_EXPORTS = ["dlfp_quantize_w4", "dlfp_dequantize_w4", "dlfp_linear_w4",
-               "dlfp_gated_linear_bf16", "dlfp_gated_linear_w4"]
+               "dlfp_gated_linear_bf16", "dlfp_gated_linear_w4", "dlfp_projection_workspace"]
 W4_GROUP = 32
 ACTIVATIONS = {"silu": 0, "gelu": 1}
+LINEAR_W4, GATED_LINEAR_BF16, GATED_LINEAR_W4 = range(3)
 
 
 class dlfp_rope(ctypes.Structure):
@@ -156,13 +157,16 @@ def lib():
     L.dlfp_attention_kv8.argtypes = attention + [vp, vp] + rest
     L.dlfp_quantize_w4.argtypes = [i32, i32, vp, i64, vp, vp, vp]
     L.dlfp_dequantize_w4.argtypes = [i32, i32, vp, vp, vp, i64, vp]
-    L.dlfp_linear_w4.argtypes = [i32, i32, i32, vp, i64, vp, vp, vp, i64, i32, vp]
-    L.dlfp_gated_linear_bf16.argtypes = [i32, i32, i32, vp, i64, vp, vp, i32, vp, i64, i32, vp]
+    L.dlfp_linear_w4.argtypes = [i32, i32, i32, vp, i64, vp, vp, vp, i64, i32, vp, sz, vp]
+    L.dlfp_gated_linear_bf16.argtypes = [i32, i32, i32, vp, i64, vp, vp, i32, vp, i64, i32, vp, sz,
+                                         vp]
     L.dlfp_gated_linear_w4.argtypes = [i32, i32, i32, vp, i64, vp, vp, vp, vp, i32, vp, i64, i32,
-                                       vp]
+                                       vp, sz, vp]
+    L.dlfp_projection_workspace.argtypes = [i32, i32, i32, i32]
     for name in EXPORTS + CACHE_EXPORTS + FFN_EXPORTS:
         if name != "dlfp_status_string":
             getattr(L, name).restype = ctypes.c_int
+    L.dlfp_projection_workspace.restype = i64
     _lib = L
     return L
 
@@ -607,20 +611,36 @@ def dlfp_dequantize_w4(codes, exps, w, stream=None) -> None:
         _check(st, "dlfp_dequantize_w4")
 
 
-def dlfp_linear_w4(x, codes, exps, out, stream=None) -> None:
+def _workspace_args(workspace, device):
+    """(address, bytes) of a workspace that may be None."""
+    if workspace is None:
+        return None, 0
+    if workspace.get_device() != device or not workspace.is_contiguous():
+        raise ValueError("the workspace must be contiguous and beside the tensors")
+    return workspace.data_ptr(), workspace.nbytes
+
+
+def dlfp_projection_workspace(kind: int, m: int, n: int, k: int) -> int:
+    """Bytes of workspace that the fastest form of a projection takes (kind: LINEAR_W4,
+    GATED_LINEAR_BF16 or GATED_LINEAR_W4)."""
+    return lib().dlfp_projection_workspace(kind, m, n, k)
+
+
+def dlfp_linear_w4(x, codes, exps, out, workspace=None, stream=None) -> None:
     """out[i][j] = sum_l x[i][l] W[j][l]; x: bf16 [m][k] (rows may be strided), W in 4 bits, out:
     bf16 or float32 [m][n] (rows may be strided)."""
     n, k = _check_codes(codes, exps)
-    _linear_w4(x, codes, exps, n, k, out, stream)
+    _linear_w4(x, codes, exps, n, k, out, workspace, stream)
 
 
-def _linear_w4(x, codes, exps, n, k, out, stream):
+def _linear_w4(x, codes, exps, n, k, out, workspace, stream):
     """The call with codes and exponents that are a Weights4's."""
     m, ldx, ldo, code = _projection_rows(x, n, k, out)
     device = x.get_device()
     _check_device(device == codes.get_device() == exps.get_device() == out.get_device(), device, m)
     st = lib().dlfp_linear_w4(m, n, k, x.data_ptr(), ldx, codes.data_ptr(), exps.data_ptr(),
-                              out.data_ptr(), ldo, code, _stream(stream))
+                              out.data_ptr(), ldo, code, *_workspace_args(workspace, device),
+                              _stream(stream))
     if st:
         _check(st, "dlfp_linear_w4")
 
@@ -632,7 +652,8 @@ def _activation(name) -> int:
     return code
 
 
-def dlfp_gated_linear_bf16(x, w_gate, w_up, out, activation: str = "silu", stream=None) -> None:
+def dlfp_gated_linear_bf16(x, w_gate, w_up, out, activation: str = "silu", workspace=None,
+                           stream=None) -> None:
     """out = act(x G^T) * (x U^T); x: bf16 [m][k] (rows may be strided), w_gate, w_up: bf16 [n][k],
     out: bf16 or float32 [m][n] (rows may be strided)."""
     n, k = w_gate.shape
@@ -646,21 +667,24 @@ def dlfp_gated_linear_bf16(x, w_gate, w_up, out, activation: str = "silu", strea
     _check_device(device == w_gate.get_device() == w_up.get_device() == out.get_device(), device, m)
     st = lib().dlfp_gated_linear_bf16(m, n, k, x.data_ptr(), ldx, w_gate.data_ptr(),
                                       w_up.data_ptr(), _activation(activation), out.data_ptr(),
-                                      ldo, code, _stream(stream))
+                                      ldo, code, *_workspace_args(workspace, device),
+                                      _stream(stream))
     if st:
         _check(st, "dlfp_gated_linear_bf16")
 
 
 def dlfp_gated_linear_w4(x, gate_codes, gate_exps, up_codes, up_exps, out,
-                         activation: str = "silu", stream=None) -> None:
+                         activation: str = "silu", workspace=None, stream=None) -> None:
     """The same with both weights in 4 bits."""
     n, k = _check_codes(gate_codes, gate_exps)
     if _check_codes(up_codes, up_exps) != (n, k):
         raise ValueError("gate and up must be [n][k] both")
-    _gated_linear_w4(x, gate_codes, gate_exps, up_codes, up_exps, n, k, out, activation, stream)
+    _gated_linear_w4(x, gate_codes, gate_exps, up_codes, up_exps, n, k, out, activation, workspace,
+                     stream)
 
 
-def _gated_linear_w4(x, gate_codes, gate_exps, up_codes, up_exps, n, k, out, activation, stream):
+def _gated_linear_w4(x, gate_codes, gate_exps, up_codes, up_exps, n, k, out, activation, workspace,
+                     stream):
     m, ldx, ldo, code = _projection_rows(x, n, k, out)
     device = x.get_device()
     _check_device(device == gate_codes.get_device() == gate_exps.get_device() ==
@@ -668,7 +692,7 @@ def _gated_linear_w4(x, gate_codes, gate_exps, up_codes, up_exps, n, k, out, act
     st = lib().dlfp_gated_linear_w4(m, n, k, x.data_ptr(), ldx, gate_codes.data_ptr(),
                                     gate_exps.data_ptr(), up_codes.data_ptr(), up_exps.data_ptr(),
                                     _activation(activation), out.data_ptr(), ldo, code,
-                                    _stream(stream))
+                                    *_workspace_args(workspace, device), _stream(stream))
     if st:
         _check(st, "dlfp_gated_linear_w4")
 

@@ -178,27 +178,53 @@ class Weights4:
         _d.dlfp_dequantize_w4(self.codes, self.exps, w, stream)
 
 
-def linear(x: torch.Tensor, w, out: torch.Tensor, stream=None):
-    """out = x W^T: x bf16 [m][k], w a Weights4 or bf16 [n][k], out bf16 or float32 [m][n]."""
+_projection_bytes = {}
+
+
+def _projection_workspace(kind: int, x: torch.Tensor, n: int, k: int, workspace, stream):
+    """The workspace of a projection: the caller's, or one of this call alone where the fastest
+    form takes any.  Memory of PyTorch's allocator belongs to the current stream (and to a graph
+    that is being captured on it), so that a call on a stream given by hand does without."""
+    if workspace is not None or stream is not None:
+        return workspace
+    m = x.size(0)
+    key = kind, m, n, k
+    need = _projection_bytes.get(key)
+    if need is None:
+        if len(_projection_bytes) >= 65536:
+            _projection_bytes.clear()
+        need = _projection_bytes[key] = _d.dlfp_projection_workspace(kind, m, n, k)
+    return torch.empty(need, dtype=torch.uint8, device=x.device) if need else None
+
+
+def linear(x: torch.Tensor, w, out: torch.Tensor, workspace: Optional[torch.Tensor] = None,
+           stream=None):
+    """out = x W^T: x bf16 [m][k], w a Weights4 or bf16 [n][k], out bf16 or float32 [m][n].
+    ``workspace``: for 4-bit weights, a tensor of dlfp_projection_workspace bytes that no call
+    beside this one uses (None: taken from PyTorch's allocator, if ``stream`` is None)."""
     if isinstance(w, Weights4):
-        _d._linear_w4(x, w.codes, w.exps, w.n, w.k, out, stream)
+        ws = _projection_workspace(_d.LINEAR_W4, x, w.n, w.k, workspace, stream)
+        _d._linear_w4(x, w.codes, w.exps, w.n, w.k, out, ws, stream)
     else:
         _d.dlfp_linear_bf16(x, w, out, stream)
 
 
 def gated_linear(x: torch.Tensor, gate, up, out: torch.Tensor, activation: str = "silu",
-                 stream=None):
+                 workspace: Optional[torch.Tensor] = None, stream=None):
     """out = act(x G^T) * (x U^T), both weights a Weights4 or both bf16 [n][k]; activation "silu"
-    or "gelu" (the tanh form)."""
+    or "gelu" (the tanh form); ``workspace`` as for linear."""
     four = isinstance(gate, Weights4)
     if four != isinstance(up, Weights4):
         raise ValueError("gate and up must be of one kind")
     if not four:
-        return _d.dlfp_gated_linear_bf16(x, gate, up, out, activation, stream)
+        ws = _projection_workspace(_d.GATED_LINEAR_BF16, x, gate.size(0), gate.size(1), workspace,
+                                   stream)
+        return _d.dlfp_gated_linear_bf16(x, gate, up, out, activation, ws, stream)
     if (gate.n, gate.k) != (up.n, up.k):
         raise ValueError("gate and up must be [n][k] both")
+    ws = _projection_workspace(_d.GATED_LINEAR_W4, x, gate.n, gate.k, workspace, stream)
     _d._gated_linear_w4(x, gate.codes, gate.exps, up.codes, up.exps, gate.n, gate.k, out,
-                        activation, stream)
+                        activation, ws, stream)
 
 
 class Workspace:

@@ -19,7 +19,7 @@ ROOT = os.path.dirname(os.path.dirname(os.path.abspath(__file__)))
 def test_library_exports_every_declared_symbol():
     txt = open(os.path.join(ROOT, "include", "dlfp_ffn.h")).read()
     txt = re.sub(r"/\*.*?\*/", "", txt, flags=re.S)
-    declared = sorted(re.findall(r"\bint\s+(dlfp_\w+)\s*\(", txt))
+    declared = sorted(re.findall(r"\bint(?:64_t)?\s+(dlfp_\w+)\s*\(", txt))
     assert declared == sorted(D.FFN_EXPORTS)
     for name in declared:
         assert hasattr(D.lib(), name)
@@ -100,16 +100,20 @@ def test_bounds_reject_what_is_wrong():
 P = 1 << 20        # an address: nothing is launched
 
 
-def _linear(m=4, n=32, k=64, x=P, ldx=64, codes=P, exps=P, out=P, ldo=32, dtype=0):
-    return D.lib().dlfp_linear_w4(m, n, k, x, ldx, codes, exps, out, ldo, dtype, None)
+def _linear(m=4, n=32, k=64, x=P, ldx=64, codes=P, exps=P, out=P, ldo=32, dtype=0, ws=None):
+    return D.lib().dlfp_linear_w4(m, n, k, x, ldx, codes, exps, out, ldo, dtype, ws, 64, None)
 
 
-def _gated4(m=4, n=32, k=64, x=P, ldx=64, gc=P, ge=P, uc=P, ue=P, act=0, out=P, ldo=32, dtype=0):
-    return D.lib().dlfp_gated_linear_w4(m, n, k, x, ldx, gc, ge, uc, ue, act, out, ldo, dtype, None)
+def _gated4(m=4, n=32, k=64, x=P, ldx=64, gc=P, ge=P, uc=P, ue=P, act=0, out=P, ldo=32, dtype=0,
+            ws=None):
+    return D.lib().dlfp_gated_linear_w4(m, n, k, x, ldx, gc, ge, uc, ue, act, out, ldo, dtype, ws, 64,
+                                        None)
 
 
-def _gated(m=4, n=32, k=64, x=P, ldx=64, gate=P, up=P, act=0, out=P, ldo=32, dtype=0):
-    return D.lib().dlfp_gated_linear_bf16(m, n, k, x, ldx, gate, up, act, out, ldo, dtype, None)
+def _gated(m=4, n=32, k=64, x=P, ldx=64, gate=P, up=P, act=0, out=P, ldo=32, dtype=0,
+           ws=None):
+    return D.lib().dlfp_gated_linear_bf16(m, n, k, x, ldx, gate, up, act, out, ldo, dtype, ws, 64,
+                                          None)
 
 
 COMMON = [(dict(m=-1), -1), (dict(n=0), -1), (dict(n=-16), -1), (dict(k=0), -1), (dict(k=-64), -1),
@@ -117,18 +121,19 @@ COMMON = [(dict(m=-1), -1), (dict(n=0), -1), (dict(n=-16), -1), (dict(k=0), -1),
           (dict(ldx=56), -1), (dict(ldx=68), -1), (dict(ldo=28), -1), (dict(ldo=34), -1),
           (dict(ldx=0), -1), (dict(ldo=-32), -1), (dict(dtype=2), -1), (dict(dtype=-1), -1),
           (dict(x=None), -1), (dict(out=None), -1), (dict(x=P + 8), -1), (dict(out=P + 4), -1),
-          (dict(out=P + 8, dtype=1), -1)]
+          (dict(out=P + 8, dtype=1), -1), (dict(ws=P + 8), -1)]
 
 
 @pytest.mark.parametrize("change,status", COMMON + [(dict(codes=None), -1), (dict(exps=None), -1),
-                                                    (dict(codes=P + 8), -1)])
+                                                    (dict(codes=P + 8), -1),
+                                                    (dict(exps=P + 4), -1)])
 def test_linear_w4_refusals(change, status):
     assert _linear(**change) == status
 
 
 @pytest.mark.parametrize("change,status", COMMON + [(dict(gc=None), -1), (dict(ge=None), -1),
                                                     (dict(uc=None), -1), (dict(ue=None), -1),
-                                                    (dict(gc=P + 4), -1), (dict(uc=P + 8), -1),
+                                                    (dict(gc=P + 4), -1), (dict(ge=P + 8), -1), (dict(uc=P + 8), -1),
                                                     (dict(act=2), -1), (dict(act=-1), -1)])
 def test_gated_linear_w4_refusals(change, status):
     assert _gated4(**change) == status
@@ -162,6 +167,22 @@ def test_conversion_refusals(change, status):
                                 None) == status
 
 
+def test_workspace_sizes():
+    """None where the tiles fill the device or K is short, at most 32 MiB, 0 for refused sizes;
+    what a form is given is enough for it."""
+    size = D.dlfp_projection_workspace
+    for kind in (D.LINEAR_W4, D.GATED_LINEAR_W4):
+        assert size(kind, 1, 2048, 1024) == 0 and size(kind, 4096, 12288, 4096) == 0
+        assert 0 < size(kind, 256, 2560, 25600) <= 32 << 20
+        for m, n, k in ((0, 16, 64), (1, 8, 64), (1, 16, 96), (-1, 16, 64), (1, 16, 0)):
+            assert size(kind, m, n, k) == 0
+        rng = np.random.default_rng(5)
+        for _ in range(2000):
+            m, n, k = (int(2 ** rng.uniform(0, h)) for h in (14, 11, 9))
+            assert 0 <= size(kind, m, 16 * n, 64 * k) <= 32 << 20
+    assert size(7, 256, 2560, 25600) == 0
+
+
 # ------------------------------------------------------------------- refusals from Python
 
 def _bf16(*shape):
@@ -185,6 +206,7 @@ def test_python_refusals():
            lambda: rt.gated_linear(x, _bf16(32, 64), _bf16(16, 64), out),
            lambda: rt.gated_linear(x, _bf16(32, 64), _bf16(32, 64).float(), out),
            lambda: rt.gated_linear(x, _bf16(32, 128)[:, :64], _bf16(32, 64), out),
+           lambda: rt.linear(x, w, out, workspace=torch.zeros(8, device="meta")),
            lambda: rt.Weights4(4, 48, "cpu"),
            lambda: rt.Weights4.of(w.codes, w.exps[:, :1]),
            lambda: rt.Weights4.of(w.codes.int(), w.exps),

@@ -110,7 +110,9 @@ def test_every_code_in_every_scale(dev):
 SIZES = [(1, 16, 64), (1, 2048, 1024), (2, 48, 128), (5, 80, 192), (15, 1008, 320), (16, 32, 4160),
          (17, 64, 64), (31, 272, 1088), (33, 1024, 128), (63, 144, 576), (64, 64, 2048),
          (65, 16, 64), (100, 528, 448), (129, 256, 64), (200, 1040, 192), (257, 96, 512),
-         (300, 2064, 128), (513, 304, 64), (777, 512, 1024), (1025, 272, 320)]
+         (300, 2064, 128), (513, 304, 64), (777, 512, 1024), (1025, 272, 320), (256, 512, 8192),
+         (40, 256, 16384), (3, 128, 16448), (130, 1040, 4160), (600, 336, 3136), (20, 4112, 576),
+         (1100, 1040, 192)]
 
 
 @pytest.mark.parametrize("m,n,k", SIZES)
@@ -131,6 +133,52 @@ def test_linear_w4(dev, m, n, k):
         pj.check(big[:m, left:left + n], *pj.linear(pj.f64(x), values, dtype))
         assert (big[:m, :left] == 7.0).all() and (big[:m, left + n:] == 7.0).all()
         assert (big[m] == 7.0).all()
+
+
+def _some_sizes(seed):
+    """Sizes over the whole range, their products bounded by what the oracle does quickly."""
+    rng = np.random.default_rng(seed)
+    k = 64 * int(round(2 ** rng.uniform(0, 8.6)))
+    m = int(round(2 ** rng.uniform(0, 11.5)))
+    most = max(1, int(4e8 / (m * k) / 16))
+    return m, 16 * max(1, min(most, int(round(2 ** rng.uniform(0, 9))))), k
+
+
+@pytest.mark.parametrize("seed", range(60))
+def test_projections_of_some_sizes(dev, seed):
+    """Both 4-bit calls and the bf16 one, with the workspace that the fastest form takes, one that
+    is too small for it, and none; what the workspace held before is NaN."""
+    m, n, k = _some_sizes(seed)
+    gen = _gen(dev, seed)
+    x = _bf16(dev, gen, (m, k))
+    gate, up = _weights4(dev, gen, n, k), _weights4(dev, gen, n, k)
+    g64, u64 = _values(gate), _values(up)
+    x *= 1.5 / math.sqrt(float((g64 ** 2).sum(1).mean()))
+    dense = [torch.empty((n, k), dtype=torch.bfloat16, device=dev) for _ in range(2)]
+    for w, d in zip((gate, up), dense):
+        w.dequantize(d)
+    x64 = pj.f64(x)
+    act = ("silu", "gelu")[seed % 2]
+    plain, both = pj.linear(x64, g64, torch.float32), pj.gated(x64, g64, u64, act, torch.float32)
+    out = torch.empty((m, n), dtype=torch.float32, device=dev)
+    calls = ((D.LINEAR_W4, plain, lambda ws: rt.linear(x, gate, out, workspace=ws, stream=0)),
+             (D.GATED_LINEAR_W4, both,
+              lambda ws: rt.gated_linear(x, gate, up, out, act, workspace=ws, stream=0)),
+             (D.GATED_LINEAR_BF16, both,
+              lambda ws: rt.gated_linear(x, *dense, out, act, workspace=ws, stream=0)))
+    for kind, want, call in calls:
+        need = D.dlfp_projection_workspace(kind, m, n, k)
+        for size in {need, need * 2 // 3 // 16 * 16, 0}:
+            ws = None
+            if size:
+                room = torch.full((size // 4 + 64,), math.nan, dtype=torch.float32, device=dev)
+                ws = room[:size // 4]
+            out.fill_(math.nan)
+            torch.cuda.synchronize()
+            call(ws)
+            torch.cuda.synchronize()
+            pj.check(out, *want)
+            assert not size or room[size // 4:].isnan().all()
 
 
 @pytest.mark.parametrize("four", [False, True])
@@ -268,13 +316,15 @@ def test_gate_and_up_halves_of_one_buffer(dev):
 def test_graph_replays(dev, m):
     """A captured block (quantised weights, gated, down) replayed with new inputs, eager work
     between the replays."""
-    hidden, mlp = 256, 512
+    hidden, mlp = 256, 16384
     gen = _gen(dev, m + 100)
     ws = [rt.Weights4.from_bf16(_bf16(dev, gen, s, 0.06)) for s in ((mlp, hidden), (mlp, hidden),
                                                                     (hidden, mlp))]
     x = _bf16(dev, gen, (m, hidden))
     h = torch.empty((m, mlp), dtype=torch.bfloat16, device=dev)
     out, eager = (torch.empty((m, hidden), dtype=torch.float32, device=dev) for _ in range(2))
+    if m > 1:
+        assert D.dlfp_projection_workspace(D.LINEAR_W4, m, hidden, mlp) > 0
 
     def block(y):
         rt.gated_linear(x, ws[0], ws[1], h)
