@@ -1,19 +1,20 @@
 // Projections with 4-bit weights: dlfp_linear_w4, dlfp_gated_linear_w4.  The kernels are those
 // of projection_few4.h and projection_tiles4.h, and a plain one for rows that are far apart.
-#include <algorithm>
-
 #include "dlfp_ffn.h"
+#include "projection_choice.h"
 #include "projection_few4.h"
 #include "projection_tiles4.h"
 
 namespace {
+
+using dlfp::FAR_STRIDE;
 
 // ---------------------------------------------------------------- far rows
 
 // Rows of x or of weights 2^22 elements and more apart: 16 features and 16 tokens a workgroup,
 // operands straight from memory with 64-bit addresses, K over eight wavefronts in steps of 128
 // columns.  (The other kernels' copies have 32-bit offsets from a tile's first row.)
-constexpr int FAR_STRIDE = 1 << 22, FAR_WAVES = 8, FAR_STEP = 128;
+constexpr int FAR_WAVES = 8, FAR_STEP = 128;
 
 template <bool GATED>
 __global__ __launch_bounds__(64 * FAR_WAVES) void far4_kernel(dlfp::ProjectionArgs a) {
@@ -67,29 +68,19 @@ int launch_far(const dlfp::ProjectionArgs& a, hipStream_t stream) {
 
 // ---------------------------------------------------------------- launches
 
-// `down` x `across` tiles of tokens and features.
-struct Grid {
-  int64_t down, across;
-};
-
 template <bool GATED, int BLOCKS, int TOKENS, int WAVES, int DEPTH>
 int launch_few(const dlfp::ProjectionArgs& a, Grid g, dlfp::Split split, hipStream_t stream) {
-  if constexpr (GATED && BLOCKS % 2) {
-    return DLFP_EUNSUPPORTED;
-  } else {
-    using Shape = FewShape<BLOCKS, TOKENS, WAVES, DEPTH>;
-    const int64_t tiles = g.down * g.across;
-    if (tiles * split.splits * (64 * WAVES) >= (int64_t)1 << 32) return DLFP_ERANGE;
-    few4_kernel<BLOCKS, TOKENS, WAVES, DEPTH, GATED>
-        <<<(uint32_t)(tiles * split.splits), 64 * WAVES, (size_t)Shape::lds(a.k), stream>>>(a,
-                                                                                          split);
-    if (split.splits > 1) {
-      constexpr int UNITS = (GATED ? BLOCKS / 2 : BLOCKS) * Shape::TB;
-      sum_few_kernel<BLOCKS, TOKENS, GATED><<<(uint32_t)(tiles * UNITS), 64, 0, stream>>>(
-          a, (int)g.across, (int)tiles, split);
-    }
-    return hipGetLastError() == hipSuccess ? DLFP_OK : DLFP_EHIP;
+  using Shape = FewShape<BLOCKS, TOKENS, WAVES, DEPTH>;
+  const int64_t tiles = g.down * g.across;
+  if (tiles * split.splits * (64 * WAVES) >= (int64_t)1 << 32) return DLFP_ERANGE;
+  few4_kernel<BLOCKS, TOKENS, WAVES, DEPTH, GATED>
+      <<<(uint32_t)(tiles * split.splits), 64 * WAVES, (size_t)Shape::lds(a.k), stream>>>(a, split);
+  if (split.splits > 1) {
+    constexpr int UNITS = (GATED ? BLOCKS / 2 : BLOCKS) * Shape::TB;
+    sum_few_kernel<BLOCKS, TOKENS, GATED><<<(uint32_t)(tiles * UNITS), 64, 0, stream>>>(
+        a, (int)g.across, (int)tiles, split);
   }
+  return hipGetLastError() == hipSuccess ? DLFP_OK : DLFP_EHIP;
 }
 
 template <bool GATED, int TN, int TM, int WN, int WM, int DEPTH, int STAGES, bool WHOLE>
@@ -109,95 +100,53 @@ int launch_tile(const dlfp::ProjectionArgs& a, Grid g, dlfp::Split split, hipStr
 
 // ---------------------------------------------------------------- choice
 
-typedef int (*Launch)(const dlfp::ProjectionArgs&, Grid, dlfp::Split, hipStream_t);
+template <int BLOCKS, int TOKENS, int WAVES, int DEPTH>
+constexpr Launch few_gated() {
+  if constexpr (BLOCKS % 2)
+    return nullptr;  // (blocks of the gate and of the up come in pairs)
+  else
+    return launch_few<true, BLOCKS, TOKENS, WAVES, DEPTH>;
+}
 
-// A tile of `rows` rows of weights and `tokens` tokens.  Its time in microseconds, of u = units
-// (tiles times splits) / 256 and s = K steps of a unit (of 64 columns; in few4_kernel of 256 of
-// a wavefront):
-//   start + step s + (unit + work s) u + (round + turn s) ceil(u)
-//   + with splits: join + partial sums * (units' fp32 MB)
-struct Variant {
-  int rows, tokens;
-  int waves;        // that share the K steps of a unit; 0: of tile4_kernel
-  int rings, blocks;  // LDS of few4_kernel beside the exponents, and its blocks of 16 rows
-  float start, step, unit, work, round, turn, join, part;
-  Launch plain, gated;
-};
-#define FEW(B, T, W, D)                                                                       \
-  16 * B, T, W, FewShape<B, T, W, D>::RINGS, B
-#define FEW_LAUNCH(B, T, W, D) launch_few<false, B, T, W, D>, launch_few<true, B, T, W, D>
-#define TILE(TN, TM) TN, TM, 0, 0, 0
-#define TILE_LAUNCH(...) launch_tile<false, __VA_ARGS__>, launch_tile<true, __VA_ARGS__>
+// Fitted to 1000 sizes of 1-4096 tokens, 64-25600 features and columns, every variant with every
+// split, plain and gated, weights read from memory.  The choice takes 1.026 times the fastest
+// one's time on average (geometric mean; 1.09 in nine of ten sizes, 1.4 at worst).
+#define FEW(B, T, W, D) 16 * B, T, W, FSTEP, FewShape<B, T, W, D>::RINGS, B, true
+#define TILE(TN, TM, ...) TN, TM, 0, 0, 0, 0, true
+#define FEW_CALLS(B, T, W, D) {launch_few<false, B, T, W, D>, few_gated<B, T, W, D>()}
+#define TILE_CALLS(...) {launch_tile<false, __VA_ARGS__>, launch_tile<true, __VA_ARGS__>}
 constexpr Variant VARIANTS[] = {
-    {FEW(1, 2, 4, 2), 2.559f, 0.146f, 0.f, 0.103f, 0.f, 0.174f, 2.266f, 0.261f, FEW_LAUNCH(1, 2, 4, 2)},
-    {FEW(2, 2, 4, 1), 2.677f, 0.215f, 0.f, 0.299f, 0.f, 0.238f, 2.37f, 0.406f, FEW_LAUNCH(2, 2, 4, 1)},
-    {FEW(1, 4, 8, 2), 2.417f, 0.091f, 0.f, 0.26f, 0.276f, 0.36f, 2.103f, 0.593f, FEW_LAUNCH(1, 4, 8, 2)},
-    {FEW(2, 4, 4, 2), 2.734f, 0.131f, 0.03f, 0.248f, 0.f, 0.363f, 2.287f, 0.727f, FEW_LAUNCH(2, 4, 4, 2)},
-    {FEW(1, 8, 8, 2), 1.559f, 0.f, 0.f, 0.301f, 1.141f, 0.553f, 2.133f, 1.015f, FEW_LAUNCH(1, 8, 8, 2)},
-    {FEW(2, 8, 4, 1), 2.744f, 0.291f, 0.f, 0.394f, 0.f, 0.22f, 2.391f, 0.332f, FEW_LAUNCH(2, 8, 4, 1)},
-    {FEW(1, 16, 4, 1), 2.551f, 0.177f, 0.f, 0.249f, 0.f, 0.294f, 2.289f, 0.029f, FEW_LAUNCH(1, 16, 4, 1)},
-    {FEW(2, 16, 4, 1), 2.753f, 0.27f, 0.f, 0.423f, 0.f, 0.37f, 2.317f, 0.701f, FEW_LAUNCH(2, 16, 4, 1)},
-    {FEW(4, 16, 4, 1), 2.912f, 0.334f, 0.f, 0.828f, 0.f, 0.632f, 2.558f, 0.522f, FEW_LAUNCH(4, 16, 4, 1)},
-    {FEW(2, 32, 2, 1), 2.678f, 0.42f, 0.021f, 0.13f, 0.313f, 0.396f, 2.639f, 0.193f, FEW_LAUNCH(2, 32, 2, 1)},
-    {FEW(2, 32, 6, 1), 1.225f, 0.101f, 0.f, 0.598f, 1.725f, 1.117f, 2.738f, 0.338f, FEW_LAUNCH(2, 32, 6, 1)},
-    {TILE(128, 32), 2.453f, 0.143f, 0.274f, 0.068f, 0.777f, 0.085f, 2.792f, 0.261f, TILE_LAUNCH(128, 32, 4, 1, 4, 3, true)},
-    {TILE(128, 64), 2.922f, 0.294f, 0.708f, 0.131f, 0.269f, 0.06f, 2.599f, 0.254f, TILE_LAUNCH(128, 64, 4, 1, 2, 2, false)},
-    {TILE(256, 64), 2.059f, 0.026f, 1.4f, 0.112f, 1.967f, 0.365f, 2.636f, 0.304f, TILE_LAUNCH(256, 64, 8, 1, 4, 3, true)},
-    {TILE(256, 128), 2.222f, 0.f, 2.68f, 0.161f, 2.569f, 0.649f, 2.767f, 0.229f, TILE_LAUNCH(256, 128, 8, 1, 4, 3, false)},
-    {TILE(256, 256), 3.128f, 0.f, 5.166f, 0.311f, 2.721f, 1.109f, 3.928f, 0.162f, TILE_LAUNCH(256, 256, 8, 1, 2, 2, false)},
+    {FEW(1, 2, 4, 2), {2.645f, 0.078f, 0.f, 0.064f, 0.053f, 0.163f, 0.046f, 2.393f, 0.03f}, FEW_CALLS(1, 2, 4, 2)},
+    {FEW(2, 2, 4, 1), {2.554f, 0.253f, 0.f, 0.098f, 0.106f, 0.249f, 0.084f, 2.369f, 0.f}, FEW_CALLS(2, 2, 4, 1)},
+    {FEW(1, 4, 8, 2), {2.488f, 0.014f, 0.f, 0.115f, 0.329f, 0.395f, 0.051f, 2.206f, 0.159f}, FEW_CALLS(1, 4, 8, 2)},
+    {FEW(2, 4, 4, 2), {2.879f, 0.001f, 0.027f, 0.111f, 0.046f, 0.369f, 0.066f, 2.461f, 0.273f}, FEW_CALLS(2, 4, 4, 2)},
+    {FEW(1, 8, 4, 2), {2.641f, 0.03f, 0.f, 0.086f, 0.126f, 0.25f, 0.046f, 2.343f, 0.f}, FEW_CALLS(1, 8, 4, 2)},
+    {FEW(2, 8, 4, 2), {2.741f, 0.f, 0.f, 0.159f, 0.23f, 0.413f, 0.055f, 2.533f, 0.09f}, FEW_CALLS(2, 8, 4, 2)},
+    {FEW(2, 8, 4, 1), {2.753f, 0.236f, 0.f, 0.193f, 0.002f, 0.291f, 0.067f, 2.423f, 0.07f}, FEW_CALLS(2, 8, 4, 1)},
+    {FEW(1, 16, 4, 2), {1.491f, 0.f, 0.f, 0.155f, 1.331f, 0.347f, 0.029f, 2.4f, 0.156f}, FEW_CALLS(1, 16, 4, 2)},
+    {FEW(2, 16, 4, 1), {2.755f, 0.187f, 0.f, 0.199f, 0.045f, 0.449f, 0.065f, 2.358f, 0.339f}, FEW_CALLS(2, 16, 4, 1)},
+    {FEW(2, 32, 4, 1), {1.314f, 0.038f, 0.267f, 0.212f, 1.758f, 0.819f, 0.068f, 2.699f, 0.081f}, FEW_CALLS(2, 32, 4, 1)},
+    {FEW(4, 32, 4, 1), {1.425f, 0.f, 0.37f, 0.14f, 1.857f, 1.435f, 0.102f, 2.851f, 0.175f}, FEW_CALLS(4, 32, 4, 1)},
+    {TILE(128, 32, 4, 1, 4, 3, true), {2.385f, 0.127f, 0.165f, 0.054f, 0.945f, 0.089f, 0.075f, 2.803f, 0.194f}, TILE_CALLS(128, 32, 4, 1, 4, 3, true)},
+    {TILE(128, 64, 4, 1, 2, 2, false), {2.827f, 0.289f, 0.587f, 0.133f, 0.476f, 0.045f, 0.069f, 2.926f, 0.187f}, TILE_CALLS(128, 64, 4, 1, 2, 2, false)},
+    {TILE(256, 64, 8, 1, 4, 3, true), {1.819f, 0.f, 1.216f, 0.086f, 2.281f, 0.385f, 0.062f, 2.771f, 0.249f}, TILE_CALLS(256, 64, 8, 1, 4, 3, true)},
+    {TILE(256, 128, 8, 1, 4, 3, false), {2.35f, 0.f, 2.881f, 0.165f, 2.443f, 0.645f, 0.f, 2.764f, 0.236f}, TILE_CALLS(256, 128, 8, 1, 4, 3, false)},
+    {TILE(256, 256, 8, 1, 2, 2, false), {2.837f, 0.f, 4.467f, 0.353f, 3.364f, 1.089f, 0.008f, 3.975f, 0.142f}, TILE_CALLS(256, 256, 8, 1, 2, 2, false)},
 };
 #undef FEW
-#undef FEW_LAUNCH
 #undef TILE
-#undef TILE_LAUNCH
-constexpr int CUS = 256;
-constexpr int SPLITS[] = {1, 2, 3, 4, 6, 8};
-constexpr int64_t MOST_PARTS = 32 << 20;  // bytes of partial sums
+#undef FEW_CALLS
+#undef TILE_CALLS
 
-struct Plan {
-  const Variant* variant;
-  Grid grid;
-  int splits;
-  int64_t bytes;  // of partial sums
-};
-
-// The variant and the number of splits whose estimated time is lowest, of those whose partial
-// sums fit into `room` bytes.
-Plan choose(bool gated, int m, int n, int k, int64_t room) {
-  Plan best{nullptr, {0, 0}, 1, 0};
-  float least = 0.f;
-  const int steps = (k + FSTEP - 1) / FSTEP;
-  for (const Variant& v : VARIANTS) {
-    if (gated && v.rows < 32) continue;
-    if (v.waves && v.rings + v.blocks * (((int64_t)k / 2 + 1023) / 1024 * 1024) > LDS_MAX) continue;
-    const int features = gated ? v.rows / 2 : v.rows;
-    const Grid g{((int64_t)m + v.tokens - 1) / v.tokens, ((int64_t)n + features - 1) / features};
-    const int64_t tiles = g.down * g.across;
-    const int64_t bytes = (int64_t)v.rows * std::max(v.tokens, 16) * 4 * tiles;
-    for (int splits : SPLITS) {
-      if (splits > 1 && (splits * bytes > room || splits * std::max(v.waves, 2) > steps)) break;
-      const float u = (float)(tiles * splits) / CUS;
-      const float r = (float)((tiles * splits + CUS - 1) / CUS);
-      const int per = splits * v.waves;
-      const float s = v.waves ? (float)((steps + per - 1) / per) : (float)k / KSTEP / (float)splits;
-      float t = v.start + v.step * s + (v.unit + v.work * s) * u + (v.round + v.turn * s) * r;
-      if (splits > 1) t += v.join + v.part * 1e-6f * (float)(splits * bytes);
-      if (best.variant && t >= least) continue;
-      least = t;
-      best = Plan{&v, g, splits, splits > 1 ? splits * bytes : 0};
-    }
-  }
-  return best;
+int64_t weight_bytes(bool gated, int n, int k) {
+  return (int64_t)n * k / 32 * (gated ? 34 : 17);
 }
 
 template <bool GATED>
 int launch(const dlfp::ProjectionArgs& a, void* workspace, size_t bytes, hipStream_t stream) {
   (void)hipGetLastError();
   if (std::max<int64_t>(a.ldx, a.k) >= FAR_STRIDE) return launch_far<GATED>(a, stream);
-  const int64_t room = workspace ? (int64_t)std::min<size_t>(bytes, MOST_PARTS) : 0;
-  const Plan p = choose(GATED, a.m, a.n, a.k, room);
-  const dlfp::Split split{static_cast<float*>(workspace), p.splits};
-  return (GATED ? p.variant->gated : p.variant->plain)(a, p.grid, split, stream);
+  return launch_best(VARIANTS, GATED, a, weight_bytes(GATED, a.n, a.k), workspace, bytes, stream);
 }
 
 }  // namespace
@@ -253,9 +202,20 @@ extern "C" int dlfp_gated_linear_w4(int32_t m, int32_t n, int32_t k, const void*
   return st != DLFP_OK || m == 0 ? st : launch<true>(a, workspace, workspace_bytes, stream);
 }
 
+namespace dlfp {
+
+int64_t workspace_w4(bool gated, int m, int n, int k) {
+  return choose(VARIANTS, gated, m, n, k, weight_bytes(gated, n, k), MOST_PARTS).bytes;
+}
+
+}  // namespace dlfp
+
 extern "C" int64_t dlfp_projection_workspace(int32_t kind, int32_t m, int32_t n, int32_t k) {
   if (m <= 0 || n <= 0 || k <= 0 || n % 16 || k % 64 || k >= FAR_STRIDE) return 0;
-  if (kind == DLFP_LINEAR_W4 || kind == DLFP_GATED_LINEAR_W4)
-    return choose(kind == DLFP_GATED_LINEAR_W4, m, n, k, MOST_PARTS).bytes;
+  switch (kind) {
+    case DLFP_LINEAR_W4: return dlfp::workspace_w4(false, m, n, k);
+    case DLFP_GATED_LINEAR_W4: return dlfp::workspace_w4(true, m, n, k);
+    case DLFP_GATED_LINEAR_BF16: return dlfp::workspace_gated(m, n, k);
+  }
   return 0;
 }

@@ -25,6 +25,13 @@ struct Split {
   int32_t splits;
 };
 
+// Row strides from here on take 64-bit offsets (255 rows of 2 bytes each fit 32 bits below).
+constexpr int FAR_STRIDE = 1 << 22;
+
+// Bytes of partial sums of the fastest form.
+int64_t workspace_w4(bool gated, int m, int n, int k);
+int64_t workspace_gated(int m, int n, int k);
+
 // DLFP_OK, or what is wrong with them; sets wide.
 int check_projection(ProjectionArgs& a, bool gated, bool codes, int32_t out_dtype,
                      const void* workspace);

@@ -1,0 +1,89 @@
+// Which kernel and tile a projection takes, and over how many workgroups K is split: those
+// whose estimated time is lowest.
+#pragma once
+
+#include <algorithm>
+#include <cstdint>
+
+#include "projection.h"
+
+namespace {
+
+// `down` x `across` tiles of tokens and features.
+struct Grid {
+  int64_t down, across;
+};
+typedef int (*Launch)(const dlfp::ProjectionArgs&, Grid, dlfp::Split, hipStream_t);
+
+// A tile of `rows` rows of weights and `tokens` tokens.  Its wavefronts share steps of `columns`
+// columns, or take all of them (waves 0).  `lds` bytes besides `blocks` times half a row, where
+// that matters (blocks > 0).
+//
+// Time in microseconds, with u = tiles times splits / 256, s = steps of a unit (of a wavefront
+// where they share them, of 64 columns otherwise) and b = MB of weights:
+//   c0 + c1 s + (c2 + c3 s) u + (c4 + c5 s) ceil(u) + c6 b, with splits + c7 + c8 MB of sums
+struct Variant {
+  int rows, tokens, waves, columns, lds, blocks;
+  bool splits;
+  float c[9];
+  Launch launch[2];  // plain and gated
+};
+
+constexpr int CUS = 256;
+constexpr int SPLITS[] = {1, 2, 3, 4, 6, 8};
+constexpr int SPLIT_COLUMNS = 512;           // at least, of a split of a tile
+constexpr int64_t MOST_PARTS = 32 << 20;     // bytes of partial sums
+constexpr int64_t MOST_GRID_Y = 65535;
+
+struct Plan {
+  const Variant* variant;
+  Grid grid;
+  int splits;
+  int64_t bytes;  // of partial sums
+};
+
+// The least estimate among those whose partial sums fit into `room` bytes.
+template <int COUNT>
+Plan choose(const Variant (&variants)[COUNT], bool gated, int m, int n, int k, int64_t weight_bytes,
+            int64_t room) {
+  Plan best{nullptr, {0, 0}, 1, 0};
+  float least = 0.f;
+  for (const Variant& v : variants) {
+    if (!v.launch[gated]) continue;
+    if (v.blocks && v.lds + v.blocks * (((int64_t)k / 2 + 1023) / 1024 * 1024) > 160 * 1024) continue;
+    const int features = gated ? v.rows / 2 : v.rows;
+    const Grid g{((int64_t)m + v.tokens - 1) / v.tokens, ((int64_t)n + features - 1) / features};
+    if (g.down > MOST_GRID_Y && !v.splits) continue;
+    const int64_t tiles = g.down * g.across;
+    const int64_t bytes = (int64_t)v.rows * std::max(v.tokens, 16) * 4 * tiles;
+    const float* c = v.c;
+    const float fixed = c[0] + c[6] * 1e-6f * (float)weight_bytes;
+    const int steps = v.waves ? (k + v.columns - 1) / v.columns : 0;
+    for (int splits : SPLITS) {
+      if (splits > 1 && (!v.splits || splits * bytes > room ||
+                         (v.waves ? splits * v.waves > steps : splits * SPLIT_COLUMNS > k)))
+        break;
+      const float u = (float)(tiles * splits) / CUS;
+      const float r = (float)((tiles * splits + CUS - 1) / CUS);
+      const int share = splits * v.waves;
+      const float s = v.waves ? (float)((steps + share - 1) / share) : (float)k / 64 / (float)splits;
+      float t = fixed + c[1] * s + (c[2] + c[3] * s) * u + (c[4] + c[5] * s) * r;
+      if (splits > 1) t += c[7] + c[8] * 1e-6f * (float)(splits * bytes);
+      if (best.variant && t >= least) continue;
+      least = t;
+      best = Plan{&v, g, splits, splits > 1 ? splits * bytes : 0};
+    }
+  }
+  return best;
+}
+
+template <int COUNT>
+int launch_best(const Variant (&variants)[COUNT], bool gated, const dlfp::ProjectionArgs& a,
+                int64_t weight_bytes, void* workspace, size_t bytes, hipStream_t stream) {
+  const int64_t room = workspace ? (int64_t)std::min<size_t>(bytes, MOST_PARTS) : 0;
+  const Plan p = choose(variants, gated, a.m, a.n, a.k, weight_bytes, room);
+  return p.variant->launch[gated](a, p.grid, dlfp::Split{static_cast<float*>(workspace), p.splits},
+                                  stream);
+}
+
+}  // namespace

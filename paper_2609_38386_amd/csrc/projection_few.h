@@ -1,0 +1,83 @@
+// Projections of few tokens: weights and tokens through LDS, by copies of whole row segments,
+// into v_mfma_f32_16x16x32_bf16 as out^T = W x^T.
+//
+// A workgroup takes BLOCKS blocks of 16 rows of weights (gated: rows of the gate and of the up
+// in turn) and TOKENS tokens.  Its wavefronts (and, with splits, several workgroups) share K,
+// each through a ring of its own without barriers, and their results are added through LDS, in
+// wavefront order.
+#pragma once
+
+#include "projection_tiles.h"
+
+namespace {
+
+// Four features of a token.
+__device__ __forceinline__ void store4(const dlfp::ProjectionArgs& a, int m, int n, f32x4_t v) {
+  const int64_t at = (int64_t)m * a.ldo + n;
+  if (a.out_f32)
+    *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.out) + at) = v;
+  else
+    *reinterpret_cast<u32x2_t*>(static_cast<uint16_t*>(a.out) + at) =
+        u32x2_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
+}
+
+// The end of a unit, when its wavefront is done: lane l holds features 4 (l / 16) .. + 3 of
+// token l % 16 of a block.
+template <int BLOCKS, int TOKENS, int WAVES, bool GATED, int TB>
+__device__ __forceinline__ void store_few(const dlfp::ProjectionArgs& a, dlfp::Split split,
+                                          f32x4_t (&acc)[BLOCKS][TB], char* smem, int tid,
+                                          int wave, uint32_t unit, uint32_t part, int n0, int m0) {
+  const int lane = tid & 63;
+  wait_copies_barrier<0>();
+  f32x4_t* sums = reinterpret_cast<f32x4_t*>(smem);
+#pragma unroll
+  for (int b = 0; b < BLOCKS; ++b)
+#pragma unroll
+    for (int u = 0; u < TB; ++u) sums[((wave * BLOCKS + b) * TB + u) * 64 + lane] = acc[b][u];
+  __syncthreads();
+  constexpr int OUT = GATED ? BLOCKS / 2 : BLOCKS;
+  for (int i = tid; i < OUT * TB * 64; i += 64 * WAVES) {
+    const int l = i & 63, u = (i >> 6) % TB, r = (i >> 6) / TB;
+    auto sum = [&](int b) {
+      f32x4_t v = sums[(b * TB + u) * 64 + l];
+#pragma unroll
+      for (int w = 1; w < WAVES; ++w) v += sums[((w * BLOCKS + b) * TB + u) * 64 + l];
+      return v;
+    };
+    f32x4_t v = sum(GATED ? 2 * r : r);
+    if (split.splits > 1) {
+      // Unit (r, u, l) of the gate, then of the up.
+      f32x4_t* out = reinterpret_cast<f32x4_t*>(split.part) +
+                     ((int64_t)part * (gridDim.x / split.splits) + unit) * (BLOCKS * TB * 64) + i;
+      *out = v;
+      if constexpr (GATED) out[OUT * TB * 64] = sum(2 * r + 1);
+      continue;
+    }
+    if constexpr (GATED) v = gated4(v, sum(2 * r + 1), a.act);
+    const int tok = 16 * u + (l & 15), m = m0 + tok, n = n0 + 16 * r + 4 * (l >> 4);
+    if (tok < TOKENS && m < a.m && n < a.n) store4(a, m, n, v);
+  }
+}
+
+// The sum of the splits of a tile, in split order: a thread for each unit of the output.
+template <int BLOCKS, int TOKENS, bool GATED>
+__global__ __launch_bounds__(64) void sum_few_kernel(dlfp::ProjectionArgs a, int gn, int tiles,
+                                                     dlfp::Split split) {
+  constexpr int TB = TOKENS < 16 ? 1 : TOKENS / 16, OUT = GATED ? BLOCKS / 2 : BLOCKS;
+  const int i = blockIdx.x % (OUT * TB), t = blockIdx.x / (OUT * TB), l = threadIdx.x;
+  const int u = i % TB, r = i / TB, tok = 16 * u + (l & 15);
+  const int m = t / gn * TOKENS + tok, n = t % gn * (16 * OUT) + 16 * r + 4 * (l >> 4);
+  if (tok >= TOKENS || m >= a.m || n >= a.n) return;
+  constexpr int UNITS = BLOCKS * TB * 64;
+  const f32x4_t* p = reinterpret_cast<const f32x4_t*>(split.part) + (int64_t)t * UNITS + i * 64 + l;
+  f32x4_t v = p[0], up{};
+  if constexpr (GATED) up = p[OUT * TB * 64];
+  for (int s = 1; s < split.splits; ++s) {
+    v += p[(int64_t)s * tiles * UNITS];
+    if constexpr (GATED) up += p[(int64_t)s * tiles * UNITS + OUT * TB * 64];
+  }
+  if constexpr (GATED) v = gated4(v, up, a.act);
+  store4(a, m, n, v);
+}
+
+}  // namespace

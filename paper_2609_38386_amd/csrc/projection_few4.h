@@ -1,16 +1,11 @@
-// Projections of few tokens with 4-bit weights: codes, exponents and tokens through LDS, by
-// copies of whole row segments, into v_mfma_f32_16x16x32_bf16 as out^T = W x^T.
-//
-// A workgroup takes BLOCKS blocks of 16 rows of weights (gated: rows of the gate and of the up
-// in turn) and TOKENS tokens.  Its wavefronts split K in steps of 256 columns, each through a
-// ring of its own without barriers, and their results are added through LDS, in wavefront
-// order.  Of a block, lane l takes row l % 16 and, of half h of a step, group 4 h + l / 16:
-// 16 bytes of codes that are the operands of four products; which columns a product takes is
-// free as long as both operands agree.  The exponents of the block's rows are one contiguous
-// piece of memory, copied whole before the first step.
+// Projections of few tokens with 4-bit weights: the kernel of projection_few.h whose steps are
+// 256 columns deep.  Of a block, lane l takes row l % 16 and, of half h of a step, group
+// 4 h + l / 16: 16 bytes of codes that are the operands of four products; which columns a
+// product takes is free as long as both operands agree.  The exponents of the block's rows are
+// one contiguous piece of memory, copied whole before the first step.
 #pragma once
 
-#include "projection_tiles4.h"
+#include "projection_few.h"
 
 namespace {
 
@@ -72,9 +67,10 @@ __global__ __launch_bounds__(64 * WAVES) void few4_kernel(dlfp::ProjectionArgs a
   const char* xbase = reinterpret_cast<const char*>(a.x + (int64_t)m0 * a.ldx);
   char* ring = smem + wave * Shape::RING;
   const uint32_t lds0 = lds_addr(ring);
-  auto issue = [&](int t, int slot) {
+  auto issue = [&](auto inside, int t, int slot) {
     const int s = first + t;
-    const bool whole = 8 * s + 8 <= groups;  // else past the row's end the step's first again
+    // Past the row's end the step's first group again.
+    const bool whole = inside.value || 8 * s + 8 <= groups;
     const uint32_t d = lds0 + slot * SLOT;
 #pragma unroll
     for (int b = 0; b < BLOCKS; ++b)
@@ -103,7 +99,7 @@ __global__ __launch_bounds__(64 * WAVES) void few4_kernel(dlfp::ProjectionArgs a
   }
 #pragma unroll
   for (int t = 0; t < DEPTH; ++t)
-    if (t < count) issue(t, t);
+    if (t < count) issue(std::false_type{}, t, t);
 
   f32x4_t acc[BLOCKS][TB];
 #pragma unroll
@@ -114,8 +110,12 @@ __global__ __launch_bounds__(64 * WAVES) void few4_kernel(dlfp::ProjectionArgs a
   const char* ex = smem + Shape::RINGS + lr * groups + quad;
   wait_stages<DEPTH, L, true>(count);  // the exponents of every wavefront are there
   int slot = 0;
-  for (int t = 0; t < count; ++t) {
-    wait_stages<DEPTH - 1, L, false>(count - 1 - t);
+  // `inside`: the steps that a step looks ahead to are there, and it and they are whole ones.
+  auto step = [&](auto inside, int t) {
+    if constexpr (decltype(inside)::value)
+      wait_copies<(DEPTH - 1) * L>();
+    else
+      wait_stages<DEPTH - 1, L, false>(count - 1 - t);
     const char* p = ring + slot * SLOT;
     u32x4_t codes[2][BLOCKS];
     bf16x8_t xf[2][TB][4];
@@ -137,8 +137,8 @@ __global__ __launch_bounds__(64 * WAVES) void few4_kernel(dlfp::ProjectionArgs a
               (((16 * h + 4 * quad + i) ^ tr) << 4));
     }
     wait_lds();  // the slot's reads have returned before it is refilled
-    if (t + DEPTH < count) issue(t + DEPTH, slot);
-    if (8 * (first + t) + 8 > groups) {  // past the end of the rows: zeros
+    if (inside.value || t + DEPTH < count) issue(inside, t + DEPTH, slot);
+    if (!inside.value && 8 * (first + t) + 8 > groups) {  // past the end of the rows: zeros
 #pragma unroll
       for (int h = 0; h < 2; ++h)
         if (8 * (first + t) + 4 * h + quad >= groups) {
@@ -162,59 +162,12 @@ __global__ __launch_bounds__(64 * WAVES) void few4_kernel(dlfp::ProjectionArgs a
             acc[b][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(w, xf[h][u][i], acc[b][u], 0, 0, 0);
         }
     slot = slot + 1 == DEPTH ? 0 : slot + 1;
-  }
+  };
+  int t = 0;
+  for (; t + DEPTH + 1 < count; ++t) step(std::true_type{}, t);
+  for (; t < count; ++t) step(std::false_type{}, t);
 
-  // Lane l holds features 4 (l / 16) .. + 3 of token l % 16 of a block: the waves' sum.
-  wait_copies_barrier<0>();
-  f32x4_t* sums = reinterpret_cast<f32x4_t*>(smem);
-#pragma unroll
-  for (int b = 0; b < BLOCKS; ++b)
-#pragma unroll
-    for (int u = 0; u < TB; ++u) sums[((wave * BLOCKS + b) * TB + u) * 64 + lane] = acc[b][u];
-  __syncthreads();
-  constexpr int OUT = GATED ? BLOCKS / 2 : BLOCKS;
-  for (int i = tid; i < OUT * TB * 64; i += 64 * WAVES) {
-    const int l = i & 63, u = (i >> 6) % TB, r = (i >> 6) / TB;
-    auto sum = [&](int b) {
-      f32x4_t v = sums[(b * TB + u) * 64 + l];
-#pragma unroll
-      for (int w = 1; w < WAVES; ++w) v += sums[((w * BLOCKS + b) * TB + u) * 64 + l];
-      return v;
-    };
-    f32x4_t v = sum(GATED ? 2 * r : r);
-    if (split.splits > 1) {
-      // Unit (r, u, l) of the gate, then of the up.
-      f32x4_t* out = reinterpret_cast<f32x4_t*>(split.part) +
-                     ((int64_t)part * (gridDim.x / split.splits) + unit) * (BLOCKS * TB * 64) + i;
-      *out = v;
-      if constexpr (GATED) out[OUT * TB * 64] = sum(2 * r + 1);
-      continue;
-    }
-    if constexpr (GATED) v = gated4(v, sum(2 * r + 1), a.act);
-    const int tok = 16 * u + (l & 15), m = m0 + tok, n = n0 + 16 * r + 4 * (l >> 4);
-    if (tok < TOKENS && m < a.m && n < a.n) store4(a, m, n, v);
-  }
-}
-
-// The sum of the splits of a tile, in split order: a thread for each unit of the output.
-template <int BLOCKS, int TOKENS, bool GATED>
-__global__ __launch_bounds__(64) void sum_few_kernel(dlfp::ProjectionArgs a, int gn, int tiles,
-                                                     dlfp::Split split) {
-  constexpr int TB = TOKENS < 16 ? 1 : TOKENS / 16, OUT = GATED ? BLOCKS / 2 : BLOCKS;
-  const int i = blockIdx.x % (OUT * TB), t = blockIdx.x / (OUT * TB), l = threadIdx.x;
-  const int u = i % TB, r = i / TB, tok = 16 * u + (l & 15);
-  const int m = t / gn * TOKENS + tok, n = t % gn * (16 * OUT) + 16 * r + 4 * (l >> 4);
-  if (tok >= TOKENS || m >= a.m || n >= a.n) return;
-  constexpr int UNITS = BLOCKS * TB * 64;
-  const f32x4_t* p = reinterpret_cast<const f32x4_t*>(split.part) + (int64_t)t * UNITS + i * 64 + l;
-  f32x4_t v = p[0], up{};
-  if constexpr (GATED) up = p[OUT * TB * 64];
-  for (int s = 1; s < split.splits; ++s) {
-    v += p[(int64_t)s * tiles * UNITS];
-    if constexpr (GATED) up += p[(int64_t)s * tiles * UNITS + OUT * TB * 64];
-  }
-  if constexpr (GATED) v = gated4(v, up, a.act);
-  store4(a, m, n, v);
+  store_few<BLOCKS, TOKENS, WAVES, GATED>(a, split, acc, smem, tid, wave, unit, part, n0, m0);
 }
 
 }  // namespace

@@ -12,7 +12,7 @@
 
 #include <type_traits>
 
-#include "projection_tiles.h"
+#include "projection_sums.h"
 
 namespace {
 
@@ -30,16 +30,6 @@ __device__ __forceinline__ u32x2_t load_exps(const uint8_t* row, int g, int grou
     for (int i = 0; i < groups; i += 2) v |= (uint64_t)row[i + lh] << (8 * i);
   }
   return u32x2_t{(uint32_t)v, (uint32_t)(v >> 32)};
-}
-
-// Four features of a token.
-__device__ __forceinline__ void store4(const dlfp::ProjectionArgs& a, int m, int n, f32x4_t v) {
-  const int64_t at = (int64_t)m * a.ldo + n;
-  if (a.out_f32)
-    *reinterpret_cast<f32x4_t*>(static_cast<float*>(a.out) + at) = v;
-  else
-    *reinterpret_cast<u32x2_t*>(static_cast<uint16_t*>(a.out) + at) =
-        u32x2_t{pack_bf16(v[0], v[1]), pack_bf16(v[2], v[3])};
 }
 
 // The batch of copies of token stage t holds quarter (t + 3) % 4 of weight stage (t + 3) / 4,
@@ -284,56 +274,13 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile4_kernel(dlfp::Projection
   for (; st < stages; ++st) stage(std::false_type{}, st);
 
   if (split.splits > 1) {
-    // Unit (wave, q, u, g, lane): features 8 g + 4 (lane / 32) .. + 3 of block wn BN + q, token
-    // lane % 32 of block wm BM + u.
-    f32x4_t* out = reinterpret_cast<f32x4_t*>(split.part) +
-                   ((int64_t)unit * WAVES + wave) * (BN * BM * 256) + lane;
-#pragma unroll
-    for (int q = 0; q < BN; ++q)
-#pragma unroll
-      for (int u = 0; u < BM; ++u)
-#pragma unroll
-        for (int g = 0; g < 4; ++g)
-          out[((q * BM + u) * 4 + g) * 64] = f32x4_t{acc[q][u][4 * g], acc[q][u][4 * g + 1],
-                                                     acc[q][u][4 * g + 2], acc[q][u][4 * g + 3]};
+    store_parts(split, acc, (int64_t)unit * WAVES + wave, lane);
     return;
   }
   constexpr int SLICE = LDS / WAVES / 16 * 16;
   wait_copies_barrier<0>();
   store_tile<BN, BM, SLICE, GATED>(a, acc, smem + wave * SLICE, lane,
                                    n0 + (GATED ? 16 : 32) * wn * BN, m0 + 32 * wm * BM);
-}
-
-// The sum of the splits of a tile, in split order: a thread for each unit of the output.
-template <int TN, int TM, int WN, int WM, bool GATED>
-__global__ __launch_bounds__(256) void sum_tiles_kernel(dlfp::ProjectionArgs a, int gm, int gn,
-                                                        dlfp::Split split) {
-  constexpr int BN = TN / WN / 32, BM = TM / WM / 32, GROUPS = GATED ? 2 : 4;
-  constexpr int OUT = TN * TM / 16 * GROUPS, UNITS = TN * TM / 4;
-  constexpr int BLOCKS = OUT / 256;
-  static_assert(OUT % 256 == 0, "whole workgroups");
-  const int t = blockIdx.x / BLOCKS;
-  int i = (blockIdx.x - t * BLOCKS) * 256 + threadIdx.x;
-  const int lane = i & 63, g = (i >> 6) % GROUPS;
-  i = (i >> 6) / GROUPS;
-  const int u = i % BM, q = i / BM % BN, wave = i / BM / BN;
-  constexpr int BAND = 8;
-  const int first = t / (BAND * gn) * BAND, h = min(BAND, gm - first), in = t - first * gn;
-  const int b = wave / WM * BN + q;
-  const int n = (in / h) * (GATED ? TN / 2 : TN) + (GATED ? 16 : 32) * b + 8 * g + 4 * (lane >> 5);
-  const int m = (first + in % h) * TM + 32 * (wave % WM * BM + u) + (lane & 31);
-  if (m >= a.m || n >= a.n) return;
-  const f32x4_t* p = reinterpret_cast<const f32x4_t*>(split.part) + (int64_t)t * UNITS +
-                     (((wave * BN + q) * BM + u) * 4 + g) * 64 + lane;
-  const int64_t step = (int64_t)gm * gn * UNITS;
-  f32x4_t v = p[0], up{};
-  if constexpr (GATED) up = p[2 * 64];
-  for (int s = 1; s < split.splits; ++s) {
-    v += p[s * step];
-    if constexpr (GATED) up += p[s * step + 2 * 64];
-  }
-  if constexpr (GATED) v = gated4(v, up, a.act);
-  store4(a, m, n, v);
 }
 
 }  // namespace

@@ -171,7 +171,7 @@ def test_workspace_sizes():
     """None where the tiles fill the device or K is short, at most 32 MiB, 0 for refused sizes;
     what a form is given is enough for it."""
     size = D.dlfp_projection_workspace
-    for kind in (D.LINEAR_W4, D.GATED_LINEAR_W4):
+    for kind in (D.LINEAR_W4, D.GATED_LINEAR_BF16, D.GATED_LINEAR_W4):
         assert size(kind, 1, 2048, 1024) == 0 and size(kind, 4096, 12288, 4096) == 0
         assert 0 < size(kind, 256, 2560, 25600) <= 32 << 20
         for m, n, k in ((0, 16, 64), (1, 8, 64), (1, 16, 96), (-1, 16, 64), (1, 16, 0)):
