@@ -576,10 +576,20 @@ def _row_stride(t, rows, columns, what):
 
 def _projection_rows(x, n, k, out):
     """(m, row strides of x and out, code of out's type)."""
-    m = x.size(0)
-    if x.dtype is not (_types or _bind_types())[0]:
+    m, columns = x.shape
+    if columns != k or out.shape != (m, n):
+        raise ValueError(f"x must be [m][{k}] and out [m][{n}]")
+    bf16, fp32, _ = _types or _bind_types()
+    if x.dtype is not bf16:
         raise ValueError("x must be bf16")
-    return m, _row_stride(x, m, k, "x"), _row_stride(out, m, n, "out"), _out_code(out.dtype)
+    kind = out.dtype
+    code = 0 if kind is bf16 else 1 if kind is fp32 else _out_code(kind)
+    (ldx, one), (ldo, step) = x.stride(), out.stride()
+    if not one == step == 1:
+        raise ValueError("rows of x and out must be contiguous")
+    if m > 1:
+        return m, ldx, ldo, code
+    return m, k + -k % 8, n + -n % 8, code
 
 
 def _convert_args(w, codes, exps):
@@ -612,9 +622,7 @@ def dlfp_dequantize_w4(codes, exps, w, stream=None) -> None:
 
 
 def _workspace_args(workspace, device):
-    """(address, bytes) of a workspace that may be None."""
-    if workspace is None:
-        return None, 0
+    """(address, bytes) of a workspace."""
     if workspace.get_device() != device or not workspace.is_contiguous():
         raise ValueError("the workspace must be contiguous and beside the tensors")
     return workspace.data_ptr(), workspace.nbytes
@@ -638,9 +646,10 @@ def _linear_w4(x, codes, exps, n, k, out, workspace, stream):
     m, ldx, ldo, code = _projection_rows(x, n, k, out)
     device = x.get_device()
     _check_device(device == codes.get_device() == exps.get_device() == out.get_device(), device, m)
-    st = lib().dlfp_linear_w4(m, n, k, x.data_ptr(), ldx, codes.data_ptr(), exps.data_ptr(),
-                              out.data_ptr(), ldo, code, *_workspace_args(workspace, device),
-                              _stream(stream))
+    room, size = (None, 0) if workspace is None else _workspace_args(workspace, device)
+    st = (_lib or lib()).dlfp_linear_w4(m, n, k, x.data_ptr(), ldx, codes.data_ptr(),
+                                        exps.data_ptr(), out.data_ptr(), ldo, code, room, size,
+                                        _stream(stream))
     if st:
         _check(st, "dlfp_linear_w4")
 
@@ -665,10 +674,10 @@ def dlfp_gated_linear_bf16(x, w_gate, w_up, out, activation: str = "silu", works
     m, ldx, ldo, code = _projection_rows(x, n, k, out)
     device = x.get_device()
     _check_device(device == w_gate.get_device() == w_up.get_device() == out.get_device(), device, m)
-    st = lib().dlfp_gated_linear_bf16(m, n, k, x.data_ptr(), ldx, w_gate.data_ptr(),
-                                      w_up.data_ptr(), _activation(activation), out.data_ptr(),
-                                      ldo, code, *_workspace_args(workspace, device),
-                                      _stream(stream))
+    room, size = (None, 0) if workspace is None else _workspace_args(workspace, device)
+    st = (_lib or lib()).dlfp_gated_linear_bf16(
+        m, n, k, x.data_ptr(), ldx, w_gate.data_ptr(), w_up.data_ptr(), _activation(activation),
+        out.data_ptr(), ldo, code, room, size, _stream(stream))
     if st:
         _check(st, "dlfp_gated_linear_bf16")
 
@@ -689,10 +698,11 @@ def _gated_linear_w4(x, gate_codes, gate_exps, up_codes, up_exps, n, k, out, act
     device = x.get_device()
     _check_device(device == gate_codes.get_device() == gate_exps.get_device() ==
                   up_codes.get_device() == up_exps.get_device() == out.get_device(), device, m)
-    st = lib().dlfp_gated_linear_w4(m, n, k, x.data_ptr(), ldx, gate_codes.data_ptr(),
-                                    gate_exps.data_ptr(), up_codes.data_ptr(), up_exps.data_ptr(),
-                                    _activation(activation), out.data_ptr(), ldo, code,
-                                    *_workspace_args(workspace, device), _stream(stream))
+    room, size = (None, 0) if workspace is None else _workspace_args(workspace, device)
+    st = (_lib or lib()).dlfp_gated_linear_w4(
+        m, n, k, x.data_ptr(), ldx, gate_codes.data_ptr(), gate_exps.data_ptr(),
+        up_codes.data_ptr(), up_exps.data_ptr(), _activation(activation), out.data_ptr(), ldo, code,
+        room, size, _stream(stream))
     if st:
         _check(st, "dlfp_gated_linear_w4")
 

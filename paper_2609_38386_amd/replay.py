@@ -116,6 +116,11 @@ class ReplayConfig:
     layer_proxy: bool = False
     hidden: int = 1024
     mlp: int = 3072
+    # The proxy's weights and feed-forward block.  weight_bits 4 keeps all weights in 4 bits
+    # (e2m1 with an exponent for each 32 columns).  gated: gate, up, activation and product are
+    # one launch whose rows the down projection reads (otherwise it reads the gate's rows).
+    weight_bits: int = 16
+    gated: bool = False
     # The layer's cache and mask.  kv_bits 8 keeps it in e4m3 pages; a window lets a
     # row see its last `window` keys and the first `sinks`; rotary turns queries and
     # keys to their positions on the way to the cache.  With none of them the layer is
@@ -406,6 +411,10 @@ class GpuExecutor:
         self.num_blocks = cfg.num_blocks()
         if cfg.kv_bits not in (8, 16):
             raise ValueError("kv_bits must be 8 or 16")
+        if cfg.weight_bits not in (4, 16):
+            raise ValueError("weight_bits must be 4 or 16")
+        if not cfg.layer_proxy and (cfg.gated or cfg.weight_bits != 16):
+            raise ValueError("gated and weight_bits are of the layer proxy")
         gen = torch.Generator(device=device)
         gen.manual_seed(cfg.seed + seed)
         self.windowed = cfg.windowed
@@ -424,6 +433,7 @@ class GpuExecutor:
         self.out = torch.empty_like(self.q)
         self.proxy = cfg.layer_proxy
         if self.proxy:
+            self.rt = rt
             # weights N(0, 1/fan_in) in bf16, [out features][in features]
             def weight(n_out, n_in):
                 w = torch.empty((n_out, n_in), dtype=torch.float32, device=device)
@@ -432,6 +442,16 @@ class GpuExecutor:
             self.w_q, self.w_k, self.w_v = weight(hq, hid), weight(hkv, hid), weight(hkv, hid)
             self.w_o = weight(hid, hq)
             self.w_gu, self.w_d = weight(2 * cfg.mlp, hid), weight(hid, cfg.mlp)
+            self.gated = cfg.gated
+            if self.gated:
+                self.w_g, self.w_u = self.w_gu[:cfg.mlp], self.w_gu[cfg.mlp:]
+            self.project = D.dlfp_linear_bf16
+            if cfg.weight_bits == 4:
+                self.project = rt.linear
+                names = ("w_q", "w_k", "w_v", "w_o", "w_d") + (("w_g", "w_u") if self.gated else
+                                                               ("w_gu",))
+                for name in names:
+                    setattr(self, name, rt.Weights4.from_bf16(getattr(self, name)))
             self.x = torch.empty((rows, hid), dtype=torch.bfloat16, device=device)
             self.x.normal_(generator=gen)
             self.y = torch.empty((rows, hid), dtype=torch.bfloat16, device=device)
@@ -509,9 +529,9 @@ class GpuExecutor:
         self.timer.start()
         if self.proxy:
             x = self.x[:T]
-            D.dlfp_linear_bf16(x, self.w_q, self.q[:T].view(T, -1))
-            D.dlfp_linear_bf16(x, self.w_k, self.k[:T].view(T, -1))
-            D.dlfp_linear_bf16(x, self.w_v, self.v[:T].view(T, -1))
+            self.project(x, self.w_q, self.q[:T].view(T, -1))
+            self.project(x, self.w_k, self.k[:T].view(T, -1))
+            self.project(x, self.w_v, self.v[:T].view(T, -1))
         if self.windowed:
             self.rt.rope_append(self.dims, self.rope, self.pool, st.d_positions, st.d_slots,
                                 self.q[:T], self.k[:T], self.v[:T], self.q_turned[:T])
@@ -522,9 +542,12 @@ class GpuExecutor:
                                           self.k[:T], self.v[:T], self.pool.k, self.pool.v,
                                           self.scale, self.out[:T], ws)
         if self.proxy:
-            D.dlfp_linear_bf16(self.out[:T].view(T, -1), self.w_o, self.y[:T])
-            D.dlfp_linear_bf16(self.y[:T], self.w_gu, self.gu[:T])
-            D.dlfp_linear_bf16(self.gu[:T, :self.mlp], self.w_d, self.y2[:T])
+            self.project(self.out[:T].view(T, -1), self.w_o, self.y[:T])
+            if self.gated:
+                self.rt.gated_linear(self.y[:T], self.w_g, self.w_u, self.gu[:T, :self.mlp])
+            else:
+                self.project(self.y[:T], self.w_gu, self.gu[:T])
+            self.project(self.gu[:T, :self.mlp], self.w_d, self.y2[:T])
         self.timer.stop()
         enqueue_us = (time.perf_counter() - t_hold) * 1e6
         return self.timer.elapsed_ms(), enqueue_us

@@ -181,12 +181,9 @@ class Weights4:
 _projection_bytes = {}
 
 
-def _projection_workspace(kind: int, x: torch.Tensor, n: int, k: int, workspace, stream):
-    """The workspace of a projection: the caller's, or one of this call alone where the fastest
-    form takes any.  Memory of PyTorch's allocator belongs to the current stream (and to a graph
-    that is being captured on it), so that a call on a stream given by hand does without."""
-    if workspace is not None or stream is not None:
-        return workspace
+def _projection_workspace(kind: int, x: torch.Tensor, n: int, k: int):
+    """The workspace of one call, where the fastest form takes any: memory of PyTorch's allocator,
+    which belongs to the current stream (and to a graph that is being captured on it)."""
     m = x.size(0)
     key = kind, m, n, k
     need = _projection_bytes.get(key)
@@ -201,10 +198,13 @@ def linear(x: torch.Tensor, w, out: torch.Tensor, workspace: Optional[torch.Tens
            stream=None):
     """out = x W^T: x bf16 [m][k], w a Weights4 or bf16 [n][k], out bf16 or float32 [m][n].
     ``workspace``: for 4-bit weights, a tensor of dlfp_projection_workspace bytes that no call
-    beside this one uses (None: taken from PyTorch's allocator, if ``stream`` is None)."""
+    beside this one uses (None: taken from PyTorch's allocator, or, with a ``stream`` given by
+    hand, none)."""
     if isinstance(w, Weights4):
-        ws = _projection_workspace(_d.LINEAR_W4, x, w.n, w.k, workspace, stream)
-        _d._linear_w4(x, w.codes, w.exps, w.n, w.k, out, ws, stream)
+        n, k = w.n, w.k
+        if workspace is None and stream is None:
+            workspace = _projection_workspace(_d.LINEAR_W4, x, n, k)
+        _d._linear_w4(x, w.codes, w.exps, n, k, out, workspace, stream)
     else:
         _d.dlfp_linear_bf16(x, w, out, stream)
 
@@ -217,14 +217,16 @@ def gated_linear(x: torch.Tensor, gate, up, out: torch.Tensor, activation: str =
     if four != isinstance(up, Weights4):
         raise ValueError("gate and up must be of one kind")
     if not four:
-        ws = _projection_workspace(_d.GATED_LINEAR_BF16, x, gate.size(0), gate.size(1), workspace,
-                                   stream)
-        return _d.dlfp_gated_linear_bf16(x, gate, up, out, activation, ws, stream)
-    if (gate.n, gate.k) != (up.n, up.k):
+        if workspace is None and stream is None:
+            workspace = _projection_workspace(_d.GATED_LINEAR_BF16, x, *gate.shape)
+        return _d.dlfp_gated_linear_bf16(x, gate, up, out, activation, workspace, stream)
+    n, k = gate.n, gate.k
+    if up.n != n or up.k != k:
         raise ValueError("gate and up must be [n][k] both")
-    ws = _projection_workspace(_d.GATED_LINEAR_W4, x, gate.n, gate.k, workspace, stream)
-    _d._gated_linear_w4(x, gate.codes, gate.exps, up.codes, up.exps, gate.n, gate.k, out,
-                        activation, ws, stream)
+    if workspace is None and stream is None:
+        workspace = _projection_workspace(_d.GATED_LINEAR_W4, x, n, k)
+    _d._gated_linear_w4(x, gate.codes, gate.exps, up.codes, up.exps, n, k, out, activation,
+                        workspace, stream)
 
 
 class Workspace:

@@ -230,3 +230,11 @@ def test_python_takes_empty_batches():
     rt.gated_linear(_bf16(0, 64), w, w, _bf16(0, 32), stream=0)
     rt.gated_linear(_bf16(0, 64), _bf16(32, 64), _bf16(32, 64), _bf16(0, 32), stream=0)
     rt.Weights4(0, 64, "cpu").quantize(_bf16(0, 64), stream=0)
+
+
+def test_replay_refuses_weights_that_it_has_not():
+    from paper_2609_38386_amd import replay as rp
+    for cfg in (rp.ReplayConfig(layer_proxy=True, weight_bits=8), rp.ReplayConfig(gated=True),
+                rp.ReplayConfig(weight_bits=4)):
+        with pytest.raises(ValueError):
+            rp.GpuExecutor(cfg, "cpu")
