@@ -69,7 +69,7 @@ constexpr Variant VARIANTS[] = {
 #undef WHOLE_K_CALLS
 #undef TILE_CALLS
 
-int launch(const dlfp::ProjectionArgs& a, void* workspace, size_t bytes, hipStream_t stream) {
+int launch(dlfp::ProjectionArgs& a, void* workspace, size_t bytes, hipStream_t stream) {
   (void)hipGetLastError();
   if (std::max<int64_t>(a.ldx, a.k) < dlfp::FAR_STRIDE)
     return launch_best(VARIANTS, true, a, (int64_t)a.n * a.k * 4, workspace, bytes, stream);
@@ -95,7 +95,7 @@ extern "C" int dlfp_gated_linear_bf16(int32_t m, int32_t n, int32_t k, const voi
                                       void* out, int64_t ldo, int32_t out_dtype, void* workspace,
                                       size_t workspace_bytes, hipStream_t stream) {
   dlfp::ProjectionArgs a{static_cast<const uint16_t*>(x), {w_gate, w_up}, {nullptr, nullptr}, out,
-                         ldx, ldo, m, n, k, activation, out_dtype, 0};
+                         ldx, ldo, m, n, k, activation, out_dtype, 0, 0};
   const int st = dlfp::check_projection(a, true, false, out_dtype, workspace);
   return st != DLFP_OK || m == 0 ? st : launch(a, workspace, workspace_bytes, stream);
 }

@@ -143,7 +143,7 @@ int64_t weight_bytes(bool gated, int n, int k) {
 }
 
 template <bool GATED>
-int launch(const dlfp::ProjectionArgs& a, void* workspace, size_t bytes, hipStream_t stream) {
+int launch(dlfp::ProjectionArgs& a, void* workspace, size_t bytes, hipStream_t stream) {
   (void)hipGetLastError();
   if (std::max<int64_t>(a.ldx, a.k) >= FAR_STRIDE) return launch_far<GATED>(a, stream);
   return launch_best(VARIANTS, GATED, a, weight_bytes(GATED, a.n, a.k), workspace, bytes, stream);
@@ -183,7 +183,7 @@ extern "C" int dlfp_linear_w4(int32_t m, int32_t n, int32_t k, const void* x, in
   dlfp::ProjectionArgs a{static_cast<const uint16_t*>(x),
                          {codes, nullptr},
                          {static_cast<const uint8_t*>(exps), nullptr},
-                         out, ldx, ldo, m, n, k, 0, out_dtype, 0};
+                         out, ldx, ldo, m, n, k, 0, out_dtype, 0, 0};
   const int st = dlfp::check_projection(a, false, true, out_dtype, workspace);
   return st != DLFP_OK || m == 0 ? st : launch<false>(a, workspace, workspace_bytes, stream);
 }
@@ -197,7 +197,7 @@ extern "C" int dlfp_gated_linear_w4(int32_t m, int32_t n, int32_t k, const void*
       static_cast<const uint16_t*>(x),
       {gate_codes, up_codes},
       {static_cast<const uint8_t*>(gate_exps), static_cast<const uint8_t*>(up_exps)},
-      out, ldx, ldo, m, n, k, activation, out_dtype, 0};
+      out, ldx, ldo, m, n, k, activation, out_dtype, 0, 0};
   const int st = dlfp::check_projection(a, true, true, out_dtype, workspace);
   return st != DLFP_OK || m == 0 ? st : launch<true>(a, workspace, workspace_bytes, stream);
 }

@@ -15,7 +15,8 @@ struct ProjectionArgs {
   void* out;
   int64_t ldx, ldo;
   int32_t m, n, k, act, out_f32;
-  int32_t wide;  // bf16 output rows take 16-byte stores
+  int32_t wide;    // bf16 output rows take 16-byte stores
+  int32_t stream;  // weights are read past the caches
 };
 
 // A launch whose K is split over `splits` workgroups a tile: the partial sums go to `part`,

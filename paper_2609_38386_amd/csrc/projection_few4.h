@@ -77,7 +77,11 @@ __global__ __launch_bounds__(64 * WAVES) void few4_kernel(dlfp::ProjectionArgs a
 #pragma unroll
       for (int c = 0; c < 2; ++c) {
         const uint32_t off = whole || 8 * s + wg[c] < groups ? woff[c] : woff[c] - 16 * wg[c];
-        lds_copy16(wbase[b] + (int64_t)s * 128, off, d + b * 2048 + c * 1024);
+        const uint32_t to = d + b * 2048 + c * 1024;
+        if (a.stream)
+          lds_stream16(wbase[b] + (int64_t)s * 128, off, to);
+        else
+          lds_copy16(wbase[b] + (int64_t)s * 128, off, to);
       }
 #pragma unroll
     for (int c = 0; c < XC; ++c)

@@ -70,9 +70,14 @@ __global__ __launch_bounds__(64 * WAVES) void gated_few_kernel(dlfp::ProjectionA
 #pragma unroll
     for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
-      for (int c = 0; c < 4; ++c)
-        lds_copy16(wbase[b] + (int64_t)s * (2 * BSTEP), whole || wg[c] < 8 ? woff[c] : woff[c] - 128,
-                   d + b * 4096 + c * 1024);
+      for (int c = 0; c < 4; ++c) {
+        const uint32_t off = whole || wg[c] < 8 ? woff[c] : woff[c] - 128;
+        const uint32_t to = d + b * 4096 + c * 1024;
+        if (a.stream)
+          lds_stream16(wbase[b] + (int64_t)s * (2 * BSTEP), off, to);
+        else
+          lds_copy16(wbase[b] + (int64_t)s * (2 * BSTEP), off, to);
+      }
 #pragma unroll
     for (int c = 0; c < XC; ++c)
       if (TOKENS >= 4 || lane < 16 * TOKENS)
@@ -165,7 +170,12 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void gated_tile_kernel(dlfp::Proje
     const int64_t ko = (int64_t)ks * ROW_BYTES;
     const uint32_t d = lds0 + slot * STAGE;
 #pragma unroll
-    for (int j = 0; j < NL; ++j) lds_copy16(wbase + ko, woff[j], d + j * WAVES * 1024);
+    for (int j = 0; j < NL; ++j) {
+      if (a.stream)
+        lds_stream16(wbase + ko, woff[j], d + j * WAVES * 1024);
+      else
+        lds_copy16(wbase + ko, woff[j], d + j * WAVES * 1024);
+    }
 #pragma unroll
     for (int j = 0; j < ML; ++j)
       lds_copy16(xbase + ko, xoff[j], d + TN * ROW_BYTES + j * WAVES * 1024);

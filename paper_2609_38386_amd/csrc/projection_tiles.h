@@ -60,6 +60,14 @@ __device__ __forceinline__ void lds_copy16(const char* src, uint32_t lds) {
                : "memory", "m0");
 }
 
+// The same past the caches.
+__device__ __forceinline__ void lds_stream16(const char* base, uint32_t off, uint32_t lds) {
+  asm volatile("s_mov_b32 m0, %2\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %0, %1 nt"
+               :
+               : "v"(off), "s"(base), "s"(lds)
+               : "memory", "m0");
+}
+
 // Wait until at most N of this wave's vector-memory operations are in flight.
 template <int N>
 __device__ __forceinline__ void wait_copies() {
