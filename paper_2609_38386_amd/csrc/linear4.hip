@@ -109,29 +109,29 @@ constexpr Launch few_gated() {
 }
 
 // Fitted to 1000 sizes of 1-4096 tokens, 64-25600 features and columns, every variant with every
-// split, plain and gated, weights read from memory.  The choice takes 1.026 times the fastest
-// one's time on average (geometric mean; 1.09 in nine of ten sizes, 1.4 at worst).
+// split, plain and gated, weights read from memory.  The choice takes 1.019 times the fastest
+// one's time on average (geometric mean; 1.06 in nine of ten sizes, 1.29 at worst).
 #define FEW(B, T, W, D) 16 * B, T, W, FSTEP, FewShape<B, T, W, D>::RINGS, B, true
 #define TILE(TN, TM, ...) TN, TM, 0, 0, 0, 0, true
 #define FEW_CALLS(B, T, W, D) {launch_few<false, B, T, W, D>, few_gated<B, T, W, D>()}
 #define TILE_CALLS(...) {launch_tile<false, __VA_ARGS__>, launch_tile<true, __VA_ARGS__>}
 constexpr Variant VARIANTS[] = {
-    {FEW(1, 2, 4, 2), {2.645f, 0.078f, 0.f, 0.064f, 0.053f, 0.163f, 0.046f, 2.393f, 0.03f}, FEW_CALLS(1, 2, 4, 2)},
-    {FEW(2, 2, 4, 1), {2.554f, 0.253f, 0.f, 0.098f, 0.106f, 0.249f, 0.084f, 2.369f, 0.f}, FEW_CALLS(2, 2, 4, 1)},
-    {FEW(1, 4, 8, 2), {2.488f, 0.014f, 0.f, 0.115f, 0.329f, 0.395f, 0.051f, 2.206f, 0.159f}, FEW_CALLS(1, 4, 8, 2)},
-    {FEW(2, 4, 4, 2), {2.879f, 0.001f, 0.027f, 0.111f, 0.046f, 0.369f, 0.066f, 2.461f, 0.273f}, FEW_CALLS(2, 4, 4, 2)},
-    {FEW(1, 8, 4, 2), {2.641f, 0.03f, 0.f, 0.086f, 0.126f, 0.25f, 0.046f, 2.343f, 0.f}, FEW_CALLS(1, 8, 4, 2)},
-    {FEW(2, 8, 4, 2), {2.741f, 0.f, 0.f, 0.159f, 0.23f, 0.413f, 0.055f, 2.533f, 0.09f}, FEW_CALLS(2, 8, 4, 2)},
-    {FEW(2, 8, 4, 1), {2.753f, 0.236f, 0.f, 0.193f, 0.002f, 0.291f, 0.067f, 2.423f, 0.07f}, FEW_CALLS(2, 8, 4, 1)},
-    {FEW(1, 16, 4, 2), {1.491f, 0.f, 0.f, 0.155f, 1.331f, 0.347f, 0.029f, 2.4f, 0.156f}, FEW_CALLS(1, 16, 4, 2)},
-    {FEW(2, 16, 4, 1), {2.755f, 0.187f, 0.f, 0.199f, 0.045f, 0.449f, 0.065f, 2.358f, 0.339f}, FEW_CALLS(2, 16, 4, 1)},
-    {FEW(2, 32, 4, 1), {1.314f, 0.038f, 0.267f, 0.212f, 1.758f, 0.819f, 0.068f, 2.699f, 0.081f}, FEW_CALLS(2, 32, 4, 1)},
-    {FEW(4, 32, 4, 1), {1.425f, 0.f, 0.37f, 0.14f, 1.857f, 1.435f, 0.102f, 2.851f, 0.175f}, FEW_CALLS(4, 32, 4, 1)},
-    {TILE(128, 32, 4, 1, 4, 3, true), {2.385f, 0.127f, 0.165f, 0.054f, 0.945f, 0.089f, 0.075f, 2.803f, 0.194f}, TILE_CALLS(128, 32, 4, 1, 4, 3, true)},
-    {TILE(128, 64, 4, 1, 2, 2, false), {2.827f, 0.289f, 0.587f, 0.133f, 0.476f, 0.045f, 0.069f, 2.926f, 0.187f}, TILE_CALLS(128, 64, 4, 1, 2, 2, false)},
-    {TILE(256, 64, 8, 1, 4, 3, true), {1.819f, 0.f, 1.216f, 0.086f, 2.281f, 0.385f, 0.062f, 2.771f, 0.249f}, TILE_CALLS(256, 64, 8, 1, 4, 3, true)},
-    {TILE(256, 128, 8, 1, 4, 3, false), {2.35f, 0.f, 2.881f, 0.165f, 2.443f, 0.645f, 0.f, 2.764f, 0.236f}, TILE_CALLS(256, 128, 8, 1, 4, 3, false)},
-    {TILE(256, 256, 8, 1, 2, 2, false), {2.837f, 0.f, 4.467f, 0.353f, 3.364f, 1.089f, 0.008f, 3.975f, 0.142f}, TILE_CALLS(256, 256, 8, 1, 2, 2, false)},
+    {FEW(1, 2, 4, 2), 0, {2.645f, 0.078f, 0.f, 0.064f, 0.053f, 0.163f, 0.046f, 0.f, 0.f, 2.393f, 0.03f}, FEW_CALLS(1, 2, 4, 2)},
+    {FEW(2, 2, 4, 1), 0, {2.554f, 0.253f, 0.f, 0.098f, 0.106f, 0.249f, 0.084f, 0.f, 0.f, 2.369f, 0.f}, FEW_CALLS(2, 2, 4, 1)},
+    {FEW(1, 4, 8, 2), 0, {2.488f, 0.014f, 0.f, 0.115f, 0.329f, 0.395f, 0.051f, 0.f, 0.f, 2.206f, 0.159f}, FEW_CALLS(1, 4, 8, 2)},
+    {FEW(2, 4, 4, 2), 0, {2.879f, 0.001f, 0.027f, 0.111f, 0.046f, 0.369f, 0.066f, 0.f, 0.f, 2.461f, 0.273f}, FEW_CALLS(2, 4, 4, 2)},
+    {FEW(1, 8, 4, 2), 0, {2.641f, 0.03f, 0.f, 0.086f, 0.126f, 0.25f, 0.046f, 0.f, 0.f, 2.343f, 0.f}, FEW_CALLS(1, 8, 4, 2)},
+    {FEW(2, 8, 4, 2), 0, {2.741f, 0.f, 0.f, 0.159f, 0.23f, 0.413f, 0.055f, 0.f, 0.f, 2.533f, 0.09f}, FEW_CALLS(2, 8, 4, 2)},
+    {FEW(2, 8, 4, 1), 0, {2.753f, 0.236f, 0.f, 0.193f, 0.002f, 0.291f, 0.067f, 0.f, 0.f, 2.423f, 0.07f}, FEW_CALLS(2, 8, 4, 1)},
+    {FEW(1, 16, 4, 2), 0, {1.491f, 0.f, 0.f, 0.155f, 1.331f, 0.347f, 0.029f, 0.f, 0.f, 2.4f, 0.156f}, FEW_CALLS(1, 16, 4, 2)},
+    {FEW(2, 16, 4, 1), 0, {2.755f, 0.187f, 0.f, 0.199f, 0.045f, 0.449f, 0.065f, 0.f, 0.f, 2.358f, 0.339f}, FEW_CALLS(2, 16, 4, 1)},
+    {FEW(2, 32, 4, 1), 0, {1.314f, 0.038f, 0.267f, 0.212f, 1.758f, 0.819f, 0.068f, 0.f, 0.f, 2.699f, 0.081f}, FEW_CALLS(2, 32, 4, 1)},
+    {FEW(4, 32, 4, 1), 0, {1.425f, 0.f, 0.37f, 0.14f, 1.857f, 1.435f, 0.102f, 0.f, 0.f, 2.851f, 0.175f}, FEW_CALLS(4, 32, 4, 1)},
+    {TILE(128, 32, 4, 1, 4, 3, true), 2, {1.983f, 0.005f, 0.225f, 0.04f, 0.489f, 0.017f, 0.101f, 0.817f, 0.206f, 2.794f, 0.208f}, TILE_CALLS(128, 32, 4, 1, 4, 3, true)},
+    {TILE(128, 64, 4, 1, 2, 2, false), 3, {2.846f, 0.f, 0.577f, 0.11f, 0.353f, 0.f, 0.097f, 0.f, 0.368f, 2.515f, 0.246f}, TILE_CALLS(128, 64, 4, 1, 2, 2, false)},
+    {TILE(256, 64, 8, 1, 4, 3, true), 0, {1.819f, 0.f, 1.216f, 0.086f, 2.281f, 0.385f, 0.062f, 0.f, 0.f, 2.771f, 0.249f}, TILE_CALLS(256, 64, 8, 1, 4, 3, true)},
+    {TILE(256, 128, 8, 1, 4, 3, false), 0, {2.35f, 0.f, 2.881f, 0.165f, 2.443f, 0.645f, 0.f, 0.f, 0.f, 2.764f, 0.236f}, TILE_CALLS(256, 128, 8, 1, 4, 3, false)},
+    {TILE(256, 256, 8, 1, 2, 2, false), 0, {2.837f, 0.f, 4.467f, 0.353f, 3.364f, 1.089f, 0.008f, 0.f, 0.f, 3.975f, 0.142f}, TILE_CALLS(256, 256, 8, 1, 2, 2, false)},
 };
 #undef FEW
 #undef TILE

@@ -21,11 +21,14 @@ typedef int (*Launch)(const dlfp::ProjectionArgs&, Grid, dlfp::Split, hipStream_
 //
 // Time in microseconds, with u = tiles times splits / 256, s = steps of a unit (of a wavefront
 // where they share them, of 64 columns otherwise) and b = MB of weights:
-//   c0 + c1 s + (c2 + c3 s) u + (c4 + c5 s) ceil(u) + c6 b, with splits + c7 + c8 MB of sums
+//   c0 + c1 s + (c2 + c3 s) u + (c4 + c5 s) ceil(u) + c6 b + (c7 + c8 s) ceil(u / resident)
+// and with splits + c9 + c10 times the MB of partial sums, where `resident` workgroups fit a
+// compute unit (0: left out).
 struct Variant {
   int rows, tokens, waves, columns, lds, blocks;
   bool splits;
-  float c[9];
+  int resident;
+  float c[11];
   Launch launch[2];  // plain and gated
 };
 
@@ -68,7 +71,11 @@ Plan choose(const Variant (&variants)[COUNT], bool gated, int m, int n, int k, i
       const int share = splits * v.waves;
       const float s = v.waves ? (float)((steps + share - 1) / share) : (float)k / 64 / (float)splits;
       float t = fixed + c[1] * s + (c[2] + c[3] * s) * u + (c[4] + c[5] * s) * r;
-      if (splits > 1) t += c[7] + c[8] * 1e-6f * (float)(splits * bytes);
+      if (v.resident) {
+        const int64_t most = (int64_t)CUS * v.resident;
+        t += (c[7] + c[8] * s) * (float)((tiles * splits + most - 1) / most);
+      }
+      if (splits > 1) t += c[9] + c[10] * 1e-6f * (float)(splits * bytes);
       if (best.variant && t >= least) continue;
       least = t;
       best = Plan{&v, g, splits, splits > 1 ? splits * bytes : 0};

@@ -245,6 +245,17 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile4_kernel(dlfp::Projection
         read_x(slot, kk + 1, set ^ 1);
         convert(s, kk + 1, set ^ 1);
         multiply(set, set);
+        if constexpr (BN == 1 && BM == 4) {
+          // A read of the next operands and half of a row block's conversions beside each product:
+          // 2-3% of a 256 x 128 tile's time (2048 x 4096 x 12288 176 -> 172 us); other shapes lose
+          // by it (256 x 256 9%).
+#pragma unroll
+          for (int i = 0; i < BN * BM; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x008, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x002, 2, 0);
+          }
+        }
       }
       if (INSIDE || ks + 1 < steps)
         advance([&](int w) {
