@@ -71,9 +71,10 @@ int dlfp_dequantize_w4(int32_t n, int32_t k, const void* codes, const void* exps
  * fastest form takes dlfp_projection_workspace says; with fewer (0 with null) a form that
  * fits is taken.  Its contents matter neither before nor after; calls that may overlap (on
  * two streams, or as parts of graphs that may) need workspaces of their own.
- * Errors: DLFP_EINVAL, DLFP_EUNSUPPORTED, DLFP_ERANGE (2^32 threads or more: a launch of
- * many tokens has up to 512 for each 256 of them and 256 features, one with rows 2^22
- * elements or more apart 512 for each 16 and 16), DLFP_EHIP. */
+ * Errors: DLFP_EINVAL, DLFP_EUNSUPPORTED, DLFP_ERANGE (more than 2^31 - 1025 tokens or
+ * features, or 2^32 threads or more: a launch of many tokens has up to 512 for each 256 of
+ * them and 256 features, one with rows 2^22 elements or more apart 512 for each 16 and 16),
+ * DLFP_EHIP (of the second launch: the first stays enqueued). */
 int dlfp_linear_w4(int32_t m, int32_t n, int32_t k, const void* x, int64_t ldx, const void* codes,
                    const void* exps, void* out, int64_t ldo, int32_t out_dtype, void* workspace,
                    size_t workspace_bytes, hipStream_t stream);

@@ -160,6 +160,7 @@ int check_projection(ProjectionArgs& a, bool gated, bool codes, int32_t out_dtyp
   if (gated && a.act != DLFP_SILU && a.act != DLFP_GELU) return DLFP_EINVAL;
   if (a.n % 16 || a.k % 64) return DLFP_EUNSUPPORTED;
   if (a.ldx < a.k || a.ldo < a.n || a.ldx % 8 || a.ldo % 4) return DLFP_EINVAL;
+  if (a.m > MOST_ROWS || a.n > MOST_ROWS) return DLFP_ERANGE;
   if (a.m == 0) return DLFP_OK;
   const auto aligned = [](const void* p, uintptr_t to) {
     return p && reinterpret_cast<uintptr_t>(p) % to == 0;

@@ -29,6 +29,9 @@ struct Split {
 // Row strides from here on take 64-bit offsets (255 rows of 2 bytes each fit 32 bits below).
 constexpr int FAR_STRIDE = 1 << 22;
 
+// Tokens and features at most, so that the index of a tile's last row fits 31 bits.
+constexpr int MOST_ROWS = 0x7fffffff - 1024;
+
 // Bytes of partial sums of the fastest form.
 int64_t workspace_w4(bool gated, int m, int n, int k);
 int64_t workspace_gated(int m, int n, int k);

@@ -121,7 +121,11 @@ COMMON = [(dict(m=-1), -1), (dict(n=0), -1), (dict(n=-16), -1), (dict(k=0), -1),
           (dict(ldx=56), -1), (dict(ldx=68), -1), (dict(ldo=28), -1), (dict(ldo=34), -1),
           (dict(ldx=0), -1), (dict(ldo=-32), -1), (dict(dtype=2), -1), (dict(dtype=-1), -1),
           (dict(x=None), -1), (dict(out=None), -1), (dict(x=P + 8), -1), (dict(out=P + 4), -1),
-          (dict(out=P + 8, dtype=1), -1), (dict(ws=P + 8), -1)]
+          (dict(out=P + 8, dtype=1), -1), (dict(ws=P + 8), -1),
+          (dict(n=(1 << 31) - 16, ldo=(1 << 31) - 16), -2), (dict(m=(1 << 31) - 1), -2),
+          (dict(m=1 << 30, n=1 << 24, ldo=1 << 24), -2),
+          (dict(m=1 << 30, k=1 << 22, ldx=1 << 22, n=1 << 12, ldo=1 << 12), -2),
+          (dict(m=1 << 30, ldx=1 << 22, n=1 << 12, ldo=1 << 12), -2)]
 
 
 @pytest.mark.parametrize("change,status", COMMON + [(dict(codes=None), -1), (dict(exps=None), -1),
@@ -199,6 +203,8 @@ def test_python_refusals():
            lambda: rt.linear(x, w, _bf16(3, 32)),
            lambda: rt.linear(_bf16(2, 128)[:, ::2], w, out),
            lambda: rt.linear(x, w, _bf16(32, 2).T),
+           lambda: rt.linear(x[0], w, out),
+           lambda: rt.linear(x, w, out, workspace=torch.zeros(64)[::2]),
            lambda: rt.gated_linear(x, w, w, out, activation="relu"),
            lambda: rt.gated_linear(x, w, rt.Weights4(16, 64, "cpu"), out),
            lambda: rt.gated_linear(x, w, _bf16(32, 64), out),
