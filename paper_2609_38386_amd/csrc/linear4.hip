@@ -68,12 +68,12 @@ int launch_far(const dlfp::ProjectionArgs& a, hipStream_t stream) {
 
 // ---------------------------------------------------------------- launches
 
-template <bool GATED, int BLOCKS, int TOKENS, int WAVES, int DEPTH>
+template <bool GATED, int BLOCKS, int TOKENS, int WAVES, int DEPTH, int HALVES>
 int launch_few(const dlfp::ProjectionArgs& a, Grid g, dlfp::Split split, hipStream_t stream) {
-  using Shape = FewShape<BLOCKS, TOKENS, WAVES, DEPTH>;
+  using Shape = FewShape<BLOCKS, TOKENS, WAVES, DEPTH, HALVES>;
   const int64_t tiles = g.down * g.across;
   if (tiles * split.splits * (64 * WAVES) >= (int64_t)1 << 32) return DLFP_ERANGE;
-  few4_kernel<BLOCKS, TOKENS, WAVES, DEPTH, GATED>
+  few4_kernel<BLOCKS, TOKENS, WAVES, DEPTH, HALVES, GATED>
       <<<(uint32_t)(tiles * split.splits), 64 * WAVES, (size_t)Shape::lds(a.k), stream>>>(a, split);
   if (split.splits > 1) {
     constexpr int UNITS = (GATED ? BLOCKS / 2 : BLOCKS) * Shape::TB;
@@ -100,38 +100,40 @@ int launch_tile(const dlfp::ProjectionArgs& a, Grid g, dlfp::Split split, hipStr
 
 // ---------------------------------------------------------------- choice
 
-template <int BLOCKS, int TOKENS, int WAVES, int DEPTH>
+template <int BLOCKS, int TOKENS, int WAVES, int DEPTH, int HALVES>
 constexpr Launch few_gated() {
   if constexpr (BLOCKS % 2)
     return nullptr;  // (blocks of the gate and of the up come in pairs)
   else
-    return launch_few<true, BLOCKS, TOKENS, WAVES, DEPTH>;
+    return launch_few<true, BLOCKS, TOKENS, WAVES, DEPTH, HALVES>;
 }
 
 // Fitted to 1000 sizes of 1-4096 tokens, 64-25600 features and columns, every variant with every
-// split, plain and gated, weights read from memory.  The choice takes 1.019 times the fastest
-// one's time on average (geometric mean; 1.06 in nine of ten sizes, 1.29 at worst).
-#define FEW(B, T, W, D) 16 * B, T, W, FSTEP, FewShape<B, T, W, D>::RINGS, B, true
+// split, plain and gated, weights read from memory.  The choice takes 1.017 times the fastest
+// one's time on average (geometric mean; 1.06 in nine of ten sizes, 1.34 at worst).
+#define FEW(B, T, W, D, H) 16 * B, T, W, H* FHALF, FewShape<B, T, W, D, H>::RINGS, B, true
 #define TILE(TN, TM, ...) TN, TM, 0, 0, 0, 0, true
-#define FEW_CALLS(B, T, W, D) {launch_few<false, B, T, W, D>, few_gated<B, T, W, D>()}
+#define FEW_CALLS(B, T, W, D, H) {launch_few<false, B, T, W, D, H>, few_gated<B, T, W, D, H>()}
 #define TILE_CALLS(...) {launch_tile<false, __VA_ARGS__>, launch_tile<true, __VA_ARGS__>}
 constexpr Variant VARIANTS[] = {
-    {FEW(1, 2, 4, 2), 0, {2.645f, 0.078f, 0.f, 0.064f, 0.053f, 0.163f, 0.046f, 0.f, 0.f, 2.393f, 0.03f}, FEW_CALLS(1, 2, 4, 2)},
-    {FEW(2, 2, 4, 1), 0, {2.554f, 0.253f, 0.f, 0.098f, 0.106f, 0.249f, 0.084f, 0.f, 0.f, 2.369f, 0.f}, FEW_CALLS(2, 2, 4, 1)},
-    {FEW(1, 4, 8, 2), 0, {2.488f, 0.014f, 0.f, 0.115f, 0.329f, 0.395f, 0.051f, 0.f, 0.f, 2.206f, 0.159f}, FEW_CALLS(1, 4, 8, 2)},
-    {FEW(2, 4, 4, 2), 0, {2.879f, 0.001f, 0.027f, 0.111f, 0.046f, 0.369f, 0.066f, 0.f, 0.f, 2.461f, 0.273f}, FEW_CALLS(2, 4, 4, 2)},
-    {FEW(1, 8, 4, 2), 0, {2.641f, 0.03f, 0.f, 0.086f, 0.126f, 0.25f, 0.046f, 0.f, 0.f, 2.343f, 0.f}, FEW_CALLS(1, 8, 4, 2)},
-    {FEW(2, 8, 4, 2), 0, {2.741f, 0.f, 0.f, 0.159f, 0.23f, 0.413f, 0.055f, 0.f, 0.f, 2.533f, 0.09f}, FEW_CALLS(2, 8, 4, 2)},
-    {FEW(2, 8, 4, 1), 0, {2.753f, 0.236f, 0.f, 0.193f, 0.002f, 0.291f, 0.067f, 0.f, 0.f, 2.423f, 0.07f}, FEW_CALLS(2, 8, 4, 1)},
-    {FEW(1, 16, 4, 2), 0, {1.491f, 0.f, 0.f, 0.155f, 1.331f, 0.347f, 0.029f, 0.f, 0.f, 2.4f, 0.156f}, FEW_CALLS(1, 16, 4, 2)},
-    {FEW(2, 16, 4, 1), 0, {2.755f, 0.187f, 0.f, 0.199f, 0.045f, 0.449f, 0.065f, 0.f, 0.f, 2.358f, 0.339f}, FEW_CALLS(2, 16, 4, 1)},
-    {FEW(2, 32, 4, 1), 0, {1.314f, 0.038f, 0.267f, 0.212f, 1.758f, 0.819f, 0.068f, 0.f, 0.f, 2.699f, 0.081f}, FEW_CALLS(2, 32, 4, 1)},
-    {FEW(4, 32, 4, 1), 0, {1.425f, 0.f, 0.37f, 0.14f, 1.857f, 1.435f, 0.102f, 0.f, 0.f, 2.851f, 0.175f}, FEW_CALLS(4, 32, 4, 1)},
-    {TILE(128, 32, 4, 1, 4, 3, true), 2, {1.983f, 0.005f, 0.225f, 0.04f, 0.489f, 0.017f, 0.101f, 0.817f, 0.206f, 2.794f, 0.208f}, TILE_CALLS(128, 32, 4, 1, 4, 3, true)},
-    {TILE(128, 64, 4, 1, 2, 2, false), 3, {2.846f, 0.f, 0.577f, 0.11f, 0.353f, 0.f, 0.097f, 0.f, 0.368f, 2.515f, 0.246f}, TILE_CALLS(128, 64, 4, 1, 2, 2, false)},
-    {TILE(256, 64, 8, 1, 4, 3, true), 0, {1.819f, 0.f, 1.216f, 0.086f, 2.281f, 0.385f, 0.062f, 0.f, 0.f, 2.771f, 0.249f}, TILE_CALLS(256, 64, 8, 1, 4, 3, true)},
-    {TILE(256, 128, 8, 1, 4, 3, false), 0, {2.35f, 0.f, 2.881f, 0.165f, 2.443f, 0.645f, 0.f, 0.f, 0.f, 2.764f, 0.236f}, TILE_CALLS(256, 128, 8, 1, 4, 3, false)},
-    {TILE(256, 256, 8, 1, 2, 2, false), 0, {2.837f, 0.f, 4.467f, 0.353f, 3.364f, 1.089f, 0.008f, 0.f, 0.f, 3.975f, 0.142f}, TILE_CALLS(256, 256, 8, 1, 2, 2, false)},
+    {FEW(1, 2, 4, 2, 2), 0, {2.638f, 0.117f, 0.045f, 0.023f, 0.018f, 0.195f, 0.043f, 0.f, 0.f, 2.376f, 0.052f}, FEW_CALLS(1, 2, 4, 2, 2)},
+    {FEW(2, 2, 4, 1, 2), 0, {2.673f, 0.288f, 0.f, 0.12f, 0.058f, 0.223f, 0.083f, 0.f, 0.f, 2.392f, 0.f}, FEW_CALLS(2, 2, 4, 1, 2)},
+    {FEW(1, 4, 8, 2, 2), 0, {2.524f, 0.004f, 0.f, 0.097f, 0.326f, 0.422f, 0.051f, 0.f, 0.f, 2.237f, 0.015f}, FEW_CALLS(1, 4, 8, 2, 2)},
+    {FEW(2, 4, 4, 2, 2), 0, {2.868f, 0.034f, 0.072f, 0.029f, 0.f, 0.466f, 0.06f, 0.f, 0.f, 2.396f, 0.352f}, FEW_CALLS(2, 4, 4, 2, 2)},
+    {FEW(1, 8, 4, 2, 2), 0, {2.658f, 0.053f, 0.075f, 0.038f, 0.056f, 0.309f, 0.039f, 0.f, 0.f, 2.302f, 0.f}, FEW_CALLS(1, 8, 4, 2, 2)},
+    {FEW(2, 8, 4, 2, 2), 0, {2.756f, 0.044f, 0.087f, 0.11f, 0.162f, 0.483f, 0.049f, 0.f, 0.f, 2.469f, 0.104f}, FEW_CALLS(2, 8, 4, 2, 2)},
+    {FEW(2, 8, 4, 1, 2), 0, {2.817f, 0.243f, 0.f, 0.204f, 0.f, 0.289f, 0.063f, 0.f, 0.f, 2.411f, 0.086f}, FEW_CALLS(2, 8, 4, 1, 2)},
+    {FEW(1, 16, 4, 2, 2), 0, {1.513f, 0.f, 0.f, 0.143f, 1.323f, 0.393f, 0.023f, 0.f, 0.f, 2.37f, 0.233f}, FEW_CALLS(1, 16, 4, 2, 2)},
+    {FEW(4, 16, 4, 1, 2), 0, {2.999f, 0.061f, 0.f, 0.285f, 0.f, 0.924f, 0.095f, 0.f, 0.f, 2.505f, 0.044f}, FEW_CALLS(4, 16, 4, 1, 2)},
+    {FEW(2, 16, 8, 1, 1), 0, {2.465f, 0.107f, 0.f, 0.119f, 0.f, 0.894f, 0.13f, 0.f, 0.f, 2.7f, 0.f}, FEW_CALLS(2, 16, 8, 1, 1)},
+    {FEW(2, 32, 8, 1, 1), 0, {1.214f, 0.031f, 0.f, 0.349f, 1.327f, 1.29f, 0.093f, 0.f, 0.f, 2.889f, 0.255f}, FEW_CALLS(2, 32, 8, 1, 1)},
+    {FEW(4, 32, 4, 1, 1), 0, {2.749f, 0.34f, 0.f, 0.061f, 0.f, 1.074f, 0.138f, 0.f, 0.f, 2.831f, 0.256f}, FEW_CALLS(4, 32, 4, 1, 1)},
+    {FEW(4, 32, 4, 1, 2), 0, {1.283f, 0.f, 0.362f, 0.08f, 2.199f, 1.339f, 0.088f, 0.f, 0.f, 2.923f, 0.258f}, FEW_CALLS(4, 32, 4, 1, 2)},
+    {TILE(128, 32, 4, 1, 4, 3, true), 2, {1.821f, 0.011f, 0.181f, 0.044f, 0.505f, 0.019f, 0.097f, 0.981f, 0.197f, 2.762f, 0.208f}, TILE_CALLS(128, 32, 4, 1, 4, 3, true)},
+    {TILE(128, 64, 4, 1, 2, 2, false), 3, {2.797f, 0.f, 0.605f, 0.103f, 0.37f, 0.f, 0.096f, 0.f, 0.376f, 2.371f, 0.273f}, TILE_CALLS(128, 64, 4, 1, 2, 2, false)},
+    {TILE(256, 64, 8, 1, 4, 3, true), 0, {1.763f, 0.f, 1.289f, 0.085f, 2.341f, 0.385f, 0.063f, 0.f, 0.f, 2.764f, 0.252f}, TILE_CALLS(256, 64, 8, 1, 4, 3, true)},
+    {TILE(256, 128, 8, 1, 4, 3, false), 0, {1.982f, 0.f, 2.434f, 0.19f, 2.871f, 0.603f, 0.004f, 0.f, 0.f, 2.768f, 0.229f}, TILE_CALLS(256, 128, 8, 1, 4, 3, false)},
+    {TILE(256, 256, 8, 1, 2, 2, false), 0, {3.31f, 0.f, 5.732f, 0.32f, 2.461f, 1.113f, 0.014f, 0.f, 0.f, 3.875f, 0.157f}, TILE_CALLS(256, 256, 8, 1, 2, 2, false)},
 };
 #undef FEW
 #undef TILE

@@ -1,5 +1,5 @@
 // Projections of few tokens with 4-bit weights: the kernel of projection_few.h whose steps are
-// 256 columns deep.  Of a block, lane l takes row l % 16 and, of half h of a step, group
+// 128 or 256 columns deep.  Of a block, lane l takes row l % 16 and, of half h of a step, group
 // 4 h + l / 16: 16 bytes of codes that are the operands of four products; which columns a
 // product takes is free as long as both operands agree.  The exponents of the block's rows are
 // one contiguous piece of memory, copied whole before the first step.
@@ -9,14 +9,14 @@
 
 namespace {
 
-constexpr int FSTEP = 256;  // columns of a step
+constexpr int FHALF = 128;  // columns of a half: a step has one or two
 
-template <int BLOCKS, int TOKENS, int WAVES, int DEPTH>
+template <int BLOCKS, int TOKENS, int WAVES, int DEPTH, int HALVES>
 struct FewShape {
   static constexpr int TB = TOKENS < 16 ? 1 : TOKENS / 16;           // token blocks
-  static constexpr int WC = 2 * BLOCKS;                              // copies: of weights
-  static constexpr int XC = TOKENS < 2 ? 1 : TOKENS / 2;             // of tokens
-  static constexpr int SLOT = BLOCKS * 2048 + TOKENS * 512;
+  static constexpr int WC = HALVES * BLOCKS;                         // copies: of weights
+  static constexpr int XC = (TOKENS * HALVES + 3) / 4;               // of tokens
+  static constexpr int SLOT = HALVES * (BLOCKS * 1024 + TOKENS * 256);
   static constexpr int RING = DEPTH * SLOT, RESULT = BLOCKS * TB * 1024;
   static constexpr int RINGS = WAVES * (RING > RESULT ? RING : RESULT);
   // LDS of a launch: the rings, then each block's exponents in whole copies.
@@ -24,10 +24,18 @@ struct FewShape {
   static int64_t lds(int k) { return RINGS + BLOCKS * exps(k); }
 };
 
-template <int BLOCKS, int TOKENS, int WAVES, int DEPTH, bool GATED>
+// Position of a row's 16 bytes of weights: rows of 128 bytes as in a tile, of 64 bytes spread over
+// the banks by bits 2-3 of the row.
+template <int HALVES>
+__device__ __forceinline__ int few_swz(int row) {
+  return HALVES == 2 ? swz(row) : (row >> 2) & 3;
+}
+
+template <int BLOCKS, int TOKENS, int WAVES, int DEPTH, int HALVES, bool GATED>
 __global__ __launch_bounds__(64 * WAVES) void few4_kernel(dlfp::ProjectionArgs a,
                                                                 dlfp::Split split) {
-  using Shape = FewShape<BLOCKS, TOKENS, WAVES, DEPTH>;
+  using Shape = FewShape<BLOCKS, TOKENS, WAVES, DEPTH, HALVES>;
+  constexpr int STEP = HALVES * FHALF, GROUPS = STEP / 32;  // of a step
   constexpr int TB = Shape::TB, WC = Shape::WC, XC = Shape::XC, L = WC + XC, SLOT = Shape::SLOT;
   extern __shared__ __attribute__((aligned(16))) char few_lds[];
   char* smem = few_lds;
@@ -36,27 +44,28 @@ __global__ __launch_bounds__(64 * WAVES) void few4_kernel(dlfp::ProjectionArgs a
   const uint32_t gn = (uint32_t)(a.n + FEATURES - 1) / FEATURES;
   const uint32_t unit = blockIdx.x / split.splits, part = blockIdx.x - unit * split.splits;
   const int n0 = (int)(unit % gn) * FEATURES, m0 = (int)(unit / gn) * TOKENS;
-  const int groups = a.k >> 5, steps = (a.k + FSTEP - 1) / FSTEP;
+  const int groups = a.k >> 5, steps = (a.k + STEP - 1) / STEP;
   const int64_t shares = (int64_t)WAVES * split.splits, share = (int64_t)WAVES * part + wave;
   const int first = (int)(steps * share / shares);
   const int count = (int)(steps * (share + 1) / shares) - first;
   // First row of block b in its weights: past the end, the last 16 again.
   auto row0 = [&](int b) { return min(n0 + 16 * (GATED ? b >> 1 : b), a.n - 16); };
 
-  // Copies of weights: rows 8 c + lane / 8, the group that belongs at position lane % 8; of
-  // tokens: row 2 c + lane / 32, the 16 bytes that belong at position lane % 32.
-  uint32_t woff[2], xoff[XC];
-  int wg[2], xg[XC];
+  // Copies of weights: rows WROWS c + lane / GROUPS, the group that belongs at position
+  // lane % GROUPS; of tokens: rows of 4 GROUPS pieces of 16 bytes.
+  constexpr int WROWS = 64 / GROUPS, XPIECES = 4 * GROUPS, XROWS = 64 / XPIECES;
+  uint32_t woff[HALVES], xoff[XC];
+  int wg[HALVES], xg[XC];
 #pragma unroll
-  for (int c = 0; c < 2; ++c) {
-    const int r = 8 * c + (lane >> 3);
-    wg[c] = (lane & 7) ^ swz(r);
+  for (int c = 0; c < HALVES; ++c) {
+    const int r = WROWS * c + lane / GROUPS;
+    wg[c] = (lane % GROUPS) ^ few_swz<HALVES>(r);
     woff[c] = (uint32_t)(r * (a.k >> 1) + 16 * wg[c]);
   }
 #pragma unroll
   for (int c = 0; c < XC; ++c) {
-    const int r = 2 * c + (lane >> 5);
-    xg[c] = (lane & 31) ^ (r & 15);
+    const int r = XROWS * c + lane / XPIECES;
+    xg[c] = (lane % XPIECES) ^ (r & (TOKENS < 16 ? TOKENS - 1 : 15));
     xoff[c] = (uint32_t)(min(r, a.m - 1 - m0) * (int)a.ldx * 2 + 16 * xg[c]);
   }
   const char* wbase[BLOCKS];
@@ -70,24 +79,28 @@ __global__ __launch_bounds__(64 * WAVES) void few4_kernel(dlfp::ProjectionArgs a
   auto issue = [&](auto inside, int t, int slot) {
     const int s = first + t;
     // Past the row's end the step's first group again.
-    const bool whole = inside.value || 8 * s + 8 <= groups;
+    const bool whole = inside.value || GROUPS * s + GROUPS <= groups;
     const uint32_t d = lds0 + slot * SLOT;
 #pragma unroll
     for (int b = 0; b < BLOCKS; ++b)
 #pragma unroll
-      for (int c = 0; c < 2; ++c) {
-        const uint32_t off = whole || 8 * s + wg[c] < groups ? woff[c] : woff[c] - 16 * wg[c];
-        const uint32_t to = d + b * 2048 + c * 1024;
+      for (int c = 0; c < HALVES; ++c) {
+        const uint32_t off =
+            whole || GROUPS * s + wg[c] < groups ? woff[c] : woff[c] - 16 * wg[c];
+        const uint32_t to = d + (b * HALVES + c) * 1024;
+        const char* from = wbase[b] + (int64_t)s * (STEP / 2);
         if (a.stream)
-          lds_stream16(wbase[b] + (int64_t)s * 128, off, to);
+          lds_stream16(from, off, to);
         else
-          lds_copy16(wbase[b] + (int64_t)s * 128, off, to);
+          lds_copy16(from, off, to);
       }
 #pragma unroll
     for (int c = 0; c < XC; ++c)
-      if (TOKENS >= 2 || lane < 32) {
-        const uint32_t off = whole || 8 * s + (xg[c] >> 2) < groups ? xoff[c] : xoff[c] - 16 * xg[c];
-        lds_copy16(xbase + (int64_t)s * (2 * FSTEP), off, d + BLOCKS * 2048 + c * 1024);
+      if (TOKENS >= XROWS || lane < XPIECES * TOKENS) {
+        const uint32_t off =
+            whole || GROUPS * s + (xg[c] >> 2) < groups ? xoff[c] : xoff[c] - 16 * xg[c];
+        lds_copy16(xbase + (int64_t)s * (2 * STEP), off,
+                   d + BLOCKS * HALVES * 1024 + c * 1024);
       }
   };
 
@@ -121,31 +134,32 @@ __global__ __launch_bounds__(64 * WAVES) void few4_kernel(dlfp::ProjectionArgs a
     else
       wait_stages<DEPTH - 1, L, false>(count - 1 - t);
     const char* p = ring + slot * SLOT;
-    u32x4_t codes[2][BLOCKS];
-    bf16x8_t xf[2][TB][4];
-    uint32_t e[2][BLOCKS];
+    u32x4_t codes[HALVES][BLOCKS];
+    bf16x8_t xf[HALVES][TB][4];
+    uint32_t e[HALVES][BLOCKS];
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
+    for (int h = 0; h < HALVES; ++h) {
 #pragma unroll
       for (int b = 0; b < BLOCKS; ++b) {
         codes[h][b] = *reinterpret_cast<const u32x4_t*>(
-            p + b * 2048 + lr * 128 + (((4 * h + quad) ^ swz(lr)) << 4));
-        e[h][b] = *reinterpret_cast<const uint8_t*>(ex + b * eblock + 8 * (first + t) + 4 * h);
+            p + (b * 16 + lr) * (16 * GROUPS) + (((4 * h + quad) ^ few_swz<HALVES>(lr)) << 4));
+        e[h][b] =
+            *reinterpret_cast<const uint8_t*>(ex + b * eblock + GROUPS * (first + t) + 4 * h);
       }
 #pragma unroll
       for (int u = 0; u < TB; ++u)
 #pragma unroll
         for (int i = 0; i < 4; ++i)
           xf[h][u][i] = *reinterpret_cast<const bf16x8_t*>(
-              p + BLOCKS * 2048 + (16 * u + tr) * 512 +
+              p + BLOCKS * HALVES * 1024 + (16 * u + tr) * (16 * XPIECES) +
               (((16 * h + 4 * quad + i) ^ tr) << 4));
     }
     wait_lds();  // the slot's reads have returned before it is refilled
     if (inside.value || t + DEPTH < count) issue(inside, t + DEPTH, slot);
-    if (!inside.value && 8 * (first + t) + 8 > groups) {  // past the end of the rows: zeros
+    if (!inside.value && GROUPS * (first + t) + GROUPS > groups) {  // past the end of the rows: zeros
 #pragma unroll
-      for (int h = 0; h < 2; ++h)
-        if (8 * (first + t) + 4 * h + quad >= groups) {
+      for (int h = 0; h < HALVES; ++h)
+        if (GROUPS * (first + t) + 4 * h + quad >= groups) {
 #pragma unroll
           for (int b = 0; b < BLOCKS; ++b) codes[h][b] = u32x4_t{}, e[h][b] = 0;
 #pragma unroll
@@ -155,7 +169,7 @@ __global__ __launch_bounds__(64 * WAVES) void few4_kernel(dlfp::ProjectionArgs a
         }
     }
 #pragma unroll
-    for (int h = 0; h < 2; ++h)
+    for (int h = 0; h < HALVES; ++h)
 #pragma unroll
       for (int i = 0; i < 4; ++i)
 #pragma unroll
