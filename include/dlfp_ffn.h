@@ -69,8 +69,9 @@ int dlfp_dequantize_w4(int32_t n, int32_t k, const void* codes, const void* exps
  * workspace: device, 16-byte aligned, or null: where there are few tiles, K is split over
  * workgroups, whose partial sums pass through it into a second launch.  How many bytes the
  * fastest form takes dlfp_projection_workspace says; with fewer (0 with null) a form that
- * fits is taken.  Its contents matter neither before nor after; calls that may overlap (on
- * two streams, or as parts of graphs that may) need workspaces of their own.
+ * fits is taken.  It overlaps no other buffer, and its contents matter neither before
+ * nor after; calls that may overlap (on two streams, or as parts of graphs that may) need
+ * workspaces of their own.
  * Errors: DLFP_EINVAL, DLFP_EUNSUPPORTED, DLFP_ERANGE (more than 2^31 - 1025 tokens or
  * features, or 2^32 threads or more: a launch of many tokens has up to 512 for each 256 of
  * them and 256 features, one with rows 2^22 elements or more apart 512 for each 16 and 16),

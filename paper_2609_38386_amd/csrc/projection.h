@@ -32,6 +32,13 @@ constexpr int FAR_STRIDE = 1 << 22;
 // Tokens and features at most, so that the index of a tile's last row fits 31 bits.
 constexpr int MOST_ROWS = 0x7fffffff - 1024;
 
+// Outputs from here on are 2^32 threads or more in any form (512 for each 256 x 256 at least),
+// below it the products of sizes that the choice takes fit 63 bits.
+constexpr int64_t MOST_OUTPUTS = (int64_t)1 << 39;
+inline bool too_many(int m, int n) {
+  return m > MOST_ROWS || n > MOST_ROWS || (int64_t)m * n >= MOST_OUTPUTS;
+}
+
 // Bytes of partial sums of the fastest form.
 int64_t workspace_w4(bool gated, int m, int n, int k);
 int64_t workspace_gated(int m, int n, int k);

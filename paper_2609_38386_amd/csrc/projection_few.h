@@ -5,6 +5,18 @@
 // in turn) and TOKENS tokens.  Its wavefronts (and, with splits, several workgroups) share K,
 // each through a ring of its own without barriers, and their results are added through LDS, in
 // wavefront order.
+//
+// Why through LDS: as operands come, neighbouring lanes hold 16 bytes of different rows, and a
+// load of 64 such pieces keeps the address unit busy four times as long as a copy of whole row
+// segments (weights and tokens straight from memory into registers: 1 token of 4096 x 12288
+// in 4 bits 10.7 us with any number of loads in flight, this way 7.4).  Products of 16 x 16
+// leave the fewest idle columns to 1-16 tokens and need half the operand reads of 32 x 32.
+//
+// Bound by memory: a compute unit gets about 33 GB/s of weights from HBM and 85 GB/s of tokens
+// from L2, one after the other (its copies in flight are what is limited), so that few tokens
+// run at the card's rate (2 x 12288 x 4096 bf16, 8 tokens: 31.6 us, 6.4 TB/s) and 16-32 tokens
+// of few features below it (5120 x 25600 in 4 bits, 32 tokens: 22 us, 3.2 TB/s of weights while
+// the tokens' 131 MB come from L2).
 #pragma once
 
 #include "projection_tiles.h"

@@ -1,6 +1,8 @@
 // Gated projections with bf16 weights: the kernel of projection_few.h whose steps are 128 columns
 // deep, and tile_kernel of projection_tiles.h with K over workgroups and with loops whose slots
-// and conditions are settled when they are compiled.
+// and conditions are settled when they are compiled (4096 tokens of 2 x 12288 x 4096: 671-684 us
+// as GATED tile_kernel, 650-669 this way, 1.23-1.27 PFLOP/s, the matrix cores 65% busy: bound by
+// what the power limit leaves of them; 64 tokens: 201 MB in 40-43 us, bound by HBM).
 #pragma once
 
 #include <type_traits>

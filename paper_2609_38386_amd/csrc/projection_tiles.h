@@ -1,5 +1,6 @@
 // Projections with bf16 weights in LDS tiles: out = x W^T (dlfp_linear_bf16) and, with
-// GATED, act(x G^T) * (x U^T) (dlfp_gated_linear_bf16).
+// GATED, act(x G^T) * (x U^T): of dlfp_gated_linear_bf16 the tiles of few features and
+// tokens (split_kernel) and rows that are far apart (tile_kernel with FAR).
 //
 // The products are computed as out^T = W x^T on v_mfma_f32_32x32x16_bf16, so that a
 // lane's accumulator holds four consecutive features of one token.  Two kernels share

@@ -1,8 +1,12 @@
 // Weights to 4 bits and back (the format of dlfp_ffn.h).
 //
 // A thread holds 8 columns and four neighbours a group of 32: the group's largest
-// magnitude is a maximum over their bit patterns, with no shared memory.  Bound by
-// the bytes (2 + 17/32 a weight).
+// magnitude is a maximum over their bit patterns, exchanged between the four lanes with
+// no shared memory, and its exponent follows from that pattern's fields, with no
+// logarithm; codes are the conversion instruction's.  16 bytes are read or written a lane,
+// whole rows by neighbouring lanes.  Bound by the bytes (2 + 17/32 a weight): 25600 x 5120
+// takes 71 us to 4 bits and 53 us back (4.7 and 6.4 TB/s; a large copy reaches 5.1), 1024 x
+// 2048 2.6 us, of which 2 are the launch.
 #include <hip/hip_runtime.h>
 
 #include <cstdint>

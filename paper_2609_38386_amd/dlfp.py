@@ -551,7 +551,14 @@ def _check_codes(codes, exps):
         raise ValueError("codes and exponents must be uint8")
     if not (codes.is_contiguous() and exps.is_contiguous()):
         raise ValueError("codes and exponents must be contiguous")
+    _check_sizes(n, 2 * half)
     return n, 2 * half
+
+
+def _check_sizes(*sizes):
+    """The C calls take sizes as 32-bit integers, and ctypes would keep the low bits of others."""
+    if max(sizes) >> 31:
+        raise ValueError("sizes must be below 2^31")
 
 
 _byte = None
@@ -579,6 +586,8 @@ def _projection_rows(x, n, k, out):
     m, columns = x.shape
     if columns != k or out.shape != (m, n):
         raise ValueError(f"x must be [m][{k}] and out [m][{n}]")
+    if (m | n | k) >> 31:
+        _check_sizes(m, n, k)
     bf16, fp32, _ = _types or _bind_types()
     if x.dtype is not bf16:
         raise ValueError("x must be bf16")

@@ -146,14 +146,21 @@ class Weights4:
     def __init__(self, n: int, k: int, device):
         if k % _d.W4_GROUP:
             raise ValueError("k must be a multiple of 32")
+        _d._check_sizes(n, k)
         self._set(torch.zeros((n, k // 2), dtype=torch.uint8, device=device),
                   torch.full((n, k // _d.W4_GROUP), 127, dtype=torch.uint8, device=device))
 
     def _set(self, codes, exps):
-        self.codes, self.exps = codes, exps
-        self.n, self.k = _d._check_codes(codes, exps)
+        self._codes, self._exps = codes, exps
+        self._n, self._k = _d._check_codes(codes, exps)
         if codes.device != exps.device:
             raise ValueError("codes and exponents are on different devices")
+
+    # Checked once, so that a call need not: they stay as they are.
+    codes = property(lambda self: self._codes)
+    exps = property(lambda self: self._exps)
+    n = property(lambda self: self._n)
+    k = property(lambda self: self._k)
 
     @classmethod
     def of(cls, codes: torch.Tensor, exps: torch.Tensor) -> "Weights4":
@@ -201,10 +208,10 @@ def linear(x: torch.Tensor, w, out: torch.Tensor, workspace: Optional[torch.Tens
     beside this one uses (None: taken from PyTorch's allocator, or, with a ``stream`` given by
     hand, none)."""
     if isinstance(w, Weights4):
-        n, k = w.n, w.k
+        n, k = w._n, w._k
         if workspace is None and stream is None:
             workspace = _projection_workspace(_d.LINEAR_W4, x, n, k)
-        _d._linear_w4(x, w.codes, w.exps, n, k, out, workspace, stream)
+        _d._linear_w4(x, w._codes, w._exps, n, k, out, workspace, stream)
     else:
         _d.dlfp_linear_bf16(x, w, out, stream)
 
@@ -218,14 +225,15 @@ def gated_linear(x: torch.Tensor, gate, up, out: torch.Tensor, activation: str =
         raise ValueError("gate and up must be of one kind")
     if not four:
         if workspace is None and stream is None:
-            workspace = _projection_workspace(_d.GATED_LINEAR_BF16, x, *gate.shape)
+            n, k = gate.shape
+            workspace = _projection_workspace(_d.GATED_LINEAR_BF16, x, n, k)
         return _d.dlfp_gated_linear_bf16(x, gate, up, out, activation, workspace, stream)
-    n, k = gate.n, gate.k
-    if up.n != n or up.k != k:
+    n, k = gate._n, gate._k
+    if up._n != n or up._k != k:
         raise ValueError("gate and up must be [n][k] both")
     if workspace is None and stream is None:
         workspace = _projection_workspace(_d.GATED_LINEAR_W4, x, n, k)
-    _d._gated_linear_w4(x, gate.codes, gate.exps, up.codes, up.exps, n, k, out, activation,
+    _d._gated_linear_w4(x, gate._codes, gate._exps, up._codes, up._exps, n, k, out, activation,
                         workspace, stream)
 
 

@@ -187,6 +187,16 @@ def test_workspace_sizes():
     assert size(7, 256, 2560, 25600) == 0
 
 
+@pytest.mark.parametrize("m,n", [((1 << 31) - 1040, (1 << 31) - 1040), (1 << 30, 1 << 30),
+                                 (1 << 25, 1 << 14), (1 << 14, 1 << 25), (1, (1 << 31) - 1024)])
+def test_more_outputs_than_a_launch_can_have(m, n):
+    """Sizes whose products pass 64 bits are refused as well, and take no workspace."""
+    for call in (_linear, _gated4, _gated):
+        assert call(m=m, n=n, ldo=n) == -2
+    for kind in (D.LINEAR_W4, D.GATED_LINEAR_BF16, D.GATED_LINEAR_W4):
+        assert D.dlfp_projection_workspace(kind, m, n, 8192) == 0
+
+
 # ------------------------------------------------------------------- refusals from Python
 
 def _bf16(*shape):
@@ -228,6 +238,38 @@ def test_python_refusals():
             pytest.fail(f"call {i} was taken")
     with pytest.raises(KeyError):
         rt.linear(x, w, torch.zeros((2, 32), dtype=torch.float16))
+
+
+def test_python_refuses_sizes_past_31_bits():
+    """Of which a C integer would keep the low bits, here the sizes of w."""
+    far = 1 << 32
+    def meta(*shape, dtype=torch.bfloat16):
+        return torch.zeros(shape, dtype=dtype, device="meta")
+    x, out = _bf16(2, 64), _bf16(2, 32)
+    tall = rt.Weights4(32, 64, "cpu")
+    bad = [lambda: rt.Weights4(far + 32, 64, "meta"),
+           lambda: rt.Weights4(32, far + 64, "meta"),
+           lambda: D.dlfp_linear_w4(x, meta(far + 32, 32, dtype=torch.uint8),
+                                    meta(far + 32, 2, dtype=torch.uint8), out),
+           lambda: rt.linear(meta(far + 2, 64), tall, meta(far + 2, 32), stream=0),
+           lambda: rt.gated_linear(x, meta(far + 32, 64), meta(far + 32, 64), meta(2, far + 32),
+                                   stream=0),
+           lambda: rt.gated_linear(meta(2, far + 64), meta(32, far + 64), meta(32, far + 64), out,
+                                   stream=0)]
+    for i, call in enumerate(bad):
+        with pytest.raises(ValueError, match="2\\^31"):
+            call()
+            pytest.fail(f"call {i} was taken")
+
+
+def test_weights_keep_their_sizes():
+    """Tensors of other sizes cannot be put in a Weights4's place; three sizes are no matrix."""
+    w = rt.Weights4(32, 64, "cpu")
+    for name in ("codes", "exps", "n", "k"):
+        with pytest.raises(AttributeError):
+            setattr(w, name, None)
+    with pytest.raises(ValueError):
+        rt.gated_linear(_bf16(2, 64), _bf16(1, 32, 64), _bf16(1, 32, 64), _bf16(2, 32))
 
 
 def test_python_takes_empty_batches():

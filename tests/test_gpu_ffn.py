@@ -412,6 +412,28 @@ def test_far_rows(dev, m):
     pj.check(out, *pj.gated(pj.f64(x), pj.f64(gate), pj.f64(up), "silu", torch.bfloat16))
 
 
+@pytest.mark.parametrize("m", [1, 3, 90])
+def test_far_rows_of_one_side(dev, m):
+    """4-bit gate and up with far rows of x; far rows of out, x's beside each other; a single
+    row of a far view."""
+    gen = _gen(dev, 4)
+    n, k, ld = 96, 320, (1 << 22) + 16
+    far = lambda cols: torch.empty(((m - 1) * ld + cols,), dtype=torch.bfloat16,
+                                   device=dev).as_strided((m, cols), (ld, 1))
+    near, x = _bf16(dev, gen, (m, k)), far(k)
+    x.copy_(near)
+    gate, up, out, one = _weights4(dev, gen, n, k), _weights4(dev, gen, n, k), far(n), far(n)
+    rt.gated_linear(x, gate, up, out, "gelu")
+    want = pj.gated(pj.f64(x), _values(gate), _values(up), "gelu", torch.bfloat16)
+    pj.check(out, *want)
+    rt.gated_linear(near, gate, up, one, "gelu")
+    pj.check(one, *want)
+    rt.linear(near, gate, one)
+    pj.check(one, *pj.linear(pj.f64(near), _values(gate), torch.bfloat16))
+    rt.linear(x[m - 1:], gate, one[m - 1:])
+    pj.check(one[m - 1:], *pj.linear(pj.f64(near[m - 1:]), _values(gate), torch.bfloat16))
+
+
 def test_many_tokens(dev):
     """More tokens than a grid's second dimension has blocks of 16."""
     gen = _gen(dev, 31)
