@@ -2,7 +2,7 @@
 // whose estimated time is lowest.
 //
 // K over workgroups pays where the tiles leave compute units empty (5120 x 25600 in 4 bits, 256
-// tokens: 225 us whole, 71 in 6 parts; 128: 74 and 47; 32: 30.5 and 25.7); it costs the second
+// tokens: 106 us whole, 71 in 6 parts; 128: 60 and 47; 32: 29.6 and 25.6); it costs the second
 // launch's 2-3 us and the partial sums' bytes twice.  A second launch and not the last of a
 // tile's workgroups adds them: it needs no counters that someone has to have zeroed.
 #pragma once

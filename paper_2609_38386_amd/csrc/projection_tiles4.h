@@ -13,14 +13,13 @@
 // rate, so that widening them once for the whole workgroup, through LDS, would only add traffic.
 // Wavefronts are laid out along the features, since a wave widens its own rows and reads all
 // tokens of its part: 256 x 256 tiles as 8 x 1 wavefronts run 4096 tokens of 12288 x 4096 in
-// 314 us (1.31 PFLOP/s), as 4 x 2 in 317, as 2 x 4 in 342.  Large tiles are bound by what the
-// power limit leaves of the matrix cores (57-65% busy), small ones by the latency of a step:
-// its conditions, slots and waits took a third of it and are settled when the kernel is compiled
-// (all stages but the last two; 2048 tokens of 4096 x 12288 193 -> 166-172 us, 128 of 25600 x
-// 5120 51.8 -> 43.7).
+// 314-318 us (1.30 PFLOP/s), as 4 x 2 in 347.  Large tiles are bound by what the power limit
+// leaves of the matrix cores (57-65% busy), small ones by the latency of a step: its conditions,
+// slots and waits took a third of it and are settled when the kernel is compiled (all stages but
+// the last two; 4096 tokens of 12288 x 4096 360 -> 314 us).
 //
-// WHOLE: all operands of a step are read a step ahead, where the registers are there (tiles of
-// 32 and 64 tokens; 128 x 128 tiles gain by it too, larger ones do not).
+// WHOLE: all operands of a step are read a step ahead, where the registers are there: tiles of
+// 32 and 64 tokens (256 x 128 tiles lose by it, 2048 tokens of 4096 x 12288 169 -> 182 us).
 #pragma once
 
 #include <type_traits>
