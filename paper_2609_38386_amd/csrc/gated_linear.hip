@@ -50,17 +50,17 @@ int launch_tile(const dlfp::ProjectionArgs& a, Grid g, dlfp::Split split, hipStr
 #define WHOLE_K_CALLS(...) {nullptr, launch_whole<__VA_ARGS__>}
 #define TILE_CALLS(...) {nullptr, launch_tile<__VA_ARGS__>}
 constexpr Variant VARIANTS[] = {
-    {FEW(2, 16, 4, 2), 0, {1.644f, 0.f, 0.f, 0.384f, 1.178f, 0.343f, 0.075f, 0.f, 0.f, 2.397f, 0.139f}, FEW_CALLS(2, 16, 4, 2)},
-    {FEW(2, 8, 4, 2), 0, {2.747f, 0.f, 0.f, 0.405f, 0.054f, 0.303f, 0.076f, 0.f, 0.f, 2.279f, 0.233f}, FEW_CALLS(2, 8, 4, 2)},
-    {FEW(2, 32, 4, 2), 0, {1.614f, 0.f, 0.f, 0.466f, 1.346f, 0.44f, 0.06f, 0.f, 0.f, 2.655f, 0.025f}, FEW_CALLS(2, 32, 4, 2)},
-    {WHOLE_K(64, 32, 4, 3), 0, {1.311f, 0.f, 0.f, 0.087f, 1.648f, 0.089f, 0.082f, 0.f, 0.f, 0.f, 0.f}, WHOLE_K_CALLS(64, 32, 4, 3)},
-    {WHOLE_K(32, 32, 8, 2), 0, {1.384f, 0.f, 0.f, 0.054f, 1.718f, 0.054f, 0.065f, 0.f, 0.f, 0.f, 0.f}, WHOLE_K_CALLS(32, 32, 8, 2)},
-    {TILE(128, 64, 4, 2, 3), 2, {1.978f, 0.f, 0.313f, 0.09f, 0.211f, 0.227f, 0.101f, 1.067f, 0.f, 2.497f, 0.092f}, TILE_CALLS(128, 64, 4, 2, 3)},
-    {TILE(256, 128, 4, 2, 3), 0, {1.077f, 0.f, 0.907f, 0.298f, 4.184f, 0.546f, 0.059f, 0.f, 0.f, 2.4f, 0.114f}, TILE_CALLS(256, 128, 4, 2, 3)},
-    {TILE(128, 32, 4, 1, 4), 2, {2.166f, 0.f, 0.058f, 0.033f, 0.354f, 0.171f, 0.122f, 0.78f, 0.f, 2.345f, 0.096f}, TILE_CALLS(128, 32, 4, 1, 4)},
-    {TILE(256, 256, 4, 2, 2), 0, {1.732f, 0.f, 2.072f, 0.544f, 5.764f, 1.041f, 0.04f, 0.f, 0.f, 0.396f, 0.109f}, TILE_CALLS(256, 256, 4, 2, 2)},
-    {TILE(128, 128, 2, 4, 4), 0, {1.279f, 0.f, 0.317f, 0.218f, 2.971f, 0.29f, 0.048f, 0.f, 0.f, 2.764f, 0.106f}, TILE_CALLS(128, 128, 2, 4, 4)},
-    {TILE(128, 64, 2, 2, 2), 3, {2.51f, 0.f, 0.424f, 0.126f, 0.061f, 0.052f, 0.102f, 0.524f, 0.349f, 2.655f, 0.126f}, TILE_CALLS(128, 64, 2, 2, 2)},
+    {FEW(2, 16, 4, 2), 0, {1.644f, 0.f, 0.f, 0.384f, 1.178f, 0.343f, 0.075f, 0.f, 0.f, 2.397f, 0.139f, 0.f}, FEW_CALLS(2, 16, 4, 2)},
+    {FEW(2, 8, 4, 2), 0, {2.747f, 0.f, 0.f, 0.405f, 0.054f, 0.303f, 0.076f, 0.f, 0.f, 2.279f, 0.233f, 0.f}, FEW_CALLS(2, 8, 4, 2)},
+    {FEW(2, 32, 4, 2), 0, {1.614f, 0.f, 0.f, 0.466f, 1.346f, 0.44f, 0.06f, 0.f, 0.f, 2.655f, 0.025f, 0.f}, FEW_CALLS(2, 32, 4, 2)},
+    {WHOLE_K(64, 32, 4, 3), 0, {1.311f, 0.f, 0.f, 0.087f, 1.648f, 0.089f, 0.082f, 0.f, 0.f, 0.f, 0.f, 0.f}, WHOLE_K_CALLS(64, 32, 4, 3)},
+    {WHOLE_K(32, 32, 8, 2), 0, {1.384f, 0.f, 0.f, 0.054f, 1.718f, 0.054f, 0.065f, 0.f, 0.f, 0.f, 0.f, 0.f}, WHOLE_K_CALLS(32, 32, 8, 2)},
+    {TILE(128, 64, 4, 2, 3), 2, {1.978f, 0.f, 0.313f, 0.09f, 0.211f, 0.227f, 0.101f, 1.067f, 0.f, 2.497f, 0.092f, 0.f}, TILE_CALLS(128, 64, 4, 2, 3)},
+    {TILE(256, 128, 4, 2, 3), 0, {1.077f, 0.f, 0.907f, 0.298f, 4.184f, 0.546f, 0.059f, 0.f, 0.f, 2.4f, 0.114f, 0.f}, TILE_CALLS(256, 128, 4, 2, 3)},
+    {TILE(128, 32, 4, 1, 4), 2, {2.166f, 0.f, 0.058f, 0.033f, 0.354f, 0.171f, 0.122f, 0.78f, 0.f, 2.345f, 0.096f, 0.f}, TILE_CALLS(128, 32, 4, 1, 4)},
+    {TILE(256, 256, 4, 2, 2), 0, {1.732f, 0.f, 2.072f, 0.544f, 5.764f, 1.041f, 0.04f, 0.f, 0.f, 0.396f, 0.109f, 0.f}, TILE_CALLS(256, 256, 4, 2, 2)},
+    {TILE(128, 128, 2, 4, 4), 0, {1.279f, 0.f, 0.317f, 0.218f, 2.971f, 0.29f, 0.048f, 0.f, 0.f, 2.764f, 0.106f, 0.f}, TILE_CALLS(128, 128, 2, 4, 4)},
+    {TILE(128, 64, 2, 2, 2), 3, {2.51f, 0.f, 0.424f, 0.126f, 0.061f, 0.052f, 0.102f, 0.524f, 0.349f, 2.655f, 0.126f, 0.f}, TILE_CALLS(128, 64, 2, 2, 2)},
 };
 #undef FEW
 #undef WHOLE_K

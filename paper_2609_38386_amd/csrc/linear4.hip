@@ -77,7 +77,8 @@ int launch_few(const dlfp::ProjectionArgs& a, Grid g, dlfp::Split split, hipStre
   const int64_t tiles = g.down * g.across;
   if (tiles * split.splits * (64 * WAVES) >= (int64_t)1 << 32) return DLFP_ERANGE;
   few4_kernel<BLOCKS, TOKENS, WAVES, DEPTH, HALVES, GATED>
-      <<<(uint32_t)(tiles * split.splits), 64 * WAVES, (size_t)Shape::lds(a.k), stream>>>(a, split);
+      <<<(uint32_t)(tiles * split.splits), 64 * WAVES, (size_t)Shape::lds(a.k, split.splits),
+         stream>>>(a, split);
   if (split.splits > 1) {
     constexpr int UNITS = (GATED ? BLOCKS / 2 : BLOCKS) * Shape::TB;
     sum_few_kernel<BLOCKS, TOKENS, GATED><<<(uint32_t)(tiles * UNITS), 64, 0, stream>>>(
@@ -112,31 +113,31 @@ constexpr Launch few_gated() {
 }
 
 // Fitted to 1000 sizes of 1-4096 tokens, 64-25600 features and columns, every variant with every
-// split, plain and gated, weights read from memory.  The choice takes 1.017 times the fastest
-// one's time on average (geometric mean; 1.06 in nine of ten sizes, 1.34 at worst).
+// split, plain and gated, weights read from memory.  The choice takes 1.014 times the fastest
+// one's time on average (geometric mean; 1.05 in nine of ten sizes, 1.31 at worst).
 #define FEW(B, T, W, D, H) 16 * B, T, W, H* FHALF, FewShape<B, T, W, D, H>::RINGS, B, true
 #define TILE(TN, TM, ...) TN, TM, 0, 0, 0, 0, true
 #define FEW_CALLS(B, T, W, D, H) {launch_few<false, B, T, W, D, H>, few_gated<B, T, W, D, H>()}
 #define TILE_CALLS(...) {launch_tile<false, __VA_ARGS__>, launch_tile<true, __VA_ARGS__>}
 constexpr Variant VARIANTS[] = {
-    {FEW(1, 2, 4, 2, 2), 0, {2.638f, 0.117f, 0.045f, 0.023f, 0.018f, 0.195f, 0.043f, 0.f, 0.f, 2.376f, 0.052f}, FEW_CALLS(1, 2, 4, 2, 2)},
-    {FEW(2, 2, 4, 1, 2), 0, {2.673f, 0.288f, 0.f, 0.12f, 0.058f, 0.223f, 0.083f, 0.f, 0.f, 2.392f, 0.f}, FEW_CALLS(2, 2, 4, 1, 2)},
-    {FEW(1, 4, 8, 2, 2), 0, {2.524f, 0.004f, 0.f, 0.097f, 0.326f, 0.422f, 0.051f, 0.f, 0.f, 2.237f, 0.015f}, FEW_CALLS(1, 4, 8, 2, 2)},
-    {FEW(2, 4, 4, 2, 2), 0, {2.868f, 0.034f, 0.072f, 0.029f, 0.f, 0.466f, 0.06f, 0.f, 0.f, 2.396f, 0.352f}, FEW_CALLS(2, 4, 4, 2, 2)},
-    {FEW(1, 8, 4, 2, 2), 0, {2.658f, 0.053f, 0.075f, 0.038f, 0.056f, 0.309f, 0.039f, 0.f, 0.f, 2.302f, 0.f}, FEW_CALLS(1, 8, 4, 2, 2)},
-    {FEW(2, 8, 4, 2, 2), 0, {2.756f, 0.044f, 0.087f, 0.11f, 0.162f, 0.483f, 0.049f, 0.f, 0.f, 2.469f, 0.104f}, FEW_CALLS(2, 8, 4, 2, 2)},
-    {FEW(2, 8, 4, 1, 2), 0, {2.817f, 0.243f, 0.f, 0.204f, 0.f, 0.289f, 0.063f, 0.f, 0.f, 2.411f, 0.086f}, FEW_CALLS(2, 8, 4, 1, 2)},
-    {FEW(1, 16, 4, 2, 2), 0, {1.513f, 0.f, 0.f, 0.143f, 1.323f, 0.393f, 0.023f, 0.f, 0.f, 2.37f, 0.233f}, FEW_CALLS(1, 16, 4, 2, 2)},
-    {FEW(4, 16, 4, 1, 2), 0, {2.999f, 0.061f, 0.f, 0.285f, 0.f, 0.924f, 0.095f, 0.f, 0.f, 2.505f, 0.044f}, FEW_CALLS(4, 16, 4, 1, 2)},
-    {FEW(2, 16, 8, 1, 1), 0, {2.465f, 0.107f, 0.f, 0.119f, 0.f, 0.894f, 0.13f, 0.f, 0.f, 2.7f, 0.f}, FEW_CALLS(2, 16, 8, 1, 1)},
-    {FEW(2, 32, 8, 1, 1), 0, {1.214f, 0.031f, 0.f, 0.349f, 1.327f, 1.29f, 0.093f, 0.f, 0.f, 2.889f, 0.255f}, FEW_CALLS(2, 32, 8, 1, 1)},
-    {FEW(4, 32, 4, 1, 1), 0, {2.749f, 0.34f, 0.f, 0.061f, 0.f, 1.074f, 0.138f, 0.f, 0.f, 2.831f, 0.256f}, FEW_CALLS(4, 32, 4, 1, 1)},
-    {FEW(4, 32, 4, 1, 2), 0, {1.283f, 0.f, 0.362f, 0.08f, 2.199f, 1.339f, 0.088f, 0.f, 0.f, 2.923f, 0.258f}, FEW_CALLS(4, 32, 4, 1, 2)},
-    {TILE(128, 32, 4, 1, 4, 3, true), 2, {1.821f, 0.011f, 0.181f, 0.044f, 0.505f, 0.019f, 0.097f, 0.981f, 0.197f, 2.762f, 0.208f}, TILE_CALLS(128, 32, 4, 1, 4, 3, true)},
-    {TILE(128, 64, 4, 1, 2, 2, false), 3, {2.797f, 0.f, 0.605f, 0.103f, 0.37f, 0.f, 0.096f, 0.f, 0.376f, 2.371f, 0.273f}, TILE_CALLS(128, 64, 4, 1, 2, 2, false)},
-    {TILE(256, 64, 8, 1, 4, 3, true), 0, {1.763f, 0.f, 1.289f, 0.085f, 2.341f, 0.385f, 0.063f, 0.f, 0.f, 2.764f, 0.252f}, TILE_CALLS(256, 64, 8, 1, 4, 3, true)},
-    {TILE(256, 128, 8, 1, 4, 3, false), 0, {1.982f, 0.f, 2.434f, 0.19f, 2.871f, 0.603f, 0.004f, 0.f, 0.f, 2.768f, 0.229f}, TILE_CALLS(256, 128, 8, 1, 4, 3, false)},
-    {TILE(256, 256, 8, 1, 2, 2, false), 0, {3.31f, 0.f, 5.732f, 0.32f, 2.461f, 1.113f, 0.014f, 0.f, 0.f, 3.875f, 0.157f}, TILE_CALLS(256, 256, 8, 1, 2, 2, false)},
+    {FEW(1, 2, 4, 2, 2), 0, {2.639f, 0.091f, 0.f, 0.015f, 0.024f, 0.204f, 0.04f, 0.f, 0.f, 2.265f, 0.197f, 0.278f}, FEW_CALLS(1, 2, 4, 2, 2)},
+    {FEW(2, 2, 4, 1, 2), 0, {2.689f, 0.233f, 0.f, 0.101f, 0.01f, 0.255f, 0.069f, 0.f, 0.f, 2.235f, 0.f, 0.275f}, FEW_CALLS(2, 2, 4, 1, 2)},
+    {FEW(1, 4, 8, 2, 2), 0, {2.469f, 0.f, 0.f, 0.082f, 0.247f, 0.379f, 0.062f, 0.f, 0.f, 2.205f, 0.142f, 0.175f}, FEW_CALLS(1, 4, 8, 2, 2)},
+    {FEW(2, 4, 4, 2, 2), 0, {2.807f, 0.01f, 0.082f, 0.007f, 0.f, 0.475f, 0.054f, 0.f, 0.f, 2.233f, 0.045f, 0.18f}, FEW_CALLS(2, 4, 4, 2, 2)},
+    {FEW(2, 8, 4, 1, 2), 0, {2.773f, 0.21f, 0.f, 0.151f, 0.006f, 0.312f, 0.059f, 0.f, 0.f, 2.239f, 0.018f, 0.097f}, FEW_CALLS(2, 8, 4, 1, 2)},
+    {FEW(2, 8, 8, 1, 1), 0, {2.743f, 0.074f, 0.f, 0.167f, 0.008f, 0.343f, 0.069f, 0.f, 0.f, 2.255f, 0.f, 0.143f}, FEW_CALLS(2, 8, 8, 1, 1)},
+    {FEW(1, 16, 8, 2, 1), 0, {1.479f, 0.f, 0.f, 0.178f, 1.225f, 0.322f, 0.023f, 0.f, 0.f, 2.318f, 0.353f, 0.021f}, FEW_CALLS(1, 16, 8, 2, 1)},
+    {FEW(2, 16, 8, 1, 1), 0, {2.712f, 0.025f, 0.f, 0.176f, 0.054f, 0.456f, 0.07f, 0.f, 0.f, 2.289f, 0.f, 0.023f}, FEW_CALLS(2, 16, 8, 1, 1)},
+    {FEW(4, 16, 8, 1, 1), 0, {2.714f, 0.f, 0.053f, 0.231f, 0.176f, 0.78f, 0.086f, 0.f, 0.f, 2.219f, 0.f, 0.031f}, FEW_CALLS(4, 16, 8, 1, 1)},
+    {FEW(2, 32, 8, 1, 1), 0, {1.303f, 0.f, 0.f, 0.249f, 1.664f, 0.636f, 0.066f, 0.f, 0.f, 2.385f, 0.f, 0.037f}, FEW_CALLS(2, 32, 8, 1, 1)},
+    {FEW(4, 32, 4, 1, 1), 0, {3.06f, 0.153f, 0.f, 0.172f, 0.253f, 0.524f, 0.058f, 0.f, 0.f, 2.354f, 0.195f, 0.017f}, FEW_CALLS(4, 32, 4, 1, 1)},
+    {FEW(4, 32, 8, 1, 1), 0, {1.2f, 0.f, 0.064f, 0.337f, 2.03f, 0.959f, 0.078f, 0.f, 0.f, 2.52f, 0.f, 0.043f}, FEW_CALLS(4, 32, 8, 1, 1)},
+    {FEW(6, 32, 4, 1, 2), 0, {0.986f, 0.f, 0.703f, 0.088f, 2.74f, 1.856f, 0.083f, 0.f, 0.f, 2.809f, 0.095f, 0.02f}, FEW_CALLS(6, 32, 4, 1, 2)},
+    {TILE(128, 32, 4, 1, 4, 3, true), 2, {1.862f, 0.014f, 0.172f, 0.045f, 0.479f, 0.02f, 0.093f, 0.982f, 0.194f, 2.32f, 0.226f, 0.f}, TILE_CALLS(128, 32, 4, 1, 4, 3, true)},
+    {TILE(128, 64, 4, 1, 2, 2, false), 3, {2.782f, 0.f, 0.52f, 0.105f, 0.434f, 0.f, 0.092f, 0.f, 0.375f, 1.872f, 0.302f, 0.f}, TILE_CALLS(128, 64, 4, 1, 2, 2, false)},
+    {TILE(256, 64, 8, 1, 4, 3, true), 0, {1.715f, 0.f, 1.17f, 0.081f, 2.407f, 0.391f, 0.057f, 0.f, 0.f, 2.363f, 0.265f, 0.f}, TILE_CALLS(256, 64, 8, 1, 4, 3, true)},
+    {TILE(256, 128, 8, 1, 4, 3, false), 0, {1.981f, 0.f, 2.306f, 0.187f, 2.833f, 0.605f, 0.006f, 0.f, 0.f, 2.407f, 0.235f, 0.f}, TILE_CALLS(256, 128, 8, 1, 4, 3, false)},
+    {TILE(256, 256, 8, 1, 2, 2, false), 0, {3.25f, 0.f, 4.988f, 0.334f, 2.831f, 1.111f, 0.004f, 0.f, 0.f, 3.23f, 0.171f, 0.f}, TILE_CALLS(256, 256, 8, 1, 2, 2, false)},
 };
 #undef FEW
 #undef TILE

@@ -39,6 +39,18 @@ inline bool too_many(int m, int n) {
   return m > MOST_ROWS || n > MOST_ROWS || (int64_t)m * n >= MOST_OUTPUTS;
 }
 
+// Few tokens with 4-bit weights: bytes between the exponents of rows in LDS.  All of K: as in
+// memory; a split of it: its own groups, and up to 15 before them that a 16-byte piece begins with.
+inline __host__ __device__ int exps_pitch(int k, int splits, int step_columns) {
+  if (splits == 1) return k / 32;
+  const int steps = (k + step_columns - 1) / step_columns;
+  return ((steps + splits - 1) / splits * (step_columns / 32) + 30) / 16 * 16;
+}
+// Bytes of 16 rows of them, in whole copies.
+inline __host__ __device__ int exps_bytes(int k, int splits, int step_columns) {
+  return (16 * exps_pitch(k, splits, step_columns) + 1023) / 1024 * 1024;
+}
+
 // Bytes of partial sums of the fastest form.
 int64_t workspace_w4(bool gated, int m, int n, int k);
 int64_t workspace_gated(int m, int n, int k);

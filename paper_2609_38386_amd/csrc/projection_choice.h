@@ -21,24 +21,25 @@ struct Grid {
 typedef int (*Launch)(const dlfp::ProjectionArgs&, Grid, dlfp::Split, hipStream_t);
 
 // A tile of `rows` rows of weights and `tokens` tokens.  Its wavefronts share steps of `columns`
-// columns, or take all of them (waves 0).  `lds` bytes besides `blocks` times half a row, where
+// columns, or take all of them (waves 0).  `lds` bytes besides the exponents of `blocks` blocks, where
 // that matters (blocks > 0).
 //
 // Time in microseconds, with u = tiles times splits / 256, s = steps of a unit (of a wavefront
 // where they share them, of 64 columns otherwise) and b = MB of weights:
 //   c0 + c1 s + (c2 + c3 s) u + (c4 + c5 s) ceil(u) + c6 b + (c7 + c8 s) ceil(u / resident)
 // and with splits + c9 + c10 times the MB of partial sums, where `resident` workgroups fit a
-// compute unit (0: left out).
+// compute unit (0: left out), and where wavefronts share the steps + c11 times the MB of tokens that
+// the L2s read (each all of them, as far as there are tiles across).
 struct Variant {
   int rows, tokens, waves, columns, lds, blocks;
   bool splits;
   int resident;
-  float c[11];
+  float c[12];
   Launch launch[2];  // plain and gated
 };
 
 constexpr int CUS = 256;
-constexpr int SPLITS[] = {1, 2, 3, 4, 6, 8};
+constexpr int SPLITS[] = {1, 2, 3, 4, 6, 8};  // (those of sum_splits)
 constexpr int SPLIT_COLUMNS = 512;           // at least, of a split of a tile
 constexpr int64_t MOST_PARTS = 32 << 20;     // bytes of partial sums
 constexpr int64_t MOST_GRID_Y = 65535;
@@ -58,7 +59,6 @@ Plan choose(const Variant (&variants)[COUNT], bool gated, int m, int n, int k, i
   float least = 0.f;
   for (const Variant& v : variants) {
     if (!v.launch[gated]) continue;
-    if (v.blocks && v.lds + v.blocks * (((int64_t)k / 2 + 1023) / 1024 * 1024) > 160 * 1024) continue;
     const int features = gated ? v.rows / 2 : v.rows;
     const Grid g{((int64_t)m + v.tokens - 1) / v.tokens, ((int64_t)n + features - 1) / features};
     if (g.down > MOST_GRID_Y && !v.splits) continue;
@@ -71,6 +71,9 @@ Plan choose(const Variant (&variants)[COUNT], bool gated, int m, int n, int k, i
       if (splits > 1 && (!v.splits || splits * bytes > room ||
                          (v.waves ? splits * v.waves > steps : splits * SPLIT_COLUMNS > k)))
         break;
+      if (v.blocks &&
+          v.lds + v.blocks * (int64_t)dlfp::exps_bytes(k, splits, v.columns) > 160 * 1024)
+        continue;
       const float u = (float)(tiles * splits) / CUS;
       const float r = (float)((tiles * splits + CUS - 1) / CUS);
       const int share = splits * v.waves;
@@ -81,6 +84,7 @@ Plan choose(const Variant (&variants)[COUNT], bool gated, int m, int n, int k, i
         t += (c[7] + c[8] * s) * (float)((tiles * splits + most - 1) / most);
       }
       if (splits > 1) t += c[9] + c[10] * 1e-6f * (float)(splits * bytes);
+      if (v.waves) t += c[11] * 2e-6f * (float)((int64_t)m * k * std::min<int64_t>(8, g.across));
       if (best.variant && t >= least) continue;
       least = t;
       best = Plan{&v, g, splits, splits > 1 ? splits * bytes : 0};

@@ -23,6 +23,33 @@
 
 namespace {
 
+// A workgroup's unit: its tile's first feature and token, and its part of the steps of K, which
+// its wavefronts take in turn (so that they read neighbouring pieces of a row at about the same
+// time: GAIN).  Divisions only where there is something to divide.
+struct Unit {
+  uint32_t tile, part;
+  int n0, m0, from, to;
+};
+template <int FEATURES, int TOKENS>
+__device__ __forceinline__ Unit unit_of(const dlfp::ProjectionArgs& a, dlfp::Split split,
+                                        int steps) {
+  Unit r{blockIdx.x, 0, 0, 0, 0, steps};
+  if (split.splits > 1) {
+    r.tile = blockIdx.x / split.splits;
+    r.part = blockIdx.x - r.tile * split.splits;
+    r.from = (uint32_t)steps * r.part / split.splits;
+    r.to = (uint32_t)steps * (r.part + 1) / split.splits;
+  }
+  uint32_t across = r.tile;
+  if (a.m > TOKENS) {
+    const uint32_t gn = (uint32_t)(a.n + FEATURES - 1) / FEATURES, down = r.tile / gn;
+    across -= down * gn;
+    r.m0 = (int)down * TOKENS;
+  }
+  r.n0 = (int)across * FEATURES;
+  return r;
+}
+
 // Four features of a token.
 __device__ __forceinline__ void store4(const dlfp::ProjectionArgs& a, int m, int n, f32x4_t v) {
   const int64_t at = (int64_t)m * a.ldo + n;
@@ -38,7 +65,7 @@ __device__ __forceinline__ void store4(const dlfp::ProjectionArgs& a, int m, int
 template <int BLOCKS, int TOKENS, int WAVES, bool GATED, int TB>
 __device__ __forceinline__ void store_few(const dlfp::ProjectionArgs& a, dlfp::Split split,
                                           f32x4_t (&acc)[BLOCKS][TB], char* smem, int tid,
-                                          int wave, uint32_t unit, uint32_t part, int n0, int m0) {
+                                          int wave, const Unit& own) {
   const int lane = tid & 63;
   wait_copies_barrier<0>();
   f32x4_t* sums = reinterpret_cast<f32x4_t*>(smem);
@@ -60,14 +87,43 @@ __device__ __forceinline__ void store_few(const dlfp::ProjectionArgs& a, dlfp::S
     if (split.splits > 1) {
       // Unit (r, u, l) of the gate, then of the up.
       f32x4_t* out = reinterpret_cast<f32x4_t*>(split.part) +
-                     ((int64_t)part * (gridDim.x / split.splits) + unit) * (BLOCKS * TB * 64) + i;
+                     ((int64_t)own.part * (gridDim.x / split.splits) + own.tile) * (BLOCKS * TB * 64) + i;
       *out = v;
       if constexpr (GATED) out[OUT * TB * 64] = sum(2 * r + 1);
       continue;
     }
     if constexpr (GATED) v = gated4(v, sum(2 * r + 1), a.act);
-    const int tok = 16 * u + (l & 15), m = m0 + tok, n = n0 + 16 * r + 4 * (l >> 4);
+    const int tok = 16 * u + (l & 15), m = own.m0 + tok, n = own.n0 + 16 * r + 4 * (l >> 4);
     if (tok < TOKENS && m < a.m && n < a.n) store4(a, m, n, v);
+  }
+}
+
+// p[0] + p[step] + ... in that order, of SPLITS addresses: all of them are read before the first
+// is waited for.
+template <int SPLITS, int UNITS>
+__device__ __forceinline__ void sum_parts(f32x4_t (&v)[UNITS], const f32x4_t* p, int64_t step,
+                                          int unit_step) {
+  f32x4_t parts[SPLITS][UNITS];
+#pragma unroll
+  for (int s = 0; s < SPLITS; ++s)
+#pragma unroll
+    for (int i = 0; i < UNITS; ++i) parts[s][i] = p[s * step + i * unit_step];
+#pragma unroll
+  for (int i = 0; i < UNITS; ++i) {
+    v[i] = parts[0][i];
+#pragma unroll
+    for (int s = 1; s < SPLITS; ++s) v[i] += parts[s][i];
+  }
+}
+template <int UNITS>
+__device__ __forceinline__ void sum_splits(f32x4_t (&v)[UNITS], const f32x4_t* p, int64_t step,
+                                           int unit_step, int splits) {
+  switch (splits) {
+    case 2: return sum_parts<2>(v, p, step, unit_step);
+    case 3: return sum_parts<3>(v, p, step, unit_step);
+    case 4: return sum_parts<4>(v, p, step, unit_step);
+    case 6: return sum_parts<6>(v, p, step, unit_step);
+    default: return sum_parts<8>(v, p, step, unit_step);
   }
 }
 
@@ -82,14 +138,10 @@ __global__ __launch_bounds__(64) void sum_few_kernel(dlfp::ProjectionArgs a, int
   if (tok >= TOKENS || m >= a.m || n >= a.n) return;
   constexpr int UNITS = BLOCKS * TB * 64;
   const f32x4_t* p = reinterpret_cast<const f32x4_t*>(split.part) + (int64_t)t * UNITS + i * 64 + l;
-  f32x4_t v = p[0], up{};
-  if constexpr (GATED) up = p[OUT * TB * 64];
-  for (int s = 1; s < split.splits; ++s) {
-    v += p[(int64_t)s * tiles * UNITS];
-    if constexpr (GATED) up += p[(int64_t)s * tiles * UNITS + OUT * TB * 64];
-  }
-  if constexpr (GATED) v = gated4(v, up, a.act);
-  store4(a, m, n, v);
+  f32x4_t v[GATED ? 2 : 1];
+  sum_splits(v, p, (int64_t)tiles * UNITS, OUT * TB * 64, split.splits);
+  if constexpr (GATED) v[0] = gated4(v[0], v[1], a.act);
+  store4(a, m, n, v[0]);
 }
 
 }  // namespace

@@ -3,8 +3,8 @@
 // 4 h + l / 16: 16 bytes of codes that are the operands of four products; which columns a
 // product takes is free as long as both operands agree.
 //
-// The exponents of the block's rows are one contiguous piece of memory, copied whole before the
-// first step: as 4-byte pieces with each step they took a third of the copies' time (4096 x
+// The exponents of the block's rows are copied before the first step, one contiguous piece of
+// memory (with K over workgroups, of each row the workgroup's part): as 4-byte pieces with each step they took a third of the copies' time (4096 x
 // 12288, 1 token: 9.6 us against 8.4 without any), and loaded into registers beside the copies
 // they made every step wait for all copies in flight (16 tokens of 5120 x 25600: 22.9 against
 // 21.2 us).  They are what limits k here: with more than the LDS holds, tiles are taken.
@@ -28,9 +28,10 @@ struct FewShape {
   static constexpr int SLOT = HALVES * (BLOCKS * 1024 + TOKENS * 256);
   static constexpr int RING = DEPTH * SLOT, RESULT = BLOCKS * TB * 1024;
   static constexpr int RINGS = WAVES * (RING > RESULT ? RING : RESULT);
-  // LDS of a launch: the rings, then each block's exponents in whole copies.
-  static int64_t exps(int k) { return ((int64_t)k / 2 + 1023) / 1024 * 1024; }
-  static int64_t lds(int k) { return RINGS + BLOCKS * exps(k); }
+  // LDS of a launch: the rings, then each block's exponents.
+  static int64_t lds(int k, int splits) {
+    return RINGS + (int64_t)BLOCKS * dlfp::exps_bytes(k, splits, HALVES * FHALF);
+  }
 };
 
 // Position of a row's 16 bytes of weights: rows of 128 bytes as in a tile, of 64 bytes spread over
@@ -50,13 +51,9 @@ __global__ __launch_bounds__(64 * WAVES) void few4_kernel(dlfp::ProjectionArgs a
   char* smem = few_lds;
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   constexpr int FEATURES = 16 * (GATED ? BLOCKS / 2 : BLOCKS);
-  const uint32_t gn = (uint32_t)(a.n + FEATURES - 1) / FEATURES;
-  const uint32_t unit = blockIdx.x / split.splits, part = blockIdx.x - unit * split.splits;
-  const int n0 = (int)(unit % gn) * FEATURES, m0 = (int)(unit / gn) * TOKENS;
-  const int groups = a.k >> 5, steps = (a.k + STEP - 1) / STEP;
-  const int64_t shares = (int64_t)WAVES * split.splits, share = (int64_t)WAVES * part + wave;
-  const int first = (int)(steps * share / shares);
-  const int count = (int)(steps * (share + 1) / shares) - first;
+  const Unit own = unit_of<FEATURES, TOKENS>(a, split, (a.k + STEP - 1) / STEP);
+  const int n0 = own.n0, m0 = own.m0, groups = a.k >> 5;
+  const int first = own.from + wave, count = (own.to - first + WAVES - 1) / WAVES;
   // First row of block b in its weights: past the end, the last 16 again.
   auto row0 = [&](int b) { return min(n0 + 16 * (GATED ? b >> 1 : b), a.n - 16); };
 
@@ -86,7 +83,7 @@ __global__ __launch_bounds__(64 * WAVES) void few4_kernel(dlfp::ProjectionArgs a
   char* ring = smem + wave * Shape::RING;
   const uint32_t lds0 = lds_addr(ring);
   auto issue = [&](auto inside, int t, int slot) {
-    const int s = first + t;
+    const int s = first + WAVES * t;
     // Past the row's end the step's first group again.
     const bool whole = inside.value || GROUPS * s + GROUPS <= groups;
     const uint32_t d = lds0 + slot * SLOT;
@@ -98,7 +95,7 @@ __global__ __launch_bounds__(64 * WAVES) void few4_kernel(dlfp::ProjectionArgs a
             whole || GROUPS * s + wg[c] < groups ? woff[c] : woff[c] - 16 * wg[c];
         const uint32_t to = d + (b * HALVES + c) * 1024;
         const char* from = wbase[b] + (int64_t)s * (STEP / 2);
-        if (a.stream)
+        if (HALVES == 2 && a.stream)  // (halves of a line would be read from HBM twice)
           lds_stream16(from, off, to);
         else
           lds_copy16(from, off, to);
@@ -114,14 +111,22 @@ __global__ __launch_bounds__(64 * WAVES) void few4_kernel(dlfp::ProjectionArgs a
   };
 
   // Exponents: 16 rows of groups bytes are one piece of k / 2 bytes; the copies of a block are
-  // dealt to the wavefronts.
-  const int epieces = ((a.k >> 1) + 1023) / 1024, eblock = epieces * 1024;
+  // dealt to the wavefronts.  Of a split, a row's pieces of 16 bytes from the one on in which its
+  // first group is.
+  const int pitch = dlfp::exps_pitch(a.k, split.splits, STEP);
+  const int eblock = dlfp::exps_bytes(a.k, split.splits, STEP), epieces = eblock / 1024;
+  const int g0 = GROUPS * own.from;
   const uint32_t elds = lds_addr(smem) + Shape::RINGS;
   for (int i = wave; i < BLOCKS * epieces; i += WAVES) {
     const int b = i / epieces, p = i - b * epieces;
     const char* src = reinterpret_cast<const char*>(a.exps[GATED ? b & 1 : 0]) +
                       (int64_t)row0(b) * groups;
-    lds_copy16(src, (uint32_t)min(p * 1024 + lane * 16, (a.k >> 1) - 16), elds + i * 1024);
+    int off = p * 1024 + lane * 16;
+    if (split.splits > 1) {
+      const int row = off / pitch;
+      off = ((row * groups + g0) & ~15) + off - row * pitch;
+    }
+    lds_copy16(src, (uint32_t)min(off, (a.k >> 1) - 16), elds + i * 1024);
   }
 #pragma unroll
   for (int t = 0; t < DEPTH; ++t)
@@ -133,7 +138,8 @@ __global__ __launch_bounds__(64 * WAVES) void few4_kernel(dlfp::ProjectionArgs a
 #pragma unroll
     for (int u = 0; u < TB; ++u) acc[b][u] = f32x4_t{};
   const int lr = lane & 15, quad = lane >> 4, tr = lr & (TOKENS - 1);
-  const char* ex = smem + Shape::RINGS + lr * groups + quad;
+  const char* ex = smem + Shape::RINGS + lr * pitch + quad - g0;
+  if (split.splits > 1) ex += (lr * groups + g0) & 15;
   wait_stages<DEPTH, L, true>(count);  // the exponents of every wavefront are there
   int slot = 0;
   // `inside`: the steps that a step looks ahead to are there, and it and they are whole ones.
@@ -142,6 +148,7 @@ __global__ __launch_bounds__(64 * WAVES) void few4_kernel(dlfp::ProjectionArgs a
       wait_copies<(DEPTH - 1) * L>();
     else
       wait_stages<DEPTH - 1, L, false>(count - 1 - t);
+    const int g = GROUPS * (first + WAVES * t);
     const char* p = ring + slot * SLOT;
     u32x4_t codes[HALVES][BLOCKS];
     bf16x8_t xf[HALVES][TB][4];
@@ -153,7 +160,7 @@ __global__ __launch_bounds__(64 * WAVES) void few4_kernel(dlfp::ProjectionArgs a
         codes[h][b] = *reinterpret_cast<const u32x4_t*>(
             p + (b * 16 + lr) * (16 * GROUPS) + (((4 * h + quad) ^ few_swz<HALVES>(lr)) << 4));
         e[h][b] =
-            *reinterpret_cast<const uint8_t*>(ex + b * eblock + GROUPS * (first + t) + 4 * h);
+            *reinterpret_cast<const uint8_t*>(ex + b * eblock + g + 4 * h);
       }
 #pragma unroll
       for (int u = 0; u < TB; ++u)
@@ -165,10 +172,10 @@ __global__ __launch_bounds__(64 * WAVES) void few4_kernel(dlfp::ProjectionArgs a
     }
     wait_lds();  // the slot's reads have returned before it is refilled
     if (inside.value || t + DEPTH < count) issue(inside, t + DEPTH, slot);
-    if (!inside.value && GROUPS * (first + t) + GROUPS > groups) {  // past the end of the rows: zeros
+    if (!inside.value && g + GROUPS > groups) {  // past the end of the rows: zeros
 #pragma unroll
       for (int h = 0; h < HALVES; ++h)
-        if (GROUPS * (first + t) + 4 * h + quad >= groups) {
+        if (g + 4 * h + quad >= groups) {
 #pragma unroll
           for (int b = 0; b < BLOCKS; ++b) codes[h][b] = u32x4_t{}, e[h][b] = 0;
 #pragma unroll
@@ -194,7 +201,7 @@ __global__ __launch_bounds__(64 * WAVES) void few4_kernel(dlfp::ProjectionArgs a
   for (; t + DEPTH + 1 < count; ++t) step(std::true_type{}, t);
   for (; t < count; ++t) step(std::false_type{}, t);
 
-  store_few<BLOCKS, TOKENS, WAVES, GATED>(a, split, acc, smem, tid, wave, unit, part, n0, m0);
+  store_few<BLOCKS, TOKENS, WAVES, GATED>(a, split, acc, smem, tid, wave, own);
 }
 
 }  // namespace

@@ -34,13 +34,9 @@ __global__ __launch_bounds__(64 * WAVES) void gated_few_kernel(dlfp::ProjectionA
   __shared__ __attribute__((aligned(16))) char smem[Shape::LDS];
   const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
   constexpr int FEATURES = 8 * BLOCKS;
-  const uint32_t gn = (uint32_t)(a.n + FEATURES - 1) / FEATURES;
-  const uint32_t unit = blockIdx.x / split.splits, part = blockIdx.x - unit * split.splits;
-  const int n0 = (int)(unit % gn) * FEATURES, m0 = (int)(unit / gn) * TOKENS;
-  const int steps = (a.k + BSTEP - 1) / BSTEP;
-  const int64_t shares = (int64_t)WAVES * split.splits, share = (int64_t)WAVES * part + wave;
-  const int first = (int)(steps * share / shares);
-  const int count = (int)(steps * (share + 1) / shares) - first;
+  const Unit own = unit_of<FEATURES, TOKENS>(a, split, (a.k + BSTEP - 1) / BSTEP);
+  const int n0 = own.n0, m0 = own.m0;
+  const int first = own.from + wave, count = (own.to - first + WAVES - 1) / WAVES;
 
   // Copies: row 4 c + lane / 16 of 256 bytes, the 16 that belong at position lane % 16.
   uint32_t woff[4], xoff[XC];
@@ -66,7 +62,7 @@ __global__ __launch_bounds__(64 * WAVES) void gated_few_kernel(dlfp::ProjectionA
   char* ring = smem + wave * Shape::RING;
   const uint32_t lds0 = lds_addr(ring);
   auto issue = [&](auto inside, int t, int slot) {
-    const int s = first + t;
+    const int s = first + WAVES * t;
     const bool whole = inside.value || (s + 1) * BSTEP <= a.k;  // else its first half twice
     const uint32_t d = lds0 + slot * SLOT;
 #pragma unroll
@@ -118,7 +114,7 @@ __global__ __launch_bounds__(64 * WAVES) void gated_few_kernel(dlfp::ProjectionA
     }
     wait_lds();  // the slot's reads have returned before it is refilled
     if (inside.value || t + DEPTH < count) issue(inside, t + DEPTH, slot);
-    const bool whole = inside.value || (first + t + 1) * BSTEP <= a.k;
+    const bool whole = inside.value || (first + WAVES * t + 1) * BSTEP <= a.k;
 #pragma unroll
     for (int i = 0; i < 4; ++i)
       if (i < 2 || whole)  // (the second half of a last step of 64 columns is not there)
@@ -133,7 +129,7 @@ __global__ __launch_bounds__(64 * WAVES) void gated_few_kernel(dlfp::ProjectionA
   int t = 0;
   for (; t + DEPTH + 1 < count; ++t) step(std::true_type{}, t);
   for (; t < count; ++t) step(std::false_type{}, t);
-  store_few<BLOCKS, TOKENS, WAVES, true>(a, split, acc, smem, tid, wave, unit, part, n0, m0);
+  store_few<BLOCKS, TOKENS, WAVES, true>(a, split, acc, smem, tid, wave, own);
 }
 
 // ---------------------------------------------------------------- tiles

@@ -43,14 +43,10 @@ __global__ __launch_bounds__(256) void sum_tiles_kernel(dlfp::ProjectionArgs a, 
   const f32x4_t* p = reinterpret_cast<const f32x4_t*>(split.part) + (int64_t)t * UNITS +
                      (((wave * BN + q) * BM + u) * 4 + g) * 64 + lane;
   const int64_t step = (int64_t)gm * gn * UNITS;
-  f32x4_t v = p[0], up{};
-  if constexpr (GATED) up = p[2 * 64];
-  for (int s = 1; s < split.splits; ++s) {
-    v += p[s * step];
-    if constexpr (GATED) up += p[s * step + 2 * 64];
-  }
-  if constexpr (GATED) v = gated4(v, up, a.act);
-  store4(a, m, n, v);
+  f32x4_t v[GATED ? 2 : 1];
+  sum_splits(v, p, step, 2 * 64, split.splits);
+  if constexpr (GATED) v[0] = gated4(v[0], v[1], a.act);
+  store4(a, m, n, v[0]);
 }
 
 }  // namespace
