@@ -113,8 +113,8 @@ constexpr Launch few_gated() {
 }
 
 // Fitted to 1000 sizes of 1-4096 tokens, 64-25600 features and columns, every variant with every
-// split, plain and gated, weights read from memory.  The choice takes 1.014 times the fastest
-// one's time on average (geometric mean; 1.05 in nine of ten sizes, 1.31 at worst).
+// split, plain and gated, weights read from memory.  The choice takes 1.018 times the fastest
+// one's time on average (geometric mean; 1.07 in nine of ten sizes, 1.26 at worst).
 #define FEW(B, T, W, D, H) 16 * B, T, W, H* FHALF, FewShape<B, T, W, D, H>::RINGS, B, true
 #define TILE(TN, TM, ...) TN, TM, 0, 0, 0, 0, true
 #define FEW_CALLS(B, T, W, D, H) {launch_few<false, B, T, W, D, H>, few_gated<B, T, W, D, H>()}
