@@ -41,8 +41,8 @@ int launch_tile(const dlfp::ProjectionArgs& a, Grid g, dlfp::Split split, hipStr
 }
 
 // Fitted to 500 sizes of 1-4096 tokens, 64-25600 features and columns, every variant with every
-// split, weights read from memory.  The choice takes 1.026 times the fastest one's time on
-// average (geometric mean; 1.07 in nine of ten sizes, 1.34 at worst).
+// split, weights read from memory.  The choice takes 1.031 times the fastest one's time on
+// average (geometric mean; 1.08 in nine of ten sizes, 1.39 at worst).
 #define FEW(B, T, W, D) 16 * B, T, W, BSTEP, 0, 0, true
 #define WHOLE_K(TN, TM, ...) TN, TM, 0, 0, 0, 0, false
 #define TILE(TN, TM, ...) TN, TM, 0, 0, 0, 0, true
