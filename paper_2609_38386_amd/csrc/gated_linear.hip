@@ -35,8 +35,9 @@ int launch_tile(const dlfp::ProjectionArgs& a, Grid g, dlfp::Split split, hipStr
       <<<(uint32_t)(tiles * split.splits), 64 * WN * WM, 0, stream>>>(a, (int)g.down,
                                                                       (int)g.across, split);
   if (split.splits > 1)
-    sum_tiles_kernel<TN, TM, WN, WM, true><<<(uint32_t)(tiles * (TN * TM / 2048)), 256, 0, stream>>>(
-        a, (int)g.down, (int)g.across, split);
+    sum_tiles_kernel<TN, TM, WN, WM, true>
+        <<<(uint32_t)(tiles * (TN * TM / 2048)), 256, 0, stream>>>(a, (int)g.down, (int)g.across,
+                                                                   split);
   return hipGetLastError() == hipSuccess ? DLFP_OK : DLFP_EHIP;
 }
 

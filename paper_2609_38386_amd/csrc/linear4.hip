@@ -44,7 +44,8 @@ __global__ __launch_bounds__(64 * FAR_WAVES) void far4_kernel(dlfp::ProjectionAr
       const float scale = scale_of(in ? a.exps[b][row * (a.k >> 5) + (c >> 5)] : 0);
 #pragma unroll
       for (int t = 0; t < 4; ++t)
-        acc[b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(w[t], scale), xf[t], acc[b], 0, 0, 0);
+        acc[b] =
+            __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen(w[t], scale), xf[t], acc[b], 0, 0, 0);
     }
   }
 #pragma unroll

@@ -21,16 +21,17 @@ struct Grid {
 typedef int (*Launch)(const dlfp::ProjectionArgs&, Grid, dlfp::Split, hipStream_t);
 
 // A tile of `rows` rows of weights and `tokens` tokens.  Its wavefronts share steps of `columns`
-// columns, or take all of them (waves 0).  `lds` bytes besides the exponents of `blocks` blocks, where
-// that matters (blocks > 0).
+// columns, or take all of them (waves 0).  `lds` bytes besides the exponents of `blocks` blocks,
+// where that matters (blocks > 0).
 //
 // Time in microseconds, with u = tiles times splits / 256, s = steps of a unit (of a wavefront
 // where they share them, of 64 columns otherwise) and b = MB of weights:
 //   c0 + c1 s + (c2 + c3 s) u + (c4 + c5 s) ceil(u) + c6 b + (c7 + c8 s) ceil(u / resident)
 // and with splits + c9 + c10 times the MB of partial sums, where `resident` workgroups fit a
-// compute unit (0: left out), and where wavefronts share the steps + c11 times the MB of tokens that
-// the L2s read (each all of them, as far as there are tiles across; without this term 1084 tokens of
-// 208 x 15744 in 4 bits took 36 us by tiles of 32 tokens and 32 features, 22 by larger ones).
+// compute unit (0: left out), and where wavefronts share the steps + c11 times the MB of tokens
+// that the L2s read (each all of them, as far as there are tiles across; without this term 1084
+// tokens of 208 x 15744 in 4 bits took 36 us by tiles of 32 tokens and 32 features, 22 by larger
+// ones).
 struct Variant {
   int rows, tokens, waves, columns, lds, blocks;
   bool splits;
@@ -78,7 +79,8 @@ Plan choose(const Variant (&variants)[COUNT], bool gated, int m, int n, int k, i
       const float u = (float)(tiles * splits) / CUS;
       const float r = (float)((tiles * splits + CUS - 1) / CUS);
       const int share = splits * v.waves;
-      const float s = v.waves ? (float)((steps + share - 1) / share) : (float)k / 64 / (float)splits;
+      const float s =
+          v.waves ? (float)((steps + share - 1) / share) : (float)k / 64 / (float)splits;
       float t = fixed + c[1] * s + (c[2] + c[3] * s) * u + (c[4] + c[5] * s) * r;
       if (v.resident) {
         const int64_t most = (int64_t)CUS * v.resident;

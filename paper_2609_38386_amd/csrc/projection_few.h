@@ -87,8 +87,8 @@ __device__ __forceinline__ void store_few(const dlfp::ProjectionArgs& a, dlfp::S
     f32x4_t v = sum(GATED ? 2 * r : r);
     if (split.splits > 1) {
       // Unit (r, u, l) of the gate, then of the up.
-      f32x4_t* out = reinterpret_cast<f32x4_t*>(split.part) +
-                     ((int64_t)own.part * (gridDim.x / split.splits) + own.tile) * (BLOCKS * TB * 64) + i;
+      const int64_t at = (int64_t)own.part * (gridDim.x / split.splits) + own.tile;
+      f32x4_t* out = reinterpret_cast<f32x4_t*>(split.part) + at * (BLOCKS * TB * 64) + i;
       *out = v;
       if constexpr (GATED) out[OUT * TB * 64] = sum(2 * r + 1);
       continue;

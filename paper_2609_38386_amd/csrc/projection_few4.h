@@ -4,11 +4,12 @@
 // product takes is free as long as both operands agree.
 //
 // The exponents of the block's rows are copied before the first step, one contiguous piece of
-// memory (with K over workgroups, of each row the workgroup's part, which leaves the LDS to wider
-// blocks: 16 tokens of 5120 x 25600 in 3 parts 22.3 -> 20.3 us): as 4-byte pieces with each step they took a third of the copies' time (4096 x
-// 12288, 1 token: 9.6 us against 8.4 without any), and loaded into registers beside the copies
-// they made every step wait for all copies in flight (16 tokens of 5120 x 25600: 22.9 against
-// 21.2 us).  They are what limits k here: with more than the LDS holds, tiles are taken.
+// memory; with K over workgroups, of each row the workgroup's part, which leaves the LDS to wider
+// blocks (16 tokens of 5120 x 25600 in 3 parts 22.3 -> 20.3 us).  As 4-byte pieces with each step
+// they took a third of the copies' time (4096 x 12288, 1 token: 9.6 us against 8.4 without any),
+// and loaded into registers beside the copies they made every step wait for all copies in flight
+// (16 tokens of 5120 x 25600: 22.9 against 21.2 us).  They are what limits k here: with more than
+// the LDS holds, tiles are taken.
 //
 // Steps of 256 columns copy weights in rows of 128 bytes; steps of 128 columns (64-byte rows, which
 // are copied at half the rate) let twice the wavefronts share the LDS, which pays where the

@@ -19,7 +19,9 @@ namespace {
 constexpr int THREADS = 256;
 
 // (by value: a bit cast of a vector's element itself reads the vector's first)
-__device__ __forceinline__ bf16x2_t pair(uint32_t bits) { return __builtin_bit_cast(bf16x2_t, bits); }
+__device__ __forceinline__ bf16x2_t pair(uint32_t bits) {
+  return __builtin_bit_cast(bf16x2_t, bits);
+}
 
 __global__ __launch_bounds__(THREADS) void quantize_kernel(const uint16_t* w, int64_t ldw,
                                                            uint32_t* codes, uint8_t* exps,
