@@ -364,6 +364,52 @@ def test_two_streams_at_once(dev):
         assert torch.equal(got[i], want[i])
 
 
+def test_two_current_streams_and_their_graphs(dev):
+    """K over workgroups on two current streams at once, eager and as a graph of each replayed
+    beside the other: every call has partial sums of its own."""
+    gen = _gen(dev, 19)
+    m, n, k = 256, 1024, 16384
+    for kind in (D.LINEAR_W4, D.GATED_LINEAR_BF16, D.GATED_LINEAR_W4):
+        assert D.dlfp_projection_workspace(kind, m, n, k) > 0
+    w = [_weights4(dev, gen, n, k) for _ in range(2)]
+    dense = [_bf16(dev, gen, (n, k), 0.02) for _ in range(2)]
+    xs = [_bf16(dev, gen, (m, k)) for _ in range(2)]
+    outs = [[torch.empty((m, n), dtype=torch.float32, device=dev) for _ in range(3)]
+            for _ in range(2)]
+
+    def block(i):
+        rt.linear(xs[i], w[i], outs[i][0])
+        rt.gated_linear(xs[i], dense[i], dense[1 - i], outs[i][1])
+        rt.gated_linear(xs[i], w[i], w[1 - i], outs[i][2], "gelu")
+
+    def take():
+        torch.cuda.synchronize()
+        kept = [[t.clone() for t in ts] for ts in outs]
+        for ts in outs:
+            for t in ts:
+                t.fill_(math.nan)
+        torch.cuda.synchronize()
+        return kept
+
+    for i in range(2):
+        block(i)
+    want = take()
+    streams = [torch.cuda.Stream() for _ in range(2)]
+    graphs = []
+    for i, s in enumerate(streams):
+        graphs.append(torch.cuda.CUDAGraph())
+        with torch.cuda.graph(graphs[i], stream=s):
+            block(i)
+    for eager in (True, False, True, False):
+        for _ in range(3):
+            for i, s in enumerate(streams):
+                with torch.cuda.stream(s):
+                    block(i) if eager else graphs[i].replay()
+        for got, expected in zip(take(), want):
+            for t, u in zip(got, expected):
+                assert torch.equal(t, u)
+
+
 def test_weights_past_four_gigabytes(dev):
     """Row offsets past 32 bits: the last rows of weights of over 2^32 bytes."""
     gen = _gen(dev, 21)
