@@ -73,9 +73,10 @@ int dlfp_dequantize_w4(int32_t n, int32_t k, const void* codes, const void* exps
  * nor after; calls that may overlap (on two streams, or as parts of graphs that may) need
  * workspaces of their own.
  * Errors: DLFP_EINVAL, DLFP_EUNSUPPORTED, DLFP_ERANGE (more than 2^31 - 1025 tokens or
- * features, or 2^32 threads or more: a launch of many tokens has up to 512 for each 256 of
- * them and 256 features, one with rows 2^22 elements or more apart 512 for each 16 and 16),
- * DLFP_EHIP (of the second launch: the first stays enqueued). */
+ * features, 2^39 outputs or more, or 2^32 threads or more in every form of the call: there is
+ * one of 512 threads for each 256 tokens and 256 features (gated: 128); with rows 2^22 elements
+ * or more apart there is only one of 512 for each 16 and 16, gated with bf16 weights of 256 for
+ * each 64 and 32), DLFP_EHIP (of the second launch: the first stays enqueued). */
 int dlfp_linear_w4(int32_t m, int32_t n, int32_t k, const void* x, int64_t ldx, const void* codes,
                    const void* exps, void* out, int64_t ldo, int32_t out_dtype, void* workspace,
                    size_t workspace_bytes, hipStream_t stream);
@@ -107,6 +108,21 @@ int dlfp_gated_linear_w4(int32_t m, int32_t n, int32_t k, const void* x, int64_t
 #define DLFP_GATED_LINEAR_BF16 1
 #define DLFP_GATED_LINEAR_W4 2
 int64_t dlfp_projection_workspace(int32_t kind, int32_t m, int32_t n, int32_t k);
+
+/* The form that a call takes with so many bytes of workspace (0: with none), rows less than 2^22
+ * elements apart: for profiles and tests. */
+typedef struct {
+  int32_t variant;          /* its place among the kind's variants */
+  int32_t rows, tokens;     /* of a workgroup's tile: rows of weights (gated: both), tokens */
+  int32_t splits;           /* workgroups that share the K of a tile */
+  int32_t past_caches;      /* 1: weights are read past the caches */
+  int32_t reserved;
+  int64_t workspace_bytes;  /* that it uses */
+} dlfp_projection_form;
+
+/* DLFP_OK, or the error of a call of these sizes (m > 0, k < 2^22), which leaves form as it is. */
+int dlfp_projection_form_of(int32_t kind, int32_t m, int32_t n, int32_t k, size_t workspace_bytes,
+                            dlfp_projection_form* form);
 
 #ifdef __cplusplus
 }

@@ -8,7 +8,6 @@ namespace {
 template <int BLOCKS, int TOKENS, int WAVES, int DEPTH>
 int launch_few(const dlfp::ProjectionArgs& a, Grid g, dlfp::Split split, hipStream_t stream) {
   const int64_t tiles = g.down * g.across;
-  if (tiles * split.splits * (64 * WAVES) >= (int64_t)1 << 32) return DLFP_ERANGE;
   gated_few_kernel<BLOCKS, TOKENS, WAVES, DEPTH>
       <<<(uint32_t)(tiles * split.splits), 64 * WAVES, 0, stream>>>(a, split);
   if (split.splits > 1) {
@@ -21,7 +20,6 @@ int launch_few(const dlfp::ProjectionArgs& a, Grid g, dlfp::Split split, hipStre
 
 template <int TN, int TM, int WAVES, int STAGES>
 int launch_whole(const dlfp::ProjectionArgs& a, Grid g, dlfp::Split, hipStream_t stream) {
-  if (g.down * g.across * (64 * WAVES) >= (int64_t)1 << 32) return DLFP_ERANGE;
   split_kernel<TN, TM, WAVES, STAGES, true>
       <<<dim3((uint32_t)g.across, (uint32_t)g.down), 64 * WAVES, 0, stream>>>(a);
   return hipGetLastError() == hipSuccess ? DLFP_OK : DLFP_EHIP;
@@ -30,7 +28,6 @@ int launch_whole(const dlfp::ProjectionArgs& a, Grid g, dlfp::Split, hipStream_t
 template <int TN, int TM, int WN, int WM, int STAGES>
 int launch_tile(const dlfp::ProjectionArgs& a, Grid g, dlfp::Split split, hipStream_t stream) {
   const int64_t tiles = g.down * g.across;
-  if (tiles * split.splits * (64 * WN * WM) >= (int64_t)1 << 32) return DLFP_ERANGE;
   gated_tile_kernel<TN, TM, WN, WM, STAGES>
       <<<(uint32_t)(tiles * split.splits), 64 * WN * WM, 0, stream>>>(a, (int)g.down,
                                                                       (int)g.across, split);
@@ -44,9 +41,9 @@ int launch_tile(const dlfp::ProjectionArgs& a, Grid g, dlfp::Split split, hipStr
 // Fitted to 500 sizes of 1-4096 tokens, 64-25600 features and columns, every variant with every
 // split, weights read from memory.  The choice takes 1.031 times the fastest one's time on
 // average (geometric mean; 1.08 in nine of ten sizes, 1.39 at worst).
-#define FEW(B, T, W, D) 16 * B, T, W, BSTEP, 0, 0, true
-#define WHOLE_K(TN, TM, ...) TN, TM, 0, 0, 0, 0, false
-#define TILE(TN, TM, ...) TN, TM, 0, 0, 0, 0, true
+#define FEW(B, T, W, D) 16 * B, T, 64 * W, W, BSTEP, 0, 0, true
+#define WHOLE_K(TN, TM, W, STAGES) TN, TM, 64 * W, 0, 0, 0, 0, false
+#define TILE(TN, TM, WN, WM, STAGES) TN, TM, 64 * WN * WM, 0, 0, 0, 0, true
 #define FEW_CALLS(...) {nullptr, launch_few<__VA_ARGS__>}
 #define WHOLE_K_CALLS(...) {nullptr, launch_whole<__VA_ARGS__>}
 #define TILE_CALLS(...) {nullptr, launch_tile<__VA_ARGS__>}
@@ -75,7 +72,7 @@ int launch(dlfp::ProjectionArgs& a, void* workspace, size_t bytes, hipStream_t s
   if (std::max<int64_t>(a.ldx, a.k) < dlfp::FAR_STRIDE)
     return launch_best(VARIANTS, true, a, (int64_t)a.n * a.k * 4, workspace, bytes, stream);
   const int64_t gm = ((int64_t)a.m + 63) / 64, gn = ((int64_t)a.n + 31) / 32;
-  if (gm * gn * 256 >= (int64_t)1 << 32) return DLFP_ERANGE;
+  if (gm * gn * 256 > dlfp::MOST_THREADS) return DLFP_ERANGE;
   tile_kernel<64, 64, 2, 2, 4, true, true>
       <<<(uint32_t)(gm * gn), 256, 0, stream>>>(a, (int)gm, (int)gn);
   return hipGetLastError() == hipSuccess ? DLFP_OK : DLFP_EHIP;
@@ -85,8 +82,8 @@ int launch(dlfp::ProjectionArgs& a, void* workspace, size_t bytes, hipStream_t s
 
 namespace dlfp {
 
-int64_t workspace_gated(int m, int n, int k) {
-  return choose(VARIANTS, true, m, n, k, (int64_t)n * k * 4, MOST_PARTS).bytes;
+Form form_gated(int m, int n, int k, int64_t room) {
+  return form_of(VARIANTS, true, m, n, k, (int64_t)n * k * 4, room);
 }
 
 }  // namespace dlfp

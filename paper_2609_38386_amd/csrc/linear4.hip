@@ -65,7 +65,7 @@ __global__ __launch_bounds__(64 * FAR_WAVES) void far4_kernel(dlfp::ProjectionAr
 template <bool GATED>
 int launch_far(const dlfp::ProjectionArgs& a, hipStream_t stream) {
   const int64_t blocks = (int64_t)(a.n / 16) * (((int64_t)a.m + 15) / 16);
-  if (blocks * (64 * FAR_WAVES) >= (int64_t)1 << 32) return DLFP_ERANGE;
+  if (blocks * (64 * FAR_WAVES) > dlfp::MOST_THREADS) return DLFP_ERANGE;
   far4_kernel<GATED><<<(uint32_t)blocks, 64 * FAR_WAVES, 0, stream>>>(a);
   return hipGetLastError() == hipSuccess ? DLFP_OK : DLFP_EHIP;
 }
@@ -76,7 +76,6 @@ template <bool GATED, int BLOCKS, int TOKENS, int WAVES, int DEPTH, int HALVES>
 int launch_few(const dlfp::ProjectionArgs& a, Grid g, dlfp::Split split, hipStream_t stream) {
   using Shape = FewShape<BLOCKS, TOKENS, WAVES, DEPTH, HALVES>;
   const int64_t tiles = g.down * g.across;
-  if (tiles * split.splits * (64 * WAVES) >= (int64_t)1 << 32) return DLFP_ERANGE;
   few4_kernel<BLOCKS, TOKENS, WAVES, DEPTH, HALVES, GATED>
       <<<(uint32_t)(tiles * split.splits), 64 * WAVES, (size_t)Shape::lds(a.k, split.splits),
          stream>>>(a, split);
@@ -91,7 +90,6 @@ int launch_few(const dlfp::ProjectionArgs& a, Grid g, dlfp::Split split, hipStre
 template <bool GATED, int TN, int TM, int WN, int WM, int DEPTH, int STAGES, bool WHOLE>
 int launch_tile(const dlfp::ProjectionArgs& a, Grid g, dlfp::Split split, hipStream_t stream) {
   const int64_t tiles = g.down * g.across;
-  if (tiles * split.splits * (64 * WN * WM) >= (int64_t)1 << 32) return DLFP_ERANGE;
   tile4_kernel<TN, TM, WN, WM, DEPTH, STAGES, GATED, WHOLE>
       <<<(uint32_t)(tiles * split.splits), 64 * WN * WM, 0, stream>>>(a, (int)g.down,
                                                                       (int)g.across, split);
@@ -116,8 +114,9 @@ constexpr Launch few_gated() {
 // Fitted to 1000 sizes of 1-4096 tokens, 64-25600 features and columns, every variant with every
 // split, plain and gated, weights read from memory.  The choice takes 1.018 times the fastest
 // one's time on average (geometric mean; 1.07 in nine of ten sizes, 1.26 at worst).
-#define FEW(B, T, W, D, H) 16 * B, T, W, H* FHALF, FewShape<B, T, W, D, H>::RINGS, B, true
-#define TILE(TN, TM, ...) TN, TM, 0, 0, 0, 0, true
+#define FEW(B, T, W, D, H) \
+  16 * B, T, 64 * W, W, H* FHALF, FewShape<B, T, W, D, H>::RINGS, B, true
+#define TILE(TN, TM, WN, WM, ...) TN, TM, 64 * WN * WM, 0, 0, 0, 0, true
 #define FEW_CALLS(B, T, W, D, H) {launch_few<false, B, T, W, D, H>, few_gated<B, T, W, D, H>()}
 #define TILE_CALLS(...) {launch_tile<false, __VA_ARGS__>, launch_tile<true, __VA_ARGS__>}
 constexpr Variant VARIANTS[] = {
@@ -212,19 +211,38 @@ extern "C" int dlfp_gated_linear_w4(int32_t m, int32_t n, int32_t k, const void*
 
 namespace dlfp {
 
-int64_t workspace_w4(bool gated, int m, int n, int k) {
-  return choose(VARIANTS, gated, m, n, k, weight_bytes(gated, n, k), MOST_PARTS).bytes;
+Form form_w4(bool gated, int m, int n, int k, int64_t room) {
+  return form_of(VARIANTS, gated, m, n, k, weight_bytes(gated, n, k), room);
 }
+
+namespace {
+
+// DLFP_OK and the form of a call of near rows, or what is wrong with the sizes.
+int form_of_kind(int32_t kind, int32_t m, int32_t n, int32_t k, size_t bytes, Form& form) {
+  if (kind < DLFP_LINEAR_W4 || kind > DLFP_GATED_LINEAR_W4) return DLFP_EINVAL;
+  if (m <= 0 || n <= 0 || k <= 0) return DLFP_EINVAL;
+  if (n % 16 || k % 64) return DLFP_EUNSUPPORTED;
+  if (k >= FAR_STRIDE || too_many(m, n)) return DLFP_ERANGE;
+  const int64_t room = (int64_t)std::min<size_t>(bytes, MOST_PARTS);
+  form = kind == DLFP_GATED_LINEAR_BF16 ? form_gated(m, n, k, room)
+                                        : form_w4(kind == DLFP_GATED_LINEAR_W4, m, n, k, room);
+  return form.variant < 0 ? DLFP_ERANGE : DLFP_OK;
+}
+
+}  // namespace
 
 }  // namespace dlfp
 
 extern "C" int64_t dlfp_projection_workspace(int32_t kind, int32_t m, int32_t n, int32_t k) {
-  if (m <= 0 || n <= 0 || k <= 0 || n % 16 || k % 64 || k >= FAR_STRIDE) return 0;
-  if (dlfp::too_many(m, n)) return 0;
-  switch (kind) {
-    case DLFP_LINEAR_W4: return dlfp::workspace_w4(false, m, n, k);
-    case DLFP_GATED_LINEAR_W4: return dlfp::workspace_w4(true, m, n, k);
-    case DLFP_GATED_LINEAR_BF16: return dlfp::workspace_gated(m, n, k);
-  }
-  return 0;
+  dlfp::Form form;
+  return dlfp::form_of_kind(kind, m, n, k, SIZE_MAX, form) == DLFP_OK ? form.bytes : 0;
+}
+
+extern "C" int dlfp_projection_form_of(int32_t kind, int32_t m, int32_t n, int32_t k,
+                                       size_t workspace_bytes, dlfp_projection_form* form) {
+  if (!form) return DLFP_EINVAL;
+  dlfp::Form f;
+  const int st = dlfp::form_of_kind(kind, m, n, k, workspace_bytes, f);
+  if (st == DLFP_OK) *form = {f.variant, f.rows, f.tokens, f.splits, f.stream, 0, f.bytes};
+  return st;
 }

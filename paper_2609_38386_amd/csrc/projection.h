@@ -32,7 +32,10 @@ constexpr int FAR_STRIDE = 1 << 22;
 // Tokens and features at most, so that the index of a tile's last row fits 31 bits.
 constexpr int MOST_ROWS = 0x7fffffff - 1024;
 
-// Outputs from here on are 2^32 threads or more in any form (512 for each 256 x 256 at least),
+// Threads of a launch at most.
+constexpr int64_t MOST_THREADS = ((int64_t)1 << 32) - 1;
+
+// Outputs from here on are more threads than that in any form (512 for each 256 x 256 at least),
 // below it the products of sizes that the choice takes fit 63 bits.
 constexpr int64_t MOST_OUTPUTS = (int64_t)1 << 39;
 inline bool too_many(int m, int n) {
@@ -51,9 +54,17 @@ inline __host__ __device__ int exps_bytes(int k, int splits, int step_columns) {
   return (16 * exps_pitch(k, splits, step_columns) + 1023) / 1024 * 1024;
 }
 
-// Bytes of partial sums of the fastest form.
-int64_t workspace_w4(bool gated, int m, int n, int k);
-int64_t workspace_gated(int m, int n, int k);
+// The form that a call of near rows takes with `room` bytes of workspace: its place among the
+// variants (-1: a launch of none can have the threads), its tile, its splits and their bytes, and
+// whether weights are read past the caches.
+struct Form {
+  int variant, rows, tokens, splits, stream;
+  int64_t bytes;
+};
+Form form_w4(bool gated, int m, int n, int k, int64_t room);
+Form form_gated(int m, int n, int k, int64_t room);
+
+constexpr int64_t MOST_PARTS = 32 << 20;  // bytes of partial sums
 
 // DLFP_OK, or what is wrong with them; sets wide.
 int check_projection(ProjectionArgs& a, bool gated, bool codes, int32_t out_dtype,

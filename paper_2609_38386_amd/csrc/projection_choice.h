@@ -10,6 +10,7 @@
 #include <algorithm>
 #include <cstdint>
 
+#include "dlfp.h"
 #include "projection.h"
 
 namespace {
@@ -20,9 +21,9 @@ struct Grid {
 };
 typedef int (*Launch)(const dlfp::ProjectionArgs&, Grid, dlfp::Split, hipStream_t);
 
-// A tile of `rows` rows of weights and `tokens` tokens.  Its wavefronts share steps of `columns`
-// columns, or take all of them (waves 0).  `lds` bytes besides the exponents of `blocks` blocks,
-// where that matters (blocks > 0).
+// A tile of `rows` rows of weights and `tokens` tokens, of one workgroup of `threads`.  Its wavefronts
+// share steps of `columns` columns, or take all of them (waves 0).  `lds` bytes besides the exponents
+// of `blocks` blocks, where that matters (blocks > 0).
 //
 // Time in microseconds, with u = tiles times splits / 256, s = steps of a unit (of a wavefront
 // where they share them, of 64 columns otherwise) and b = MB of weights:
@@ -33,7 +34,7 @@ typedef int (*Launch)(const dlfp::ProjectionArgs&, Grid, dlfp::Split, hipStream_
 // tokens of 208 x 15744 in 4 bits took 36 us by tiles of 32 tokens and 32 features, 22 by larger
 // ones).
 struct Variant {
-  int rows, tokens, waves, columns, lds, blocks;
+  int rows, tokens, threads, waves, columns, lds, blocks;
   bool splits;
   int resident;
   float c[12];
@@ -43,7 +44,6 @@ struct Variant {
 constexpr int CUS = 256;
 constexpr int SPLITS[] = {1, 2, 3, 4, 6, 8};  // (those of sum_splits)
 constexpr int SPLIT_COLUMNS = 512;           // at least, of a split of a tile
-constexpr int64_t MOST_PARTS = 32 << 20;     // bytes of partial sums
 constexpr int64_t MOST_GRID_Y = 65535;
 
 struct Plan {
@@ -53,7 +53,8 @@ struct Plan {
   int64_t bytes;  // of partial sums
 };
 
-// The least estimate among those whose partial sums fit into `room` bytes.
+// The least estimate among those whose partial sums fit into `room` bytes and whose threads a launch
+// can have (no variant, if there is none: near 2^39 outputs).
 template <int COUNT>
 Plan choose(const Variant (&variants)[COUNT], bool gated, int m, int n, int k, int64_t weight_bytes,
             int64_t room) {
@@ -70,6 +71,7 @@ Plan choose(const Variant (&variants)[COUNT], bool gated, int m, int n, int k, i
     const float fixed = c[0] + c[6] * 1e-6f * (float)weight_bytes;
     const int steps = v.waves ? (k + v.columns - 1) / v.columns : 0;
     for (int splits : SPLITS) {
+      if (tiles * splits * v.threads > dlfp::MOST_THREADS) break;
       if (splits > 1 && (!v.splits || splits * bytes > room ||
                          (v.waves ? splits * v.waves > steps : splits * SPLIT_COLUMNS > k)))
         break;
@@ -103,12 +105,27 @@ Plan choose(const Variant (&variants)[COUNT], bool gated, int m, int n, int k, i
 // turn: 12.9 -> 14.8 us past it).
 constexpr int64_t STREAM_BYTES = 64 << 20;
 
+bool past_caches(const Plan& p, int64_t weight_bytes) {
+  return p.grid.down == 1 && weight_bytes >= STREAM_BYTES;
+}
+
+template <int COUNT>
+dlfp::Form form_of(const Variant (&variants)[COUNT], bool gated, int m, int n, int k,
+                   int64_t weight_bytes, int64_t room) {
+  const Plan p = choose(variants, gated, m, n, k, weight_bytes, room);
+  if (!p.variant) return dlfp::Form{-1, 0, 0, 1, 0, 0};
+  return dlfp::Form{(int)(p.variant - variants), p.variant->rows,
+                    p.variant->tokens,           p.splits,
+                    past_caches(p, weight_bytes), p.bytes};
+}
+
 template <int COUNT>
 int launch_best(const Variant (&variants)[COUNT], bool gated, dlfp::ProjectionArgs& a,
                 int64_t weight_bytes, void* workspace, size_t bytes, hipStream_t stream) {
-  const int64_t room = workspace ? (int64_t)std::min<size_t>(bytes, MOST_PARTS) : 0;
+  const int64_t room = workspace ? (int64_t)std::min<size_t>(bytes, dlfp::MOST_PARTS) : 0;
   const Plan p = choose(variants, gated, a.m, a.n, a.k, weight_bytes, room);
-  a.stream = p.grid.down == 1 && weight_bytes >= STREAM_BYTES;
+  if (!p.variant) return DLFP_ERANGE;
+  a.stream = past_caches(p, weight_bytes);
   return p.variant->launch[gated](a, p.grid, dlfp::Split{static_cast<float*>(workspace), p.splits},
                                   stream);
 }

@@ -84,7 +84,8 @@ CACHE_EXPORTS = ["dlfp_rope_append", "dlfp_rope_append_kv8", "dlfp_build_window_
 
 # Declared in dlfp_ffn.h.
 FFN_EXPORTS = ["dlfp_quantize_w4", "dlfp_dequantize_w4", "dlfp_linear_w4",
-               "dlfp_gated_linear_bf16", "dlfp_gated_linear_w4", "dlfp_projection_workspace"]
+               "dlfp_gated_linear_bf16", "dlfp_gated_linear_w4", "dlfp_projection_workspace",
+               "dlfp_projection_form_of"]
 W4_GROUP = 32
 ACTIVATIONS = {"silu": 0, "gelu": 1}
 LINEAR_W4, GATED_LINEAR_BF16, GATED_LINEAR_W4 = range(3)
@@ -101,6 +102,15 @@ class dlfp_window(ctypes.Structure):
 
 def lib_path() -> str:
     return _LIB_PATH
+
+
+class dlfp_projection_form(ctypes.Structure):
+    """The form that a projection takes: its place among the kind's variants, its tile's rows of
+    weights (gated: both) and tokens, the workgroups that share K, whether weights are read past the
+    caches, and the bytes of workspace that it uses."""
+    _fields_ = [("variant", ctypes.c_int32), ("rows", ctypes.c_int32), ("tokens", ctypes.c_int32),
+                ("splits", ctypes.c_int32), ("past_caches", ctypes.c_int32),
+                ("reserved", ctypes.c_int32), ("workspace_bytes", ctypes.c_int64)]
 
 
 def lib():
@@ -163,6 +173,7 @@ def lib():
     L.dlfp_gated_linear_w4.argtypes = [i32, i32, i32, vp, i64, vp, vp, vp, vp, i32, vp, i64, i32,
                                        vp, sz, vp]
     L.dlfp_projection_workspace.argtypes = [i32, i32, i32, i32]
+    L.dlfp_projection_form_of.argtypes = [i32, i32, i32, i32, sz, vp]
     for name in EXPORTS + CACHE_EXPORTS + FFN_EXPORTS:
         if name != "dlfp_status_string":
             getattr(L, name).restype = ctypes.c_int
@@ -641,6 +652,16 @@ def dlfp_projection_workspace(kind: int, m: int, n: int, k: int) -> int:
     """Bytes of workspace that the fastest form of a projection takes (kind: LINEAR_W4,
     GATED_LINEAR_BF16 or GATED_LINEAR_W4)."""
     return lib().dlfp_projection_workspace(kind, m, n, k)
+
+
+def dlfp_projection_form_of(kind: int, m: int, n: int, k: int,
+                            workspace_bytes: int) -> dlfp_projection_form:
+    """The form that a projection of these sizes takes with so many bytes of workspace."""
+    _check_sizes(m, n, k)
+    form = dlfp_projection_form()
+    _check(lib().dlfp_projection_form_of(kind, m, n, k, workspace_bytes, ctypes.byref(form)),
+           "dlfp_projection_form_of")
+    return form
 
 
 def dlfp_linear_w4(x, codes, exps, out, workspace=None, stream=None) -> None:
