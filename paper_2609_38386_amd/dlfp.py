@@ -568,7 +568,7 @@ def _check_codes(codes, exps):
 
 def _check_sizes(*sizes):
     """The C calls take sizes as 32-bit integers, and ctypes would keep the low bits of others."""
-    if max(sizes) >> 31:
+    if max(sizes) >> 31 > 0 or min(sizes) >> 31 < -1:
         raise ValueError("sizes must be below 2^31")
 
 
@@ -651,6 +651,7 @@ def _workspace_args(workspace, device):
 def dlfp_projection_workspace(kind: int, m: int, n: int, k: int) -> int:
     """Bytes of workspace that the fastest form of a projection takes (kind: LINEAR_W4,
     GATED_LINEAR_BF16 or GATED_LINEAR_W4)."""
+    _check_sizes(m, n, k)
     return lib().dlfp_projection_workspace(kind, m, n, k)
 
 
