@@ -441,10 +441,12 @@ class GpuExecutor:
             hq, hkv, hid = cfg.num_q_heads * 128, cfg.num_kv_heads * 128, cfg.hidden
             self.w_q, self.w_k, self.w_v = weight(hq, hid), weight(hkv, hid), weight(hkv, hid)
             self.w_o = weight(hid, hq)
-            self.w_gu, self.w_d = weight(2 * cfg.mlp, hid), weight(hid, cfg.mlp)
+            w_gu, self.w_d = weight(2 * cfg.mlp, hid), weight(hid, cfg.mlp)
             self.gated = cfg.gated
             if self.gated:
-                self.w_g, self.w_u = self.w_gu[:cfg.mlp], self.w_gu[cfg.mlp:]
+                self.w_g, self.w_u = w_gu[:cfg.mlp], w_gu[cfg.mlp:]
+            else:
+                self.w_gu = w_gu
             self.project = D.dlfp_linear_bf16
             if cfg.weight_bits == 4:
                 self.project = rt.linear
