@@ -457,7 +457,8 @@ class GpuExecutor:
             self.x = torch.empty((rows, hid), dtype=torch.bfloat16, device=device)
             self.x.normal_(generator=gen)
             self.y = torch.empty((rows, hid), dtype=torch.bfloat16, device=device)
-            self.gu = torch.empty((rows, 2 * cfg.mlp), dtype=torch.bfloat16, device=device)
+            self.gu = torch.empty((rows, cfg.mlp if self.gated else 2 * cfg.mlp),
+                                  dtype=torch.bfloat16, device=device)
             self.y2 = torch.empty_like(self.y)
             self.mlp = cfg.mlp
         if self.windowed:
@@ -546,7 +547,7 @@ class GpuExecutor:
         if self.proxy:
             self.project(self.out[:T].view(T, -1), self.w_o, self.y[:T])
             if self.gated:
-                self.rt.gated_linear(self.y[:T], self.w_g, self.w_u, self.gu[:T, :self.mlp])
+                self.rt.gated_linear(self.y[:T], self.w_g, self.w_u, self.gu[:T])
             else:
                 self.project(self.y[:T], self.w_gu, self.gu[:T])
             self.project(self.gu[:T, :self.mlp], self.w_d, self.y2[:T])

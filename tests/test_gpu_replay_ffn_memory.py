@@ -34,3 +34,11 @@ def test_4_bit_weights_replace_the_bf16_ones(gated):
     heads = (2 * cfg.num_q_heads + 2 * cfg.num_kv_heads) * 128
     weights = HIDDEN * (heads + 3 * MLP)
     assert abs((wide - four) - weights * (2 - 17 / 32)) < 8 << 20
+
+
+def test_gated_rows_are_as_wide_as_the_block():
+    """The gated launch writes `mlp` columns a row, the plain one gate and up."""
+    plain, cfg = _kept()
+    gated, _ = _kept(gated=True)
+    rows = cfg.budget + cfg.max_seqs
+    assert abs((plain - gated) - rows * MLP * 2) < 8 << 20
