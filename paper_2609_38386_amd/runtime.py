@@ -205,8 +205,9 @@ def linear(x: torch.Tensor, w, out: torch.Tensor, workspace: Optional[torch.Tens
            stream=None):
     """out = x W^T: x bf16 [m][k], w a Weights4 or bf16 [n][k], out bf16 or float32 [m][n].
     ``workspace``: for 4-bit weights, a tensor of dlfp_projection_workspace bytes that no call
-    beside this one uses (None: taken from PyTorch's allocator, or, with a ``stream`` given by
-    hand, none)."""
+    beside this one uses.  None: taken from PyTorch's allocator, which keeps memory of the current
+    stream apart; with a ``stream`` given by hand there is then none, and K is not split over
+    workgroups (256 tokens of 5120 x 25600: 98 us instead of 68)."""
     if isinstance(w, Weights4):
         n, k = w._n, w._k
         if workspace is None and stream is None:
