@@ -92,8 +92,8 @@ extern "C" int dlfp_gated_linear_bf16(int32_t m, int32_t n, int32_t k, const voi
                                       const void* w_gate, const void* w_up, int32_t activation,
                                       void* out, int64_t ldo, int32_t out_dtype, void* workspace,
                                       size_t workspace_bytes, hipStream_t stream) {
-  dlfp::ProjectionArgs a{static_cast<const uint16_t*>(x), {w_gate, w_up}, {nullptr, nullptr}, out,
-                         ldx, ldo, m, n, k, activation, out_dtype, 0, 0};
+  dlfp::ProjectionArgs a{static_cast<const uint16_t*>(x), {w_gate, w_up}, m, n, k, activation, ldx,
+                         ldo, out, {nullptr, nullptr}, out_dtype, 0, 0};
   const int st = dlfp::check_projection(a, true, false, out_dtype, workspace);
   return st != DLFP_OK || m == 0 ? st : launch(a, workspace, workspace_bytes, stream);
 }

@@ -96,8 +96,8 @@ extern "C" int dlfp_linear_bf16(int32_t m, int32_t n, int32_t k, const void* x, 
   if ((reinterpret_cast<uintptr_t>(x) | reinterpret_cast<uintptr_t>(w)) & 15) return DLFP_EINVAL;
   if (reinterpret_cast<uintptr_t>(out) & (out_dtype ? 15 : 7)) return DLFP_EINVAL;
   const bool wide = (reinterpret_cast<uintptr_t>(out) & 15) == 0 && ldo % 8 == 0;
-  const dlfp::ProjectionArgs a{static_cast<const uint16_t*>(x), {w, nullptr}, {nullptr, nullptr},
-                               out, ldx, ldo, m, n, k, 0, out_dtype, wide, 0};
+  const dlfp::ProjectionArgs a{static_cast<const uint16_t*>(x), {w, nullptr}, m, n, k, 0, ldx, ldo,
+                               out, {nullptr, nullptr}, out_dtype, wide, 0};
   (void)hipGetLastError();
   launch_linear(a, stream);
   return hipGetLastError() == hipSuccess ? DLFP_OK : DLFP_EHIP;

@@ -189,8 +189,9 @@ extern "C" int dlfp_linear_w4(int32_t m, int32_t n, int32_t k, const void* x, in
                               hipStream_t stream) {
   dlfp::ProjectionArgs a{static_cast<const uint16_t*>(x),
                          {codes, nullptr},
+                         m, n, k, 0, ldx, ldo, out,
                          {static_cast<const uint8_t*>(exps), nullptr},
-                         out, ldx, ldo, m, n, k, 0, out_dtype, 0, 0};
+                         out_dtype, 0, 0};
   const int st = dlfp::check_projection(a, false, true, out_dtype, workspace);
   return st != DLFP_OK || m == 0 ? st : launch<false>(a, workspace, workspace_bytes, stream);
 }
@@ -203,8 +204,9 @@ extern "C" int dlfp_gated_linear_w4(int32_t m, int32_t n, int32_t k, const void*
   dlfp::ProjectionArgs a{
       static_cast<const uint16_t*>(x),
       {gate_codes, up_codes},
+      m, n, k, activation, ldx, ldo, out,
       {static_cast<const uint8_t*>(gate_exps), static_cast<const uint8_t*>(up_exps)},
-      out, ldx, ldo, m, n, k, activation, out_dtype, 0, 0};
+      out_dtype, 0, 0};
   const int st = dlfp::check_projection(a, true, true, out_dtype, workspace);
   return st != DLFP_OK || m == 0 ? st : launch<true>(a, workspace, workspace_bytes, stream);
 }

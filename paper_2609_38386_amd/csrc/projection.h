@@ -8,13 +8,15 @@
 namespace dlfp {
 
 // out = x W^T, or act(x G^T) * (x U^T): weights [0] are W or G, [1] are U.
+// What a kernel needs before its first copies comes first, in one line of 64 bytes.
 struct ProjectionArgs {
   const uint16_t* x;
   const void* weights[2];        // bf16, or codes
-  const uint8_t* exps[2];        // of codes
-  void* out;
+  int32_t m, n, k, act;
   int64_t ldx, ldo;
-  int32_t m, n, k, act, out_f32;
+  void* out;
+  const uint8_t* exps[2];        // of codes
+  int32_t out_f32;
   int32_t wide;    // bf16 output rows take 16-byte stores
   int32_t stream;  // weights are read past the caches
 };

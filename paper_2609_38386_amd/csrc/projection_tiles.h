@@ -102,9 +102,13 @@ __device__ __forceinline__ void wait_stages(int later) {
 // measured 1-4% slower: the even rows of a group then share positions).
 __device__ __forceinline__ int swz(int row) { return (row >> 1) & 7; }
 
-// Eight consecutive features of a token.
-__device__ __forceinline__ void store8(const dlfp::ProjectionArgs& a, int m, int n, f32x4_t lo, f32x4_t hi) {
-  const int64_t e = (int64_t)m * a.ldo + n;
+// Eight consecutive features of a token.  NEAR: the row stride of out fits 32 bits (a 64-bit product
+// for every store took 1-2% of dlfp_linear_bf16's launches of short K: 545 tokens of 6144 x 1024
+// 11.8 -> 12.0 us).
+template <bool NEAR>
+__device__ __forceinline__ void store8(const dlfp::ProjectionArgs& a, int m, int n, f32x4_t lo,
+                                       f32x4_t hi) {
+  const int64_t e = NEAR ? (int64_t)m * (int32_t)a.ldo + n : (int64_t)m * a.ldo + n;
   if (a.out_f32) {
     f32x4_t* o = reinterpret_cast<f32x4_t*>(static_cast<float*>(a.out) + e);
     o[0] = lo;
@@ -158,6 +162,12 @@ __device__ __forceinline__ void weight_offsets(uint32_t (&off)[COUNT], int lane,
   }
 }
 
+// The first row of tokens of a tile.  NEAR: row strides fit 32 bits.
+template <bool NEAR>
+__device__ __forceinline__ const char* token_rows(const dlfp::ProjectionArgs& a, int m0) {
+  return reinterpret_cast<const char*>(a.x + (NEAR ? (int64_t)m0 * (int32_t)a.ldx : m0 * a.ldx));
+}
+
 // The first row of weights of a tile.
 __device__ __forceinline__ const char* weight_rows(const dlfp::ProjectionArgs& a, int which,
                                                    int n0) {
@@ -172,7 +182,8 @@ __device__ __forceinline__ f32x4_t gated4(f32x4_t g, f32x4_t u, int act) {
 }
 
 // The end of a tile whose K steps are split over the wavefronts: their sum, in wave order,
-// for the first TOKENS tokens.  Every wave is done with LDS.
+// for the first TOKENS tokens.  Every wave is done with LDS.  Plain ones are dlfp_linear_bf16's:
+// whole tiles of features, row strides of 32 bits.
 // A wave's accumulators are groups of four features: group (q, t, g) of lane l holds
 // features 32 q + 8 g + 4 (l / 32) .. + 3 of token 32 t + l % 32.  A thread sums and stores
 // eight consecutive features, neighbouring threads the next ones of the same token; the lane
@@ -218,7 +229,7 @@ __device__ __forceinline__ void store_sums(const dlfp::ProjectionArgs& a, f32x16
       hi = gated4(hi, uhi, a.act);
     }
     const int n = n0 + 8 * EIGHTS * q + 8 * g;
-    if (m0 + tok < a.m && n < a.n) store8(a, m0 + tok, n, lo, hi);
+    if (m0 + tok < a.m && (!GATED || n < a.n)) store8<!GATED>(a, m0 + tok, n, lo, hi);
   }
 }
 
@@ -245,7 +256,7 @@ __global__ __launch_bounds__(64 * WAVES) void split_kernel(dlfp::ProjectionArgs 
   weight_offsets<GATED>(woff, lane, a.k, GATED ? a.n - 1 - n0 : TN - 1, [](int i) { return i; });
   copy_offsets(xoff, lane, a.ldx, a.m - 1 - m0, [](int i) { return COPY_ROWS * i; });
   const char* wbase[2] = {weight_rows(a, 0, n0), GATED ? weight_rows(a, 1, n0) : nullptr};
-  const char* xbase = reinterpret_cast<const char*>(a.x + (int64_t)m0 * a.ldx);
+  const char* xbase = token_rows<!GATED>(a, m0);
   char* ring = smem + wave * (STAGES * STAGE);
   const uint32_t lds0 = lds_addr(ring);
   const int total = a.k / KSTEP;
@@ -304,8 +315,9 @@ __global__ __launch_bounds__(64 * WAVES) void split_kernel(dlfp::ProjectionArgs 
 // The end of a tile: through the wave's slice of LDS (`bytes` of them), so that whole
 // runs of a row are stored (straight from the accumulators a store covers 16 bytes of 32
 // rows; on m = 8192, n = 6144, k = 1024 the launch took 13% longer with those).  The
-// wave's part of the tile starts at feature n0 and token m0; every wave is done with LDS.
-template <int BN, int BM, int SLICE, bool GATED>
+// wave's part of the tile starts at feature n0 and token m0; every wave is done with LDS.  WHOLE: all
+// of its features are there, and row strides fit 32 bits (dlfp_linear_bf16).
+template <int BN, int BM, int SLICE, bool GATED, bool WHOLE = false>
 __device__ __forceinline__ void store_tile(const dlfp::ProjectionArgs& a, f32x16_t (&acc)[BN][BM],
                                            char* mine, int lane, int n0, int m0) {
   const int lr = lane & 31, lh = lane >> 5;
@@ -336,7 +348,7 @@ __device__ __forceinline__ void store_tile(const dlfp::ProjectionArgs& a, f32x16
         const int r = r0 + lane / PER_ROW, f = 8 * (lane % PER_ROW);
         const f32x4_t* v = reinterpret_cast<const f32x4_t*>(mine + r * RB + f * 4);
         const int m = m0 + 32 * j + r, n = n0 + OF * p * B + f;
-        if (m < a.m && n < a.n) store8(a, m, n, v[0], v[1]);
+        if (m < a.m && (WHOLE || n < a.n)) store8<WHOLE>(a, m, n, v[0], v[1]);
       }
       wait_lds();
     }
@@ -370,7 +382,7 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(dlfp::ProjectionA
   static_assert(!GATED || WAVES % 4 == 0, "the copies of a wave are of one weight");
   const char* wbase = weight_rows(a, copy_weights<GATED>(wave), n0);
   const int wlast = GATED ? a.n - 1 - n0 : TN - 1;
-  const char* xbase = reinterpret_cast<const char*>(a.x + (int64_t)m0 * a.ldx);
+  const char* xbase = token_rows<!GATED>(a, m0);
   const int xlast = a.m - 1 - m0;
   uint32_t woff[NL], xoff[ML];
   if constexpr (!FAR) {
@@ -457,8 +469,8 @@ __global__ __launch_bounds__(64 * WN * WM, 2) void tile_kernel(dlfp::ProjectionA
 
   constexpr int SLICE = STAGES * STAGE / WAVES / 16 * 16;
   wait_copies_barrier<0>();
-  store_tile<BN, BM, SLICE, GATED>(a, acc, smem + wave * SLICE, lane,
-                                   n0 + (GATED ? 16 : 32) * wn * BN, m0 + 32 * wm * BM);
+  store_tile<BN, BM, SLICE, GATED, !GATED>(a, acc, smem + wave * SLICE, lane,
+                                           n0 + (GATED ? 16 : 32) * wn * BN, m0 + 32 * wm * BM);
 }
 
 }  // namespace
