@@ -21,28 +21,49 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
-// act(g) u, the activation in fp32, then the product.  e^-y is 2^(y log2 e) with the product's
-// rounding error put back, so that SiLU's gates far below 0, whose weight is all in the power, are
-// 4 fp32 steps (2^-23) off at most; GELU's y is itself a rounded one, whose error counts |y| times
-// there (7 |y| half steps).  Where the power is past 2^125, 1 / (1 + e^-y) is e^y to the last bit
-// and its reciprocal would leave fp32's normal range before the activation does (g = -88: -5e-37):
-// 2^64 e^y is multiplied by the gate first.
-__device__ __forceinline__ float gated(float g, float u, int act) {
+// The power of an activation, e^-y, is 2^(t + rest): t the product -y log2 e as it is rounded, rest its
+// rounding error, so that SiLU's gates far below 0, whose weight is all in the power, are 4 fp32
+// steps (2^-23) off at most.  (GELU's y is itself a rounded one, whose error counts |y| times there:
+// 7 |y| half steps.)
+struct Power {
+  float t, rest;
+};
+__device__ __forceinline__ Power power_of(float g, int act) {
   const float y = act ? 1.5957691216057308f * (g + 0.044715f * g * g * g) : g;
   constexpr float LOG2E = 1.44269504088896f, LOG2E_LOW = 1.925963033500e-8f;
   const float t = -y * LOG2E;
-  const float rest = __builtin_fmaf(-y, LOG2E, -t) - y * LOG2E_LOW;
-  const bool far = t > 125.f;
-  float shifted;
-  {
-#pragma clang fp contract(off)
-    shifted = 64.f - t;  // (exact there, of t as it was rounded: `rest` belongs to that one)
+  return {t, __builtin_fmaf(-y, LOG2E, -t) - y * LOG2E_LOW};
+}
+// 2^(t + rest); of an infinite t, whose rest is NaN, 2^t.
+__device__ __forceinline__ float raise(float t, float rest) {
+  const float e = __builtin_amdgcn_exp2f(t);
+  return __builtin_fabsf(rest) < 1.f ? __builtin_fmaf(e, rest * 0.693147181f, e) : e;
+}
+
+// act(g) u of four features, the activation in fp32, then the product.
+//
+// Where the power is past 2^125, 1 / (1 + e^-y) is e^y to the last bit, and the reciprocal would leave
+// fp32's normal range before the activation does (SiLU of -88.5 is -3.2e-37): 2^64 e^y is multiplied
+// by the gate first.  One branch for four, since hardly a gate is there (as selections for each it took
+// 3-5% of a tile's launch of short K, 2048 tokens of 2 x 2816 x 1024 29.6 -> 31.0 us).
+__device__ __forceinline__ f32x4_t gated4(f32x4_t g, f32x4_t u, int act) {
+  f32x4_t v;
+  Power p[4];
+#pragma unroll
+  for (int j = 0; j < 4; ++j) {
+    p[j] = power_of(g[j], act);
+    v[j] = g[j] * __builtin_amdgcn_rcpf(1.f + raise(p[j].t, p[j].rest)) * u[j];
   }
-  float e = __builtin_amdgcn_exp2f(far ? shifted : t);
-  // (the power of an infinite y stays as it is)
-  const float turn = rest * 0.693147181f;
-  e = __builtin_fabsf(rest) < 1.f ? __builtin_fmaf(e, far ? -turn : turn, e) : e;
-  return (far ? g * e * 0x1p-64f : g * __builtin_amdgcn_rcpf(1.f + e)) * u;
+  const float most = __builtin_fmaxf(__builtin_fmaxf(p[0].t, p[1].t), __builtin_fmaxf(p[2].t, p[3].t));
+  if (__builtin_expect(most > 125.f, 0)) {
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+#pragma clang fp contract(off)
+      const float t = 64.f - p[j].t;  // (exact there, of t as it was rounded: `rest` is that one's)
+      if (p[j].t > 125.f) v[j] = g[j] * raise(t, -p[j].rest) * 0x1p-64f * u[j];
+    }
+  }
+  return v;
 }
 
 // The eight weights of a dword of codes in the scale of an exponent byte, exact for

@@ -174,13 +174,6 @@ __device__ __forceinline__ const char* weight_rows(const dlfp::ProjectionArgs& a
   return static_cast<const char*>(a.weights[which]) + (int64_t)n0 * a.k * 2;
 }
 
-__device__ __forceinline__ f32x4_t gated4(f32x4_t g, f32x4_t u, int act) {
-  f32x4_t v;
-#pragma unroll
-  for (int j = 0; j < 4; ++j) v[j] = gated(g[j], u[j], act);
-  return v;
-}
-
 // The end of a tile whose K steps are split over the wavefronts: their sum, in wave order,
 // for the first TOKENS tokens.  Every wave is done with LDS.  Plain ones are dlfp_linear_bf16's:
 // whole tiles of features, row strides of 32 bits.
