@@ -1,10 +1,11 @@
 // Which kernel and tile a projection takes, and over how many workgroups K is split: those
 // whose estimated time is lowest.
 //
-// K over workgroups pays where the tiles leave compute units empty (5120 x 25600 in 4 bits, 256
-// tokens: 106 us whole, 71 in 6 parts; 128: 60 and 47; 32: 29.6 and 25.6); it costs the second
-// launch's 2-3 us and the partial sums' bytes twice.  A second launch and not the last of a
-// tile's workgroups adds them: it needs no counters that someone has to have zeroed.
+// K over workgroups pays where the tiles leave compute units empty (5120 x 25600 in 4 bits, weights
+// from HBM, the forms that are taken without a workspace and with one: 256 tokens 106 us whole, 70
+// in 6 parts; 128: 75 and 47; 32: 38.7 and 25.8); it costs the second launch's 2-3 us and the
+// partial sums' bytes twice.  A second launch and not the last of a tile's workgroups adds them: it
+// needs no counters that someone has to have zeroed.
 #pragma once
 
 #include <algorithm>
@@ -21,9 +22,9 @@ struct Grid {
 };
 typedef int (*Launch)(const dlfp::ProjectionArgs&, Grid, dlfp::Split, hipStream_t);
 
-// A tile of `rows` rows of weights and `tokens` tokens, of one workgroup of `threads`.  Its wavefronts
-// share steps of `columns` columns, or take all of them (waves 0).  `lds` bytes besides the exponents
-// of `blocks` blocks, where that matters (blocks > 0).
+// A tile of `rows` rows of weights and `tokens` tokens, of one workgroup of `threads`.  Its
+// wavefronts share steps of `columns` columns, or take all of them (waves 0).  `lds` bytes besides
+// the exponents of `blocks` blocks, where that matters (blocks > 0).
 //
 // Time in microseconds, with u = tiles times splits / 256, s = steps of a unit (of a wavefront
 // where they share them, of 64 columns otherwise) and b = MB of weights:
@@ -53,8 +54,8 @@ struct Plan {
   int64_t bytes;  // of partial sums
 };
 
-// The least estimate among those whose partial sums fit into `room` bytes and whose threads a launch
-// can have (no variant, if there is none: near 2^39 outputs).
+// The least estimate among those whose partial sums fit into `room` bytes and whose threads a
+// launch can have (no variant, if there is none: near 2^39 outputs).
 template <int COUNT>
 Plan choose(const Variant (&variants)[COUNT], bool gated, int m, int n, int k, int64_t weight_bytes,
             int64_t room) {

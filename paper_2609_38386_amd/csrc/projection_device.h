@@ -21,10 +21,10 @@ __device__ __forceinline__ uint32_t pack_bf16(float lo, float hi) {
   return __builtin_bit_cast(uint32_t, v);
 }
 
-// The power of an activation, e^-y, is 2^(t + rest): t the product -y log2 e as it is rounded, rest its
-// rounding error, so that SiLU's gates far below 0, whose weight is all in the power, are 4 fp32
-// steps (2^-23) off at most.  (GELU's y is itself a rounded one, whose error counts |y| times there:
-// 7 |y| half steps.)
+// The power of an activation, e^-y, is 2^(t + rest): t the product -y log2 e as it is rounded, rest
+// its rounding error, so that SiLU's gates far below 0, whose weight is all in the power, are 4 fp32
+// steps (2^-23) off at most.  (GELU's y is itself a rounded one, whose error counts |y| times
+// there: 7 |y| half steps.)
 struct Power {
   float t, rest;
 };
@@ -42,10 +42,10 @@ __device__ __forceinline__ float raise(float t, float rest) {
 
 // act(g) u of four features, the activation in fp32, then the product.
 //
-// Where the power is past 2^125, 1 / (1 + e^-y) is e^y to the last bit, and the reciprocal would leave
-// fp32's normal range before the activation does (SiLU of -88.5 is -3.2e-37): 2^64 e^y is multiplied
-// by the gate first.  One branch for four, since hardly a gate is there (as selections for each it took
-// 3-5% of a tile's launch of short K, 2048 tokens of 2 x 2816 x 1024 29.6 -> 31.0 us).
+// Where the power is past 2^125, 1 / (1 + e^-y) is e^y to the last bit, and the reciprocal would
+// leave fp32's normal range before the activation does (SiLU of -88.5 is -3.2e-37): 2^64 e^y is
+// multiplied by the gate first.  One branch for four, since hardly a gate is there (as selections
+// for each it took 3-5% of a launch of short K, 2048 tokens of 2 x 2816 x 1024 29.6 -> 31.0 us).
 __device__ __forceinline__ f32x4_t gated4(f32x4_t g, f32x4_t u, int act) {
   f32x4_t v;
   Power p[4];
@@ -54,7 +54,8 @@ __device__ __forceinline__ f32x4_t gated4(f32x4_t g, f32x4_t u, int act) {
     p[j] = power_of(g[j], act);
     v[j] = g[j] * __builtin_amdgcn_rcpf(1.f + raise(p[j].t, p[j].rest)) * u[j];
   }
-  const float most = __builtin_fmaxf(__builtin_fmaxf(p[0].t, p[1].t), __builtin_fmaxf(p[2].t, p[3].t));
+  const float most =
+      __builtin_fmaxf(__builtin_fmaxf(p[0].t, p[1].t), __builtin_fmaxf(p[2].t, p[3].t));
   if (__builtin_expect(most > 125.f, 0)) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {

@@ -12,11 +12,12 @@
 // in 4 bits 10.7 us with any number of loads in flight, this way 7.4).  Products of 16 x 16
 // leave the fewest idle columns to 1-16 tokens and need half the operand reads of 32 x 32.
 //
-// Bound by memory: a compute unit gets about 33 GB/s of weights from HBM and 85 GB/s of tokens
-// from L2, one after the other (its copies in flight are what is limited), so that few tokens
-// run at the card's rate (2 x 12288 x 4096 bf16, 8 tokens: 31.6 us, 6.4 TB/s) and 16-32 tokens
-// of few features below it (5120 x 25600 in 4 bits, 32 tokens: 22.9 us, 3.1 TB/s of weights from
-// HBM while the tokens' 131 MB come from L2; the weights alone would take 16.5, the tokens 12).
+// Bound by memory: a compute unit's copies in flight are limited, and those of weights and of tokens
+// share them.  Few tokens run near the card's rate (2 x 12288 x 4096 bf16, 8 tokens: 32-34 us,
+// 6.0-6.3 TB/s), 16-32 tokens of few features below it: 32 of 5120 x 25600 in 4 bits take 23.6 us for
+// 72 MB of weights from HBM (17.9 where the caches have them) and, over all tiles, 131 MB of tokens
+// from L2, where the weights' copies alone take 17.0, the tokens' 11.9, both without most products
+// 22.7.  (The call is 25.8 us with the sum of its three parts, 20.1 from the caches.)
 #pragma once
 
 #include "projection_tiles.h"
@@ -25,8 +26,9 @@ namespace {
 
 // A workgroup's unit: its tile's first feature and token, and its part of the steps of K, which
 // its wavefronts take in turn (so that they read neighbouring pieces of a row at about the same
-// time: 32 tokens of 5120 x 25600 in 4 bits 24.0 -> 22.9 us).  Divisions only where there is
-// something to divide (0.1-0.2 us of a launch of 3).
+// time: 32 tokens of 5120 x 25600 in 4 bits, weights from HBM, took 0.95 of the launch with
+// neighbouring steps for each).  Divisions only where there is something to divide (0.1-0.2 us of a
+// launch of 3).
 struct Unit {
   uint32_t tile, part;
   int n0, m0, from, to;

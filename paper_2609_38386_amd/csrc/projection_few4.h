@@ -5,11 +5,11 @@
 //
 // The exponents of the block's rows are copied before the first step, one contiguous piece of
 // memory; with K over workgroups, of each row the workgroup's part, which leaves the LDS to wider
-// blocks (16 tokens of 5120 x 25600 in 3 parts 22.3 -> 20.3 us).  As 4-byte pieces with each step
-// they took a third of the copies' time (4096 x 12288, 1 token: 9.6 us against 8.4 without any),
-// and loaded into registers beside the copies they made every step wait for all copies in flight
-// (16 tokens of 5120 x 25600: 22.9 against 21.2 us).  They are what limits k here: with more than
-// the LDS holds, tiles are taken.
+// blocks (16 tokens of 5120 x 25600 in 3 parts, weights from HBM, 0.91 of the time).  As 4-byte pieces
+// with each step they took a third of the copies' time (4096 x 12288, 1 token: 9.6 us against 8.4
+// without any), and loaded into registers beside the copies they made every step wait for all copies
+// in flight (16 tokens of 5120 x 25600: 22.9 against 21.2 us).  They are what limits k here: with more
+// than the LDS holds, tiles are taken.
 //
 // Steps of 256 columns copy weights in rows of 128 bytes; steps of 128 columns (64-byte rows, which
 // are copied at half the rate) let twice the wavefronts share the LDS, which pays where the
@@ -97,8 +97,8 @@ __global__ __launch_bounds__(64 * WAVES) void few4_kernel(dlfp::ProjectionArgs a
             whole || GROUPS * s + wg[c] < groups ? woff[c] : woff[c] - 16 * wg[c];
         const uint32_t to = d + (b * HALVES + c) * 1024;
         const char* from = wbase[b] + (int64_t)s * (STEP / 2);
-        // Rows of 64 bytes: past the caches each line would come from HBM twice (32 tokens of
-        // 5120 x 25600 28.1 against 25.9 us).
+        // Rows of 64 bytes: past the caches each line would come from HBM twice (a call of 32
+        // tokens of 5120 x 25600, weights from HBM: 28.1 against 25.9 us).
         if (HALVES == 2 && a.stream)
           lds_stream16(from, off, to);
         else
