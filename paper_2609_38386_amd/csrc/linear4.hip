@@ -28,9 +28,10 @@ __global__ __launch_bounds__(64 * FAR_WAVES) void far4_kernel(dlfp::ProjectionAr
   const int n0 = (int)(blockIdx.x % gn) * 16, m0 = (int)(blockIdx.x / gn) * 16;
   const uint16_t* x = a.x + (int64_t)min(m0 + lr, a.m - 1) * a.ldx;
   f32x4_t acc[B] = {};
-  for (int k0 = FAR_STEP * wave; k0 < a.k; k0 += FAR_STEP * FAR_WAVES) {
+  // (k0 itself passes 31 bits behind the last step of the longest rows)
+  for (uint32_t k0 = FAR_STEP * wave; k0 < (uint32_t)a.k; k0 += FAR_STEP * FAR_WAVES) {
     // Of a last step of 64 columns half of the lanes' columns are past the row: zeros.
-    const int c = k0 + 32 * quad;
+    const int c = (int)k0 + 32 * quad;
     const bool in = c < a.k;
     bf16x8_t xf[4];
 #pragma unroll
